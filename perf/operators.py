@@ -100,7 +100,7 @@ def draw(rng):
     if kind == "linear" and rng.random() < 0.25:        # a dense layer or a shared expert
         E, k, dropped = 1, 1, 0.0
     gated = rng.random() < 0.5
-    act = rng.choice(["silu", "silu", "gelu"]) if gated or rng.random() < 0.5 else "none"
+    act = rng.choice(["silu", "silu", "gelu"]) if gated or kind == "act_bwd" or rng.random() < 0.5 else "none"
     c = _product(kind, None, _log_int(rng, 1, 32768 if dtype == "bf16" else 4096), E, k, width(),
                  width() // (16 if gated else 8) * 8, act=act if kind != "linear_bwd" else "none", gated=gated,
                  bias=kind != "linear_bwd" and rng.random() < 0.5, residual=kind == "linear" and rng.random() < 0.4,
