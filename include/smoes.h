@@ -348,6 +348,112 @@ smoes_status smoes_bin_permute_noalloc(smoes_plan plan, const int32_t* topk_idx,
                                        int32_t* perm_token, uint32_t* perm_mask, int32_t* dispatch,
                                        int32_t* expert_counts, cudaStream_t stream);
 
+/* ------------------------------------------------------------------------------ expert layer
+ * What follows the router: its top-k choice becomes rows in expert order, every expert multiplies
+ * its rows, and the rows return to their tokens, with the gradients of each step. The paper leaves
+ * this to its framework.
+ *
+ * A plan (smoes_experts) has T tokens of k selections each: R = T * k rows. The rows of expert e are
+ * [expert_offsets[e], expert_offsets[e+1]) (device, int32 [E+1], written by smoes_expert_sort); rows
+ * from expert_offsets[E] to R belong to no expert, and every call that writes rows writes zeros
+ * there. Offsets and maps that were not made by smoes_expert_sort are kept inside [0, R] by the
+ * kernels. The conventions at the head of this file hold: dense row-major device arrays, 16-byte
+ * aligned, asynchronous on the given stream, nothing allocated. Outputs do not overlap inputs.
+ * Widths are multiples of 8 on SMOES_BF16 plans and of 4 on SMOES_F32 plans (rows of whole 16-byte
+ * words), at most 2^20. "dtype" below is the plan's type; everything is summed in float32. */
+typedef struct smoes_experts_s* smoes_experts;
+
+/* T tokens (0..2^20), E experts (1..256), k selections a token (1..16). E = k = 1 is a dense layer,
+ * or a shared expert that takes every token. max_width: the widest n_z that smoes_expert_act_bwd is
+ * given with a bias gradient (sizes its partial sums in the workspace), 0 if there is none. */
+typedef struct {
+  int T, E, k;
+  smoes_dtype dtype;
+  int max_width;
+} smoes_experts_desc;
+
+smoes_status smoes_experts_create(const smoes_experts_desc* desc, smoes_experts* out);
+void smoes_experts_destroy(smoes_experts plan);
+/* The caller's workspace: 256-byte aligned, cleared once by smoes_experts_workspace_init; calls that
+ * share one are ordered on the GPU. */
+size_t smoes_experts_workspace_bytes(smoes_experts plan);
+smoes_status smoes_experts_workspace_init(smoes_experts plan, void* ws, size_t ws_bytes,
+                                          cudaStream_t stream);
+/* Limit of the bounded waits, as smoes_plan_set_wait_limit. */
+smoes_status smoes_experts_set_wait_limit(smoes_experts plan, uint64_t limit_ns);
+/* Synchronises `stream`, then SMOES_OK, SMOES_ERR_DATA (a selection >= E was met; it was dropped) or
+ * SMOES_ERR_DEVICE_TIMEOUT. */
+smoes_status smoes_experts_read_status(smoes_experts plan, const void* ws, cudaStream_t stream);
+
+/* (8) Selections in expert order: a stable counting sort by expert, then token, then slot.
+ *   topk_idx [T, k] int32: the expert of each selection; a negative one takes no part (a dropped or
+ *   padding token), one >= E neither, and sets the status. Outputs: expert_offsets [E+1] int32;
+ *   row_slot [R] int32 = the selection (token * k + slot) of each row, -1 past the last row;
+ *   slot_row [T, k] int32 = the row of each selection, -1 if it takes no part. */
+smoes_status smoes_expert_sort(smoes_experts plan, const int32_t* topk_idx, int32_t* expert_offsets,
+                               int32_t* row_slot, int32_t* slot_row, void* ws, size_t ws_bytes,
+                               cudaStream_t stream);
+
+/* (9) Tokens into expert order: Xs [R, d] with Xs[slot_row[t, s]] = X[t], X [T, d] (dtype). */
+smoes_status smoes_expert_dispatch(smoes_experts plan, const void* X, int d,
+                                   const int32_t* expert_offsets, const int32_t* slot_row, void* Xs,
+                                   cudaStream_t stream);
+/* Its gradient: dX[t] = residual[t] + sum_s dXs[slot_row[t, s]], in slot order; residual [T, d] (a
+ * gradient that reached the tokens another way, the router's own for one) or NULL. */
+smoes_status smoes_expert_dispatch_bwd(smoes_experts plan, const void* dXs, int d,
+                                       const int32_t* slot_row, const void* residual, void* dX,
+                                       cudaStream_t stream);
+
+/* (10) Rows back to their tokens: Y[t] = residual[t] + sum_s topk_w[t, s] Ys[slot_row[t, s]], in slot
+ *   order; Ys [R, d], Y and residual [T, d] (dtype; residual may be NULL), topk_w [T, k] float32. A
+ *   selection without a row adds nothing, whatever its weight. */
+smoes_status smoes_expert_combine(smoes_experts plan, const void* Ys, int d, const float* topk_w,
+                                  const int32_t* slot_row, const void* residual, void* Y,
+                                  cudaStream_t stream);
+/* Its gradient: dYs[slot_row[t, s]] = topk_w[t, s] dY[t] and d_topk_w[t, s] = <dY[t], Ys[slot_row[t, s]]>
+ * (0 without a row), the d_topk_w that smoes_router_bwd takes. The gradient of the residual is dY. */
+smoes_status smoes_expert_combine_bwd(smoes_experts plan, const void* dY, const void* Ys, int d,
+                                      const float* topk_w, const int32_t* expert_offsets,
+                                      const int32_t* slot_row, void* dYs, float* d_topk_w,
+                                      cudaStream_t stream);
+
+/* SILU: z / (1 + e^-z). GELU: z Phi(z), the exact form. */
+typedef enum { SMOES_ACT_NONE = 0, SMOES_ACT_SILU = 1, SMOES_ACT_GELU = 2 } smoes_act;
+
+/* (11) The experts' product with bias, activation and residual: for each row r of expert e
+ *     z = W_e x_r + bias_e,   out_r = act(z) + residual_r,              n_z = n_out, or gated
+ *     z = [g | u],            out_r = act(g) * u + residual_r,          n_z = 2 n_out.
+ *   X [R, n_in], W [E, n_z, n_in], residual [R, n_out] or NULL (dtype), bias [E, n_z] float32 or NULL.
+ *   out [R, n_out]; pre [R, n_z] = z rounded to dtype, what smoes_expert_act_bwd reads, or NULL. out is
+ *   formed from the unrounded z and rounded once. */
+typedef struct {
+  const void* X;
+  const void* W;
+  const float* bias;
+  const void* residual;
+  int n_in, n_out;
+  int act;                             /* smoes_act */
+  int gated;
+} smoes_linear_args;
+smoes_status smoes_expert_linear(smoes_experts plan, const smoes_linear_args* args,
+                                 const int32_t* expert_offsets, void* out, void* pre, void* ws,
+                                 size_t ws_bytes, cudaStream_t stream);
+/* Gradient of the activation: dOut [R, n_out], pre [R, n_z] (dtype) -> dZ [R, n_z] (dtype; dOut act'(z),
+ *   or gated dOut u act'(g) and dOut act(g)) and db [E, n_z] float32 = each expert's sum of the unrounded
+ *   dZ over its rows in a fixed order (bitwise reproducible), or NULL. Without an activation and not
+ *   gated dZ is dOut: pre and dZ are NULL, and db alone is formed. The gradient of the residual is dOut.
+ *   n_z <= max_width of the plan when db is given (else SMOES_ERR_WORKSPACE). */
+smoes_status smoes_expert_act_bwd(smoes_experts plan, const void* dOut, const void* pre, int n_out,
+                                  int act, int gated, const int32_t* expert_offsets, void* dZ,
+                                  float* db, void* ws, size_t ws_bytes, cudaStream_t stream);
+/* Gradients of the product: dX [R, n_in] = dZ W_e (dtype) and dW [E, n_z, n_in] float32 = sum over the
+ *   expert's rows of dZ_r x_r^T, written, or accumulated into when accumulate_dW != 0 (an expert without
+ *   rows: zeros, or left as it is). Either output may be NULL, and then W or X may be too. */
+smoes_status smoes_expert_linear_bwd(smoes_experts plan, const void* dZ, const void* X, const void* W,
+                                     int n_in, int n_z, const int32_t* expert_offsets, void* dX,
+                                     float* dW, int accumulate_dW, void* ws, size_t ws_bytes,
+                                     cudaStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

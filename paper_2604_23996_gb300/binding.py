@@ -25,6 +25,7 @@ STATUS_NAMES = {0: "SMOES_OK", -1: "SMOES_ERR_INVALID_ARG", -2: "SMOES_ERR_UNSUP
                 -6: "SMOES_ERR_DEVICE_TIMEOUT", -7: "SMOES_ERR_DATA"}
 SMOES_F32, SMOES_BF16 = 0, 1
 SMOES_GATE_SOFTMAX, SMOES_GATE_SIGMOID = 0, 1
+SMOES_ACT_NONE, SMOES_ACT_SILU, SMOES_ACT_GELU = 0, 1, 2
 SMOES_SCORE_PROVIDED, SMOES_SCORE_GAUSS, SMOES_SCORE_ATTN, SMOES_SCORE_GMM = 0, 1, 2, 3
 (SMOES_CALL_ROUTER_FWD, SMOES_CALL_ROUTER_FWD_PERMUTE, SMOES_CALL_ROUTER_BWD, SMOES_CALL_BIN_PERMUTE,
  SMOES_CALL_ATTN_SCORE) = 0, 1, 2, 3, 4
@@ -65,6 +66,15 @@ class ScoreArgs(C.Structure):
     _fields_ = [("gauss", GaussArgs), ("attn", AttnArgs), ("gmm", GmmArgs)]
 
 
+class ExpertsDesc(C.Structure):
+    _fields_ = [("T", C.c_int), ("E", C.c_int), ("k", C.c_int), ("dtype", C.c_int), ("max_width", C.c_int)]
+
+
+class LinearArgs(C.Structure):
+    _fields_ = [("X", C.c_void_p), ("W", C.c_void_p), ("bias", C.c_void_p), ("residual", C.c_void_p),
+                ("n_in", C.c_int), ("n_out", C.c_int), ("act", C.c_int), ("gated", C.c_int)]
+
+
 _vp, _i, _f, _sz = C.c_void_p, C.c_int, C.c_float, C.c_size_t
 _sig = {
     "smoes_plan_create": (_i, [C.POINTER(RouterDesc), C.POINTER(_vp)]),
@@ -88,6 +98,20 @@ _sig = {
                                          _sz, _vp]),
     "smoes_adaptive_bins": (_i, [_vp, _vp, C.c_double, _vp, _vp, _vp, _vp]),
     "smoes_bin_balance": (_i, [_vp, _vp, _f, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "smoes_experts_create": (_i, [C.POINTER(ExpertsDesc), C.POINTER(_vp)]),
+    "smoes_experts_destroy": (None, [_vp]),
+    "smoes_experts_workspace_bytes": (_sz, [_vp]),
+    "smoes_experts_workspace_init": (_i, [_vp, _vp, _sz, _vp]),
+    "smoes_experts_set_wait_limit": (_i, [_vp, C.c_uint64]),
+    "smoes_experts_read_status": (_i, [_vp, _vp, _vp]),
+    "smoes_expert_sort": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "smoes_expert_dispatch": (_i, [_vp, _vp, _i, _vp, _vp, _vp, _vp]),
+    "smoes_expert_dispatch_bwd": (_i, [_vp, _vp, _i, _vp, _vp, _vp, _vp]),
+    "smoes_expert_combine": (_i, [_vp, _vp, _i, _vp, _vp, _vp, _vp, _vp]),
+    "smoes_expert_combine_bwd": (_i, [_vp, _vp, _vp, _i, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "smoes_expert_linear": (_i, [_vp, C.POINTER(LinearArgs), _vp, _vp, _vp, _vp, _sz, _vp]),
+    "smoes_expert_act_bwd": (_i, [_vp, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "smoes_expert_linear_bwd": (_i, [_vp, _vp, _vp, _vp, _i, _i, _vp, _vp, _vp, _i, _vp, _sz, _vp]),
     "smoes_attention_fwd": (_i, [_vp, C.POINTER(AttnArgs), _vp, _i, _vp, _vp, _vp, _sz, _vp]),
 }
 for _name, (_res, _args) in _sig.items():
@@ -261,6 +285,75 @@ def smoes_adaptive_bins(plan, expert_counts, beta, C_bar, expert_bin, f_spec=Non
                                     _p(f_spec), _stream(stream))
 
 
+def smoes_experts_create(T, E, k, dtype, max_width=0):
+    """Returns (status, plan handle) of an expert layer."""
+    desc = ExpertsDesc(T, E, k, dtype, max_width)
+    h = C.c_void_p()
+    code = _lib.smoes_experts_create(C.byref(desc), C.byref(h))
+    return code, h
+
+
+def smoes_experts_destroy(plan):
+    _lib.smoes_experts_destroy(plan)
+
+
+def smoes_experts_workspace_bytes(plan) -> int:
+    return int(_lib.smoes_experts_workspace_bytes(plan))
+
+
+def smoes_experts_workspace_init(plan, ws, stream=None) -> int:
+    return _lib.smoes_experts_workspace_init(plan, _p(ws), ws.numel() * ws.element_size(), _stream(stream))
+
+
+def smoes_experts_set_wait_limit(plan, limit_ns: int) -> int:
+    return _lib.smoes_experts_set_wait_limit(plan, int(limit_ns))
+
+
+def smoes_experts_read_status(plan, ws, stream=None) -> int:
+    return _lib.smoes_experts_read_status(plan, _p(ws), _stream(stream))
+
+
+def smoes_expert_sort(plan, topk_idx, expert_offsets, row_slot, slot_row, ws, stream=None) -> int:
+    return _lib.smoes_expert_sort(plan, _p(topk_idx), _p(expert_offsets), _p(row_slot), _p(slot_row), _p(ws),
+                                  ws.numel() * ws.element_size(), _stream(stream))
+
+
+def smoes_expert_dispatch(plan, X, d, expert_offsets, slot_row, Xs, stream=None) -> int:
+    return _lib.smoes_expert_dispatch(plan, _p(X), int(d), _p(expert_offsets), _p(slot_row), _p(Xs), _stream(stream))
+
+
+def smoes_expert_dispatch_bwd(plan, dXs, d, slot_row, residual, dX, stream=None) -> int:
+    return _lib.smoes_expert_dispatch_bwd(plan, _p(dXs), int(d), _p(slot_row), _p(residual), _p(dX), _stream(stream))
+
+
+def smoes_expert_combine(plan, Ys, d, topk_w, slot_row, residual, Y, stream=None) -> int:
+    return _lib.smoes_expert_combine(plan, _p(Ys), int(d), _p(topk_w), _p(slot_row), _p(residual), _p(Y),
+                                     _stream(stream))
+
+
+def smoes_expert_combine_bwd(plan, dY, Ys, d, topk_w, expert_offsets, slot_row, dYs, d_topk_w, stream=None) -> int:
+    return _lib.smoes_expert_combine_bwd(plan, _p(dY), _p(Ys), int(d), _p(topk_w), _p(expert_offsets), _p(slot_row),
+                                         _p(dYs), _p(d_topk_w), _stream(stream))
+
+
+def smoes_expert_linear(plan, X, W, bias, residual, n_in, n_out, act, gated, expert_offsets, out, pre, ws,
+                        stream=None) -> int:
+    args = LinearArgs(_p(X), _p(W), _p(bias), _p(residual), int(n_in), int(n_out), int(act), int(gated))
+    return _lib.smoes_expert_linear(plan, C.byref(args), _p(expert_offsets), _p(out), _p(pre), _p(ws),
+                                    ws.numel() * ws.element_size(), _stream(stream))
+
+
+def smoes_expert_act_bwd(plan, dOut, pre, n_out, act, gated, expert_offsets, dZ, db, ws, stream=None) -> int:
+    return _lib.smoes_expert_act_bwd(plan, _p(dOut), _p(pre), int(n_out), int(act), int(gated), _p(expert_offsets),
+                                     _p(dZ), _p(db), _p(ws), ws.numel() * ws.element_size(), _stream(stream))
+
+
+def smoes_expert_linear_bwd(plan, dZ, X, W, n_in, n_z, expert_offsets, dX, dW, accumulate_dW, ws, stream=None) -> int:
+    return _lib.smoes_expert_linear_bwd(plan, _p(dZ), _p(X), _p(W), int(n_in), int(n_z), _p(expert_offsets), _p(dX),
+                                        _p(dW), int(accumulate_dW), _p(ws), ws.numel() * ws.element_size(),
+                                        _stream(stream))
+
+
 # ----------------------------------------------------------------------------- convenience
 
 class Router:
@@ -342,3 +435,158 @@ class Router:
     def device_status(self, stream=None):
         code, n_absent = smoes_read_device_status(self.plan, self.ws, stream)
         return code, n_absent
+
+
+class Experts:
+    """The expert layer behind a router: one plan, its workspace and the maps of its last ``sort``.
+
+    ``T`` tokens of ``k`` selections over ``E`` experts give ``R = T * k`` rows in expert order. A layer of one
+    expert and one selection (``E = k = 1``) is a dense layer and needs no sort. Tensors are contiguous, of the
+    plan's type (weights of the top-k, biases and their gradients float32) and on the plan's device; a tensor
+    that is not raises a ValueError before anything is launched. Results are new tensors unless an output is given.
+    """
+
+    def __init__(self, T, E, k, dtype=SMOES_BF16, max_width=0, device="cuda"):
+        code, self.plan = smoes_experts_create(T, E, k, dtype, max_width)
+        _check(code, "smoes_experts_create")
+        self.T, self.E, self.k, self.R = T, E, k, T * k
+        self.dtype = torch.bfloat16 if dtype == SMOES_BF16 else torch.float32
+        self.ws = torch.empty(smoes_experts_workspace_bytes(self.plan), dtype=torch.uint8, device=device)
+        self.device = self.ws.device
+        _check(smoes_experts_workspace_init(self.plan, self.ws), "smoes_experts_workspace_init")
+        self.expert_offsets = torch.zeros(E + 1, dtype=torch.int32, device=device)
+        self.row_slot = torch.full((self.R,), -1, dtype=torch.int32, device=device)
+        self.slot_row = torch.full((T, k), -1, dtype=torch.int32, device=device)
+        if E == 1 and k == 1:                          # every token is a row of the one expert
+            self.expert_offsets[1:].fill_(T)
+            torch.arange(T, out=self.row_slot)
+            torch.arange(T, out=self.slot_row.view(-1))
+
+    def __del__(self):
+        try:
+            smoes_experts_destroy(self.plan)
+        except Exception:
+            pass
+
+    def _want(self, name, t, shape, dtype=None):
+        """Checks one argument (None stays None)."""
+        if t is None:
+            return
+        dtype = dtype or self.dtype
+        if t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.device != self.device:
+            raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {tuple(shape)} on {self.device} is "
+                             f"wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
+
+    def _out(self, t, shape, dtype=None):
+        if t is None:
+            return torch.empty(shape, dtype=dtype or self.dtype, device=self.device)
+        self._want("output", t, shape, dtype)
+        return t
+
+    def sort(self, topk_idx, stream=None):
+        """Selections [T, k] int32 (negative: takes no part) into expert order; fills and returns
+        expert_offsets, row_slot, slot_row."""
+        self._want("topk_idx", topk_idx, (self.T, self.k), torch.int32)
+        _check(smoes_expert_sort(self.plan, topk_idx, self.expert_offsets, self.row_slot, self.slot_row, self.ws,
+                                 stream), "smoes_expert_sort")
+        return self.expert_offsets, self.row_slot, self.slot_row
+
+    def dispatch(self, X, out=None, stream=None):
+        """Tokens [T, d] into expert order: [R, d]."""
+        d = X.shape[-1]
+        self._want("X", X, (self.T, d))
+        out = self._out(out, (self.R, d))
+        _check(smoes_expert_dispatch(self.plan, X, d, self.expert_offsets, self.slot_row, out, stream),
+               "smoes_expert_dispatch")
+        return out
+
+    def dispatch_bwd(self, dXs, residual=None, out=None, stream=None):
+        """Gradient of the tokens from that of their rows, plus ``residual`` [T, d]."""
+        d = dXs.shape[-1]
+        self._want("dXs", dXs, (self.R, d))
+        self._want("residual", residual, (self.T, d))
+        out = self._out(out, (self.T, d))
+        _check(smoes_expert_dispatch_bwd(self.plan, dXs, d, self.slot_row, residual, out, stream),
+               "smoes_expert_dispatch_bwd")
+        return out
+
+    def combine(self, Ys, topk_w, residual=None, out=None, stream=None):
+        """Rows [R, d] back to their tokens, weighted by topk_w [T, k] float32, plus ``residual``."""
+        d = Ys.shape[-1]
+        self._want("Ys", Ys, (self.R, d))
+        self._want("topk_w", topk_w, (self.T, self.k), torch.float32)
+        self._want("residual", residual, (self.T, d))
+        out = self._out(out, (self.T, d))
+        _check(smoes_expert_combine(self.plan, Ys, d, topk_w, self.slot_row, residual, out, stream),
+               "smoes_expert_combine")
+        return out
+
+    def combine_bwd(self, dY, Ys, topk_w, dYs=None, d_topk_w=None, stream=None):
+        """Gradients of the rows and of the weights (the d_topk_w of ``Router.backward``)."""
+        d = dY.shape[-1]
+        self._want("dY", dY, (self.T, d))
+        self._want("Ys", Ys, (self.R, d))
+        self._want("topk_w", topk_w, (self.T, self.k), torch.float32)
+        dYs = self._out(dYs, (self.R, d))
+        d_topk_w = self._out(d_topk_w, (self.T, self.k), torch.float32)
+        _check(smoes_expert_combine_bwd(self.plan, dY, Ys, d, topk_w, self.expert_offsets, self.slot_row, dYs,
+                                        d_topk_w, stream), "smoes_expert_combine_bwd")
+        return dYs, d_topk_w
+
+    def linear(self, X, W, bias=None, act=SMOES_ACT_NONE, gated=False, residual=None, save_pre=False, out=None,
+               pre=None, stream=None):
+        """act(x W_e^T + b_e) + residual of rows [R, n_in] in expert order, W [E, n_z, n_in]; gated: z = [g | u],
+        act(g) u. Returns (out, pre); pre is None unless save_pre (or a tensor to write) asks for it."""
+        n_z, n_in = W.shape[-2:]
+        n_out = n_z // 2 if gated else n_z
+        if gated and n_z % 2:
+            raise ValueError(f"W: a gated layer has an even number of rows, got {n_z}")
+        self._want("X", X, (self.R, n_in))
+        self._want("W", W, (self.E, n_z, n_in))
+        self._want("bias", bias, (self.E, n_z), torch.float32)
+        self._want("residual", residual, (self.R, n_out))
+        out = self._out(out, (self.R, n_out))
+        if save_pre or pre is not None:
+            pre = self._out(pre, (self.R, n_z))
+        _check(smoes_expert_linear(self.plan, X, W, bias, residual, n_in, n_out, act, gated, self.expert_offsets,
+                                   out, pre, self.ws, stream), "smoes_expert_linear")
+        return out, pre
+
+    def act_bwd(self, dOut, pre=None, act=SMOES_ACT_NONE, gated=False, bias_grad=False, dZ=None, db=None,
+                stream=None):
+        """Gradients of the pre-activations and of the bias: (dZ, db). Without an activation and not gated dZ is
+        dOut itself. db is None unless bias_grad (or a tensor to write) asks for it."""
+        n_out = dOut.shape[-1]
+        n_z = 2 * n_out if gated else n_out
+        self._want("dOut", dOut, (self.R, n_out))
+        if bias_grad or db is not None:
+            db = self._out(db, (self.E, n_z), torch.float32)
+        if act == SMOES_ACT_NONE and not gated:
+            if db is not None:
+                _check(smoes_expert_act_bwd(self.plan, dOut, None, n_out, act, gated, self.expert_offsets, None, db,
+                                            self.ws, stream), "smoes_expert_act_bwd")
+            return dOut, db
+        if pre is None:
+            raise ValueError("pre: the pre-activations that linear saved are wanted")
+        self._want("pre", pre, (self.R, n_z))
+        dZ = self._out(dZ, (self.R, n_z))
+        _check(smoes_expert_act_bwd(self.plan, dOut, pre, n_out, act, gated, self.expert_offsets, dZ, db, self.ws,
+                                    stream), "smoes_expert_act_bwd")
+        return dZ, db
+
+    def linear_bwd(self, dZ, X, W, need_dX=True, need_dW=True, dX=None, dW=None, accumulate=False, stream=None):
+        """Gradients of the rows [R, n_in] and of the weights (float32; accumulate adds to the given dW)."""
+        n_z, n_in = W.shape[-2:]
+        self._want("dZ", dZ, (self.R, n_z))
+        self._want("X", X, (self.R, n_in))
+        self._want("W", W, (self.E, n_z, n_in))
+        if accumulate and dW is None:
+            raise ValueError("dW: a tensor to accumulate into is wanted")
+        dX = self._out(dX, (self.R, n_in)) if need_dX else None
+        dW = self._out(dW, (self.E, n_z, n_in), torch.float32) if need_dW else None
+        _check(smoes_expert_linear_bwd(self.plan, dZ, X, W, n_in, n_z, self.expert_offsets, dX, dW, accumulate,
+                                       self.ws, stream), "smoes_expert_linear_bwd")
+        return dX, dW
+
+    def device_status(self, stream=None):
+        return smoes_experts_read_status(self.plan, self.ws, stream)

@@ -1,0 +1,196 @@
+// experts.cuh -- the expert layer: plan, kernel parameters and launchers shared by experts_api.cu and
+// the kernels (expert_sort.cu, expert_rows.cu, expert_linear.cu, expert_act.cu).
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include "smoes_internal.cuh"
+
+namespace smoes {
+
+constexpr int kExpertsMax = 256;           // experts of an expert-layer plan
+constexpr int kExpertWidthMax = 1 << 20;   // widest row
+constexpr int kActChunk = 256;             // rows per partial sum of the bias gradient
+
+struct ExpertSortParams {
+  long long n;               // selections T * k
+  int E, G;                  // blocks
+  long long per;             // selections per block, a multiple of 1024
+  const int32_t* topk_idx;
+  int32_t* offsets;
+  int32_t* row_slot;
+  int32_t* slot_row;
+  int32_t* counts;           // [G][E] (workspace)
+  uint32_t* sync;            // [2] grid barrier words (workspace, zero between calls)
+  uint32_t* status;
+  uint64_t limit_ns;
+};
+
+// dispatch, combine and their gradients: rows of `d` elements, T tokens of k selections
+struct ExpertRowsParams {
+  int T, k, d, E;
+  const int32_t* offsets;    // [E+1], or null where no rows are written
+  const int32_t* slot_row;   // [T, k]
+  const void* tokens;        // X, dY or the residual (or null)
+  const void* rows;          // Ys or dXs
+  const float* w;            // [T, k] or null (1)
+  void* rows_out;            // Xs or dYs
+  void* tokens_out;          // Y or dX
+  float* dw;                 // [T, k]
+};
+
+struct ExpertLinearParams {
+  int E, n_in, n_out, n_z, act, gated;
+  long long R;
+  const int32_t* offsets;
+  const void* X;
+  const void* W;
+  const float* bias;
+  const void* residual;
+  const void* dZ;
+  void* out;                 // out, or dX
+  void* pre;
+  float* dW;
+  int accumulate;
+};
+
+struct ExpertActParams {
+  int E, n_out, n_z, act, gated;
+  long long R;
+  const int32_t* offsets;
+  const void* dOut;
+  const void* pre;
+  void* dZ;
+  float* db;
+  float* part;               // [R / kActChunk + E][n_z] (workspace)
+};
+
+cudaError_t launch_expert_sort(const ExpertSortParams& p, cudaStream_t s);
+cudaError_t launch_expert_dispatch(const ExpertRowsParams& p, bool bf16, cudaStream_t s);
+cudaError_t launch_expert_combine(const ExpertRowsParams& p, bool bf16, cudaStream_t s);
+cudaError_t launch_expert_combine_bwd(const ExpertRowsParams& p, bool bf16, cudaStream_t s);
+cudaError_t launch_expert_linear(const ExpertLinearParams& p, bool bf16, cudaStream_t s);
+cudaError_t launch_expert_dx(const ExpertLinearParams& p, bool bf16, cudaStream_t s);
+cudaError_t launch_expert_dw(const ExpertLinearParams& p, bool bf16, cudaStream_t s);
+cudaError_t launch_expert_act_bwd(const ExpertActParams& p, bool bf16, cudaStream_t s);
+
+// ------------------------------------------------------------------------------ device helpers
+
+// First row of expert e, kept inside [0, R]; expert_rows: its rows (none where offsets run backwards).
+__device__ __forceinline__ long long expert_begin(const int32_t* off, int e, long long R) {
+  const long long o = off[e];
+  return o < 0 ? 0 : o > R ? R : o;
+}
+
+// Work over the experts' rows in tiles of BM: the expert and first row of tile `tile`, found by one
+// warp (lane l counts the tiles of experts 8 l .. 8 l + 7). e = -1 past the last tile.
+struct RowTile {
+  int e;
+  long long row0, row1;      // the tile's first row, the expert's end
+  int index;                 // the tile's number within the expert
+};
+__device__ inline RowTile find_row_tile(const int32_t* off, int E, long long R, int BM, long long tile) {
+  const int lane = threadIdx.x & 31;
+  int n[8];
+  int sum = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int e = lane * 8 + i;
+    n[i] = 0;
+    if (e < E) {
+      const long long rows = expert_begin(off, e + 1, R) - expert_begin(off, e, R);
+      n[i] = rows > 0 ? static_cast<int>((rows + BM - 1) / BM) : 0;
+    }
+    sum += n[i];
+  }
+  int run = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int v = __shfl_up_sync(0xffffffffu, run, o);
+    if (lane >= o) run += v;
+  }
+  long long at = run - sum;
+  int e = -1, index = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if (tile >= at && tile < at + n[i]) {
+      e = lane * 8 + i;
+      index = static_cast<int>(tile - at);
+    }
+    at += n[i];
+  }
+  const unsigned has = __ballot_sync(0xffffffffu, e >= 0);
+  RowTile t{-1, 0, 0, 0};
+  if (!has) return t;
+  const int src = __ffs(has) - 1;
+  t.e = __shfl_sync(0xffffffffu, e, src);
+  t.index = __shfl_sync(0xffffffffu, index, src);
+  t.row0 = expert_begin(off, t.e, R) + static_cast<long long>(t.index) * BM;
+  t.row1 = expert_begin(off, t.e + 1, R);
+  return t;
+}
+
+// 16 bytes of T: 8 bf16 or 4 fp32.
+template <class T>
+struct Pack;
+template <>
+struct Pack<__nv_bfloat16> {
+  static constexpr int N = 8;
+  static __device__ __forceinline__ void unpack(const uint4& v, float (&f)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[2 * i] = __uint_as_float(w[i] << 16);
+      f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&f)[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+template <>
+struct Pack<float> {
+  static constexpr int N = 4;
+  static __device__ __forceinline__ void unpack(const uint4& v, float (&f)[4]) {
+    f[0] = __uint_as_float(v.x);
+    f[1] = __uint_as_float(v.y);
+    f[2] = __uint_as_float(v.z);
+    f[3] = __uint_as_float(v.w);
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&f)[4]) {
+    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+  }
+};
+
+// Zeros in rows [first, R) of an array of rows of `words` 16-byte words, by all threads of the grid.
+__device__ __forceinline__ void zero_rows(void* base, long long first, long long R, int words) {
+  uint4* out = static_cast<uint4*>(base);
+  const long long end = R * words;
+  for (long long i = first * words + static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x; i < end;
+       i += static_cast<long long>(gridDim.x) * blockDim.x)
+    out[i] = make_uint4(0u, 0u, 0u, 0u);
+}
+
+// Activations and their slopes. Accurate form, for fp32 results.
+__device__ __forceinline__ float act_value(int act, float z) {
+  if (act == SMOES_ACT_SILU) return z / (1.f + expf(-z));
+  if (act == SMOES_ACT_GELU) return 0.5f * z * erfcf(z * -0.70710678f);
+  return z;
+}
+__device__ __forceinline__ float act_slope(int act, float z) {
+  if (act == SMOES_ACT_SILU) {
+    const float s = 1.f / (1.f + expf(-z));
+    return s * (1.f + z * (1.f - s));
+  }
+  if (act == SMOES_ACT_GELU)
+    return 0.5f * erfcf(z * -0.70710678f) + z * expf(-0.5f * z * z) * 0.39894228f;
+  return 1.f;
+}
+
+}  // namespace smoes
