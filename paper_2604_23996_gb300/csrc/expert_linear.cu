@@ -1,4 +1,5 @@
-// expert_linear.cu -- the experts' products on the FMA units, grouped over ragged row ranges:
+// expert_linear.cu -- the experts' fp32 products on the FMA units, grouped over ragged row ranges (bf16:
+// expert_gemm.cu):
 //   forward   z = X W_e^T + b_e, out = act(z) (or act(g) u of z = [g | u]) + residual
 //   dX        dZ W_e
 //   dW        dZ^T X over the expert's rows
@@ -19,38 +20,20 @@ constexpr int kLinThreads = 256;
 
 enum LinearMode { kForward = 0, kGradX = 1, kGradW = 2 };
 
-template <class T>
-__device__ __forceinline__ float4 load4(const T* p);
-template <>
-__device__ __forceinline__ float4 load4<float>(const float* p) {
+__device__ __forceinline__ float4 load4(const float* p) {
   return __ldg(reinterpret_cast<const float4*>(p));
 }
-template <>
-__device__ __forceinline__ float4 load4<__nv_bfloat16>(const __nv_bfloat16* p) {
-  const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
-  return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16),
-                     __uint_as_float(v.y & 0xffff0000u));
-}
-template <class T>
-__device__ __forceinline__ void store4(T* p, float a, float b, float c, float d);
-template <>
-__device__ __forceinline__ void store4<float>(float* p, float a, float b, float c, float d) {
+__device__ __forceinline__ void store4(float* p, float a, float b, float c, float d) {
   *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d);
-}
-template <>
-__device__ __forceinline__ void store4<__nv_bfloat16>(__nv_bfloat16* p, float a, float b, float c, float d) {
-  const __nv_bfloat162 lo = __floats2bfloat162_rn(a, b), hi = __floats2bfloat162_rn(c, d);
-  *reinterpret_cast<uint2*>(p) =
-      make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
 }
 
 // One operand's slice in registers: along the depth (rows of `ld` elements, 8 of a row a thread) or
 // across it (16 rows of the depth, 8 neighbouring columns a thread).
-template <class T, bool kAlong>
+template <bool kAlong>
 struct Slice {
   float4 v[2];
   // along: row `outer` (already this thread's; valid when in), depth d0.. < depth_end
-  __device__ __forceinline__ void load_along(const T* row, bool in, long long d0, long long depth_end) {
+  __device__ __forceinline__ void load_along(const float* row, bool in, long long d0, long long depth_end) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const long long d = d0 + (threadIdx.x & 1) * 8 + 4 * h;
@@ -58,7 +41,7 @@ struct Slice {
     }
   }
   // across: base of depth row 0, columns c0 + ... < c_end
-  __device__ __forceinline__ void load_across(const T* base, long long ld, long long d0, long long depth_end, int c0,
+  __device__ __forceinline__ void load_across(const float* base, long long ld, long long d0, long long depth_end, int c0,
                                               int c_end) {
     const long long d = d0 + (threadIdx.x >> 4);
 #pragma unroll
@@ -85,16 +68,16 @@ struct Slice {
   }
 };
 
-template <class T, int kMode>
+template <int kMode>
 __global__ void __launch_bounds__(kLinThreads) k_expert_linear(const ExpertLinearParams p) {
   __shared__ float As[2][kDepth][kPad];
   __shared__ float Bs[2][kDepth][kPad];
   pdl_wait();
   pdl_trigger();
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const T* X = static_cast<const T*>(p.X);
-  const T* W = static_cast<const T*>(p.W);
-  const T* dZ = static_cast<const T*>(p.dZ);
+  const float* X = static_cast<const float*>(p.X);
+  const float* W = static_cast<const float*>(p.W);
+  const float* dZ = static_cast<const float*>(p.dZ);
 
   // the tile: rows [m0, m_end) of the product, columns from n0; the depth [k0, k_end)
   int e;
@@ -109,9 +92,9 @@ __global__ void __launch_bounds__(kLinThreads) k_expert_linear(const ExpertLinea
     k_end = max(k0, expert_begin(p.offsets, e + 1, p.R));
   } else {
     zero_rows(p.out, expert_begin(p.offsets, p.E, p.R), p.R,
-              static_cast<int>((kMode == kForward ? p.n_out : p.n_in) * sizeof(T) / 16));
+              static_cast<int>((kMode == kForward ? p.n_out : p.n_in) * sizeof(float) / 16));
     if (kMode == kForward && p.pre)
-      zero_rows(p.pre, expert_begin(p.offsets, p.E, p.R), p.R, static_cast<int>(p.n_z * sizeof(T) / 16));
+      zero_rows(p.pre, expert_begin(p.offsets, p.E, p.R), p.R, static_cast<int>(p.n_z * sizeof(float) / 16));
     const RowTile t = find_row_tile(p.offsets, p.E, p.R, kTile, blockIdx.x);
     if (t.e < 0) return;
     e = t.e;
@@ -120,14 +103,14 @@ __global__ void __launch_bounds__(kLinThreads) k_expert_linear(const ExpertLinea
     n0 = blockIdx.y * (kMode == kForward && p.gated ? kTile / 2 : kTile);
     k_end = kMode == kForward ? p.n_in : p.n_z;
   }
-  const T* We = W + static_cast<long long>(e) * p.n_z * p.n_in;
+  const float* We = W + static_cast<long long>(e) * p.n_z * p.n_in;
 
   constexpr bool kAlongA = kMode != kGradW, kAlongB = kMode == kForward;
-  Slice<T, kAlongA> a;
-  Slice<T, kAlongB> b;
+  Slice<kAlongA> a;
+  Slice<kAlongB> b;
   const int lr = threadIdx.x >> 1;
   const bool a_in = m0 + lr < m_end;
-  const T* a_row = kMode == kForward ? X + (m0 + lr) * p.n_in : dZ + (m0 + lr) * p.n_z;
+  const float* a_row = kMode == kForward ? X + (m0 + lr) * p.n_in : dZ + (m0 + lr) * p.n_z;
   // forward: the output feature of B's row lr; gated tiles hold 64 gate rows, then the same 64 of u
   int b_row = n0 + lr;
   bool b_in = b_row < p.n_z;
@@ -220,7 +203,7 @@ __global__ void __launch_bounds__(kLinThreads) k_expert_linear(const ExpertLinea
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int n = n0 + tx * 4 + 64 * h;
-        if (n < p.n_in) store4(static_cast<T*>(p.out) + m * p.n_in + n, z[h][0], z[h][1], z[h][2], z[h][3]);
+        if (n < p.n_in) store4(static_cast<float*>(p.out) + m * p.n_in + n, z[h][0], z[h][1], z[h][2], z[h][3]);
       }
     } else {
       const float* bias = p.bias ? p.bias + static_cast<long long>(e) * p.n_z : nullptr;
@@ -236,7 +219,7 @@ __global__ void __launch_bounds__(kLinThreads) k_expert_linear(const ExpertLinea
           z[h][2] += bv.z;
           z[h][3] += bv.w;
         }
-        if (p.pre) store4(static_cast<T*>(p.pre) + m * p.n_z + n, z[h][0], z[h][1], z[h][2], z[h][3]);
+        if (p.pre) store4(static_cast<float*>(p.pre) + m * p.n_z + n, z[h][0], z[h][1], z[h][2], z[h][3]);
       }
       const int halves = p.gated ? 1 : 2;
 #pragma unroll
@@ -245,7 +228,7 @@ __global__ void __launch_bounds__(kLinThreads) k_expert_linear(const ExpertLinea
         if (h >= halves || n >= p.n_out) continue;
         float y[4];
         float4 res = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (p.residual) res = load4(static_cast<const T*>(p.residual) + m * p.n_out + n);
+        if (p.residual) res = load4(static_cast<const float*>(p.residual) + m * p.n_out + n);
         const float rv[4] = {res.x, res.y, res.z, res.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -253,7 +236,7 @@ __global__ void __launch_bounds__(kLinThreads) k_expert_linear(const ExpertLinea
           if (p.gated) y[j] *= z[1][j];
           y[j] += rv[j];
         }
-        store4(static_cast<T*>(p.out) + m * p.n_out + n, y[0], y[1], y[2], y[3]);
+        store4(static_cast<float*>(p.out) + m * p.n_out + n, y[0], y[1], y[2], y[3]);
       }
     }
   }
@@ -267,20 +250,17 @@ dim3 row_grid(const ExpertLinearParams& p, int cols, int per) {
 
 }  // namespace
 
-cudaError_t launch_expert_linear(const ExpertLinearParams& p, bool bf16, cudaStream_t s) {
+cudaError_t launch_expert_linear(const ExpertLinearParams& p, cudaStream_t s) {
   const dim3 grid = row_grid(p, p.n_out, p.gated ? kTile / 2 : kTile);
-  return bf16 ? launch_pdl(k_expert_linear<__nv_bfloat16, kForward>, grid, dim3(kLinThreads), 0, s, p)
-              : launch_pdl(k_expert_linear<float, kForward>, grid, dim3(kLinThreads), 0, s, p);
+  return launch_pdl(k_expert_linear<kForward>, grid, dim3(kLinThreads), 0, s, p);
 }
-cudaError_t launch_expert_dx(const ExpertLinearParams& p, bool bf16, cudaStream_t s) {
+cudaError_t launch_expert_dx(const ExpertLinearParams& p, cudaStream_t s) {
   const dim3 grid = row_grid(p, p.n_in, kTile);
-  return bf16 ? launch_pdl(k_expert_linear<__nv_bfloat16, kGradX>, grid, dim3(kLinThreads), 0, s, p)
-              : launch_pdl(k_expert_linear<float, kGradX>, grid, dim3(kLinThreads), 0, s, p);
+  return launch_pdl(k_expert_linear<kGradX>, grid, dim3(kLinThreads), 0, s, p);
 }
-cudaError_t launch_expert_dw(const ExpertLinearParams& p, bool bf16, cudaStream_t s) {
+cudaError_t launch_expert_dw(const ExpertLinearParams& p, cudaStream_t s) {
   const dim3 grid((p.n_in + kTile - 1) / kTile, (p.n_z + kTile - 1) / kTile, p.E);
-  return bf16 ? launch_pdl(k_expert_linear<__nv_bfloat16, kGradW>, grid, dim3(kLinThreads), 0, s, p)
-              : launch_pdl(k_expert_linear<float, kGradW>, grid, dim3(kLinThreads), 0, s, p);
+  return launch_pdl(k_expert_linear<kGradW>, grid, dim3(kLinThreads), 0, s, p);
 }
 
 }  // namespace smoes

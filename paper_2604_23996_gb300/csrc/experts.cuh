@@ -1,5 +1,5 @@
 // experts.cuh -- the expert layer: plan, kernel parameters and launchers shared by experts_api.cu and
-// the kernels (expert_sort.cu, expert_rows.cu, expert_linear.cu, expert_act.cu).
+// the kernels (expert_sort.cu, expert_rows.cu, expert_linear.cu, expert_gemm.cu, expert_act.cu).
 #pragma once
 
 #include <cuda_bf16.h>
@@ -65,13 +65,28 @@ struct ExpertActParams {
   float* part;               // [R / kActChunk + E][n_z] (workspace)
 };
 
+// The bf16 products on the tensor cores (expert_gemm.cu): D[m, n] = sum over the depth of A[m] B[n], with
+// the features of an output row along m and the rows along n (the weights' gradient: n_in along m, n_z
+// along n, the expert's rows as the depth).
+enum ExpertGemmMode { kGemmForward = 0, kGemmGradX = 1, kGemmGradW = 2 };
+struct ExpertGemmParams {
+  ExpertLinearParams l;
+  int n_feat;                // features along m: n_out, or n_in
+  int m_tiles;
+  int n_tiles;               // tiles along n_z (weights' gradient)
+  uint32_t* status;
+  uint64_t limit_ns;
+};
+
+cudaError_t launch_expert_gemm(const ExpertLinearParams& p, ExpertGemmMode mode, uint32_t* status, uint64_t limit_ns,
+                               int n_sms, cudaStream_t s);
 cudaError_t launch_expert_sort(const ExpertSortParams& p, cudaStream_t s);
 cudaError_t launch_expert_dispatch(const ExpertRowsParams& p, bool bf16, cudaStream_t s);
 cudaError_t launch_expert_combine(const ExpertRowsParams& p, bool bf16, cudaStream_t s);
 cudaError_t launch_expert_combine_bwd(const ExpertRowsParams& p, bool bf16, cudaStream_t s);
-cudaError_t launch_expert_linear(const ExpertLinearParams& p, bool bf16, cudaStream_t s);
-cudaError_t launch_expert_dx(const ExpertLinearParams& p, bool bf16, cudaStream_t s);
-cudaError_t launch_expert_dw(const ExpertLinearParams& p, bool bf16, cudaStream_t s);
+cudaError_t launch_expert_linear(const ExpertLinearParams& p, cudaStream_t s);
+cudaError_t launch_expert_dx(const ExpertLinearParams& p, cudaStream_t s);
+cudaError_t launch_expert_dw(const ExpertLinearParams& p, cudaStream_t s);
 cudaError_t launch_expert_act_bwd(const ExpertActParams& p, bool bf16, cudaStream_t s);
 
 // ------------------------------------------------------------------------------ device helpers

@@ -244,7 +244,9 @@ smoes_status smoes_expert_linear(smoes_experts P, const smoes_linear_args* args,
   p.residual = a.residual;
   p.out = out;
   p.pre = pre;
-  return cuda_status(launch_expert_linear(p, P->desc.dtype == SMOES_BF16, stream));
+  return cuda_status(P->desc.dtype == SMOES_BF16
+                         ? launch_expert_gemm(p, kGemmForward, static_cast<uint32_t*>(ws), P->limit_ns, P->n_sms, stream)
+                         : launch_expert_linear(p, stream));
 }
 
 smoes_status smoes_expert_act_bwd(smoes_experts P, const void* dOut, const void* pre, int n_out, int act, int gated,
@@ -315,9 +317,11 @@ smoes_status smoes_expert_linear_bwd(smoes_experts P, const void* dZ, const void
   p.dW = dW;
   p.accumulate = accumulate_dW ? 1 : 0;
   const bool bf16 = P->desc.dtype == SMOES_BF16;
+  uint32_t* status = static_cast<uint32_t*>(ws);
   cudaError_t e = cudaSuccess;
-  if (dX) e = launch_expert_dx(p, bf16, stream);
-  if (e == cudaSuccess && dW) e = launch_expert_dw(p, bf16, stream);
+  if (dX) e = bf16 ? launch_expert_gemm(p, kGemmGradX, status, P->limit_ns, P->n_sms, stream) : launch_expert_dx(p, stream);
+  if (e == cudaSuccess && dW)
+    e = bf16 ? launch_expert_gemm(p, kGemmGradW, status, P->limit_ns, P->n_sms, stream) : launch_expert_dw(p, stream);
   return cuda_status(e);
 }
 

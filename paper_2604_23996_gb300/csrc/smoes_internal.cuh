@@ -265,6 +265,11 @@ cudaError_t static_perm_scratch(StaticPermScratch** out);
 cudaError_t launch_static_perm_prep(StaticPermScratch* sp, const int32_t* expert_bin,
                                     const int32_t* expert_slot, int E, cudaStream_t s);
 
+// Tiled TMA map of a row-major bf16 tensor of `rank` dimensions, innermost first (api.cu); strides in
+// bytes of dimensions 1 and up. Reads outside give zeros.
+bool encode_bf16(CUtensorMap* m, const void* ptr, int rank, const uint64_t* dims, const uint64_t* strides,
+                 const uint32_t* box);
+
 // ------------------------------------------------------------------ launchers (in .cu files)
 // Every kernel of the library is launched with programmatic stream serialization: its CTAs may
 // be scheduled while the kernel before it in the stream is finishing, which hides the launch
