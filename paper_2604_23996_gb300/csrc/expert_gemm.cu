@@ -272,7 +272,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
       const GemmTile t = gemm_tile<kMode>(p, first, tile);
       const int half_n = gemm_n<kMode>(t) / 2;
       for (int kb = 0; kb < t.blocks; ++kb) {
-        if (!warp_wait_cluster(&bars.empty[st], ph ^ 1, wc)) { ok = false; break; }
+        if (!warp_wait(&bars.empty[st], ph ^ 1, wc)) { ok = false; break; }
         if (elect_one()) {
           uint8_t* a = sa + st * kGemmHalf;
           uint8_t* b = sb + st * kGemmHalf;
@@ -286,7 +286,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
               mbar_arrive_expect_tx(&bars.tail[st], bytes);
             } else {
               bar = peer_smem(&bars.full[st], 0);
-              mbar_arrive_expect_tx_cluster(bar, bytes);
+              mbar_arrive_expect_tx_peer(bar, bytes);
             }
             const int i0 = t.m * 256 + static_cast<int>(rank) * 128;
             tma_load_2d_pair(a, &tmA, bar, i0, r0);
@@ -295,7 +295,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
             for (int i = 0; i < boxes; ++i) tma_load_2d_pair(b + i * 8192, &tmB, bar, c0 + 64 * i, r0);
           } else {
             const uint32_t bar = peer_smem(&bars.full[st], 0);
-            mbar_arrive_expect_tx_cluster(bar, kGemmHalf + half_n * 128u);
+            mbar_arrive_expect_tx_peer(bar, kGemmHalf + half_n * 128u);
             const int k0 = kb * kGemmK;
             if (kMode == kGemmForward) {
               if (l.gated) {
@@ -325,7 +325,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     }
     // every stage given back: no commit of the first CTA is still on its way to this one when it ends
     for (int i = 0; ok && i < kGemmStages; ++i) {
-      ok = warp_wait_cluster(&bars.empty[st], ph ^ 1, wc);
+      ok = warp_wait(&bars.empty[st], ph ^ 1, wc);
       if (++st == kGemmStages) { st = 0; ph ^= 1; }
     }
   } else if (warp == 1 && rank == 0) {
@@ -339,12 +339,12 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
       const uint32_t idesc = idesc_bf16(256, gemm_n<kMode>(t), kMajorA, kMajorB);
       const int chunk = kMode == kGemmGradW ? kGemmChunk : t.blocks;
       for (int k0 = 0; ok && k0 < t.blocks; k0 += chunk) {
-        if (!warp_wait_cluster(&bars.acc_empty[acc], aph ^ 1, wc)) { ok = false; break; }
+        if (!warp_wait(&bars.acc_empty[acc], aph ^ 1, wc)) { ok = false; break; }
         tc_fence_after();
         const uint32_t d = tmem + acc * 256;
         const int k1 = min(k0 + chunk, t.blocks);
         for (int kb = k0; kb < k1; ++kb) {
-          if (!warp_wait_cluster(&bars.full[st], ph, wc)) { ok = false; break; }
+          if (!warp_wait(&bars.full[st], ph, wc)) { ok = false; break; }
           tc_fence_after();
           if (elect_one()) {
             const uint32_t a = smem_u32(sa + st * kGemmHalf), b = smem_u32(sb + st * kGemmHalf);
@@ -383,7 +383,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
       }
       fence_proxy_async_smem();
       __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(peer_smem(&bars.full[s], 0));
+      if (lane == 0) mbar_arrive_peer_release(peer_smem(&bars.full[s], 0));
       __syncwarp();
     }
   } else if (warp >= 4) {
@@ -415,7 +415,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
 #pragma unroll
           for (int i = 0; i < 32; ++i) sum[c][i] = 0.f;
         for (int k0 = 0; k0 < t.blocks; k0 += kGemmChunk) {
-          if (!warp_wait_cluster(&bars.acc_full[acc], aph, wc)) { ok = false; break; }
+          if (!warp_wait(&bars.acc_full[acc], aph, wc)) { ok = false; break; }
           tc_fence_after();
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
@@ -429,7 +429,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
           }
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive_cluster(peer_smem(&bars.acc_empty[acc], 0));
+          if (lane == 0) mbar_arrive_peer(peer_smem(&bars.acc_empty[acc], 0));
           if (++acc == 2) { acc = 0; aph ^= 1; }
         }
         const int i = t.m * 256 + static_cast<int>(rank) * 128 + 32 * q + lane;
@@ -456,7 +456,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
         const bool f_in = f < p.n_feat;
         float bias = 0.f;
         if (kMode == kGemmForward && l.bias && f_in) bias = __ldg(l.bias + static_cast<long long>(t.e) * l.n_z + zf);
-        if (!warp_wait_cluster(&bars.acc_full[acc], aph, wc)) { ok = false; break; }
+        if (!warp_wait(&bars.acc_full[acc], aph, wc)) { ok = false; break; }
         tc_fence_after();
         const int chunks = (t.cols + 31) / 32;
         for (int c = g; c < chunks; c += 2) {
@@ -471,7 +471,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(peer_smem(&bars.acc_empty[acc], 0));
+        if (lane == 0) mbar_arrive_peer(peer_smem(&bars.acc_empty[acc], 0));
         if (++acc == 2) { acc = 0; aph ^= 1; }
       }
     }
