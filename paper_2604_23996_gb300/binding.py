@@ -285,6 +285,17 @@ def smoes_adaptive_bins(plan, expert_counts, beta, C_bar, expert_bin, f_spec=Non
                                     _p(f_spec), _stream(stream))
 
 
+# The expert layer's calls take addresses as plain integers (a layer of a few tokens takes less time on the
+# GPU than the marshalling of its arguments).
+
+def _ptr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
+def _raw(stream):
+    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+
+
 def smoes_experts_create(T, E, k, dtype, max_width=0):
     """Returns (status, plan handle) of an expert layer."""
     desc = ExpertsDesc(T, E, k, dtype, max_width)
@@ -302,7 +313,7 @@ def smoes_experts_workspace_bytes(plan) -> int:
 
 
 def smoes_experts_workspace_init(plan, ws, stream=None) -> int:
-    return _lib.smoes_experts_workspace_init(plan, _p(ws), ws.numel() * ws.element_size(), _stream(stream))
+    return _lib.smoes_experts_workspace_init(plan, _ptr(ws), ws.numel() * ws.element_size(), _raw(stream))
 
 
 def smoes_experts_set_wait_limit(plan, limit_ns: int) -> int:
@@ -310,48 +321,50 @@ def smoes_experts_set_wait_limit(plan, limit_ns: int) -> int:
 
 
 def smoes_experts_read_status(plan, ws, stream=None) -> int:
-    return _lib.smoes_experts_read_status(plan, _p(ws), _stream(stream))
+    return _lib.smoes_experts_read_status(plan, _ptr(ws), _raw(stream))
 
 
 def smoes_expert_sort(plan, topk_idx, expert_offsets, row_slot, slot_row, ws, stream=None) -> int:
-    return _lib.smoes_expert_sort(plan, _p(topk_idx), _p(expert_offsets), _p(row_slot), _p(slot_row), _p(ws),
-                                  ws.numel() * ws.element_size(), _stream(stream))
+    return _lib.smoes_expert_sort(plan, _ptr(topk_idx), _ptr(expert_offsets), _ptr(row_slot), _ptr(slot_row),
+                                  _ptr(ws), ws.numel() * ws.element_size(), _raw(stream))
 
 
 def smoes_expert_dispatch(plan, X, d, expert_offsets, slot_row, Xs, stream=None) -> int:
-    return _lib.smoes_expert_dispatch(plan, _p(X), int(d), _p(expert_offsets), _p(slot_row), _p(Xs), _stream(stream))
+    return _lib.smoes_expert_dispatch(plan, _ptr(X), int(d), _ptr(expert_offsets), _ptr(slot_row), _ptr(Xs),
+                                      _raw(stream))
 
 
 def smoes_expert_dispatch_bwd(plan, dXs, d, slot_row, residual, dX, stream=None) -> int:
-    return _lib.smoes_expert_dispatch_bwd(plan, _p(dXs), int(d), _p(slot_row), _p(residual), _p(dX), _stream(stream))
+    return _lib.smoes_expert_dispatch_bwd(plan, _ptr(dXs), int(d), _ptr(slot_row), _ptr(residual), _ptr(dX),
+                                          _raw(stream))
 
 
 def smoes_expert_combine(plan, Ys, d, topk_w, slot_row, residual, Y, stream=None) -> int:
-    return _lib.smoes_expert_combine(plan, _p(Ys), int(d), _p(topk_w), _p(slot_row), _p(residual), _p(Y),
-                                     _stream(stream))
+    return _lib.smoes_expert_combine(plan, _ptr(Ys), int(d), _ptr(topk_w), _ptr(slot_row), _ptr(residual), _ptr(Y),
+                                     _raw(stream))
 
 
 def smoes_expert_combine_bwd(plan, dY, Ys, d, topk_w, expert_offsets, slot_row, dYs, d_topk_w, stream=None) -> int:
-    return _lib.smoes_expert_combine_bwd(plan, _p(dY), _p(Ys), int(d), _p(topk_w), _p(expert_offsets), _p(slot_row),
-                                         _p(dYs), _p(d_topk_w), _stream(stream))
+    return _lib.smoes_expert_combine_bwd(plan, _ptr(dY), _ptr(Ys), int(d), _ptr(topk_w), _ptr(expert_offsets), _ptr(slot_row),
+                                         _ptr(dYs), _ptr(d_topk_w), _raw(stream))
 
 
 def smoes_expert_linear(plan, X, W, bias, residual, n_in, n_out, act, gated, expert_offsets, out, pre, ws,
                         stream=None) -> int:
-    args = LinearArgs(_p(X), _p(W), _p(bias), _p(residual), int(n_in), int(n_out), int(act), int(gated))
-    return _lib.smoes_expert_linear(plan, C.byref(args), _p(expert_offsets), _p(out), _p(pre), _p(ws),
-                                    ws.numel() * ws.element_size(), _stream(stream))
+    args = LinearArgs(_ptr(X), _ptr(W), _ptr(bias), _ptr(residual), int(n_in), int(n_out), int(act), int(gated))
+    return _lib.smoes_expert_linear(plan, C.byref(args), _ptr(expert_offsets), _ptr(out), _ptr(pre), _ptr(ws),
+                                    ws.numel() * ws.element_size(), _raw(stream))
 
 
 def smoes_expert_act_bwd(plan, dOut, pre, n_out, act, gated, expert_offsets, dZ, db, ws, stream=None) -> int:
-    return _lib.smoes_expert_act_bwd(plan, _p(dOut), _p(pre), int(n_out), int(act), int(gated), _p(expert_offsets),
-                                     _p(dZ), _p(db), _p(ws), ws.numel() * ws.element_size(), _stream(stream))
+    return _lib.smoes_expert_act_bwd(plan, _ptr(dOut), _ptr(pre), int(n_out), int(act), int(gated), _ptr(expert_offsets),
+                                     _ptr(dZ), _ptr(db), _ptr(ws), ws.numel() * ws.element_size(), _raw(stream))
 
 
 def smoes_expert_linear_bwd(plan, dZ, X, W, n_in, n_z, expert_offsets, dX, dW, accumulate_dW, ws, stream=None) -> int:
-    return _lib.smoes_expert_linear_bwd(plan, _p(dZ), _p(X), _p(W), int(n_in), int(n_z), _p(expert_offsets), _p(dX),
-                                        _p(dW), int(accumulate_dW), _p(ws), ws.numel() * ws.element_size(),
-                                        _stream(stream))
+    return _lib.smoes_expert_linear_bwd(plan, _ptr(dZ), _ptr(X), _ptr(W), int(n_in), int(n_z), _ptr(expert_offsets), _ptr(dX),
+                                        _ptr(dW), int(accumulate_dW), _ptr(ws), ws.numel() * ws.element_size(),
+                                        _raw(stream))
 
 
 # ----------------------------------------------------------------------------- convenience
@@ -453,6 +466,7 @@ class Experts:
         self.dtype = torch.bfloat16 if dtype == SMOES_BF16 else torch.float32
         self.ws = torch.empty(smoes_experts_workspace_bytes(self.plan), dtype=torch.uint8, device=device)
         self.device = self.ws.device
+        self._index = self.device.index
         _check(smoes_experts_workspace_init(self.plan, self.ws), "smoes_experts_workspace_init")
         self.expert_offsets = torch.zeros(E + 1, dtype=torch.int32, device=device)
         self.row_slot = torch.full((self.R,), -1, dtype=torch.int32, device=device)
@@ -467,6 +481,10 @@ class Experts:
             smoes_experts_destroy(self.plan)
         except Exception:
             pass
+
+    def _on(self, stream):
+        """The stream given, or the current one of the plan's device."""
+        return torch.cuda.current_stream(self._index) if stream is None else stream
 
     def _want(self, name, t, shape, dtype=None):
         """Checks one argument (None stays None)."""
@@ -488,7 +506,7 @@ class Experts:
         expert_offsets, row_slot, slot_row."""
         self._want("topk_idx", topk_idx, (self.T, self.k), torch.int32)
         _check(smoes_expert_sort(self.plan, topk_idx, self.expert_offsets, self.row_slot, self.slot_row, self.ws,
-                                 stream), "smoes_expert_sort")
+                                 self._on(stream)), "smoes_expert_sort")
         return self.expert_offsets, self.row_slot, self.slot_row
 
     def dispatch(self, X, out=None, stream=None):
@@ -496,7 +514,7 @@ class Experts:
         d = X.shape[-1]
         self._want("X", X, (self.T, d))
         out = self._out(out, (self.R, d))
-        _check(smoes_expert_dispatch(self.plan, X, d, self.expert_offsets, self.slot_row, out, stream),
+        _check(smoes_expert_dispatch(self.plan, X, d, self.expert_offsets, self.slot_row, out, self._on(stream)),
                "smoes_expert_dispatch")
         return out
 
@@ -506,7 +524,7 @@ class Experts:
         self._want("dXs", dXs, (self.R, d))
         self._want("residual", residual, (self.T, d))
         out = self._out(out, (self.T, d))
-        _check(smoes_expert_dispatch_bwd(self.plan, dXs, d, self.slot_row, residual, out, stream),
+        _check(smoes_expert_dispatch_bwd(self.plan, dXs, d, self.slot_row, residual, out, self._on(stream)),
                "smoes_expert_dispatch_bwd")
         return out
 
@@ -517,7 +535,7 @@ class Experts:
         self._want("topk_w", topk_w, (self.T, self.k), torch.float32)
         self._want("residual", residual, (self.T, d))
         out = self._out(out, (self.T, d))
-        _check(smoes_expert_combine(self.plan, Ys, d, topk_w, self.slot_row, residual, out, stream),
+        _check(smoes_expert_combine(self.plan, Ys, d, topk_w, self.slot_row, residual, out, self._on(stream)),
                "smoes_expert_combine")
         return out
 
@@ -530,7 +548,7 @@ class Experts:
         dYs = self._out(dYs, (self.R, d))
         d_topk_w = self._out(d_topk_w, (self.T, self.k), torch.float32)
         _check(smoes_expert_combine_bwd(self.plan, dY, Ys, d, topk_w, self.expert_offsets, self.slot_row, dYs,
-                                        d_topk_w, stream), "smoes_expert_combine_bwd")
+                                        d_topk_w, self._on(stream)), "smoes_expert_combine_bwd")
         return dYs, d_topk_w
 
     def linear(self, X, W, bias=None, act=SMOES_ACT_NONE, gated=False, residual=None, save_pre=False, out=None,
@@ -549,7 +567,7 @@ class Experts:
         if save_pre or pre is not None:
             pre = self._out(pre, (self.R, n_z))
         _check(smoes_expert_linear(self.plan, X, W, bias, residual, n_in, n_out, act, gated, self.expert_offsets,
-                                   out, pre, self.ws, stream), "smoes_expert_linear")
+                                   out, pre, self.ws, self._on(stream)), "smoes_expert_linear")
         return out, pre
 
     def act_bwd(self, dOut, pre=None, act=SMOES_ACT_NONE, gated=False, bias_grad=False, dZ=None, db=None,
@@ -564,14 +582,14 @@ class Experts:
         if act == SMOES_ACT_NONE and not gated:
             if db is not None:
                 _check(smoes_expert_act_bwd(self.plan, dOut, None, n_out, act, gated, self.expert_offsets, None, db,
-                                            self.ws, stream), "smoes_expert_act_bwd")
+                                            self.ws, self._on(stream)), "smoes_expert_act_bwd")
             return dOut, db
         if pre is None:
             raise ValueError("pre: the pre-activations that linear saved are wanted")
         self._want("pre", pre, (self.R, n_z))
         dZ = self._out(dZ, (self.R, n_z))
         _check(smoes_expert_act_bwd(self.plan, dOut, pre, n_out, act, gated, self.expert_offsets, dZ, db, self.ws,
-                                    stream), "smoes_expert_act_bwd")
+                                    self._on(stream)), "smoes_expert_act_bwd")
         return dZ, db
 
     def linear_bwd(self, dZ, X, W, need_dX=True, need_dW=True, dX=None, dW=None, accumulate=False, stream=None):
@@ -585,8 +603,8 @@ class Experts:
         dX = self._out(dX, (self.R, n_in)) if need_dX else None
         dW = self._out(dW, (self.E, n_z, n_in), torch.float32) if need_dW else None
         _check(smoes_expert_linear_bwd(self.plan, dZ, X, W, n_in, n_z, self.expert_offsets, dX, dW, accumulate,
-                                       self.ws, stream), "smoes_expert_linear_bwd")
+                                       self.ws, self._on(stream)), "smoes_expert_linear_bwd")
         return dX, dW
 
     def device_status(self, stream=None):
-        return smoes_experts_read_status(self.plan, self.ws, stream)
+        return smoes_experts_read_status(self.plan, self.ws, self._on(stream))

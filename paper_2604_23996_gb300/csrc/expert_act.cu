@@ -1,9 +1,11 @@
 // expert_act.cu -- gradient of the experts' activation and bias:
 //   dz = dout act'(z), or gated dz_g = dout u act'(g), dz_u = dout act(g);   db_e = sum over e's rows of dz
 //
-// One pass over dOut and pre. A block takes a chunk of at most 256 rows of one expert and 32 x 16 bytes
-// of columns: a row per warp, then the eight warps' column sums are added in order into one partial
-// per chunk; a second small kernel adds each expert's partials in order. Bound by HBM.
+// One pass over dOut and pre. A block takes a chunk of at most 64 rows of one expert and 32 x 16 bytes
+// of columns, a row per warp, two rows' loads in flight; the eight warps' column sums are added in order into
+// one partial per chunk, and a second small kernel adds each expert's partials in a fixed order. Bound by HBM.
+// With chunks of 256 rows, CUDA's accurate functions and two exponentials a value, 30035 x 704 gated took
+// 116 us.
 #include "experts.cuh"
 #include "ptx.cuh"
 
@@ -16,6 +18,7 @@ constexpr int kActWarps = kActThreads / 32;
 template <class T>
 __global__ void __launch_bounds__(kActThreads) k_act_bwd(const ExpertActParams p) {
   constexpr int N = Pack<T>::N;
+  constexpr bool kFast = sizeof(T) == 2;
   __shared__ float sum_s[2][kActWarps][32 * N];
   pdl_wait();
   pdl_trigger();
@@ -30,9 +33,11 @@ __global__ void __launch_bounds__(kActThreads) k_act_bwd(const ExpertActParams p
   for (int i = 0; i < N; ++i) sg[i] = su[i] = 0.f;
   const long long end = min(t.row0 + kActChunk, t.row1);
   if (in) {
+#pragma unroll 2
     for (long long r = t.row0 + warp; r < end; r += kActWarps) {
       float d[N], z[N], u[N], o[N];
-      Pack<T>::unpack(__ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(p.dOut) + r * p.n_out + c0)), d);
+      const uint4 d4 = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(p.dOut) + r * p.n_out + c0));
+      Pack<T>::unpack(d4, d);
       if (!p.dZ) {
 #pragma unroll
         for (int i = 0; i < N; ++i) sg[i] += d[i];
@@ -40,23 +45,26 @@ __global__ void __launch_bounds__(kActThreads) k_act_bwd(const ExpertActParams p
       }
       const T* pre = static_cast<const T*>(p.pre) + r * p.n_z + c0;
       T* dz = static_cast<T*>(p.dZ) + r * p.n_z + c0;
-      Pack<T>::unpack(__ldg(reinterpret_cast<const uint4*>(pre)), z);
-      if (p.gated) {
-        Pack<T>::unpack(__ldg(reinterpret_cast<const uint4*>(pre + p.n_out)), u);
+      const uint4 z4 = __ldg(reinterpret_cast<const uint4*>(pre));
+      const uint4 u4 = p.gated ? __ldg(reinterpret_cast<const uint4*>(pre + p.n_out)) : z4;
+      Pack<T>::unpack(z4, z);
+      Pack<T>::unpack(u4, u);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          o[i] = d[i] * act_value(p.act, z[i]);
-          su[i] += o[i];
-          d[i] *= u[i];
-        }
+      for (int i = 0; i < N; ++i) {
+        float value, slope;
+        act_value_slope<kFast>(p.act, z[i], value, slope);
+        o[i] = d[i] * value;
+        if (p.gated) d[i] *= u[i];
+        z[i] = d[i] * slope;
+      }
+      if (p.gated) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) su[i] += o[i];
         *reinterpret_cast<uint4*>(dz + p.n_out) = Pack<T>::pack(o);
       }
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        o[i] = d[i] * act_slope(p.act, z[i]);
-        sg[i] += o[i];
-      }
-      *reinterpret_cast<uint4*>(dz) = Pack<T>::pack(o);
+      for (int i = 0; i < N; ++i) sg[i] += z[i];
+      *reinterpret_cast<uint4*>(dz) = Pack<T>::pack(z);
     }
   }
   if (!p.db) return;
@@ -77,24 +85,47 @@ __global__ void __launch_bounds__(kActThreads) k_act_bwd(const ExpertActParams p
   }
 }
 
-// db_e = the sum of e's partials, in row order.
+// db_e = the sum of e's partials: 128 columns a block, warp w adds partials w, w + 8, ..., then the warps' sums
+// in order.
 __global__ void __launch_bounds__(kActThreads) k_act_bias(const ExpertActParams p) {
+  __shared__ float4 sum_s[kActWarps][32];
   pdl_wait();
   pdl_trigger();
-  const int e = blockIdx.y, c = blockIdx.x * kActThreads + threadIdx.x;
-  long long first = 0;                                   // the expert's first chunk
-  for (int i = 0; i < e; ++i) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int e = blockIdx.y, c = (blockIdx.x * 32 + lane) * 4;
+  // the expert's first chunk: the chunks of the experts before it, counted by the lanes of every warp
+  int before = 0;
+  for (int i = lane; i < e; i += 32) {
     const long long rows = expert_begin(p.offsets, i + 1, p.R) - expert_begin(p.offsets, i, p.R);
-    if (rows > 0) first += (rows + kActChunk - 1) / kActChunk;
+    if (rows > 0) before += static_cast<int>((rows + kActChunk - 1) / kActChunk);
   }
+  const long long first = __reduce_add_sync(0xffffffffu, before);
   const long long rows = expert_begin(p.offsets, e + 1, p.R) - expert_begin(p.offsets, e, p.R);
   long long n = rows > 0 ? (rows + kActChunk - 1) / kActChunk : 0;
   n = min(n, p.R / kActChunk + p.E - first);             // the partials there are room for
-  if (c >= p.n_z) return;
-  float a = 0.f;
+  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (c < p.n_z) {
 #pragma unroll 8
-  for (long long i = 0; i < n; ++i) a += __ldcg(p.part + (first + i) * p.n_z + c);
-  p.db[static_cast<long long>(e) * p.n_z + c] = a;
+    for (long long i = warp; i < n; i += kActWarps) {
+      const float4 v = __ldcg(reinterpret_cast<const float4*>(p.part + (first + i) * p.n_z + c));
+      a.x += v.x;
+      a.y += v.y;
+      a.z += v.z;
+      a.w += v.w;
+    }
+  }
+  sum_s[warp][lane] = a;
+  __syncthreads();
+  if (warp == 0 && c < p.n_z) {
+    for (int w = 1; w < kActWarps; ++w) {
+      const float4 v = sum_s[w][lane];
+      a.x += v.x;
+      a.y += v.y;
+      a.z += v.z;
+      a.w += v.w;
+    }
+    *reinterpret_cast<float4*>(p.db + static_cast<long long>(e) * p.n_z + c) = a;
+  }
 }
 
 }  // namespace
@@ -106,7 +137,7 @@ cudaError_t launch_expert_act_bwd(const ExpertActParams& p, bool bf16, cudaStrea
   cudaError_t e = bf16 ? launch_pdl(k_act_bwd<__nv_bfloat16>, grid, dim3(kActThreads), 0, s, p)
                        : launch_pdl(k_act_bwd<float>, grid, dim3(kActThreads), 0, s, p);
   if (e == cudaSuccess && p.db)
-    e = launch_pdl(k_act_bias, dim3((p.n_z + kActThreads - 1) / kActThreads, p.E), dim3(kActThreads), 0, s, p);
+    e = launch_pdl(k_act_bias, dim3((p.n_z + 127) / 128, p.E), dim3(kActThreads), 0, s, p);
   return e;
 }
 

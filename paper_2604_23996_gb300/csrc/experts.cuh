@@ -10,7 +10,7 @@ namespace smoes {
 
 constexpr int kExpertsMax = 256;           // experts of an expert-layer plan
 constexpr int kExpertWidthMax = 1 << 20;   // widest row
-constexpr int kActChunk = 256;             // rows per partial sum of the bias gradient
+constexpr int kActChunk = 64;              // rows per partial sum of the bias gradient
 
 struct ExpertSortParams {
   long long n;               // selections T * k
@@ -192,20 +192,53 @@ __device__ __forceinline__ void zero_rows(void* base, long long first, long long
     out[i] = make_uint4(0u, 0u, 0u, 0u);
 }
 
-// Activations and their slopes. Accurate form, for fp32 results.
+// Activations and their slopes. kFast: for results that are rounded to bf16, whose step is 2^-8: the fast
+// exponential and division (a few steps of 2^-22), and erfc by the rational form of Abramowitz and Stegun,
+// Handbook of Mathematical Functions, 7.1.26 (absolute error 1.5e-7), which shares its e^(-z^2 / 2) with the slope
+// (an epilogue with erfcf takes longer than the products it follows). Otherwise CUDA's accurate functions.
+template <bool kFast>
+__device__ __forceinline__ float sigmoid_of(float z) {
+  return kFast ? __fdividef(1.f, 1.f + __expf(-z)) : 1.f / (1.f + expf(-z));
+}
+// Phi(z) and phi(z), the normal distribution's function and density.
+template <bool kFast>
+__device__ __forceinline__ float normal_of(float z, float& density) {
+  if (!kFast) {
+    density = expf(-0.5f * z * z) * 0.39894228f;
+    return 0.5f * erfcf(z * -0.70710678f);
+  }
+  const float e = __expf(-0.5f * z * z);
+  density = e * 0.39894228f;
+  const float t = __fdividef(1.f, fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.f));
+  float q = fmaf(1.061405429f, t, -1.453152027f);        // erfc(|z| / sqrt 2) = t q(t) e^(-z^2 / 2)
+  q = fmaf(q, t, 1.421413741f);
+  q = fmaf(q, t, -0.284496736f);
+  q = fmaf(q, t, 0.254829592f);
+  const float half = 0.5f * q * t * e;
+  return z < 0.f ? half : 1.f - half;
+}
+template <bool kFast>
 __device__ __forceinline__ float act_value(int act, float z) {
-  if (act == SMOES_ACT_SILU) return z / (1.f + expf(-z));
-  if (act == SMOES_ACT_GELU) return 0.5f * z * erfcf(z * -0.70710678f);
+  float density;
+  if (act == SMOES_ACT_SILU) return kFast ? z * sigmoid_of<true>(z) : z / (1.f + expf(-z));
+  if (act == SMOES_ACT_GELU) return z * normal_of<kFast>(z, density);
   return z;
 }
-__device__ __forceinline__ float act_slope(int act, float z) {
+template <bool kFast>
+__device__ __forceinline__ void act_value_slope(int act, float z, float& value, float& slope) {
   if (act == SMOES_ACT_SILU) {
-    const float s = 1.f / (1.f + expf(-z));
-    return s * (1.f + z * (1.f - s));
+    const float s = sigmoid_of<kFast>(z);
+    value = z * s;
+    slope = fmaf(value, 1.f - s, s);
+  } else if (act == SMOES_ACT_GELU) {
+    float density;
+    const float n = normal_of<kFast>(z, density);
+    value = z * n;
+    slope = fmaf(z, density, n);
+  } else {
+    value = z;
+    slope = 1.f;
   }
-  if (act == SMOES_ACT_GELU)
-    return 0.5f * erfcf(z * -0.70710678f) + z * expf(-0.5f * z * z) * 0.39894228f;
-  return 1.f;
 }
 
 }  // namespace smoes
