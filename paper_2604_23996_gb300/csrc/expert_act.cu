@@ -2,7 +2,7 @@
 //   dz = dout act'(z), or gated dz_g = dout u act'(g), dz_u = dout act(g);   db_e = sum over e's rows of dz
 //
 // One pass over dOut and pre. A block takes a chunk of at most 64 rows of one expert and 32 x 16 bytes
-// of columns, a row per warp, two rows' loads in flight; the eight warps' column sums are added in order into
+// of columns, four rows' loads in flight a warp; the eight warps' column sums are added in order into
 // one partial per chunk, and a second small kernel adds each expert's partials in a fixed order. Bound by HBM.
 // With chunks of 256 rows, CUDA's accurate functions and two exponentials a value, 30035 x 704 gated took
 // 116 us.
@@ -14,9 +14,10 @@ namespace {
 
 constexpr int kActThreads = 256;
 constexpr int kActWarps = kActThreads / 32;
+constexpr int kActRows = 4;                      // rows a warp has in flight
 
 template <class T>
-__global__ void __launch_bounds__(kActThreads) k_act_bwd(const ExpertActParams p) {
+__global__ void __launch_bounds__(kActThreads, 2) k_act_bwd(const ExpertActParams p) {
   constexpr int N = Pack<T>::N;
   constexpr bool kFast = sizeof(T) == 2;
   __shared__ float sum_s[2][kActWarps][32 * N];
@@ -33,38 +34,50 @@ __global__ void __launch_bounds__(kActThreads) k_act_bwd(const ExpertActParams p
   for (int i = 0; i < N; ++i) sg[i] = su[i] = 0.f;
   const long long end = min(t.row0 + kActChunk, t.row1);
   if (in) {
-#pragma unroll 2
-    for (long long r = t.row0 + warp; r < end; r += kActWarps) {
-      float d[N], z[N], u[N], o[N];
-      const uint4 d4 = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(p.dOut) + r * p.n_out + c0));
-      Pack<T>::unpack(d4, d);
-      if (!p.dZ) {
+    for (long long r0 = t.row0 + warp; r0 < end; r0 += kActWarps * kActRows) {
+      uint4 d4[kActRows], z4[kActRows], u4[kActRows];    // every load of the warp's rows before the first use
 #pragma unroll
-        for (int i = 0; i < N; ++i) sg[i] += d[i];
-        continue;
-      }
-      const T* pre = static_cast<const T*>(p.pre) + r * p.n_z + c0;
-      T* dz = static_cast<T*>(p.dZ) + r * p.n_z + c0;
-      const uint4 z4 = __ldg(reinterpret_cast<const uint4*>(pre));
-      const uint4 u4 = p.gated ? __ldg(reinterpret_cast<const uint4*>(pre + p.n_out)) : z4;
-      Pack<T>::unpack(z4, z);
-      Pack<T>::unpack(u4, u);
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        float value, slope;
-        act_value_slope<kFast>(p.act, z[i], value, slope);
-        o[i] = d[i] * value;
-        if (p.gated) d[i] *= u[i];
-        z[i] = d[i] * slope;
-      }
-      if (p.gated) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) su[i] += o[i];
-        *reinterpret_cast<uint4*>(dz + p.n_out) = Pack<T>::pack(o);
+      for (int j = 0; j < kActRows; ++j) {
+        const long long r = r0 + j * kActWarps;
+        d4[j] = z4[j] = u4[j] = make_uint4(0u, 0u, 0u, 0u);
+        if (r >= end) continue;
+        d4[j] = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(p.dOut) + r * p.n_out + c0));
+        if (!p.dZ) continue;
+        const T* pre = static_cast<const T*>(p.pre) + r * p.n_z + c0;
+        z4[j] = __ldg(reinterpret_cast<const uint4*>(pre));
+        if (p.gated) u4[j] = __ldg(reinterpret_cast<const uint4*>(pre + p.n_out));
       }
 #pragma unroll
-      for (int i = 0; i < N; ++i) sg[i] += z[i];
-      *reinterpret_cast<uint4*>(dz) = Pack<T>::pack(z);
+      for (int j = 0; j < kActRows; ++j) {
+        const long long r = r0 + j * kActWarps;
+        if (r >= end) break;
+        float d[N], z[N], u[N], o[N];
+        Pack<T>::unpack(d4[j], d);
+        if (!p.dZ) {
+#pragma unroll
+          for (int i = 0; i < N; ++i) sg[i] += d[i];
+          continue;
+        }
+        Pack<T>::unpack(z4[j], z);
+        Pack<T>::unpack(u4[j], u);
+        T* dz = static_cast<T*>(p.dZ) + r * p.n_z + c0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          float value, slope;
+          act_value_slope<kFast>(p.act, z[i], value, slope);
+          o[i] = d[i] * value;
+          if (p.gated) d[i] *= u[i];
+          z[i] = d[i] * slope;
+        }
+        if (p.gated) {
+#pragma unroll
+          for (int i = 0; i < N; ++i) su[i] += o[i];
+          *reinterpret_cast<uint4*>(dz + p.n_out) = Pack<T>::pack(o);
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) sg[i] += z[i];
+        *reinterpret_cast<uint4*>(dz) = Pack<T>::pack(z);
+      }
     }
   }
   if (!p.db) return;

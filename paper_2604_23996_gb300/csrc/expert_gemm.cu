@@ -32,14 +32,14 @@ namespace {
 
 constexpr int kGemmThreads = 384;
 constexpr int kGemmEpiWarps = 8;
-constexpr int kGemmStages = 6;
+constexpr int kGemmStages = 5;
 constexpr int kGemmK = 64;                       // depth of a block: 128 bytes of bf16
 constexpr uint32_t kGemmHalf = 128 * kGemmK * 2; // one CTA's operand of a block: 16 KB
 // dW: rows summed by the tensor cores before the sum moves to fp32 registers. The tensor cores cut each
 // addition off towards zero: relative error 4.7e-7 after 512 products, 1.5e-6 after 1536, 9e-6 after 8192.
 constexpr int kGemmChunk = 8;                    // blocks of 64 rows
 
-constexpr uint32_t kGemmStaging = 16384;         // one epilogue group's output boxes
+constexpr uint32_t kGemmStaging = 32768;         // one epilogue group's output boxes: two chunks of 16 KB
 // alignment, operands, output boxes, barriers, [E + 1] row tiles before each expert
 constexpr uint32_t kGemmSmem = 1024 + kGemmStages * 2 * kGemmHalf + 2 * kGemmStaging + 512 + 4 * (kExpertsMax + 1);
 static_assert(kGemmSmem <= 227 * 1024, "shared memory of a CTA");
@@ -118,52 +118,61 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 // swizzled words lie in different banks. Stored from the lanes, 4 bytes each, the 32-byte pieces of pre made
 // dsmoe_vlm's gated layer take 557 us instead of 446 without pre.
 
-__device__ __forceinline__ void put_pair(uint8_t* boxes, int row, int f, uint32_t w) {
-  *reinterpret_cast<uint32_t*>(boxes + (f >> 6) * 4096 + sw128_offset(row, f & 63)) = w;
+// Shared addresses of a lane's words: its features f & ~1 and the next in box row 4 odd, with the row's swizzle;
+// word i of four rows c + i lies at (at ^ i << 4) + (c + i) * 128 (c a multiple of 8: the swizzle is the row's low
+// three bits, and those of i and 4 do not meet).
+__device__ __forceinline__ uint32_t pair_address(const uint8_t* boxes, int f) {
+  const int odd = f & 1;
+  return smem_u32(boxes) + (f >> 6) * 4096 + sw128_offset(4 * odd, (f & 63) - odd);
 }
-// v: features of lane's box column f (of 128), one column of D a register.
+__device__ __forceinline__ void put_pair(uint32_t at, int row, uint32_t w) {     // row: without 4 odd
+  asm volatile("st.shared.u32 [%0], %1;" ::"r"((at ^ ((row & 3) << 4)) + row * 128), "r"(w) : "memory");
+}
+// One column of D a register; f: the lane's feature among the 128 of the boxes.
 __device__ __forceinline__ void put_chunk(uint8_t* boxes, int f, const float (&v)[32]) {
-  const int odd = threadIdx.x & 1;
+  const int odd = f & 1;
+  const uint32_t at = pair_address(boxes, f);
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const int c = (i >> 2) * 8 + (i & 3);
     const float got = __shfl_xor_sync(0xffffffffu, odd ? v[c] : v[c + 4], 1);
-    put_pair(boxes, c + 4 * odd, f - odd, odd ? pack_bf16(got, v[c + 4]) : pack_bf16(v[c], got));
+    put_pair(at, c, odd ? pack_bf16(got, v[c + 4]) : pack_bf16(v[c], got));
   }
 }
 
-// z (bias added) of a chunk to out, in shared memory, by whole warps. f: the lane's feature among the CTA's; res,
-// with a residual: that of the chunk's first row at the lane's even feature, read for `rows` rows (none where the
-// feature does not exist).
+// The residual of a chunk, at the places where put_forward adds it. res: that of the chunk's first row at the lane's
+// even feature, read for `rows` rows (none where the feature does not exist).
+__device__ __forceinline__ void load_residual(const ExpertLinearParams& l, const __nv_bfloat16* res, int rows,
+                                              uint32_t (&rv)[16]) {
+  const int odd = threadIdx.x & 1, up = (threadIdx.x >> 4) & 1;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int c = l.gated ? (i >> 1) * 8 + (i & 1) + 2 * up + 4 * odd : (i >> 2) * 8 + (i & 3) + 4 * odd;
+    rv[i] = c < rows ? __ldg(reinterpret_cast<const uint32_t*>(res + c * static_cast<long long>(l.n_out))) : 0u;
+  }
+}
+
+// z (bias added) of a chunk to out, in shared memory, by whole warps. f: the lane's feature among the CTA's.
 __device__ __forceinline__ void put_forward(const ExpertLinearParams& l, uint8_t* boxes, int f, float (&v)[32],
-                                            const __nv_bfloat16* res, int rows) {
+                                            const uint32_t (&rv)[16]) {
   const int odd = threadIdx.x & 1;
   if (!l.gated) {
     if (l.act) {
 #pragma unroll
       for (int c = 0; c < 32; ++c) v[c] = act_value<true>(l.act, v[c]);
     }
-    if (!l.residual) {
-      put_chunk(boxes, f, v);
-      return;
-    }
-    uint32_t rv[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int c = (i >> 2) * 8 + (i & 3) + 4 * odd;
-      rv[i] = c < rows ? __ldg(reinterpret_cast<const uint32_t*>(res + c * static_cast<long long>(l.n_out))) : 0u;
-    }
+    const uint32_t at = pair_address(boxes, f);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const int c = (i >> 2) * 8 + (i & 3);
       const float got = __shfl_xor_sync(0xffffffffu, odd ? v[c] : v[c + 4], 1);
       const float lo = (odd ? got : v[c]) + __uint_as_float(rv[i] << 16);
       const float hi = (odd ? v[c + 4] : got) + __uint_as_float(rv[i] & 0xffff0000u);
-      put_pair(boxes, c + 4 * odd, f - odd, pack_bf16(lo, hi));
+      put_pair(at, c, pack_bf16(lo, hi));
     }
     return;
   }
-  // gated: lanes 0-15 hold g, 16-31 u; of two columns each half finishes one
+  // gated: lanes 0-15 hold g, 16-31 u; of columns c and c + 2 each half finishes one
   const int up = (threadIdx.x >> 4) & 1;
   float y[16];                                   // columns 4 (i / 2) + i % 2 + 2 up
 #pragma unroll
@@ -173,17 +182,15 @@ __device__ __forceinline__ void put_forward(const ExpertLinearParams& l, uint8_t
     const float g = up ? got : v[c], u = up ? v[c + 2] : got;
     y[i] = act_value<true>(l.act, g) * u;
   }
+  // the half's two rows further down: the swizzle's bit of 2 with it
+  const uint32_t at = (pair_address(boxes, f) ^ (up << 5)) + up * 256;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {                  // columns c and c + 4
-    const int a = (i >> 1) * 4 + (i & 1), c = (a >> 1) * 4 + (a & 1) + 2 * up + 4 * odd;
+    const int a = (i >> 1) * 4 + (i & 1), c = (i >> 1) * 8 + (i & 1);
     const float got = __shfl_xor_sync(0xffffffffu, odd ? y[a] : y[a + 2], 1);
-    float lo = odd ? got : y[a], hi = odd ? y[a + 2] : got;
-    if (l.residual && c < rows) {
-      const uint32_t r = __ldg(reinterpret_cast<const uint32_t*>(res + c * static_cast<long long>(l.n_out)));
-      lo += __uint_as_float(r << 16);
-      hi += __uint_as_float(r & 0xffff0000u);
-    }
-    put_pair(boxes, c, f - odd, pack_bf16(lo, hi));
+    const float lo = (odd ? got : y[a]) + __uint_as_float(rv[i] << 16);
+    const float hi = (odd ? y[a + 2] : got) + __uint_as_float(rv[i] & 0xffff0000u);
+    put_pair(at, c, pack_bf16(lo, hi));
   }
 }
 
@@ -406,7 +413,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
         }
       }
     }
-    uint8_t* boxes = staging + g * kGemmStaging;
+    int buf = 0;                                 // the chunk's half of the group's staging
     const bool issuer = q == 0 && elect_one();   // issues the group's stores
     int acc = 0;
     uint32_t aph = 0;
@@ -462,6 +469,10 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
         const bool whole = f0 + width <= p.n_feat;
         const long long ld = p.n_feat;
         float bias = 0.f;
+        const __nv_bfloat16* res = static_cast<const __nv_bfloat16*>(l.residual) + f0 + (fl & ~1);
+        uint32_t rv[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) rv[i] = 0u;
         if (kMode == kGemmForward && l.bias && f_in) bias = __ldg(l.bias + static_cast<long long>(t.e) * l.n_z + zf);
         // one answer for the group: its barriers below count all four warps
         ok = named_bar_all(1 + g, 128, warp_wait(&bars.acc_full[acc], aph, wc));
@@ -469,6 +480,10 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
         tc_fence_after();
         const int chunks = (t.cols + 31) / 32;
         for (int c = g; c < chunks; c += 2) {
+          const long long row = t.row0 + c * 32;
+          const int rows = min(32, t.cols - c * 32);
+          if (kMode == kGemmForward && l.residual) load_residual(l, res + row * ld, f_in ? rows : 0, rv);
+          uint8_t* boxes = staging + g * kGemmStaging + buf * (kGemmStaging / 2);
           float v[32];
           tmem_ld32(tmem + acc * 256 + c * 32 + lanes, v);
           if (c + 2 >= chunks) {                 // the accumulator's last use
@@ -476,21 +491,17 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
             __syncwarp();
             if (lane == 0) mbar_arrive_peer(peer_smem(&bars.acc_empty[acc], 0));
           }
-          const long long row = t.row0 + c * 32;
-          const int rows = min(32, t.cols - c * 32);
-          if (issuer) tma_store_wait_read<0>();
-          named_bar(1 + g, 128);                 // the boxes are free
           if (kMode == kGemmForward) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] += bias;
             if (l.pre) put_chunk(boxes + 8192, gated ? fl + (lane >> 4) * 64 : fl, v);
-            put_forward(l, boxes, fl, v, static_cast<const __nv_bfloat16*>(l.residual) + row * ld + f0 + (fl & ~1),
-                        f_in ? rows : 0);
+            put_forward(l, boxes, fl, v, rv);
           } else {
             put_chunk(boxes, fl, v);
           }
           fence_proxy_async_smem();
-          named_bar(1 + g, 128);                 // the boxes are written
+          if (issuer) tma_store_wait_read<0>();  // the chunk before this one: its boxes are free after the barrier
+          named_bar(1 + g, 128);                 // these are written
           const int n_out_boxes = width / 64;
           if (rows == 32 && (whole || !gated)) {
             if (issuer) {
@@ -514,6 +525,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
                          l.n_z, rows, p.n_feat - f);
               }
           }
+          buf ^= 1;
         }
         if (chunks <= g && lane == 0) mbar_arrive_peer(peer_smem(&bars.acc_empty[acc], 0));
         if (++acc == 2) { acc = 0; aph ^= 1; }
