@@ -31,6 +31,11 @@ namespace smoes {
 namespace {
 
 constexpr int kGemmThreads = 384;
+// dW: the launch's 384 x 168 registers dealt anew, 56 for the first four warps and 224 for the epilogue, whose
+// threads hold 128 sums each (128 x 56 + 256 x 224 = 64512, all of them). setmaxnreg.inc waits without a limit for
+// registers that the launch does not hold, so the launch is refused if the kernel was compiled to fewer.
+constexpr int kGemmFewerRegisters = 56, kGemmMoreRegisters = 224;
+constexpr int kGemmDealtRegisters = 128 * kGemmFewerRegisters + (kGemmThreads - 128) * kGemmMoreRegisters;
 constexpr int kGemmEpiWarps = 8;
 constexpr int kGemmStages = 5;
 constexpr int kGemmK = 64;                       // depth of a block: 128 bytes of bf16
@@ -40,8 +45,8 @@ constexpr uint32_t kGemmHalf = 128 * kGemmK * 2; // one CTA's operand of a block
 constexpr int kGemmChunk = 8;                    // blocks of 64 rows
 
 constexpr uint32_t kGemmStaging = 32768;         // one epilogue group's output boxes: two chunks of 16 KB
-// alignment, operands, output boxes, barriers, [E + 1] row tiles before each expert
-constexpr uint32_t kGemmSmem = 1024 + kGemmStages * 2 * kGemmHalf + 2 * kGemmStaging + 512 + 4 * (kExpertsMax + 1);
+// alignment, operands, output boxes, barriers, [E + 1] offsets
+constexpr uint32_t kGemmSmem = 1024 + kGemmStages * 2 * kGemmHalf + 2 * kGemmStaging + 256 + 4 * (kExpertsMax + 1);
 static_assert(kGemmSmem <= 227 * 1024, "shared memory of a CTA");
 
 struct GemmBars {
@@ -52,7 +57,7 @@ struct GemmBars {
   uint32_t tmem;
   int abort;
 };
-static_assert(sizeof(GemmBars) <= 512, "barriers");
+static_assert(sizeof(GemmBars) <= 256, "barriers");
 
 // A tile: expert, first feature, the N extent.
 struct GemmTile {
@@ -64,8 +69,10 @@ struct GemmTile {
   int last;                                      // dW: rows of the last block
 };
 
+// off: the offsets in shared memory (from global memory each tile began with a round trip to L2).
 template <int kMode>
-__device__ __forceinline__ GemmTile gemm_tile(const ExpertGemmParams& p, const int* first, int tile) {
+__device__ __forceinline__ GemmTile gemm_tile(const ExpertGemmParams& p, const RowTiles& rt, const int32_t* off,
+                                              int tile) {
   GemmTile t;
   if (kMode == kGemmGradW) {
     const int per = p.m_tiles * p.n_tiles;
@@ -75,25 +82,18 @@ __device__ __forceinline__ GemmTile gemm_tile(const ExpertGemmParams& p, const i
     t.m = in - j * p.m_tiles;
     t.col0 = j * 256;
     t.cols = min(256, p.l.n_z - t.col0);
-    t.row0 = expert_begin(p.l.offsets, t.e, p.l.R);
-    const long long rows = max(0ll, expert_begin(p.l.offsets, t.e + 1, p.l.R) - t.row0);
+    t.row0 = expert_begin(off, t.e, p.l.R);
+    const long long rows = max(0ll, expert_begin(off, t.e + 1, p.l.R) - t.row0);
     t.blocks = static_cast<int>((rows + kGemmK - 1) / kGemmK);
     t.last = static_cast<int>(rows - static_cast<long long>(t.blocks - 1) * kGemmK);
     return t;
   }
-  const int lane = threadIdx.x & 31;
-  const int rt = tile / p.m_tiles;
-  t.m = tile - rt * p.m_tiles;
-  // the last expert whose first row tile is at or before rt (empty experts share it with the next)
-  const int E = p.l.E;
-  const unsigned b0 = __ballot_sync(0xffffffffu, lane * 8 < E && first[min(lane * 8, E)] <= rt);
-  const int q = 31 - __clz(b0);
-  const int at = q * 8 + (lane & 7);
-  const unsigned b1 = __ballot_sync(0xffffffffu, lane < 8 && at < E && first[min(at, E)] <= rt);
-  t.e = q * 8 + 31 - __clz(b1);
-  const long long begin = expert_begin(p.l.offsets, t.e, p.l.R), end = expert_begin(p.l.offsets, t.e + 1, p.l.R);
-  t.row0 = begin + static_cast<long long>(rt - first[t.e]) * 256;
-  t.cols = static_cast<int>(min(256ll, end - t.row0));
+  const int r = tile / p.m_tiles;
+  t.m = tile - r * p.m_tiles;
+  const RowTile row = find_row_tile(rt, off, p.l.E, p.l.R, 256, r);
+  t.e = row.e;
+  t.row0 = row.row0;
+  t.cols = static_cast<int>(min(256ll, row.row1 - row.row0));
   t.col0 = 0;
   t.last = kGemmK;
   t.blocks = ((kMode == kGemmForward ? p.l.n_in : p.l.n_z) + kGemmK - 1) / kGemmK;
@@ -215,7 +215,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
   uint8_t* sb = smem + kGemmStages * kGemmHalf;
   uint8_t* staging = smem + 2 * kGemmStages * kGemmHalf;
   GemmBars& bars = *reinterpret_cast<GemmBars*>(staging + 2 * kGemmStaging);
-  int* first = reinterpret_cast<int*>(staging + 2 * kGemmStaging + 512);   // [E + 1] row tiles before e
+  int32_t* off = reinterpret_cast<int32_t*>(staging + 2 * kGemmStaging + 256);   // [E + 1] offsets
   const ExpertLinearParams& l = p.l;
   const int warp = warp_index(), lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
@@ -239,39 +239,17 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
   if (warp == 2) tmem_alloc_pair(&bars.tmem, 512);
   pdl_wait();
   pdl_trigger();
-  int n_total;                                   // tiles
-  if (kMode == kGemmGradW) {
-    n_total = l.E * p.m_tiles * p.n_tiles;
-  } else if (warp == 0) {
-    int n[8], sum = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int e = lane * 8 + i;
-      const long long rows = e < l.E ? expert_begin(l.offsets, e + 1, l.R) - expert_begin(l.offsets, e, l.R) : 0;
-      n[i] = rows > 0 ? static_cast<int>((rows + 255) / 256) : 0;
-      sum += n[i];
-    }
-    int run = sum;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int v = __shfl_up_sync(0xffffffffu, run, o);
-      if (lane >= o) run += v;
-    }
-    int at = run - sum;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (lane * 8 + i <= l.E) first[lane * 8 + i] = at;
-      at += n[i];
-    }
-    if (l.E == 256 && lane == 31) first[256] = at;
-  }
+  for (int e = threadIdx.x; e <= l.E; e += kGemmThreads) off[e] = __ldg(l.offsets + e);
   tc_fence_before();
   __syncthreads();
   cluster_sync();                                // both CTAs' barriers are ready before anything arrives on them
   tc_fence_after();
-  if (kMode != kGemmGradW) n_total = first[l.E] * p.m_tiles;
+  RowTiles rt{};
+  if (kMode != kGemmGradW) rt = count_row_tiles(off, l.E, l.R, 256);
+  const int n_total = kMode == kGemmGradW ? l.E * p.m_tiles * p.n_tiles : rt.total * p.m_tiles;   // tiles
   const uint32_t tmem = bars.tmem;
   const WaitCtx wc{&bars.abort, p.status, p.limit_ns};
+  if (kMode == kGemmGradW && warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kGemmFewerRegisters));
 
   if (warp == 0) {
     // ------------------------------------------------------------------------------- producer
@@ -279,7 +257,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     uint32_t ph = 0;
     bool ok = true;
     for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
-      const GemmTile t = gemm_tile<kMode>(p, first, tile);
+      const GemmTile t = gemm_tile<kMode>(p, rt, off, tile);
       const int half_n = gemm_n<kMode>(t) / 2;
       for (int kb = 0; kb < t.blocks; ++kb) {
         if (!warp_wait(&bars.empty[st], ph ^ 1, wc)) { ok = false; break; }
@@ -345,7 +323,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     bool ok = true;
     constexpr bool kMajorA = kMode != kGemmForward, kMajorB = kMode == kGemmGradW;   // along M / N in memory
     for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
-      const GemmTile t = gemm_tile<kMode>(p, first, tile);
+      const GemmTile t = gemm_tile<kMode>(p, rt, off, tile);
       const uint32_t idesc = idesc_bf16(256, gemm_n<kMode>(t), kMajorA, kMajorB);
       const int chunk = kMode == kGemmGradW ? kGemmChunk : t.blocks;
       for (int k0 = 0; ok && k0 < t.blocks; k0 += chunk) {
@@ -378,7 +356,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     int st = 0;
     uint32_t phases = 0;                         // bit s: parity of tail[s]
     for (int tile = pair; tile < n_total; tile += n_pairs) {
-      const GemmTile t = gemm_tile<kMode>(p, first, tile);
+      const GemmTile t = gemm_tile<kMode>(p, rt, off, tile);
       if (t.blocks == 0) continue;
       const int s = (st + t.blocks - 1) % kGemmStages;
       st = (st + t.blocks) % kGemmStages;
@@ -398,10 +376,11 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     }
   } else if (warp >= 4) {
     // ------------------------------------------------------------------------------- epilogue
+    if (kMode == kGemmGradW) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kGemmMoreRegisters));
     const int q = warp & 3, g = (warp - 4) >> 2;
     const uint32_t lanes = static_cast<uint32_t>(32 * q) << 16;
     if (kMode != kGemmGradW) {
-      const long long end = expert_begin(l.offsets, l.E, l.R);
+      const long long end = expert_begin(off, l.E, l.R);
       if (end < l.R) {                           // rows of no expert
         const int threads = 32 * kGemmEpiWarps;
         for (int which = 0; which < (l.pre ? 2 : 1); ++which) {
@@ -419,7 +398,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     uint32_t aph = 0;
     bool ok = true;
     for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
-      const GemmTile t = gemm_tile<kMode>(p, first, tile);
+      const GemmTile t = gemm_tile<kMode>(p, rt, off, tile);
       if constexpr (kMode == kGemmGradW) {
         float sum[4][32];
 #pragma unroll
@@ -558,6 +537,10 @@ cudaError_t max_pairs(int n_sms, int* out) {
     e = cudaFuncSetAttribute(k_expert_gemm<kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                              static_cast<int>(kGemmSmem));
     if (e != cudaSuccess) return e;
+    cudaFuncAttributes fa;
+    e = cudaFuncGetAttributes(&fa, k_expert_gemm<kMode>);
+    if (e != cudaSuccess) return e;
+    if (kMode == kGemmGradW && fa.numRegs * kGemmThreads < kGemmDealtRegisters) return cudaErrorInvalidConfiguration;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(n_sms / 2 * 2);
     cfg.blockDim = dim3(kGemmThreads);

@@ -95,8 +95,9 @@ __global__ void __launch_bounds__(kLinThreads) k_expert_linear(const ExpertLinea
               static_cast<int>((kMode == kForward ? p.n_out : p.n_in) * sizeof(float) / 16));
     if (kMode == kForward && p.pre)
       zero_rows(p.pre, expert_begin(p.offsets, p.E, p.R), p.R, static_cast<int>(p.n_z * sizeof(float) / 16));
-    const RowTile t = find_row_tile(p.offsets, p.E, p.R, kTile, blockIdx.x);
-    if (t.e < 0) return;
+    const RowTiles tiles = count_row_tiles(p.offsets, p.E, p.R, kTile);
+    if (static_cast<int>(blockIdx.x) >= tiles.total) return;
+    const RowTile t = find_row_tile(tiles, p.offsets, p.E, p.R, kTile, blockIdx.x);
     e = t.e;
     m0 = t.row0;
     m_end = t.row1;

@@ -10,7 +10,7 @@ namespace smoes {
 
 constexpr int kExpertsMax = 256;           // experts of an expert-layer plan
 constexpr int kExpertWidthMax = 1 << 20;   // widest row
-constexpr int kActChunk = 64;              // rows per partial sum of the bias gradient
+constexpr int kActChunk = 32;              // rows per partial sum of the bias gradient
 
 struct ExpertSortParams {
   long long n;               // selections T * k
@@ -87,7 +87,7 @@ cudaError_t launch_expert_combine_bwd(const ExpertRowsParams& p, bool bf16, cuda
 cudaError_t launch_expert_linear(const ExpertLinearParams& p, cudaStream_t s);
 cudaError_t launch_expert_dx(const ExpertLinearParams& p, cudaStream_t s);
 cudaError_t launch_expert_dw(const ExpertLinearParams& p, cudaStream_t s);
-cudaError_t launch_expert_act_bwd(const ExpertActParams& p, bool bf16, cudaStream_t s);
+cudaError_t launch_expert_act_bwd(const ExpertActParams& p, bool bf16, int n_sms, cudaStream_t s);
 
 // ------------------------------------------------------------------------------ device helpers
 
@@ -97,52 +97,53 @@ __device__ __forceinline__ long long expert_begin(const int32_t* off, int e, lon
   return o < 0 ? 0 : o > R ? R : o;
 }
 
-// Work over the experts' rows in tiles of BM: the expert and first row of tile `tile`, found by one
-// warp (lane l counts the tiles of experts 8 l .. 8 l + 7). e = -1 past the last tile.
+// Work over the experts' rows in tiles of BM rows, counted over the experts in order. Every warp that walks
+// the tiles keeps the count before every eighth expert in its lanes; `off` may be a copy in shared memory.
 struct RowTile {
   int e;
   long long row0, row1;      // the tile's first row, the expert's end
-  int index;                 // the tile's number within the expert
 };
-__device__ inline RowTile find_row_tile(const int32_t* off, int E, long long R, int BM, long long tile) {
+struct RowTiles {
+  int before;                // lane l: tiles of the experts before 8 l
+  int total;
+};
+__device__ __forceinline__ int row_tiles_of(const int32_t* off, int e, int E, long long R, int BM) {
+  if (e >= E) return 0;
+  const long long rows = expert_begin(off, e + 1, R) - expert_begin(off, e, R);
+  return rows > 0 ? static_cast<int>((rows + BM - 1) / BM) : 0;
+}
+__device__ inline RowTiles count_row_tiles(const int32_t* off, int E, long long R, int BM) {
   const int lane = threadIdx.x & 31;
-  int n[8];
   int sum = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int e = lane * 8 + i;
-    n[i] = 0;
-    if (e < E) {
-      const long long rows = expert_begin(off, e + 1, R) - expert_begin(off, e, R);
-      n[i] = rows > 0 ? static_cast<int>((rows + BM - 1) / BM) : 0;
-    }
-    sum += n[i];
-  }
+  for (int i = 0; i < 8; ++i) sum += row_tiles_of(off, lane * 8 + i, E, R, BM);
   int run = sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const int v = __shfl_up_sync(0xffffffffu, run, o);
     if (lane >= o) run += v;
   }
-  long long at = run - sum;
-  int e = -1, index = 0;
+  return RowTiles{run - sum, __shfl_sync(0xffffffffu, run, 31)};
+}
+// Tile 0 <= tile < total, by a whole warp.
+__device__ __forceinline__ RowTile find_row_tile(const RowTiles& t, const int32_t* off, int E, long long R, int BM,
+                                                 int tile) {
+  const int lane = threadIdx.x & 31;
+  const int q = 31 - __clz(__ballot_sync(0xffffffffu, t.before <= tile));   // the last group that starts at or before it
+  const int in = tile - __shfl_sync(0xffffffffu, t.before, q);
+  const int n = lane < 8 ? row_tiles_of(off, q * 8 + lane, E, R, BM) : 0;
+  int run = n;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    if (tile >= at && tile < at + n[i]) {
-      e = lane * 8 + i;
-      index = static_cast<int>(tile - at);
-    }
-    at += n[i];
+  for (int o = 1; o < 8; o <<= 1) {
+    const int v = __shfl_up_sync(0xffffffffu, run, o);
+    if (lane >= o) run += v;
   }
-  const unsigned has = __ballot_sync(0xffffffffu, e >= 0);
-  RowTile t{-1, 0, 0, 0};
-  if (!has) return t;
-  const int src = __ffs(has) - 1;
-  t.e = __shfl_sync(0xffffffffu, e, src);
-  t.index = __shfl_sync(0xffffffffu, index, src);
-  t.row0 = expert_begin(off, t.e, R) + static_cast<long long>(t.index) * BM;
-  t.row1 = expert_begin(off, t.e + 1, R);
-  return t;
+  const int src = __ffs(__ballot_sync(0xffffffffu, lane < 8 && in < run)) - 1;
+  RowTile r;
+  r.e = q * 8 + src;
+  r.row0 = expert_begin(off, r.e, R) + static_cast<long long>(in - __shfl_sync(0xffffffffu, run - n, src)) * BM;
+  r.row1 = expert_begin(off, r.e + 1, R);
+  return r;
 }
 
 // 16 bytes of T: 8 bf16 or 4 fp32.

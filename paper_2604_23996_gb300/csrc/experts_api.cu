@@ -282,7 +282,7 @@ smoes_status smoes_expert_act_bwd(smoes_experts P, const void* dOut, const void*
   p.dZ = dZ;
   p.db = db;
   p.part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + P->part);
-  return cuda_status(launch_expert_act_bwd(p, P->desc.dtype == SMOES_BF16, stream));
+  return cuda_status(launch_expert_act_bwd(p, P->desc.dtype == SMOES_BF16, P->n_sms, stream));
 }
 
 smoes_status smoes_expert_linear_bwd(smoes_experts P, const void* dZ, const void* X, const void* W, int n_in, int n_z,
