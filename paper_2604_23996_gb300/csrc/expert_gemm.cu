@@ -142,24 +142,26 @@ __device__ __forceinline__ void put_chunk(uint8_t* boxes, int f, const float (&v
 
 // The residual of a chunk, at the places where put_forward adds it. res: that of the chunk's first row at the lane's
 // even feature, read for `rows` rows (none where the feature does not exist).
+template <bool kGated>
 __device__ __forceinline__ void load_residual(const ExpertLinearParams& l, const __nv_bfloat16* res, int rows,
                                               uint32_t (&rv)[16]) {
   const int odd = threadIdx.x & 1, up = (threadIdx.x >> 4) & 1;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    const int c = l.gated ? (i >> 1) * 8 + (i & 1) + 2 * up + 4 * odd : (i >> 2) * 8 + (i & 3) + 4 * odd;
+    const int c = kGated ? (i >> 1) * 8 + (i & 1) + 2 * up + 4 * odd : (i >> 2) * 8 + (i & 3) + 4 * odd;
     rv[i] = c < rows ? __ldg(reinterpret_cast<const uint32_t*>(res + c * static_cast<long long>(l.n_out))) : 0u;
   }
 }
 
 // z (bias added) of a chunk to out, in shared memory, by whole warps. f: the lane's feature among the CTA's.
-__device__ __forceinline__ void put_forward(const ExpertLinearParams& l, uint8_t* boxes, int f, float (&v)[32],
+template <int kAct, bool kGated>
+__device__ __forceinline__ void put_forward(uint8_t* boxes, int f, float (&v)[32],
                                             const uint32_t (&rv)[16]) {
   const int odd = threadIdx.x & 1;
-  if (!l.gated) {
-    if (l.act) {
+  if (!kGated) {
+    if (kAct != SMOES_ACT_NONE) {
 #pragma unroll
-      for (int c = 0; c < 32; ++c) v[c] = act_value<true>(l.act, v[c]);
+      for (int c = 0; c < 32; ++c) v[c] = act_value<kAct, true>(v[c]);
     }
     const uint32_t at = pair_address(boxes, f);
 #pragma unroll
@@ -180,7 +182,7 @@ __device__ __forceinline__ void put_forward(const ExpertLinearParams& l, uint8_t
     const int c = (i >> 1) * 4 + (i & 1);
     const float got = __shfl_xor_sync(0xffffffffu, up ? v[c] : v[c + 2], 16);
     const float g = up ? got : v[c], u = up ? v[c + 2] : got;
-    y[i] = act_value<true>(l.act, g) * u;
+    y[i] = act_value<kAct, true>(g) * u;
   }
   // the half's two rows further down: the swizzle's bit of 2 with it
   const uint32_t at = (pair_address(boxes, f) ^ (up << 5)) + up * 256;
@@ -204,7 +206,7 @@ __device__ __forceinline__ void copy_box(const uint8_t* box, __nv_bfloat16* base
   }
 }
 
-template <int kMode>
+template <int kMode, int kAct, bool kGated>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
 k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
               const __grid_constant__ CUtensorMap tmB16, const __grid_constant__ CUtensorMap tmOut,
@@ -286,7 +288,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
             mbar_arrive_expect_tx_peer(bar, kGemmHalf + half_n * 128u);
             const int k0 = kb * kGemmK;
             if (kMode == kGemmForward) {
-              if (l.gated) {
+              if (kGated) {
                 const int f0 = t.m * 128 + static_cast<int>(rank) * 64;
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
@@ -439,7 +441,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
         }
       } else {
         // the CTA's first feature (f0) and its width, the lane's among them (fl), and of z forward (zf)
-        const bool gated = kMode == kGemmForward && l.gated;
+        constexpr bool gated = kGated;
         const int width = gated ? 64 : 128;
         const int f0 = (t.m * 2 + static_cast<int>(rank)) * width;
         const int fl = gated ? 16 * q + (lane & 15) : 32 * q + lane;
@@ -461,7 +463,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
         for (int c = g; c < chunks; c += 2) {
           const long long row = t.row0 + c * 32;
           const int rows = min(32, t.cols - c * 32);
-          if (kMode == kGemmForward && l.residual) load_residual(l, res + row * ld, f_in ? rows : 0, rv);
+          if (kMode == kGemmForward && l.residual) load_residual<kGated>(l, res + row * ld, f_in ? rows : 0, rv);
           uint8_t* boxes = staging + g * kGemmStaging + buf * (kGemmStaging / 2);
           float v[32];
           tmem_ld32(tmem + acc * 256 + c * 32 + lanes, v);
@@ -474,7 +476,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] += bias;
             if (l.pre) put_chunk(boxes + 8192, gated ? fl + (lane >> 4) * 64 : fl, v);
-            put_forward(l, boxes, fl, v, rv);
+            put_forward<kAct, kGated>(boxes, fl, v, rv);
           } else {
             put_chunk(boxes, fl, v);
           }
@@ -524,7 +526,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
 }
 
 // Pairs of CTAs that the device holds at once.
-template <int kMode>
+template <int kMode, int kAct, bool kGated>
 cudaError_t max_pairs(int n_sms, int* out) {
   static std::mutex mu;
   static int cached[64] = {};
@@ -534,11 +536,11 @@ cudaError_t max_pairs(int n_sms, int* out) {
   if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
   std::lock_guard<std::mutex> lock(mu);
   if (cached[dev] == 0) {
-    e = cudaFuncSetAttribute(k_expert_gemm<kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    e = cudaFuncSetAttribute(k_expert_gemm<kMode, kAct, kGated>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                              static_cast<int>(kGemmSmem));
     if (e != cudaSuccess) return e;
     cudaFuncAttributes fa;
-    e = cudaFuncGetAttributes(&fa, k_expert_gemm<kMode>);
+    e = cudaFuncGetAttributes(&fa, k_expert_gemm<kMode, kAct, kGated>);
     if (e != cudaSuccess) return e;
     if (kMode == kGemmGradW && fa.numRegs * kGemmThreads < kGemmDealtRegisters) return cudaErrorInvalidConfiguration;
     cudaLaunchConfig_t cfg = {};
@@ -546,7 +548,7 @@ cudaError_t max_pairs(int n_sms, int* out) {
     cfg.blockDim = dim3(kGemmThreads);
     cfg.dynamicSmemBytes = kGemmSmem;
     int n = 0;
-    e = cudaOccupancyMaxActiveClusters(&n, k_expert_gemm<kMode>, &cfg);
+    e = cudaOccupancyMaxActiveClusters(&n, k_expert_gemm<kMode, kAct, kGated>, &cfg);
     if (e != cudaSuccess) return e;
     if (n < 1) return cudaErrorLaunchOutOfResources;
     cached[dev] = n;
@@ -555,14 +557,14 @@ cudaError_t max_pairs(int n_sms, int* out) {
   return cudaSuccess;
 }
 
-template <int kMode>
+template <int kMode, int kAct, bool kGated>
 cudaError_t launch(const ExpertGemmParams& p, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& b16,
                    const CUtensorMap& out, const CUtensorMap& pre, long long tiles, int n_sms, cudaStream_t s) {
   int pairs = 0;
-  const cudaError_t e = max_pairs<kMode>(n_sms, &pairs);
+  const cudaError_t e = max_pairs<kMode, kAct, kGated>(n_sms, &pairs);
   if (e != cudaSuccess) return e;
   pairs = static_cast<int>(std::min<long long>(pairs, std::max(1ll, tiles)));
-  return launch_pdl(k_expert_gemm<kMode>, dim3(2 * pairs), dim3(kGemmThreads), kGemmSmem, s, a, b, b16, out, pre, p);
+  return launch_pdl(k_expert_gemm<kMode, kAct, kGated>, dim3(2 * pairs), dim3(kGemmThreads), kGemmSmem, s, a, b, b16, out, pre, p);
 }
 
 }  // namespace
@@ -603,9 +605,14 @@ cudaError_t launch_expert_gemm(const ExpertLinearParams& l, ExpertGemmMode mode,
   if (!ok) return cudaErrorInvalidValue;
   // at most R / 256 + min(E, R) row tiles
   const long long row_tiles = l.R / 256 + std::min<long long>(l.E, l.R);
-  if (mode == kGemmForward) return launch<kGemmForward>(p, a, b, b16, out, pre, row_tiles * p.m_tiles, n_sms, s);
-  if (mode == kGemmGradX) return launch<kGemmGradX>(p, a, b, b16, out, pre, row_tiles * p.m_tiles, n_sms, s);
-  return launch<kGemmGradW>(p, a, b, b16, out, pre, static_cast<long long>(l.E) * p.m_tiles * p.n_tiles, n_sms, s);
+  if (mode == kGemmForward)
+    return with_act(l.act, [&](auto act) {
+      constexpr int kAct = decltype(act)::value;
+      return l.gated ? launch<kGemmForward, kAct, true>(p, a, b, b16, out, pre, row_tiles * p.m_tiles, n_sms, s)
+                     : launch<kGemmForward, kAct, false>(p, a, b, b16, out, pre, row_tiles * p.m_tiles, n_sms, s);
+    });
+  if (mode == kGemmGradX) return launch<kGemmGradX, SMOES_ACT_NONE, false>(p, a, b, b16, out, pre, row_tiles * p.m_tiles, n_sms, s);
+  return launch<kGemmGradW, SMOES_ACT_NONE, false>(p, a, b, b16, out, pre, static_cast<long long>(l.E) * p.m_tiles * p.n_tiles, n_sms, s);
 }
 
 }  // namespace smoes

@@ -233,7 +233,8 @@ __global__ void __launch_bounds__(kLinThreads) k_expert_linear(const ExpertLinea
         const float rv[4] = {res.x, res.y, res.z, res.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          y[j] = act_value<false>(p.act, z[h][j]);
+          y[j] = p.act == SMOES_ACT_SILU ? act_value<SMOES_ACT_SILU, false>(z[h][j])
+                 : p.act == SMOES_ACT_GELU ? act_value<SMOES_ACT_GELU, false>(z[h][j]) : z[h][j];
           if (p.gated) y[j] *= z[1][j];
           y[j] += rv[j];
         }

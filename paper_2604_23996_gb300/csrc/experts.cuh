@@ -4,13 +4,15 @@
 
 #include <cuda_bf16.h>
 
+#include <type_traits>
+
 #include "smoes_internal.cuh"
 
 namespace smoes {
 
 constexpr int kExpertsMax = 256;           // experts of an expert-layer plan
 constexpr int kExpertWidthMax = 1 << 20;   // widest row
-constexpr int kActChunk = 32;              // rows per partial sum of the bias gradient
+constexpr int kActBlocksPerSm = 3;         // of the activation gradient, all at once
 
 struct ExpertSortParams {
   long long n;               // selections T * k
@@ -62,7 +64,8 @@ struct ExpertActParams {
   const void* pre;
   void* dZ;
   float* db;
-  float* part;               // [R / kActChunk + E][n_z] (workspace)
+  int ranges;                // row ranges: one block each and per segment of columns
+  float* part;               // [ranges + E][n_z] (workspace)
 };
 
 // The bf16 products on the tensor cores (expert_gemm.cu): D[m, n] = sum over the depth of A[m] B[n], with
@@ -87,7 +90,8 @@ cudaError_t launch_expert_combine_bwd(const ExpertRowsParams& p, bool bf16, cuda
 cudaError_t launch_expert_linear(const ExpertLinearParams& p, cudaStream_t s);
 cudaError_t launch_expert_dx(const ExpertLinearParams& p, cudaStream_t s);
 cudaError_t launch_expert_dw(const ExpertLinearParams& p, cudaStream_t s);
-cudaError_t launch_expert_act_bwd(const ExpertActParams& p, bool bf16, int n_sms, cudaStream_t s);
+cudaError_t launch_expert_act_bwd(ExpertActParams p, bool bf16, int n_sms, cudaStream_t s);   // fills ranges
+int act_ranges(int n_sms);   // most ranges of the activation gradient
 
 // ------------------------------------------------------------------------------ device helpers
 
@@ -194,12 +198,24 @@ __device__ __forceinline__ void zero_rows(void* base, long long first, long long
 }
 
 // Activations and their slopes. kFast: for results that are rounded to bf16, whose step is 2^-8: the fast
-// exponential and division (a few steps of 2^-22), and erfc by the rational form of Abramowitz and Stegun,
-// Handbook of Mathematical Functions, 7.1.26 (absolute error 1.5e-7), which shares its e^(-z^2 / 2) with the slope
-// (an epilogue with erfcf takes longer than the products it follows). Otherwise CUDA's accurate functions.
+// exponential and reciprocal (a few steps of 2^-22; what underflows is zero), and erfc by the rational form of
+// Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26 (absolute error 1.5e-7), which shares its
+// e^(-z^2 / 2) with the slope (an epilogue with erfcf takes longer than the products it follows). Otherwise CUDA's
+// accurate functions.
+__device__ __forceinline__ float fast_exp2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float fast_reciprocal(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+constexpr float kLog2E = 1.4426950408889634f;
 template <bool kFast>
 __device__ __forceinline__ float sigmoid_of(float z) {
-  return kFast ? __fdividef(1.f, 1.f + __expf(-z)) : 1.f / (1.f + expf(-z));
+  return kFast ? fast_reciprocal(1.f + fast_exp2(-kLog2E * z)) : 1.f / (1.f + expf(-z));
 }
 // Phi(z) and phi(z), the normal distribution's function and density.
 template <bool kFast>
@@ -208,9 +224,9 @@ __device__ __forceinline__ float normal_of(float z, float& density) {
     density = expf(-0.5f * z * z) * 0.39894228f;
     return 0.5f * erfcf(z * -0.70710678f);
   }
-  const float e = __expf(-0.5f * z * z);
+  const float e = fast_exp2(-0.5f * kLog2E * z * z);
   density = e * 0.39894228f;
-  const float t = __fdividef(1.f, fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.f));
+  const float t = fast_reciprocal(fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.f));
   float q = fmaf(1.061405429f, t, -1.453152027f);        // erfc(|z| / sqrt 2) = t q(t) e^(-z^2 / 2)
   q = fmaf(q, t, 1.421413741f);
   q = fmaf(q, t, -0.284496736f);
@@ -218,20 +234,20 @@ __device__ __forceinline__ float normal_of(float z, float& density) {
   const float half = 0.5f * q * t * e;
   return z < 0.f ? half : 1.f - half;
 }
-template <bool kFast>
-__device__ __forceinline__ float act_value(int act, float z) {
+template <int kAct, bool kFast>
+__device__ __forceinline__ float act_value(float z) {
   float density;
-  if (act == SMOES_ACT_SILU) return kFast ? z * sigmoid_of<true>(z) : z / (1.f + expf(-z));
-  if (act == SMOES_ACT_GELU) return z * normal_of<kFast>(z, density);
+  if (kAct == SMOES_ACT_SILU) return kFast ? z * sigmoid_of<true>(z) : z / (1.f + expf(-z));
+  if (kAct == SMOES_ACT_GELU) return z * normal_of<kFast>(z, density);
   return z;
 }
-template <bool kFast>
-__device__ __forceinline__ void act_value_slope(int act, float z, float& value, float& slope) {
-  if (act == SMOES_ACT_SILU) {
+template <int kAct, bool kFast>
+__device__ __forceinline__ void act_value_slope(float z, float& value, float& slope) {
+  if (kAct == SMOES_ACT_SILU) {
     const float s = sigmoid_of<kFast>(z);
     value = z * s;
     slope = fmaf(value, 1.f - s, s);
-  } else if (act == SMOES_ACT_GELU) {
+  } else if (kAct == SMOES_ACT_GELU) {
     float density;
     const float n = normal_of<kFast>(z, density);
     value = z * n;
@@ -240,6 +256,13 @@ __device__ __forceinline__ void act_value_slope(int act, float z, float& value, 
     value = z;
     slope = 1.f;
   }
+}
+// f with the activation as a constant.
+template <class F>
+auto with_act(int act, F&& f) {
+  if (act == SMOES_ACT_SILU) return f(std::integral_constant<int, SMOES_ACT_SILU>());
+  if (act == SMOES_ACT_GELU) return f(std::integral_constant<int, SMOES_ACT_GELU>());
+  return f(std::integral_constant<int, SMOES_ACT_NONE>());
 }
 
 }  // namespace smoes

@@ -84,7 +84,7 @@ smoes_status smoes_experts_create(const smoes_experts_desc* desc, smoes_experts*
   P->sync = take(16);
   P->header_bytes = o;
   P->counts = take(sizeof(int32_t) * static_cast<size_t>(P->sort_blocks) * d.E);
-  P->part = take(sizeof(float) * static_cast<size_t>(P->R / kActChunk + d.E) * d.max_width);
+  P->part = take(sizeof(float) * static_cast<size_t>(act_ranges(P->n_sms) + d.E) * d.max_width);
   P->total = o;
   *out = P;
   return SMOES_OK;
