@@ -244,10 +244,8 @@ smoes_status router_fwd(smoes_plan P, const void* X, const void* W, const float*
   return cuda_status(launch_router_fwd_f32(p, stream));
 }
 
-}  // namespace
-
-bool smoes::encode_bf16(CUtensorMap* m, const void* ptr, int rank, const uint64_t* dims, const uint64_t* strides,
-                        const uint32_t* box) {
+bool encode_tiled(CUtensorMap* m, CUtensorMapDataType type, CUtensorMapSwizzle swizzle, const void* ptr, int rank,
+                  const uint64_t* dims, const uint64_t* strides, const uint32_t* box) {
   EncodeTiledFn enc = get_encode();
   if (!enc || rank < 2 || rank > 5) return false;
   cuuint64_t d[5], st[4];
@@ -258,9 +256,20 @@ bool smoes::encode_bf16(CUtensorMap* m, const void* ptr, int rank, const uint64_
     one[i] = 1;
     if (i + 1 < rank) st[i] = strides[i];
   }
-  return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, static_cast<cuuint32_t>(rank), const_cast<void*>(ptr), d, st, b, one,
-             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+  return enc(m, type, static_cast<cuuint32_t>(rank), const_cast<void*>(ptr), d, st, b, one,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace
+
+bool smoes::encode_bf16(CUtensorMap* m, const void* ptr, int rank, const uint64_t* dims, const uint64_t* strides,
+                        const uint32_t* box) {
+  return encode_tiled(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, CU_TENSOR_MAP_SWIZZLE_128B, ptr, rank, dims, strides, box);
+}
+bool smoes::encode_f32(CUtensorMap* m, const void* ptr, int rank, const uint64_t* dims, const uint64_t* strides,
+                       const uint32_t* box) {
+  return encode_tiled(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, CU_TENSOR_MAP_SWIZZLE_NONE, ptr, rank, dims, strides, box);
 }
 
 extern "C" {

@@ -22,8 +22,8 @@
 // epilogue, in two groups that take alternate 32-column chunks. Two accumulators of 256 columns: the epilogue of a
 // tile runs under the next tile's products.
 #include <algorithm>
-#include <mutex>
 
+#include "expert_gemm.cuh"
 #include "experts.cuh"
 #include "ptx.cuh"
 
@@ -58,53 +58,6 @@ struct GemmBars {
   int abort;
 };
 static_assert(sizeof(GemmBars) <= 256, "barriers");
-
-// A tile: expert, first feature, the N extent.
-struct GemmTile {
-  int e, m;                                      // expert, feature tile
-  long long row0;                                // first row (dW: the expert's first row)
-  int cols;                                      // rows of the tile (dW: columns of n_z)
-  int col0;                                      // dW: first column of n_z
-  int blocks;                                    // blocks along the depth
-  int last;                                      // dW: rows of the last block
-};
-
-// off: the offsets in shared memory (from global memory each tile began with a round trip to L2).
-template <int kMode>
-__device__ __forceinline__ GemmTile gemm_tile(const ExpertGemmParams& p, const RowTiles& rt, const int32_t* off,
-                                              int tile) {
-  GemmTile t;
-  if (kMode == kGemmGradW) {
-    const int per = p.m_tiles * p.n_tiles;
-    t.e = tile / per;
-    const int in = tile - t.e * per;
-    const int j = in / p.m_tiles;
-    t.m = in - j * p.m_tiles;
-    t.col0 = j * 256;
-    t.cols = min(256, p.l.n_z - t.col0);
-    t.row0 = expert_begin(off, t.e, p.l.R);
-    const long long rows = max(0ll, expert_begin(off, t.e + 1, p.l.R) - t.row0);
-    t.blocks = static_cast<int>((rows + kGemmK - 1) / kGemmK);
-    t.last = static_cast<int>(rows - static_cast<long long>(t.blocks - 1) * kGemmK);
-    return t;
-  }
-  const int r = tile / p.m_tiles;
-  t.m = tile - r * p.m_tiles;
-  const RowTile row = find_row_tile(rt, off, p.l.E, p.l.R, 256, r);
-  t.e = row.e;
-  t.row0 = row.row0;
-  t.cols = static_cast<int>(min(256ll, row.row1 - row.row0));
-  t.col0 = 0;
-  t.last = kGemmK;
-  t.blocks = ((kMode == kGemmForward ? p.l.n_in : p.l.n_z) + kGemmK - 1) / kGemmK;
-  return t;
-}
-
-// N of the tile's products: both CTAs hold half of the rows. dW: whole 64-column boxes in each.
-template <int kMode>
-__device__ __forceinline__ int gemm_n(const GemmTile& t) {
-  return kMode == kGemmGradW ? (t.cols + 127) & ~127 : (t.cols + 31) & ~31;
-}
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
@@ -259,8 +212,8 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     uint32_t ph = 0;
     bool ok = true;
     for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
-      const GemmTile t = gemm_tile<kMode>(p, rt, off, tile);
-      const int half_n = gemm_n<kMode>(t) / 2;
+      const GemmTile t = gemm_tile<kMode, 256, kGemmK>(p, rt, off, tile);
+      const int half_n = gemm_n<kMode>(t.cols) / 2;
       for (int kb = 0; kb < t.blocks; ++kb) {
         if (!warp_wait(&bars.empty[st], ph ^ 1, wc)) { ok = false; break; }
         if (elect_one()) {
@@ -325,8 +278,8 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     bool ok = true;
     constexpr bool kMajorA = kMode != kGemmForward, kMajorB = kMode == kGemmGradW;   // along M / N in memory
     for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
-      const GemmTile t = gemm_tile<kMode>(p, rt, off, tile);
-      const uint32_t idesc = idesc_bf16(256, gemm_n<kMode>(t), kMajorA, kMajorB);
+      const GemmTile t = gemm_tile<kMode, 256, kGemmK>(p, rt, off, tile);
+      const uint32_t idesc = idesc_bf16(256, gemm_n<kMode>(t.cols), kMajorA, kMajorB);
       const int chunk = kMode == kGemmGradW ? kGemmChunk : t.blocks;
       for (int k0 = 0; ok && k0 < t.blocks; k0 += chunk) {
         if (!warp_wait(&bars.acc_empty[acc], aph ^ 1, wc)) { ok = false; break; }
@@ -358,7 +311,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     int st = 0;
     uint32_t phases = 0;                         // bit s: parity of tail[s]
     for (int tile = pair; tile < n_total; tile += n_pairs) {
-      const GemmTile t = gemm_tile<kMode>(p, rt, off, tile);
+      const GemmTile t = gemm_tile<kMode, 256, kGemmK>(p, rt, off, tile);
       if (t.blocks == 0) continue;
       const int s = (st + t.blocks - 1) % kGemmStages;
       st = (st + t.blocks) % kGemmStages;
@@ -366,7 +319,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
       if (!warp_wait(&bars.tail[s], (phases >> s) & 1, wc)) break;
       phases ^= 1u << s;
       // rows [last, round_up(last, 16)) of every 64-column box: 8 words of 16 bytes a row
-      const int boxes = gemm_n<kMode>(t) / 128, words = (16 - (t.last & 15)) * 8;
+      const int boxes = gemm_n<kMode>(t.cols) / 128, words = (16 - (t.last & 15)) * 8;
       for (int x = 0; x < 2 + boxes; ++x) {
         uint8_t* box = x < 2 ? sa + s * kGemmHalf + x * 8192 : sb + s * kGemmHalf + (x - 2) * 8192;
         for (int i = lane; i < words; i += 32) *reinterpret_cast<uint4*>(box + t.last * 128 + i * 16) = make_uint4(0u, 0u, 0u, 0u);
@@ -400,7 +353,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     uint32_t aph = 0;
     bool ok = true;
     for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
-      const GemmTile t = gemm_tile<kMode>(p, rt, off, tile);
+      const GemmTile t = gemm_tile<kMode, 256, kGemmK>(p, rt, off, tile);
       if constexpr (kMode == kGemmGradW) {
         float sum[4][32];
 #pragma unroll
@@ -525,43 +478,13 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
   if (warp == 2) tmem_dealloc_pair(tmem, 512);
 }
 
-// Pairs of CTAs that the device holds at once.
-template <int kMode, int kAct, bool kGated>
-cudaError_t max_pairs(int n_sms, int* out) {
-  static std::mutex mu;
-  static int cached[64] = {};
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
-  std::lock_guard<std::mutex> lock(mu);
-  if (cached[dev] == 0) {
-    e = cudaFuncSetAttribute(k_expert_gemm<kMode, kAct, kGated>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             static_cast<int>(kGemmSmem));
-    if (e != cudaSuccess) return e;
-    cudaFuncAttributes fa;
-    e = cudaFuncGetAttributes(&fa, k_expert_gemm<kMode, kAct, kGated>);
-    if (e != cudaSuccess) return e;
-    if (kMode == kGemmGradW && fa.numRegs * kGemmThreads < kGemmDealtRegisters) return cudaErrorInvalidConfiguration;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(n_sms / 2 * 2);
-    cfg.blockDim = dim3(kGemmThreads);
-    cfg.dynamicSmemBytes = kGemmSmem;
-    int n = 0;
-    e = cudaOccupancyMaxActiveClusters(&n, k_expert_gemm<kMode, kAct, kGated>, &cfg);
-    if (e != cudaSuccess) return e;
-    if (n < 1) return cudaErrorLaunchOutOfResources;
-    cached[dev] = n;
-  }
-  *out = cached[dev];
-  return cudaSuccess;
-}
-
 template <int kMode, int kAct, bool kGated>
 cudaError_t launch(const ExpertGemmParams& p, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& b16,
                    const CUtensorMap& out, const CUtensorMap& pre, long long tiles, int n_sms, cudaStream_t s) {
+  static GemmResidency held;
   int pairs = 0;
-  const cudaError_t e = max_pairs<kMode, kAct, kGated>(n_sms, &pairs);
+  const cudaError_t e = gemm_pairs(held, k_expert_gemm<kMode, kAct, kGated>, kGemmThreads, kGemmSmem,
+                                   kMode == kGemmGradW ? kGemmDealtRegisters : 0, n_sms, &pairs);
   if (e != cudaSuccess) return e;
   pairs = static_cast<int>(std::min<long long>(pairs, std::max(1ll, tiles)));
   return launch_pdl(k_expert_gemm<kMode, kAct, kGated>, dim3(2 * pairs), dim3(kGemmThreads), kGemmSmem, s, a, b, b16, out, pre, p);

@@ -1,0 +1,90 @@
+// expert_gemm.cuh -- the tiles of the experts' products on the tensor cores, shared by the bf16 and fp32 kernels.
+#pragma once
+
+#include <mutex>
+
+#include "experts.cuh"
+
+namespace smoes {
+
+// A tile: 256 features (along M) by up to kCols rows (along N; for dW n_in by n_z), blocks of kBlock along the depth.
+struct GemmTile {
+  int e, m;                                      // expert, feature tile
+  long long row0;                                // first row (dW: the expert's first row)
+  int cols;                                      // rows of the tile (dW: columns of n_z)
+  int col0;                                      // dW: first column of n_z
+  int blocks;                                    // blocks along the depth
+  int last;                                      // dW: rows of the last block
+};
+
+// off: the offsets in shared memory (from global memory each tile began with a round trip to L2).
+template <int kMode, int kCols, int kBlock>
+__device__ __forceinline__ GemmTile gemm_tile(const ExpertGemmParams& p, const RowTiles& rt, const int32_t* off,
+                                              int tile) {
+  GemmTile t;
+  if (kMode == kGemmGradW) {
+    const int per = p.m_tiles * p.n_tiles;
+    t.e = tile / per;
+    const int in = tile - t.e * per;
+    const int j = in / p.m_tiles;
+    t.m = in - j * p.m_tiles;
+    t.col0 = j * kCols;
+    t.cols = min(kCols, p.l.n_z - t.col0);
+    t.row0 = expert_begin(off, t.e, p.l.R);
+    const long long rows = max(0ll, expert_begin(off, t.e + 1, p.l.R) - t.row0);
+    t.blocks = static_cast<int>((rows + kBlock - 1) / kBlock);
+    t.last = static_cast<int>(rows - static_cast<long long>(t.blocks - 1) * kBlock);
+    return t;
+  }
+  const int r = tile / p.m_tiles;
+  t.m = tile - r * p.m_tiles;
+  const RowTile row = find_row_tile(rt, off, p.l.E, p.l.R, kCols, r);
+  t.e = row.e;
+  t.row0 = row.row0;
+  t.cols = static_cast<int>(min(static_cast<long long>(kCols), row.row1 - row.row0));
+  t.col0 = 0;
+  t.last = kBlock;
+  t.blocks = ((kMode == kGemmForward ? p.l.n_in : p.l.n_z) + kBlock - 1) / kBlock;
+  return t;
+}
+
+// N of a tile's products: both CTAs hold half of the rows. dW: whole 64-column boxes in each.
+template <int kMode>
+__device__ __forceinline__ int gemm_n(int cols) {
+  return kMode == kGemmGradW ? (cols + 127) & ~127 : (cols + 31) & ~31;
+}
+
+// Pairs of CTAs of a kernel that the device holds at once, and its shared memory allowed (once per kernel and device).
+struct GemmResidency {
+  std::mutex mu;
+  int pairs[64] = {};
+};
+template <class K>
+cudaError_t gemm_pairs(GemmResidency& r, K kernel, int threads, uint32_t smem, int dealt_registers, int n_sms, int* out) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  std::lock_guard<std::mutex> lock(r.mu);
+  if (r.pairs[dev] == 0) {
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    if (e != cudaSuccess) return e;
+    cudaFuncAttributes fa;
+    e = cudaFuncGetAttributes(&fa, kernel);
+    if (e != cudaSuccess) return e;
+    if (fa.numRegs * threads < dealt_registers) return cudaErrorInvalidConfiguration;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(n_sms / 2 * 2);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    int n = 0;
+    e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
+    if (e != cudaSuccess) return e;
+    if (n < 1) return cudaErrorLaunchOutOfResources;
+    r.pairs[dev] = n;
+  }
+  *out = r.pairs[dev];
+  return cudaSuccess;
+}
+
+}  // namespace smoes

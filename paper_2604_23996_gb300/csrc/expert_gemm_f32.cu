@@ -1,0 +1,443 @@
+// expert_gemm_f32.cu -- the experts' fp32 products on the bf16 tensor cores (tcgen05), grouped over ragged rows
+// (formulas: expert_linear's in include/smoes.h; tiles: expert_gemm.cuh).
+//
+// Each fp32 value is the sum of three bf16 values, x = h + m + l to 2^-27 of x, each the rounding of what the ones
+// before it leave. Of the nine products of two such sums the six that reach 2^-18 are formed, l h, h l, m m, m h,
+// h m and h h; the other three are below 2^-26 of |x y| (with cut instead of rounded parts they reach 2^-22 and
+// all have one sign). The tensor cores sum them in fp32 but cut each addition off, so h h has an accumulator of its
+// own, the five small products another, whose cuts are 2^-8 smaller, and after every 256 of the depth both move
+// to fp32 sums in registers (relative error 2.4e-7 from sixteen additions). Infinities and magnitudes above
+// 3.38e38, which round to one, give NaN.
+//
+// A pair of CTAs forms 256 features by up to 128 rows, as in expert_gemm.cu. Roles of a CTA's warps: 0 copies fp32
+// blocks of 32 of the depth to shared memory, 1 issues the products (first CTA), 2 holds tensor memory, 4-11
+// split the blocks and, one 256-deep chunk behind, move the sums and store finished tiles.
+// A block's planes: along the depth 128-byte rows of [h | m] and [l | -]; across it one box of 32 depth rows
+// per plane and 64 features. Rows behind an expert's last one are cleared where they are split.
+//
+// Bound by shared memory: a block's 24 KB arrive, are read and written as 36 KB, and the products read 72 KB, 1220
+// clocks at 128 bytes each against 770 of the products. On the FMA units (128 x 128 a block of threads) 8192 x 512 x
+// 256 of 16 experts took 187 us for both gradients.
+#include <algorithm>
+
+#include "expert_gemm.cuh"
+#include "experts.cuh"
+#include "ptx.cuh"
+
+namespace smoes {
+namespace {
+
+constexpr int kF32Threads = 384;
+constexpr int kF32Warps = 8;                     // splitting and epilogue
+constexpr int kF32K = 32;                        // depth of a block
+constexpr int kF32Chunk = 8;                     // blocks between moves of the sums
+constexpr int kF32Cols = 128;
+constexpr int kF32Stages = 3;
+constexpr uint32_t kRawA = 128 * kF32K * 4, kRawB = 64 * kF32K * 4;     // one CTA's fp32 operands of a block
+constexpr uint32_t kSplitA = 2 * 128 * 128, kSplitB = 2 * 64 * 128;     // and their planes
+constexpr uint32_t kF32Smem = 1024 + kF32Stages * (kRawA + kRawB + kSplitA + kSplitB) + 256 + 4 * (kExpertsMax + 1);
+static_assert(kF32Smem <= 227 * 1024, "shared memory of a CTA");
+
+struct F32Bars {
+  uint64_t raw_full[kF32Stages], raw_empty[kF32Stages];
+  uint64_t split_full[kF32Stages];               // planes of both CTAs (first CTA's)
+  uint64_t split_empty[kF32Stages];
+  uint64_t acc_full[2], acc_empty[2];
+  uint32_t tmem;
+  int abort;
+};
+static_assert(sizeof(F32Bars) <= 256, "barriers");
+
+// Four values, split, to their places in the planes.
+__device__ __forceinline__ uint2 split_off(float (&x)[4]) {             // x becomes what is left
+  uint2 w;
+  uint32_t* half[2] = {&w.x, &w.y};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+    const uint32_t u = *reinterpret_cast<const uint32_t*>(&b);
+    x[2 * i] -= __uint_as_float(u << 16);
+    x[2 * i + 1] -= __uint_as_float(u & 0xffff0000u);
+    *half[i] = u;
+  }
+  return w;
+}
+__device__ __forceinline__ void split_store(const float4& v, uint8_t* h, uint8_t* m, uint8_t* l) {
+  float x[4] = {v.x, v.y, v.z, v.w};
+  *reinterpret_cast<uint2*>(h) = split_off(x);
+  *reinterpret_cast<uint2*>(m) = split_off(x);
+  *reinterpret_cast<uint2*>(l) = split_off(x);
+}
+
+// Word `u` (16 bytes) of a raw operand of kRows rows or columns, split into its planes. kAcross: the depth runs over
+// the rows of the block, of which `depth` exist.
+template <bool kAcross, int kRows>
+__device__ __forceinline__ void split_word(const uint8_t* raw, uint8_t* planes, int u, int depth) {
+  float4 v = *reinterpret_cast<const float4*>(raw + u * 16);
+  if (kAcross) {
+    const int k = u / (kRows / 4), c = u % (kRows / 4) * 4;
+    if (k >= depth) v = make_float4(0.f, 0.f, 0.f, 0.f);
+    constexpr uint32_t kPlane = kRows * kF32K * 2;
+    uint8_t* at = planes + (c >> 6) * (kF32K * 128) + sw128_offset(k, c & 63);
+    split_store(v, at, at + kPlane, at + 2 * kPlane);
+  } else {
+    const int r = u >> 3, k = (u & 7) * 4;
+    uint8_t* h = planes + sw128_offset(r, k);
+    split_store(v, h, planes + sw128_offset(r, k + kF32K), h + kRows * 128);
+  }
+}
+
+// A chunk whose sums are still in tensor memory.
+struct Pending {
+  GemmTile t;
+  bool any, first, last;     // of its tile
+};
+
+template <int kMode, int kAct, bool kGated>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kF32Threads, 1)
+k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+                  const ExpertGemmParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  uint8_t* split_a = smem;                       // [stage] each
+  uint8_t* split_b = split_a + kF32Stages * kSplitA;
+  uint8_t* raw_a = split_b + kF32Stages * kSplitB;
+  uint8_t* raw_b = raw_a + kF32Stages * kRawA;
+  F32Bars& bars = *reinterpret_cast<F32Bars*>(raw_b + kF32Stages * kRawB);
+  int32_t* off = reinterpret_cast<int32_t*>(reinterpret_cast<uint8_t*>(&bars) + 256);   // [E + 1] offsets
+  const ExpertLinearParams& l = p.l;
+  const int warp = warp_index(), lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_rank();
+  const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+  constexpr bool kAcrossA = kMode != kGemmForward, kAcrossB = kMode == kGemmGradW;   // the depth is not contiguous
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kF32Stages; ++i) {
+      mbar_init(&bars.raw_full[i], 1);
+      mbar_init(&bars.raw_empty[i], kF32Warps);
+      mbar_init(&bars.split_full[i], 2 * kF32Warps);
+      mbar_init(&bars.split_empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&bars.acc_full[i], 1);
+      mbar_init(&bars.acc_empty[i], 2 * kF32Warps);
+    }
+    bars.abort = 0;
+    fence_mbar_init();
+    tma_prefetch_desc(&tmA);
+    tma_prefetch_desc(&tmB);
+  }
+  if (warp == 2) tmem_alloc_pair(&bars.tmem, 512);
+  pdl_wait();
+  pdl_trigger();
+  for (int e = threadIdx.x; e <= l.E; e += kF32Threads) off[e] = __ldg(l.offsets + e);
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();                                // both CTAs' barriers are ready before anything arrives on them
+  tc_fence_after();
+  RowTiles rt{};
+  if (kMode != kGemmGradW) rt = count_row_tiles(off, l.E, l.R, kF32Cols);
+  const int n_total = kMode == kGemmGradW ? l.E * p.m_tiles * p.n_tiles : rt.total * p.m_tiles;   // tiles
+  const uint32_t tmem = bars.tmem;               // accumulator b: h h at columns 256 b, the small products at 256 b + 128
+  const WaitCtx wc{&bars.abort, p.status, p.limit_ns};
+
+  if (warp == 0) {
+    // ------------------------------------------------------------------------------- producer
+    int st = 0;
+    uint32_t ph = 0;
+    bool ok = true;
+    for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
+      const GemmTile t = gemm_tile<kMode, kF32Cols, kF32K>(p, rt, off, tile);
+      const int half_n = gemm_n<kMode>(t.cols) / 2;
+      for (int kb = 0; kb < t.blocks; ++kb) {
+        if (!warp_wait(&bars.raw_empty[st], ph ^ 1, wc)) { ok = false; break; }
+        if (elect_one()) {
+          uint8_t* a = raw_a + st * kRawA;
+          uint8_t* b = raw_b + st * kRawB;
+          const uint32_t bar = smem_u32(&bars.raw_full[st]);
+          mbar_arrive_expect_tx(&bars.raw_full[st], kRawA + kRawB);
+          const int k0 = kb * kF32K, r = static_cast<int>(rank);
+          if (kMode == kGemmGradW) {
+            const int r0 = static_cast<int>(t.row0) + k0;
+            tma_load_2d_pair(a, &tmA, bar, t.m * 256 + r * 128, r0);
+            tma_load_2d_pair(b, &tmB, bar, t.col0 + r * half_n, r0);
+          } else {
+            if (kMode == kGemmGradX) {
+              tma_load_3d_pair(a, &tmA, bar, t.m * 256 + r * 128, k0, t.e);
+            } else if (kGated) {
+              const int f0 = t.m * 128 + r * 64;
+#pragma unroll
+              for (int i = 0; i < 8; ++i)
+                tma_load_3d_pair(a + i * 2048, &tmA, bar, k0, (i & 1) * l.n_out + f0 + (i >> 1) * 16, t.e);
+            } else {
+              tma_load_3d_pair(a, &tmA, bar, k0, t.m * 256 + r * 128, t.e);
+            }
+            tma_load_2d_pair(b, &tmB, bar, k0, static_cast<int>(t.row0) + r * half_n);
+          }
+        }
+        __syncwarp();
+        if (++st == kF32Stages) { st = 0; ph ^= 1; }
+      }
+    }
+  } else if (warp == 1 && rank == 0) {
+    // ----------------------------------------------------------------------------- MMA issuer
+    int st = 0, acc = 0;
+    uint32_t ph = 0, aph = 0;
+    bool ok = true;
+    for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
+      const GemmTile t = gemm_tile<kMode, kF32Cols, kF32K>(p, rt, off, tile);
+      const uint32_t idesc = idesc_bf16(256, gemm_n<kMode>(t.cols), kAcrossA, kAcrossB);
+      for (int k0 = 0; ok && k0 < t.blocks; k0 += kF32Chunk) {
+        if (!warp_wait(&bars.acc_empty[acc], aph ^ 1, wc)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t d = tmem + acc * 256;
+        const int k1 = min(k0 + kF32Chunk, t.blocks);
+        for (int kb = k0; kb < k1; ++kb) {
+          if (!warp_wait(&bars.split_full[st], ph, wc)) { ok = false; break; }
+          tc_fence_after();
+          if (elect_one()) {
+            const uint32_t a = smem_u32(split_a + st * kSplitA), b = smem_u32(split_b + st * kSplitB);
+            // plane 0 h, 1 m, 2 l; the products of planes (x, y) with x + y <= 2, small ones first
+            constexpr int kX[6] = {2, 0, 1, 1, 0, 0}, kY[6] = {0, 2, 1, 0, 1, 0};
+#pragma unroll
+            for (int c = 0; c < 6; ++c) {
+#pragma unroll
+              for (int s = 0; s < 2; ++s) {
+                const uint32_t pa = kAcrossA ? a + kX[c] * (128 * kF32K * 2) + s * 2048
+                                             : a + (kX[c] >> 1) * (128 * 128) + (kX[c] & 1) * 64 + s * 32;
+                const uint32_t pb = kAcrossB ? b + kY[c] * (64 * kF32K * 2) + s * 2048
+                                             : b + (kY[c] >> 1) * (64 * 128) + (kY[c] & 1) * 64 + s * 32;
+                const uint64_t da = sdesc_sw128(pa, kAcrossA ? kF32K * 128 : 16, 1024);
+                const uint64_t db = sdesc_sw128(pb, kAcrossB ? kF32K * 128 : 16, 1024);
+                umma_bf16_pair(c == 5 ? d : d + 128, da, db, idesc, kb > k0 || s > 0 || (c > 0 && c < 5));
+              }
+            }
+            umma_commit_pair(&bars.split_empty[st]);
+            if (kb == k1 - 1) umma_commit_pair(&bars.acc_full[acc]);
+          }
+          __syncwarp();
+          if (++st == kF32Stages) { st = 0; ph ^= 1; }
+        }
+        if (++acc == 2) { acc = 0; aph ^= 1; }
+      }
+    }
+  } else if (warp >= 4) {
+    // ------------------------------------------------- splitting, and the sums one chunk behind
+    const int q = warp & 3, g = (warp - 4) >> 2, tid = threadIdx.x - 128;
+    const uint32_t lanes = static_cast<uint32_t>(32 * q) << 16;
+    if (kMode != kGemmGradW) {
+      const long long end = expert_begin(off, l.E, l.R);
+      if (end < l.R) {                           // rows of no expert
+        for (int which = 0; which < (l.pre ? 2 : 1); ++which) {
+          uint4* o = static_cast<uint4*>(which ? l.pre : l.out);
+          const int words = (which ? l.n_z : p.n_feat) / 4;
+          for (long long i = end * words + static_cast<long long>(blockIdx.x) * 256 + tid; i < l.R * words;
+               i += static_cast<long long>(gridDim.x) * 256)
+            o[i] = make_uint4(0u, 0u, 0u, 0u);
+        }
+      }
+    }
+    float sum[2][32];                            // columns 64 g + 32 c + j
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int j = 0; j < 32; ++j) sum[c][j] = 0.f;
+
+    // the finished tile's sums to memory: lanes hold neighbouring features, a column is an output row (dW: a row of dW)
+    auto store = [&](const GemmTile& t) {
+      if constexpr (kMode == kGemmForward) {
+        const int fl = kGated ? 16 * q + (lane & 15) : 32 * q + lane;
+        const int f = (t.m * 2 + static_cast<int>(rank)) * (kGated ? 64 : 128) + fl;
+        const int up = lane >> 4;
+        const int zf = f + (kGated ? up * l.n_out : 0);
+        const bool in = f < p.n_feat;
+        const float bias = l.bias && in ? __ldg(l.bias + static_cast<long long>(t.e) * l.n_z + zf) : 0.f;
+        const long long row = t.row0 + g * 64;
+        float* out = static_cast<float*>(l.out) + row * l.n_out + f;
+        float* pre = static_cast<float*>(l.pre) + row * l.n_z + zf;
+        const float* res = static_cast<const float*>(l.residual) + row * l.n_out + f;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) {
+            sum[c][j] += bias;
+            const int col = c * 32 + j;
+            if (l.pre && in && g * 64 + col < t.cols) pre[static_cast<long long>(col) * l.n_z] = sum[c][j];
+          }
+          if (kGated) {                          // of two columns each half of the warp finishes one
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) {
+              const float got = __shfl_xor_sync(0xffffffffu, up ? sum[c][j] : sum[c][j + 1], 16);
+              const float y = act_value<kAct, false>(up ? got : sum[c][j]) * (up ? sum[c][j + 1] : got);
+              const int col = c * 32 + j + up;
+              if (in && g * 64 + col < t.cols) {
+                const long long at = static_cast<long long>(col) * l.n_out;
+                out[at] = l.residual ? y + __ldg(res + at) : y;
+              }
+            }
+          } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+              const int col = c * 32 + j;
+              if (in && g * 64 + col < t.cols) {
+                const long long at = static_cast<long long>(col) * l.n_out;
+                const float y = act_value<kAct, false>(sum[c][j]);
+                out[at] = l.residual ? y + __ldg(res + at) : y;
+              }
+            }
+          }
+        }
+      } else {
+        const int f = t.m * 256 + static_cast<int>(rank) * 128 + 32 * q + lane;
+        const long long row = kMode == kGemmGradW ? static_cast<long long>(t.e) * l.n_z + t.col0 : t.row0;
+        float* out = (kMode == kGemmGradW ? l.dW : static_cast<float*>(l.out)) + (row + g * 64) * l.n_in + f;
+        const bool add = kMode == kGemmGradW && l.accumulate;
+        if (f < l.n_in) {
+#pragma unroll
+          for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+              if (g * 64 + c * 32 + j < t.cols) {
+                float* at = out + static_cast<long long>(c * 32 + j) * l.n_in;
+                *at = add ? *at + sum[c][j] : sum[c][j];
+              }
+            }
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int j = 0; j < 32; ++j) sum[c][j] = 0.f;
+    };
+
+    int st = 0, acc = 0;
+    uint32_t ph = 0, aph = 0;
+    bool ok = true;
+    Pending pend{};
+    auto drain = [&]() {                         // the pending chunk's sums; false when the wait ran out
+      if (!pend.any) return true;
+      pend.any = false;
+      if (!warp_wait(&bars.acc_full[acc], aph, wc)) return false;
+      tc_fence_after();
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const int col = g * 64 + c * 32;
+        if (col < pend.t.cols) {
+          float v[32];
+          tmem_ld32(tmem + acc * 256 + 128 + col + lanes, v);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) sum[c][j] += v[j];
+          tmem_ld32(tmem + acc * 256 + col + lanes, v);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) sum[c][j] += v[j];
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_peer(peer_smem(&bars.acc_empty[acc], 0));
+      if (++acc == 2) { acc = 0; aph ^= 1; }
+      if (pend.last) store(pend.t);
+      return true;
+    };
+    for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
+      const GemmTile t = gemm_tile<kMode, kF32Cols, kF32K>(p, rt, off, tile);
+      if (t.blocks == 0) {                       // dW of an expert without rows
+        ok = drain();
+        if (ok && !l.accumulate) store(t);
+        continue;
+      }
+      for (int k0 = 0; ok && k0 < t.blocks; k0 += kF32Chunk) {
+        const int k1 = min(k0 + kF32Chunk, t.blocks);
+        for (int kb = k0; kb < k1; ++kb) {
+          if (!warp_wait(&bars.raw_full[st], ph, wc) || !warp_wait(&bars.split_empty[st], ph ^ 1, wc)) { ok = false; break; }
+          const int depth = kb == t.blocks - 1 ? t.last : kF32K;
+          const uint8_t* ra = raw_a + st * kRawA;
+          const uint8_t* rb = raw_b + st * kRawB;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) split_word<kAcrossA, 128>(ra, split_a + st * kSplitA, tid + 256 * i, kMode == kGemmGradW ? depth : kF32K);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) split_word<kAcrossB, 64>(rb, split_b + st * kSplitB, tid + 256 * i, depth);
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive_peer(peer_smem(&bars.split_full[st], 0));
+            mbar_arrive(&bars.raw_empty[st]);
+          }
+          if (++st == kF32Stages) { st = 0; ph ^= 1; }
+        }
+        if (!ok) break;
+        ok = drain();
+        pend = Pending{t, true, k0 == 0, k1 == t.blocks};
+      }
+    }
+    if (ok) ok = drain();
+    // every plane given back: no commit of the first CTA is still on its way to this one when it ends
+    for (int i = 0; ok && i < kF32Stages; ++i) {
+      ok = warp_wait(&bars.split_empty[st], ph ^ 1, wc);
+      if (++st == kF32Stages) { st = 0; ph ^= 1; }
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (bars.abort && threadIdx.x == 0)            // copies and products in flight end long before this does
+    for (int i = 0; i < 1000; ++i) __nanosleep(1000);
+  __syncthreads();
+  cluster_sync();
+  tc_fence_after();
+  if (warp == 2) tmem_dealloc_pair(tmem, 512);
+}
+
+template <int kMode, int kAct, bool kGated>
+cudaError_t launch(const ExpertGemmParams& p, const CUtensorMap& a, const CUtensorMap& b, long long tiles, int n_sms,
+                   cudaStream_t s) {
+  static GemmResidency held;
+  int pairs = 0;
+  const cudaError_t e = gemm_pairs(held, k_expert_gemm_f32<kMode, kAct, kGated>, kF32Threads, kF32Smem, 0, n_sms, &pairs);
+  if (e != cudaSuccess) return e;
+  pairs = static_cast<int>(std::min<long long>(pairs, std::max(1ll, tiles)));
+  return launch_pdl(k_expert_gemm_f32<kMode, kAct, kGated>, dim3(2 * pairs), dim3(kF32Threads), kF32Smem, s, a, b, p);
+}
+
+}  // namespace
+
+cudaError_t launch_expert_gemm_f32(const ExpertLinearParams& l, ExpertGemmMode mode, uint32_t* status,
+                                   uint64_t limit_ns, int n_sms, cudaStream_t s) {
+  ExpertGemmParams p{};
+  p.l = l;
+  p.status = status;
+  p.limit_ns = limit_ns;
+  p.n_feat = mode == kGemmForward ? l.n_out : l.n_in;
+  const int per = mode == kGemmForward && l.gated ? 128 : 256;
+  p.m_tiles = (p.n_feat + per - 1) / per;
+  p.n_tiles = (l.n_z + kF32Cols - 1) / kF32Cols;
+  const uint64_t R = static_cast<uint64_t>(l.R), ni = l.n_in, nz = l.n_z, E = l.E;
+  CUtensorMap a, b;
+  bool ok;
+  if (mode == kGemmGradW) {
+    const uint64_t da[2] = {ni, R}, sta[1] = {ni * 4}, db[2] = {nz, R}, stb[1] = {nz * 4};
+    const uint32_t boxa[2] = {128, kF32K}, boxb[2] = {64, kF32K};
+    ok = encode_f32(&a, l.X, 2, da, sta, boxa) && encode_f32(&b, l.dZ, 2, db, stb, boxb);
+  } else {
+    const uint64_t da[3] = {ni, nz, E}, sta[2] = {ni * 4, ni * nz * 4};
+    const uint32_t across[3] = {128, kF32K, 1}, along[3] = {kF32K, l.gated ? 16u : 128u, 1};
+    const uint64_t depth = mode == kGemmForward ? ni : nz;
+    const uint64_t db[2] = {depth, R}, stb[1] = {depth * 4};
+    const uint32_t boxb[2] = {kF32K, 64};
+    ok = encode_f32(&a, l.W, 3, da, sta, mode == kGemmGradX ? across : along) &&
+         encode_f32(&b, mode == kGemmForward ? l.X : l.dZ, 2, db, stb, boxb);
+  }
+  if (!ok) return cudaErrorInvalidValue;
+  // at most R / 128 + min(E, R) row tiles
+  const long long tiles = (l.R / kF32Cols + std::min<long long>(l.E, l.R)) * p.m_tiles;
+  if (mode == kGemmForward)
+    return with_act(l.act, [&](auto act) {
+      constexpr int kAct = decltype(act)::value;
+      return l.gated ? launch<kGemmForward, kAct, true>(p, a, b, tiles, n_sms, s)
+                     : launch<kGemmForward, kAct, false>(p, a, b, tiles, n_sms, s);
+    });
+  if (mode == kGemmGradX) return launch<kGemmGradX, SMOES_ACT_NONE, false>(p, a, b, tiles, n_sms, s);
+  return launch<kGemmGradW, SMOES_ACT_NONE, false>(p, a, b, static_cast<long long>(l.E) * p.m_tiles * p.n_tiles, n_sms, s);
+}
+
+}  // namespace smoes

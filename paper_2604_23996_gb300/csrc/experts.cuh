@@ -1,5 +1,5 @@
 // experts.cuh -- the expert layer: plan, kernel parameters and launchers shared by experts_api.cu and
-// the kernels (expert_sort.cu, expert_rows.cu, expert_linear.cu, expert_gemm.cu, expert_act.cu).
+// the kernels (expert_sort.cu, expert_rows.cu, expert_gemm.cu, expert_gemm_f32.cu, expert_act.cu).
 #pragma once
 
 #include <cuda_bf16.h>
@@ -68,7 +68,7 @@ struct ExpertActParams {
   float* part;               // [ranges + E][n_z] (workspace)
 };
 
-// The bf16 products on the tensor cores (expert_gemm.cu): D[m, n] = sum over the depth of A[m] B[n], with
+// The products on the tensor cores (expert_gemm.cu, expert_gemm_f32.cu): D[m, n] = sum over the depth of A[m] B[n], with
 // the features of an output row along m and the rows along n (the weights' gradient: n_in along m, n_z
 // along n, the expert's rows as the depth).
 enum ExpertGemmMode { kGemmForward = 0, kGemmGradX = 1, kGemmGradW = 2 };
@@ -83,13 +83,12 @@ struct ExpertGemmParams {
 
 cudaError_t launch_expert_gemm(const ExpertLinearParams& p, ExpertGemmMode mode, uint32_t* status, uint64_t limit_ns,
                                int n_sms, cudaStream_t s);
+cudaError_t launch_expert_gemm_f32(const ExpertLinearParams& p, ExpertGemmMode mode, uint32_t* status,
+                                   uint64_t limit_ns, int n_sms, cudaStream_t s);
 cudaError_t launch_expert_sort(const ExpertSortParams& p, cudaStream_t s);
 cudaError_t launch_expert_dispatch(const ExpertRowsParams& p, bool bf16, cudaStream_t s);
 cudaError_t launch_expert_combine(const ExpertRowsParams& p, bool bf16, cudaStream_t s);
 cudaError_t launch_expert_combine_bwd(const ExpertRowsParams& p, bool bf16, cudaStream_t s);
-cudaError_t launch_expert_linear(const ExpertLinearParams& p, cudaStream_t s);
-cudaError_t launch_expert_dx(const ExpertLinearParams& p, cudaStream_t s);
-cudaError_t launch_expert_dw(const ExpertLinearParams& p, cudaStream_t s);
 cudaError_t launch_expert_act_bwd(ExpertActParams p, bool bf16, int n_sms, cudaStream_t s);   // fills ranges
 int act_ranges(int n_sms);   // most ranges of the activation gradient
 

@@ -46,6 +46,13 @@ smoes_status check_aligned(Ptrs... ptrs) {
 
 bool known_act(int act) { return act == SMOES_ACT_NONE || act == SMOES_ACT_SILU || act == SMOES_ACT_GELU; }
 
+cudaError_t launch_product(const smoes_experts_s* P, const ExpertLinearParams& p, ExpertGemmMode mode, void* ws,
+                           cudaStream_t stream) {
+  uint32_t* status = static_cast<uint32_t*>(ws);
+  return P->desc.dtype == SMOES_BF16 ? launch_expert_gemm(p, mode, status, P->limit_ns, P->n_sms, stream)
+                                     : launch_expert_gemm_f32(p, mode, status, P->limit_ns, P->n_sms, stream);
+}
+
 ExpertRowsParams rows_params(const smoes_experts_s* P, int d) {
   ExpertRowsParams p{};
   p.T = P->desc.T;
@@ -244,9 +251,7 @@ smoes_status smoes_expert_linear(smoes_experts P, const smoes_linear_args* args,
   p.residual = a.residual;
   p.out = out;
   p.pre = pre;
-  return cuda_status(P->desc.dtype == SMOES_BF16
-                         ? launch_expert_gemm(p, kGemmForward, static_cast<uint32_t*>(ws), P->limit_ns, P->n_sms, stream)
-                         : launch_expert_linear(p, stream));
+  return cuda_status(launch_product(P, p, kGemmForward, ws, stream));
 }
 
 smoes_status smoes_expert_act_bwd(smoes_experts P, const void* dOut, const void* pre, int n_out, int act, int gated,
@@ -316,12 +321,9 @@ smoes_status smoes_expert_linear_bwd(smoes_experts P, const void* dZ, const void
   p.out = dX;
   p.dW = dW;
   p.accumulate = accumulate_dW ? 1 : 0;
-  const bool bf16 = P->desc.dtype == SMOES_BF16;
-  uint32_t* status = static_cast<uint32_t*>(ws);
   cudaError_t e = cudaSuccess;
-  if (dX) e = bf16 ? launch_expert_gemm(p, kGemmGradX, status, P->limit_ns, P->n_sms, stream) : launch_expert_dx(p, stream);
-  if (e == cudaSuccess && dW)
-    e = bf16 ? launch_expert_gemm(p, kGemmGradW, status, P->limit_ns, P->n_sms, stream) : launch_expert_dw(p, stream);
+  if (dX) e = launch_product(P, p, kGemmGradX, ws, stream);
+  if (e == cudaSuccess && dW) e = launch_product(P, p, kGemmGradW, ws, stream);
   return cuda_status(e);
 }
 

@@ -265,8 +265,10 @@ cudaError_t static_perm_scratch(StaticPermScratch** out);
 cudaError_t launch_static_perm_prep(StaticPermScratch* sp, const int32_t* expert_bin,
                                     const int32_t* expert_slot, int E, cudaStream_t s);
 
-// Tiled TMA map of a row-major bf16 tensor of `rank` dimensions, innermost first (api.cu); strides in
-// bytes of dimensions 1 and up. Reads outside give zeros.
+// Tiled TMA maps of a row-major tensor of `rank` dimensions, innermost first (api.cu); strides in bytes of
+// dimensions 1 and up. Reads outside give zeros. bf16 boxes have the 128-byte swizzle, fp32 boxes none.
+bool encode_f32(CUtensorMap* m, const void* ptr, int rank, const uint64_t* dims, const uint64_t* strides,
+                const uint32_t* box);
 bool encode_bf16(CUtensorMap* m, const void* ptr, int rank, const uint64_t* dims, const uint64_t* strides,
                  const uint32_t* box);
 
