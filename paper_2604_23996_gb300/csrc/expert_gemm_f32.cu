@@ -87,12 +87,6 @@ __device__ __forceinline__ void split_word(const uint8_t* raw, uint8_t* planes, 
   }
 }
 
-// A chunk whose sums are still in tensor memory.
-struct Pending {
-  GemmTile t;
-  bool any, first, last;     // of its tile
-};
-
 template <int kMode, int kAct, bool kGated>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kF32Threads, 1)
 k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
@@ -293,14 +287,14 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         float* out = (kMode == kGemmGradW ? l.dW : static_cast<float*>(l.out)) + (row + g * 64) * l.n_in + f;
         const bool add = kMode == kGemmGradW && l.accumulate;
         if (f < l.n_in) {
+          const int cols = t.cols - g * 64;      // (a pointer that steps: 64 addresses at once do not fit the registers)
 #pragma unroll
           for (int c = 0; c < 2; ++c)
 #pragma unroll
             for (int j = 0; j < 32; ++j) {
-              if (g * 64 + c * 32 + j < t.cols) {
-                float* at = out + static_cast<long long>(c * 32 + j) * l.n_in;
-                *at = add ? *at + sum[c][j] : sum[c][j];
-              }
+              if (c * 32 + j < cols) *out = add ? *out + sum[c][j] : sum[c][j];
+              out += l.n_in;
+              asm volatile("" : "+l"(out));
             }
         }
       }
@@ -310,67 +304,70 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         for (int j = 0; j < 32; ++j) sum[c][j] = 0.f;
     };
 
+    // a chunk is split, then the one before it drained (one place each: inlined twice the sums do not fit the registers)
     int st = 0, acc = 0;
     uint32_t ph = 0, aph = 0;
     bool ok = true;
-    Pending pend{};
-    auto drain = [&]() {                         // the pending chunk's sums; false when the wait ran out
-      if (!pend.any) return true;
-      pend.any = false;
-      if (!warp_wait(&bars.acc_full[acc], aph, wc)) return false;
-      tc_fence_after();
+    int tile = pair, k0 = 0;
+    bool more = tile < n_total;
+    GemmTile t{}, done{};                        // the chunk's tile; that of the chunk before
+    if (more) t = gemm_tile<kMode, kF32Cols, kF32K>(p, rt, off, tile);
+    bool pending = false, pending_last = false;
+    while (more || pending) {
+      const int k1 = more ? min(k0 + kF32Chunk, t.blocks) : k0;
+      for (int kb = k0; kb < k1; ++kb) {
+        if (!warp_wait(&bars.raw_full[st], ph, wc) || !warp_wait(&bars.split_empty[st], ph ^ 1, wc)) { ok = false; break; }
+        const int depth = kMode == kGemmGradW && kb == t.blocks - 1 ? t.last : kF32K;
+        const uint8_t* ra = raw_a + st * kRawA;
+        const uint8_t* rb = raw_b + st * kRawB;
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const int col = g * 64 + c * 32;
-        if (col < pend.t.cols) {
-          float v[32];
-          tmem_ld32(tmem + acc * 256 + 128 + col + lanes, v);
+        for (int i = 0; i < 4; ++i) split_word<kAcrossA, 128>(ra, split_a + st * kSplitA, tid + 256 * i, depth);
 #pragma unroll
-          for (int j = 0; j < 32; ++j) sum[c][j] += v[j];
-          tmem_ld32(tmem + acc * 256 + col + lanes, v);
-#pragma unroll
-          for (int j = 0; j < 32; ++j) sum[c][j] += v[j];
+        for (int i = 0; i < 2; ++i) split_word<kAcrossB, 64>(rb, split_b + st * kSplitB, tid + 256 * i, depth);
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive_peer(peer_smem(&bars.split_full[st], 0));
+          mbar_arrive(&bars.raw_empty[st]);
         }
+        if (++st == kF32Stages) { st = 0; ph ^= 1; }
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_peer(peer_smem(&bars.acc_empty[acc], 0));
-      if (++acc == 2) { acc = 0; aph ^= 1; }
-      if (pend.last) store(pend.t);
-      return true;
-    };
-    for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
-      const GemmTile t = gemm_tile<kMode, kF32Cols, kF32K>(p, rt, off, tile);
-      if (t.blocks == 0) {                       // dW of an expert without rows
-        ok = drain();
-        if (ok && !l.accumulate) store(t);
-        continue;
-      }
-      for (int k0 = 0; ok && k0 < t.blocks; k0 += kF32Chunk) {
-        const int k1 = min(k0 + kF32Chunk, t.blocks);
-        for (int kb = k0; kb < k1; ++kb) {
-          if (!warp_wait(&bars.raw_full[st], ph, wc) || !warp_wait(&bars.split_empty[st], ph ^ 1, wc)) { ok = false; break; }
-          const int depth = kb == t.blocks - 1 ? t.last : kF32K;
-          const uint8_t* ra = raw_a + st * kRawA;
-          const uint8_t* rb = raw_b + st * kRawB;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) split_word<kAcrossA, 128>(ra, split_a + st * kSplitA, tid + 256 * i, kMode == kGemmGradW ? depth : kF32K);
-#pragma unroll
-          for (int i = 0; i < 2; ++i) split_word<kAcrossB, 64>(rb, split_b + st * kSplitB, tid + 256 * i, depth);
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) {
-            mbar_arrive_peer(peer_smem(&bars.split_full[st], 0));
-            mbar_arrive(&bars.raw_empty[st]);
-          }
-          if (++st == kF32Stages) { st = 0; ph ^= 1; }
-        }
+      if (!ok) break;
+      if (pending && done.blocks > 0) {
+        ok = warp_wait(&bars.acc_full[acc], aph, wc);
         if (!ok) break;
-        ok = drain();
-        pend = Pending{t, true, k0 == 0, k1 == t.blocks};
+        tc_fence_after();
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const int col = g * 64 + c * 32;
+          if (col < done.cols) {
+            float v[32];
+            tmem_ld32(tmem + acc * 256 + 128 + col + lanes, v);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) sum[c][j] += v[j];
+            tmem_ld32(tmem + acc * 256 + col + lanes, v);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) sum[c][j] += v[j];
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_peer(peer_smem(&bars.acc_empty[acc], 0));
+        if (++acc == 2) { acc = 0; aph ^= 1; }
+      }
+      // (dW of an expert without rows: one chunk of no blocks)
+      if (pending && pending_last && (kMode != kGemmGradW || done.blocks > 0 || !l.accumulate)) store(done);
+      pending = more;
+      pending_last = k1 == t.blocks;
+      done = t;
+      k0 = k1;
+      if (more && pending_last) {
+        tile += n_pairs;
+        k0 = 0;
+        more = tile < n_total;
+        if (more) t = gemm_tile<kMode, kF32Cols, kF32K>(p, rt, off, tile);
       }
     }
-    if (ok) ok = drain();
     // every plane given back: no commit of the first CTA is still on its way to this one when it ends
     for (int i = 0; ok && i < kF32Stages; ++i) {
       ok = warp_wait(&bars.split_empty[st], ph ^ 1, wc);
