@@ -457,6 +457,8 @@ class Experts:
     expert and one selection (``E = k = 1``) is a dense layer and needs no sort. Tensors are contiguous, of the
     plan's type (weights of the top-k, biases and their gradients float32) and on the plan's device; a tensor
     that is not raises a ValueError before anything is launched. Results are new tensors unless an output is given.
+    Calls run on the stream given, or the current one of the plan's device. The methods call the library themselves:
+    a decoding step's calls are bound by their time on the host.
     """
 
     def __init__(self, T, E, k, dtype=SMOES_BF16, max_width=0, device="cuda"):
@@ -482,73 +484,76 @@ class Experts:
         except Exception:
             pass
 
-    def _on(self, stream):
-        """The stream given, or the current one of the plan's device."""
-        return torch.cuda.current_stream(self._index) if stream is None else stream
+    def _stream(self, stream):
+        return torch._C._cuda_getCurrentRawStream(self._index) if stream is None else stream.cuda_stream
 
-    def _want(self, name, t, shape, dtype=None):
-        """Checks one argument (None stays None)."""
+    def _in(self, name, t, shape, dtype):
+        """Address of one checked argument; None stays None."""
         if t is None:
-            return
-        dtype = dtype or self.dtype
-        if t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.device != self.device:
+            return None
+        if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != self._index:
             raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {tuple(shape)} on {self.device} is "
                              f"wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        return t.data_ptr()
 
-    def _out(self, t, shape, dtype=None):
+    def _new(self, t, shape, dtype):
+        """The output given, checked, or a new one."""
         if t is None:
-            return torch.empty(shape, dtype=dtype or self.dtype, device=self.device)
-        self._want("output", t, shape, dtype)
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        self._in("output", t, shape, dtype)
         return t
 
     def sort(self, topk_idx, stream=None):
         """Selections [T, k] int32 (negative: takes no part) into expert order; fills and returns
         expert_offsets, row_slot, slot_row."""
-        self._want("topk_idx", topk_idx, (self.T, self.k), torch.int32)
-        _check(smoes_expert_sort(self.plan, topk_idx, self.expert_offsets, self.row_slot, self.slot_row, self.ws,
-                                 self._on(stream)), "smoes_expert_sort")
+        idx = self._in("topk_idx", topk_idx, (self.T, self.k), torch.int32)
+        ws = self.ws
+        _check(_lib.smoes_expert_sort(self.plan, idx, self.expert_offsets.data_ptr(), self.row_slot.data_ptr(),
+                                      self.slot_row.data_ptr(), ws.data_ptr(), ws.numel(), self._stream(stream)),
+               "smoes_expert_sort")
         return self.expert_offsets, self.row_slot, self.slot_row
 
     def dispatch(self, X, out=None, stream=None):
         """Tokens [T, d] into expert order: [R, d]."""
         d = X.shape[-1]
-        self._want("X", X, (self.T, d))
-        out = self._out(out, (self.R, d))
-        _check(smoes_expert_dispatch(self.plan, X, d, self.expert_offsets, self.slot_row, out, self._on(stream)),
-               "smoes_expert_dispatch")
+        x = self._in("X", X, (self.T, d), self.dtype)
+        out = self._new(out, (self.R, d), self.dtype)
+        _check(_lib.smoes_expert_dispatch(self.plan, x, d, self.expert_offsets.data_ptr(), self.slot_row.data_ptr(),
+                                          out.data_ptr(), self._stream(stream)), "smoes_expert_dispatch")
         return out
 
     def dispatch_bwd(self, dXs, residual=None, out=None, stream=None):
         """Gradient of the tokens from that of their rows, plus ``residual`` [T, d]."""
         d = dXs.shape[-1]
-        self._want("dXs", dXs, (self.R, d))
-        self._want("residual", residual, (self.T, d))
-        out = self._out(out, (self.T, d))
-        _check(smoes_expert_dispatch_bwd(self.plan, dXs, d, self.slot_row, residual, out, self._on(stream)),
-               "smoes_expert_dispatch_bwd")
+        dx = self._in("dXs", dXs, (self.R, d), self.dtype)
+        res = self._in("residual", residual, (self.T, d), self.dtype)
+        out = self._new(out, (self.T, d), self.dtype)
+        _check(_lib.smoes_expert_dispatch_bwd(self.plan, dx, d, self.slot_row.data_ptr(), res, out.data_ptr(),
+                                              self._stream(stream)), "smoes_expert_dispatch_bwd")
         return out
 
     def combine(self, Ys, topk_w, residual=None, out=None, stream=None):
         """Rows [R, d] back to their tokens, weighted by topk_w [T, k] float32, plus ``residual``."""
         d = Ys.shape[-1]
-        self._want("Ys", Ys, (self.R, d))
-        self._want("topk_w", topk_w, (self.T, self.k), torch.float32)
-        self._want("residual", residual, (self.T, d))
-        out = self._out(out, (self.T, d))
-        _check(smoes_expert_combine(self.plan, Ys, d, topk_w, self.slot_row, residual, out, self._on(stream)),
-               "smoes_expert_combine")
+        ys = self._in("Ys", Ys, (self.R, d), self.dtype)
+        w = self._in("topk_w", topk_w, (self.T, self.k), torch.float32)
+        res = self._in("residual", residual, (self.T, d), self.dtype)
+        out = self._new(out, (self.T, d), self.dtype)
+        _check(_lib.smoes_expert_combine(self.plan, ys, d, w, self.slot_row.data_ptr(), res, out.data_ptr(),
+                                         self._stream(stream)), "smoes_expert_combine")
         return out
 
     def combine_bwd(self, dY, Ys, topk_w, dYs=None, d_topk_w=None, stream=None):
         """Gradients of the rows and of the weights (the d_topk_w of ``Router.backward``)."""
         d = dY.shape[-1]
-        self._want("dY", dY, (self.T, d))
-        self._want("Ys", Ys, (self.R, d))
-        self._want("topk_w", topk_w, (self.T, self.k), torch.float32)
-        dYs = self._out(dYs, (self.R, d))
-        d_topk_w = self._out(d_topk_w, (self.T, self.k), torch.float32)
-        _check(smoes_expert_combine_bwd(self.plan, dY, Ys, d, topk_w, self.expert_offsets, self.slot_row, dYs,
-                                        d_topk_w, self._on(stream)), "smoes_expert_combine_bwd")
+        dy = self._in("dY", dY, (self.T, d), self.dtype)
+        ys = self._in("Ys", Ys, (self.R, d), self.dtype)
+        w = self._in("topk_w", topk_w, (self.T, self.k), torch.float32)
+        dYs = self._new(dYs, (self.R, d), self.dtype)
+        d_topk_w = self._new(d_topk_w, (self.T, self.k), torch.float32)
+        _check(_lib.smoes_expert_combine_bwd(self.plan, dy, ys, d, w, self.expert_offsets.data_ptr(),
+                                             self.slot_row.data_ptr(), dYs.data_ptr(), d_topk_w.data_ptr(),
+                                             self._stream(stream)), "smoes_expert_combine_bwd")
         return dYs, d_topk_w
 
     def linear(self, X, W, bias=None, act=SMOES_ACT_NONE, gated=False, residual=None, save_pre=False, out=None,
@@ -559,15 +564,15 @@ class Experts:
         n_out = n_z // 2 if gated else n_z
         if gated and n_z % 2:
             raise ValueError(f"W: a gated layer has an even number of rows, got {n_z}")
-        self._want("X", X, (self.R, n_in))
-        self._want("W", W, (self.E, n_z, n_in))
-        self._want("bias", bias, (self.E, n_z), torch.float32)
-        self._want("residual", residual, (self.R, n_out))
-        out = self._out(out, (self.R, n_out))
+        dt, ws = self.dtype, self.ws
+        args = LinearArgs(self._in("X", X, (self.R, n_in), dt), self._in("W", W, (self.E, n_z, n_in), dt),
+                          self._in("bias", bias, (self.E, n_z), torch.float32),
+                          self._in("residual", residual, (self.R, n_out), dt), n_in, n_out, act, gated)
+        out = self._new(out, (self.R, n_out), dt)
         if save_pre or pre is not None:
-            pre = self._out(pre, (self.R, n_z))
-        _check(smoes_expert_linear(self.plan, X, W, bias, residual, n_in, n_out, act, gated, self.expert_offsets,
-                                   out, pre, self.ws, self._on(stream)), "smoes_expert_linear")
+            pre = self._new(pre, (self.R, n_z), dt)
+        _check(_lib.smoes_expert_linear(self.plan, args, self.expert_offsets.data_ptr(), out.data_ptr(), _ptr(pre),
+                                        ws.data_ptr(), ws.numel(), self._stream(stream)), "smoes_expert_linear")
         return out, pre
 
     def act_bwd(self, dOut, pre=None, act=SMOES_ACT_NONE, gated=False, bias_grad=False, dZ=None, db=None,
@@ -576,35 +581,42 @@ class Experts:
         dOut itself. db is None unless bias_grad (or a tensor to write) asks for it."""
         n_out = dOut.shape[-1]
         n_z = 2 * n_out if gated else n_out
-        self._want("dOut", dOut, (self.R, n_out))
+        dout = self._in("dOut", dOut, (self.R, n_out), self.dtype)
         if bias_grad or db is not None:
-            db = self._out(db, (self.E, n_z), torch.float32)
+            db = self._new(db, (self.E, n_z), torch.float32)
         if act == SMOES_ACT_NONE and not gated:
-            if db is not None:
-                _check(smoes_expert_act_bwd(self.plan, dOut, None, n_out, act, gated, self.expert_offsets, None, db,
-                                            self.ws, self._on(stream)), "smoes_expert_act_bwd")
-            return dOut, db
-        if pre is None:
+            z, dz, dZ = None, None, dOut
+            if db is None:
+                return dZ, None
+        elif pre is None:
             raise ValueError("pre: the pre-activations that linear saved are wanted")
-        self._want("pre", pre, (self.R, n_z))
-        dZ = self._out(dZ, (self.R, n_z))
-        _check(smoes_expert_act_bwd(self.plan, dOut, pre, n_out, act, gated, self.expert_offsets, dZ, db, self.ws,
-                                    self._on(stream)), "smoes_expert_act_bwd")
+        else:
+            z = self._in("pre", pre, (self.R, n_z), self.dtype)
+            dZ = self._new(dZ, (self.R, n_z), self.dtype)
+            dz = dZ.data_ptr()
+        ws = self.ws
+        _check(_lib.smoes_expert_act_bwd(self.plan, dout, z, n_out, act, gated, self.expert_offsets.data_ptr(), dz,
+                                         _ptr(db), ws.data_ptr(), ws.numel(), self._stream(stream)),
+               "smoes_expert_act_bwd")
         return dZ, db
 
     def linear_bwd(self, dZ, X, W, need_dX=True, need_dW=True, dX=None, dW=None, accumulate=False, stream=None):
         """Gradients of the rows [R, n_in] and of the weights (float32; accumulate adds to the given dW)."""
         n_z, n_in = W.shape[-2:]
-        self._want("dZ", dZ, (self.R, n_z))
-        self._want("X", X, (self.R, n_in))
-        self._want("W", W, (self.E, n_z, n_in))
+        dz = self._in("dZ", dZ, (self.R, n_z), self.dtype)
+        x = self._in("X", X, (self.R, n_in), self.dtype)
+        w = self._in("W", W, (self.E, n_z, n_in), self.dtype)
         if accumulate and dW is None:
             raise ValueError("dW: a tensor to accumulate into is wanted")
-        dX = self._out(dX, (self.R, n_in)) if need_dX else None
-        dW = self._out(dW, (self.E, n_z, n_in), torch.float32) if need_dW else None
-        _check(smoes_expert_linear_bwd(self.plan, dZ, X, W, n_in, n_z, self.expert_offsets, dX, dW, accumulate,
-                                       self.ws, self._on(stream)), "smoes_expert_linear_bwd")
+        dX = self._new(dX, (self.R, n_in), self.dtype) if need_dX else None
+        dW = self._new(dW, (self.E, n_z, n_in), torch.float32) if need_dW else None
+        ws = self.ws
+        _check(_lib.smoes_expert_linear_bwd(self.plan, dz, x, w, n_in, n_z, self.expert_offsets.data_ptr(), _ptr(dX),
+                                            _ptr(dW), accumulate, ws.data_ptr(), ws.numel(), self._stream(stream)),
+               "smoes_expert_linear_bwd")
         return dX, dW
 
     def device_status(self, stream=None):
-        return smoes_experts_read_status(self.plan, self.ws, self._on(stream))
+        if stream is None:
+            stream = torch.cuda.current_stream(self._index)
+        return smoes_experts_read_status(self.plan, self.ws, stream)

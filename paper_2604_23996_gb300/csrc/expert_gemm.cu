@@ -355,6 +355,10 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
       const GemmTile t = gemm_tile<kMode, 256, kGemmK>(p, rt, off, tile);
       if constexpr (kMode == kGemmGradW) {
+        if (t.blocks == 0) {                     // an expert without rows
+          if (!l.accumulate) zero_weight_tile(l, t, 256, static_cast<int>(rank), warp - 4, kGemmEpiWarps);
+          continue;
+        }
         float sum[4][32];
 #pragma unroll
         for (int c = 0; c < 4; ++c)
@@ -379,16 +383,15 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
           if (++acc == 2) { acc = 0; aph ^= 1; }
         }
         const int i = t.m * 256 + static_cast<int>(rank) * 128 + 32 * q + lane;
-        if (ok && i < l.n_in && !(l.accumulate && t.blocks == 0)) {
+        if (ok && i < l.n_in) {
           float* w = l.dW + (static_cast<long long>(t.e) * l.n_z + t.col0 + g * 128) * l.n_in + i;
+          const int cols = t.cols - g * 128;
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) {
-              if (g * 128 + c * 32 + j < t.cols) {
-                float* at = w + static_cast<long long>(c * 32 + j) * l.n_in;
-                *at = l.accumulate ? *at + sum[c][j] : sum[c][j];
-              }
+              if (c * 32 + j < cols) *w = l.accumulate ? *w + sum[c][j] : sum[c][j];
+              w += l.n_in;
             }
           }
         }

@@ -54,6 +54,17 @@ __device__ __forceinline__ int gemm_n(int cols) {
   return kMode == kGemmGradW ? (cols + 127) & ~127 : (cols + 31) & ~31;
 }
 
+// Zeros in a CTA's half of a tile of dW, by `warps` warps of which this is number w: a row of 128 features a warp at a
+// time, 16 bytes a lane.
+__device__ __forceinline__ void zero_weight_tile(const ExpertLinearParams& l, const GemmTile& t, int cols, int rank,
+                                                 int w, int warps) {
+  const int f = t.m * 256 + rank * 128 + (threadIdx.x & 31) * 4;
+  if (f >= l.n_in) return;                       // (n_in is a multiple of 4)
+  float* row = l.dW + (static_cast<long long>(t.e) * l.n_z + t.col0) * l.n_in + f;
+  for (int c = w; c < min(cols, t.cols); c += warps)
+    *reinterpret_cast<float4*>(row + static_cast<long long>(c) * l.n_in) = make_float4(0.f, 0.f, 0.f, 0.f);
+}
+
 // Pairs of CTAs of a kernel that the device holds at once, and its shared memory allowed (once per kernel and device).
 struct GemmResidency {
   std::mutex mu;

@@ -32,16 +32,17 @@ constexpr int kF32Warps = 8;                     // splitting and epilogue
 constexpr int kF32K = 32;                        // depth of a block
 constexpr int kF32Chunk = 8;                     // blocks between moves of the sums
 constexpr int kF32Cols = 128;
-constexpr int kF32Stages = 3;
+constexpr int kRawStages = 5, kSplitStages = 2;
 constexpr uint32_t kRawA = 128 * kF32K * 4, kRawB = 64 * kF32K * 4;     // one CTA's fp32 operands of a block
 constexpr uint32_t kSplitA = 2 * 128 * 128, kSplitB = 2 * 64 * 128;     // and their planes
-constexpr uint32_t kF32Smem = 1024 + kF32Stages * (kRawA + kRawB + kSplitA + kSplitB) + 256 + 4 * (kExpertsMax + 1);
+constexpr uint32_t kF32Smem =
+    1024 + kRawStages * (kRawA + kRawB) + kSplitStages * (kSplitA + kSplitB) + 256 + 4 * (kExpertsMax + 1);
 static_assert(kF32Smem <= 227 * 1024, "shared memory of a CTA");
 
 struct F32Bars {
-  uint64_t raw_full[kF32Stages], raw_empty[kF32Stages];
-  uint64_t split_full[kF32Stages];               // planes of both CTAs (first CTA's)
-  uint64_t split_empty[kF32Stages];
+  uint64_t raw_full[kRawStages], raw_empty[kRawStages];
+  uint64_t split_full[kSplitStages];               // planes of both CTAs (first CTA's)
+  uint64_t split_empty[kSplitStages];
   uint64_t acc_full[2], acc_empty[2];
   uint32_t tmem;
   int abort;
@@ -90,14 +91,14 @@ __device__ __forceinline__ void split_word(const uint8_t* raw, uint8_t* planes, 
 template <int kMode, int kAct, bool kGated>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kF32Threads, 1)
 k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
-                  const ExpertGemmParams p) {
+                  const __grid_constant__ CUtensorMap tmB16, const ExpertGemmParams p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   uint8_t* split_a = smem;                       // [stage] each
-  uint8_t* split_b = split_a + kF32Stages * kSplitA;
-  uint8_t* raw_a = split_b + kF32Stages * kSplitB;
-  uint8_t* raw_b = raw_a + kF32Stages * kRawA;
-  F32Bars& bars = *reinterpret_cast<F32Bars*>(raw_b + kF32Stages * kRawB);
+  uint8_t* split_b = split_a + kSplitStages * kSplitA;
+  uint8_t* raw_a = split_b + kSplitStages * kSplitB;
+  uint8_t* raw_b = raw_a + kRawStages * kRawA;
+  F32Bars& bars = *reinterpret_cast<F32Bars*>(raw_b + kRawStages * kRawB);
   int32_t* off = reinterpret_cast<int32_t*>(reinterpret_cast<uint8_t*>(&bars) + 256);   // [E + 1] offsets
   const ExpertLinearParams& l = p.l;
   const int warp = warp_index(), lane = threadIdx.x & 31;
@@ -106,9 +107,11 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
   constexpr bool kAcrossA = kMode != kGemmForward, kAcrossB = kMode == kGemmGradW;   // the depth is not contiguous
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kF32Stages; ++i) {
+    for (int i = 0; i < kRawStages; ++i) {
       mbar_init(&bars.raw_full[i], 1);
       mbar_init(&bars.raw_empty[i], kF32Warps);
+    }
+    for (int i = 0; i < kSplitStages; ++i) {
       mbar_init(&bars.split_full[i], 2 * kF32Warps);
       mbar_init(&bars.split_empty[i], 1);
     }
@@ -149,7 +152,9 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
           uint8_t* a = raw_a + st * kRawA;
           uint8_t* b = raw_b + st * kRawB;
           const uint32_t bar = smem_u32(&bars.raw_full[st]);
-          mbar_arrive_expect_tx(&bars.raw_full[st], kRawA + kRawB);
+          // few rows: boxes of 16
+          const bool few = kMode != kGemmGradW && half_n < 64;
+          mbar_arrive_expect_tx(&bars.raw_full[st], kRawA + (few ? half_n * (kF32K * 4) : kRawB));
           const int k0 = kb * kF32K, r = static_cast<int>(rank);
           if (kMode == kGemmGradW) {
             const int r0 = static_cast<int>(t.row0) + k0;
@@ -166,11 +171,16 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
             } else {
               tma_load_3d_pair(a, &tmA, bar, k0, t.m * 256 + r * 128, t.e);
             }
-            tma_load_2d_pair(b, &tmB, bar, k0, static_cast<int>(t.row0) + r * half_n);
+            const int r0 = static_cast<int>(t.row0) + r * half_n;
+            if (!few) {
+              tma_load_2d_pair(b, &tmB, bar, k0, r0);
+            } else {
+              for (int i = 0; i < half_n; i += 16) tma_load_2d_pair(b + i * (kF32K * 4), &tmB16, bar, k0, r0 + i);
+            }
           }
         }
         __syncwarp();
-        if (++st == kF32Stages) { st = 0; ph ^= 1; }
+        if (++st == kRawStages) { st = 0; ph ^= 1; }
       }
     }
   } else if (warp == 1 && rank == 0) {
@@ -210,7 +220,7 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
             if (kb == k1 - 1) umma_commit_pair(&bars.acc_full[acc]);
           }
           __syncwarp();
-          if (++st == kF32Stages) { st = 0; ph ^= 1; }
+          if (++st == kSplitStages) { st = 0; ph ^= 1; }
         }
         if (++acc == 2) { acc = 0; aph ^= 1; }
       }
@@ -305,8 +315,8 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     };
 
     // a chunk is split, then the one before it drained (one place each: inlined twice the sums do not fit the registers)
-    int st = 0, acc = 0;
-    uint32_t ph = 0, aph = 0;
+    int st = 0, raw = 0, acc = 0;
+    uint32_t ph = 0, rph = 0, aph = 0;
     bool ok = true;
     int tile = pair, k0 = 0;
     bool more = tile < n_total;
@@ -316,21 +326,24 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     while (more || pending) {
       const int k1 = more ? min(k0 + kF32Chunk, t.blocks) : k0;
       for (int kb = k0; kb < k1; ++kb) {
-        if (!warp_wait(&bars.raw_full[st], ph, wc) || !warp_wait(&bars.split_empty[st], ph ^ 1, wc)) { ok = false; break; }
+        if (!warp_wait(&bars.raw_full[raw], rph, wc) || !warp_wait(&bars.split_empty[st], ph ^ 1, wc)) { ok = false; break; }
         const int depth = kMode == kGemmGradW && kb == t.blocks - 1 ? t.last : kF32K;
-        const uint8_t* ra = raw_a + st * kRawA;
-        const uint8_t* rb = raw_b + st * kRawB;
+        const uint8_t* ra = raw_a + raw * kRawA;
+        const uint8_t* rb = raw_b + raw * kRawB;
 #pragma unroll
         for (int i = 0; i < 4; ++i) split_word<kAcrossA, 128>(ra, split_a + st * kSplitA, tid + 256 * i, depth);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) split_word<kAcrossB, 64>(rb, split_b + st * kSplitB, tid + 256 * i, depth);
+        for (int i = 0; i < 2; ++i)
+          if (kAcrossB || 32 * i < gemm_n<kMode>(t.cols) / 2)   // (rows 32 i and on)
+            split_word<kAcrossB, 64>(rb, split_b + st * kSplitB, tid + 256 * i, depth);
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) {
           mbar_arrive_peer(peer_smem(&bars.split_full[st], 0));
-          mbar_arrive(&bars.raw_empty[st]);
+          mbar_arrive(&bars.raw_empty[raw]);
         }
-        if (++st == kF32Stages) { st = 0; ph ^= 1; }
+        if (++raw == kRawStages) { raw = 0; rph ^= 1; }
+        if (++st == kSplitStages) { st = 0; ph ^= 1; }
       }
       if (!ok) break;
       if (pending && done.blocks > 0) {
@@ -355,8 +368,9 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         if (lane == 0) mbar_arrive_peer(peer_smem(&bars.acc_empty[acc], 0));
         if (++acc == 2) { acc = 0; aph ^= 1; }
       }
-      // (dW of an expert without rows: one chunk of no blocks)
-      if (pending && pending_last && (kMode != kGemmGradW || done.blocks > 0 || !l.accumulate)) store(done);
+      if (pending && pending_last && done.blocks > 0) store(done);
+      if (kMode == kGemmGradW && pending && done.blocks == 0 && !l.accumulate)   // an expert without rows
+        zero_weight_tile(l, done, kF32Cols, static_cast<int>(rank), warp - 4, kF32Warps);
       pending = more;
       pending_last = k1 == t.blocks;
       done = t;
@@ -369,9 +383,9 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
       }
     }
     // every plane given back: no commit of the first CTA is still on its way to this one when it ends
-    for (int i = 0; ok && i < kF32Stages; ++i) {
+    for (int i = 0; ok && i < kSplitStages; ++i) {
       ok = warp_wait(&bars.split_empty[st], ph ^ 1, wc);
-      if (++st == kF32Stages) { st = 0; ph ^= 1; }
+      if (++st == kSplitStages) { st = 0; ph ^= 1; }
     }
   }
   __syncwarp();
@@ -386,14 +400,14 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
 }
 
 template <int kMode, int kAct, bool kGated>
-cudaError_t launch(const ExpertGemmParams& p, const CUtensorMap& a, const CUtensorMap& b, long long tiles, int n_sms,
-                   cudaStream_t s) {
+cudaError_t launch(const ExpertGemmParams& p, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& b16,
+                   long long tiles, int n_sms, cudaStream_t s) {
   static GemmResidency held;
   int pairs = 0;
   const cudaError_t e = gemm_pairs(held, k_expert_gemm_f32<kMode, kAct, kGated>, kF32Threads, kF32Smem, 0, n_sms, &pairs);
   if (e != cudaSuccess) return e;
   pairs = static_cast<int>(std::min<long long>(pairs, std::max(1ll, tiles)));
-  return launch_pdl(k_expert_gemm_f32<kMode, kAct, kGated>, dim3(2 * pairs), dim3(kF32Threads), kF32Smem, s, a, b, p);
+  return launch_pdl(k_expert_gemm_f32<kMode, kAct, kGated>, dim3(2 * pairs), dim3(kF32Threads), kF32Smem, s, a, b, b16, p);
 }
 
 }  // namespace
@@ -409,20 +423,22 @@ cudaError_t launch_expert_gemm_f32(const ExpertLinearParams& l, ExpertGemmMode m
   p.m_tiles = (p.n_feat + per - 1) / per;
   p.n_tiles = (l.n_z + kF32Cols - 1) / kF32Cols;
   const uint64_t R = static_cast<uint64_t>(l.R), ni = l.n_in, nz = l.n_z, E = l.E;
-  CUtensorMap a, b;
+  CUtensorMap a, b, b16;
   bool ok;
   if (mode == kGemmGradW) {
     const uint64_t da[2] = {ni, R}, sta[1] = {ni * 4}, db[2] = {nz, R}, stb[1] = {nz * 4};
     const uint32_t boxa[2] = {128, kF32K}, boxb[2] = {64, kF32K};
     ok = encode_f32(&a, l.X, 2, da, sta, boxa) && encode_f32(&b, l.dZ, 2, db, stb, boxb);
+    b16 = b;
   } else {
     const uint64_t da[3] = {ni, nz, E}, sta[2] = {ni * 4, ni * nz * 4};
     const uint32_t across[3] = {128, kF32K, 1}, along[3] = {kF32K, l.gated ? 16u : 128u, 1};
     const uint64_t depth = mode == kGemmForward ? ni : nz;
     const uint64_t db[2] = {depth, R}, stb[1] = {depth * 4};
-    const uint32_t boxb[2] = {kF32K, 64};
+    const uint32_t boxb[2] = {kF32K, 64}, box16[2] = {kF32K, 16};
+    const void* rows = mode == kGemmForward ? l.X : l.dZ;
     ok = encode_f32(&a, l.W, 3, da, sta, mode == kGemmGradX ? across : along) &&
-         encode_f32(&b, mode == kGemmForward ? l.X : l.dZ, 2, db, stb, boxb);
+         encode_f32(&b, rows, 2, db, stb, boxb) && encode_f32(&b16, rows, 2, db, stb, box16);
   }
   if (!ok) return cudaErrorInvalidValue;
   // at most R / 128 + min(E, R) row tiles
@@ -430,11 +446,11 @@ cudaError_t launch_expert_gemm_f32(const ExpertLinearParams& l, ExpertGemmMode m
   if (mode == kGemmForward)
     return with_act(l.act, [&](auto act) {
       constexpr int kAct = decltype(act)::value;
-      return l.gated ? launch<kGemmForward, kAct, true>(p, a, b, tiles, n_sms, s)
-                     : launch<kGemmForward, kAct, false>(p, a, b, tiles, n_sms, s);
+      return l.gated ? launch<kGemmForward, kAct, true>(p, a, b, b16, tiles, n_sms, s)
+                     : launch<kGemmForward, kAct, false>(p, a, b, b16, tiles, n_sms, s);
     });
-  if (mode == kGemmGradX) return launch<kGemmGradX, SMOES_ACT_NONE, false>(p, a, b, tiles, n_sms, s);
-  return launch<kGemmGradW, SMOES_ACT_NONE, false>(p, a, b, static_cast<long long>(l.E) * p.m_tiles * p.n_tiles, n_sms, s);
+  if (mode == kGemmGradX) return launch<kGemmGradX, SMOES_ACT_NONE, false>(p, a, b, b16, tiles, n_sms, s);
+  return launch<kGemmGradW, SMOES_ACT_NONE, false>(p, a, b, b16, static_cast<long long>(l.E) * p.m_tiles * p.n_tiles, n_sms, s);
 }
 
 }  // namespace smoes
