@@ -382,18 +382,28 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
           if (lane == 0) mbar_arrive_peer(peer_smem(&bars.acc_empty[acc], 0));
           if (++acc == 2) { acc = 0; aph ^= 1; }
         }
-        const int i = t.m * 256 + static_cast<int>(rank) * 128 + 32 * q + lane;
-        if (ok && i < l.n_in) {
-          float* w = l.dW + (static_cast<long long>(t.e) * l.n_z + t.col0 + g * 128) * l.n_in + i;
-          const int cols = t.cols - g * 128;
+        // [32 rows of n_z][128 features] a chunk, to the copy engine, which leaves out what lies past n_z and n_in
+        ok = named_bar_all(1 + g, 128, ok);      // one answer for the group: its barriers below count all four warps
+        if (!ok) break;
+        const int i0 = t.m * 256 + static_cast<int>(rank) * 128;
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
+        for (int c = 0; c < 4; ++c) {
+          const int col = g * 128 + c * 32;
+          if (col >= t.cols) break;
+          float* box = reinterpret_cast<float*>(staging + g * kGemmStaging + buf * (kGemmStaging / 2));
 #pragma unroll
-            for (int j = 0; j < 32; ++j) {
-              if (c * 32 + j < cols) *w = l.accumulate ? *w + sum[c][j] : sum[c][j];
-              w += l.n_in;
-            }
+          for (int j = 0; j < 32; ++j) box[j * 128 + 32 * q + lane] = sum[c][j];
+          fence_proxy_async_smem();
+          if (issuer) tma_store_wait_read<0>();  // the chunk before this one: its box is free after the barrier
+          named_bar(1 + g, 128);                 // this one is written
+          if (issuer && i0 < l.n_in) {
+            if (l.accumulate)
+              tma_add_3d(&tmOut, box, i0, t.col0 + col, t.e);
+            else
+              tma_store_3d(&tmOut, box, i0, t.col0 + col, t.e);
+            tma_store_commit();
           }
+          buf ^= 1;
         }
       } else {
         // the CTA's first feature (f0) and its width, the lane's among them (fl), and of z forward (zf)
@@ -512,7 +522,10 @@ cudaError_t launch_expert_gemm(const ExpertLinearParams& l, ExpertGemmMode mode,
     const uint64_t da[2] = {ni, R}, sta[1] = {ni * 2}, db[2] = {nz, R}, stb[1] = {nz * 2};
     const uint32_t box[2] = {64, 64};
     ok = encode_bf16(&a, l.X, 2, da, sta, box) && encode_bf16(&b, l.dZ, 2, db, stb, box);
-    b16 = out = pre = b;
+    const uint64_t dout[3] = {ni, nz, E}, stout[2] = {ni * 4, ni * nz * 4};
+    const uint32_t boxout[3] = {128, 32, 1};
+    ok = ok && encode_f32(&out, l.dW, 3, dout, stout, boxout);
+    b16 = pre = b;
   } else {
     const uint64_t da[3] = {ni, nz, E}, sta[2] = {ni * 2, ni * nz * 2};
     const uint32_t boxa[3] = {64, mode == kGemmGradX ? 64u : l.gated ? 16u : 128u, 1};
