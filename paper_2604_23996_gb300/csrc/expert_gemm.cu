@@ -66,10 +66,11 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 
 // A chunk is 32 columns of D (a feature per lane, an output row per column) by a CTA's 128 features. It leaves
 // through shared memory as boxes of 64 features by 32 rows, 128 bytes a row in the copy engine's swizzle:
-// out's boxes (two, gated one), then at 8 KB those of pre (two; gated one of g and one of u). Lanes exchange
-// values so that each writes two neighbouring features of a row at once, and rows 4 (2, 6) apart at a time, whose
-// swizzled words lie in different banks. Stored from the lanes, 4 bytes each, the 32-byte pieces of pre made
-// dsmoe_vlm's gated layer take 557 us instead of 446 without pre.
+// out's boxes (two, gated one), then at 8 KB those of pre (two; gated one of g and one of u). A lane rounds two columns
+// into one word, exchanges it with its neighbour and picks two neighbouring features of one row out of both; rows 4 (2,
+// 6) apart are written at a time, whose swizzled words lie in different banks. Stored from the lanes, 4 bytes
+// each, the 32-byte pieces of pre made dsmoe_vlm's gated layer take 557 us instead of 446 without pre.
+// Chunks are bound by issue slots: 131072 x 144 x 1024 of 64 experts with silu and pre took 19 instructions a value.
 
 // Shared addresses of a lane's words: its features f & ~1 and the next in box row 4 odd, with the row's swizzle;
 // word i of four rows c + i lies at (at ^ i << 4) + (c + i) * 128 (c a multiple of 8: the swizzle is the row's low
@@ -78,53 +79,63 @@ __device__ __forceinline__ uint32_t pair_address(const uint8_t* boxes, int f) {
   const int odd = f & 1;
   return smem_u32(boxes) + (f >> 6) * 4096 + sw128_offset(4 * odd, (f & 63) - odd);
 }
-__device__ __forceinline__ void put_pair(uint32_t at, int row, uint32_t w) {     // row: without 4 odd
+// One lane's values of rows `row` and row + 4 (x0, x4) to the boxes, with its neighbour's.
+__device__ __forceinline__ void put_pair(uint32_t at, int row, float x0, float x4, uint32_t pick) {
+  const uint32_t own = pack_bf16(x0, x4);
+  const uint32_t w = __byte_perm(own, __shfl_xor_sync(0xffffffffu, own, 1), pick);
   asm volatile("st.shared.u32 [%0], %1;" ::"r"((at ^ ((row & 3) << 4)) + row * 128), "r"(w) : "memory");
 }
+// Even lanes take the low halves (row `row`), odd ones the high halves (row + 4), the lower feature first.
+__device__ __forceinline__ uint32_t pair_pick() { return (threadIdx.x & 1) ? 0x3276u : 0x5410u; }
+
 // One column of D a register; f: the lane's feature among the 128 of the boxes.
 __device__ __forceinline__ void put_chunk(uint8_t* boxes, int f, const float (&v)[32]) {
-  const int odd = f & 1;
-  const uint32_t at = pair_address(boxes, f);
+  const uint32_t at = pair_address(boxes, f), pick = pair_pick();
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const int c = (i >> 2) * 8 + (i & 3);
-    const float got = __shfl_xor_sync(0xffffffffu, odd ? v[c] : v[c + 4], 1);
-    put_pair(at, c, odd ? pack_bf16(got, v[c + 4]) : pack_bf16(v[c], got));
+    put_pair(at, c, v[c], v[c + 4], pick);
   }
 }
 
-// The residual of a chunk, at the places where put_forward adds it. res: that of the chunk's first row at the lane's
-// even feature, read for `rows` rows (none where the feature does not exist).
+// The residual of a chunk in words of two features, rows as put_pair writes them. res: that of the chunk's first row at
+// the lane's even feature, read for `rows` rows (none where the feature does not exist).
 template <bool kGated>
 __device__ __forceinline__ void load_residual(const ExpertLinearParams& l, const __nv_bfloat16* res, int rows,
                                               uint32_t (&rv)[16]) {
   const int odd = threadIdx.x & 1, up = (threadIdx.x >> 4) & 1;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
+  for (int i = 0; i < (kGated ? 8 : 16); ++i) {
     const int c = kGated ? (i >> 1) * 8 + (i & 1) + 2 * up + 4 * odd : (i >> 2) * 8 + (i & 3) + 4 * odd;
     rv[i] = c < rows ? __ldg(reinterpret_cast<const uint32_t*>(res + c * static_cast<long long>(l.n_out))) : 0u;
   }
 }
+// Adds one of its words (and the neighbour's) to the lane's values of the two rows.
+__device__ __forceinline__ void add_residual(float& x0, float& x4, uint32_t w) {
+  const bool odd = threadIdx.x & 1;
+  const uint32_t got = __shfl_xor_sync(0xffffffffu, w, 1);
+  const uint32_t w0 = odd ? got : w, w4 = odd ? w : got;
+  x0 += __uint_as_float(odd ? w0 & 0xffff0000u : w0 << 16);
+  x4 += __uint_as_float(odd ? w4 & 0xffff0000u : w4 << 16);
+}
 
-// z (bias added) of a chunk to out, in shared memory, by whole warps. f: the lane's feature among the CTA's.
+// z (bias added) of a chunk to out, in shared memory, by whole warps. f: the lane's feature among the CTA's; rv: its
+// residual, when there is one.
 template <int kAct, bool kGated>
-__device__ __forceinline__ void put_forward(uint8_t* boxes, int f, float (&v)[32],
+__device__ __forceinline__ void put_forward(uint8_t* boxes, int f, float (&v)[32], bool residual,
                                             const uint32_t (&rv)[16]) {
-  const int odd = threadIdx.x & 1;
+  const uint32_t pick = pair_pick();
+  uint32_t at = pair_address(boxes, f);
   if (!kGated) {
     if (kAct != SMOES_ACT_NONE) {
 #pragma unroll
       for (int c = 0; c < 32; ++c) v[c] = act_value<kAct, true>(v[c]);
     }
-    const uint32_t at = pair_address(boxes, f);
+    if (residual) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int c = (i >> 2) * 8 + (i & 3);
-      const float got = __shfl_xor_sync(0xffffffffu, odd ? v[c] : v[c + 4], 1);
-      const float lo = (odd ? got : v[c]) + __uint_as_float(rv[i] << 16);
-      const float hi = (odd ? v[c + 4] : got) + __uint_as_float(rv[i] & 0xffff0000u);
-      put_pair(at, c, pack_bf16(lo, hi));
+      for (int i = 0; i < 16; ++i) add_residual(v[(i >> 2) * 8 + (i & 3)], v[(i >> 2) * 8 + (i & 3) + 4], rv[i]);
     }
+    put_chunk(boxes, f, v);
     return;
   }
   // gated: lanes 0-15 hold g, 16-31 u; of columns c and c + 2 each half finishes one
@@ -137,16 +148,37 @@ __device__ __forceinline__ void put_forward(uint8_t* boxes, int f, float (&v)[32
     const float g = up ? got : v[c], u = up ? v[c + 2] : got;
     y[i] = act_value<kAct, true>(g) * u;
   }
-  // the half's two rows further down: the swizzle's bit of 2 with it
-  const uint32_t at = (pair_address(boxes, f) ^ (up << 5)) + up * 256;
+  if (residual) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {                  // columns c and c + 4
-    const int a = (i >> 1) * 4 + (i & 1), c = (i >> 1) * 8 + (i & 1);
-    const float got = __shfl_xor_sync(0xffffffffu, odd ? y[a] : y[a + 2], 1);
-    const float lo = (odd ? got : y[a]) + __uint_as_float(rv[i] << 16);
-    const float hi = (odd ? y[a + 2] : got) + __uint_as_float(rv[i] & 0xffff0000u);
-    put_pair(at, c, pack_bf16(lo, hi));
+    for (int i = 0; i < 8; ++i) add_residual(y[(i >> 1) * 4 + (i & 1)], y[(i >> 1) * 4 + (i & 1) + 2], rv[i]);
   }
+  at = (at ^ (up << 5)) + up * 256;              // the half's rows are two further down: the swizzle's bit of 2 with it
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int a = (i >> 1) * 4 + (i & 1);
+    put_pair(at, (i >> 1) * 8 + (i & 1), y[a], y[a + 2], pick);
+  }
+}
+
+// The group's staging between its four warps: they fill a chunk's half and arrive; warp 0 of the group waits for them and
+// hands the half to the copy engine. Before the next chunk but one goes into the same half, warp 0 has seen it read and
+// says so when it begins that chunk itself; so the others run up to a chunk ahead instead of meeting at every chunk.
+constexpr int kBarVote = 1, kBarFull = 3, kBarFree = 5;   // + group
+__device__ __forceinline__ void staging_acquire(int g, bool first_warp, bool issuer) {
+  if (first_warp) {
+    if (issuer) tma_store_wait_read<1>();        // all but the chunk before this one
+    __syncwarp();
+    named_bar_arrive(kBarFree + g, 128);
+  } else {
+    named_bar(kBarFree + g, 128);
+  }
+}
+// all: every warp waits (to copy the chunk itself), not just the first.
+__device__ __forceinline__ void staging_filled(int g, bool first_warp, bool all) {
+  if (first_warp || all)
+    named_bar(kBarFull + g, 128);
+  else
+    named_bar_arrive(kBarFull + g, 128);
 }
 
 // Rows [0, rows) of one box to memory, for a chunk that the copy engine would write past: its expert's rows end
@@ -383,7 +415,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
           if (++acc == 2) { acc = 0; aph ^= 1; }
         }
         // [32 rows of n_z][128 features] a chunk, to the copy engine, which leaves out what lies past n_z and n_in
-        ok = named_bar_all(1 + g, 128, ok);      // one answer for the group: its barriers below count all four warps
+        ok = named_bar_all(kBarVote + g, 128, ok);   // one answer for the group: its barriers below count all four warps
         if (!ok) break;
         const int i0 = t.m * 256 + static_cast<int>(rank) * 128;
 #pragma unroll
@@ -391,18 +423,18 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
           const int col = g * 128 + c * 32;
           if (col >= t.cols) break;
           float* box = reinterpret_cast<float*>(staging + g * kGemmStaging + buf * (kGemmStaging / 2));
+          staging_acquire(g, q == 0, issuer);
 #pragma unroll
           for (int j = 0; j < 32; ++j) box[j * 128 + 32 * q + lane] = sum[c][j];
           fence_proxy_async_smem();
-          if (issuer) tma_store_wait_read<0>();  // the chunk before this one: its box is free after the barrier
-          named_bar(1 + g, 128);                 // this one is written
+          staging_filled(g, q == 0, false);
           if (issuer && i0 < l.n_in) {
             if (l.accumulate)
               tma_add_3d(&tmOut, box, i0, t.col0 + col, t.e);
             else
               tma_store_3d(&tmOut, box, i0, t.col0 + col, t.e);
-            tma_store_commit();
           }
+          if (issuer) tma_store_commit();        // (every chunk is a group, an empty one too: staging_acquire counts them)
           buf ^= 1;
         }
       } else {
@@ -418,11 +450,9 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
         float bias = 0.f;
         const __nv_bfloat16* res = static_cast<const __nv_bfloat16*>(l.residual) + f0 + (fl & ~1);
         uint32_t rv[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) rv[i] = 0u;
         if (kMode == kGemmForward && l.bias && f_in) bias = __ldg(l.bias + static_cast<long long>(t.e) * l.n_z + zf);
         // one answer for the group: its barriers below count all four warps
-        ok = named_bar_all(1 + g, 128, warp_wait(&bars.acc_full[acc], aph, wc));
+        ok = named_bar_all(kBarVote + g, 128, warp_wait(&bars.acc_full[acc], aph, wc));
         if (!ok) break;
         tc_fence_after();
         const int chunks = (t.cols + 31) / 32;
@@ -438,19 +468,20 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
             __syncwarp();
             if (lane == 0) mbar_arrive_peer(peer_smem(&bars.acc_empty[acc], 0));
           }
+          staging_acquire(g, q == 0, issuer);
           if (kMode == kGemmForward) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] += bias;
             if (l.pre) put_chunk(boxes + 8192, gated ? fl + (lane >> 4) * 64 : fl, v);
-            put_forward<kAct, kGated>(boxes, fl, v, rv);
+            put_forward<kAct, kGated>(boxes, fl, v, l.residual != nullptr, rv);
           } else {
             put_chunk(boxes, fl, v);
           }
           fence_proxy_async_smem();
-          if (issuer) tma_store_wait_read<0>();  // the chunk before this one: its boxes are free after the barrier
-          named_bar(1 + g, 128);                 // these are written
           const int n_out_boxes = width / 64;
-          if (rows == 32 && (whole || !gated)) {
+          const bool engine = rows == 32 && (whole || !gated);
+          staging_filled(g, q == 0, !engine);
+          if (engine) {
             if (issuer) {
               for (int i = 0; i < n_out_boxes; ++i)
                 if (f0 + 64 * i < p.n_feat) tma_store_2d(&tmOut, boxes + i * 4096, f0 + 64 * i, static_cast<int>(row));
@@ -459,7 +490,6 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
                   const int x = gated ? f0 + i * l.n_out : f0 + 64 * i;
                   if (x < l.n_z) tma_store_2d(&tmPre, boxes + 8192 + i * 4096, x, static_cast<int>(row));
                 }
-              tma_store_commit();
             }
           } else {
             for (int i = 0; i < n_out_boxes; ++i)
@@ -472,6 +502,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
                          l.n_z, rows, p.n_feat - f);
               }
           }
+          if (issuer) tma_store_commit();        // (every chunk is a group, an empty one too: staging_acquire counts them)
           buf ^= 1;
         }
         if (chunks <= g && lane == 0) mbar_arrive_peer(peer_smem(&bars.acc_empty[acc], 0));

@@ -158,7 +158,12 @@ __device__ __forceinline__ void named_bar(int id, int n) {
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n) : "memory");
 }
 
-// The same, and whether `ok` held in all of its threads.
+// Arrives there without waiting (the others' named_bar or arrivals complete it).
+__device__ __forceinline__ void named_bar_arrive(int id, int n) {
+  asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(n) : "memory");
+}
+
+// named_bar, and whether `ok` held in all of its threads.
 __device__ __forceinline__ bool named_bar_all(int id, int n, bool ok) {
   uint32_t r;
   asm volatile(
