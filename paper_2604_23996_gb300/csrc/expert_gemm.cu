@@ -30,13 +30,15 @@
 namespace smoes {
 namespace {
 
-constexpr int kGemmThreads = 384;
+constexpr int kGemmThreads = 640;
 // dW: the launch's 384 x 168 registers dealt anew, 56 for the first four warps and 224 for the epilogue, whose
 // threads hold 128 sums each (128 x 56 + 256 x 224 = 64512, all of them). setmaxnreg.inc waits without a limit for
 // registers that the launch does not hold, so the launch is refused if the kernel was compiled to fewer.
-constexpr int kGemmFewerRegisters = 56, kGemmMoreRegisters = 224;
+constexpr int kGemmFewerRegisters = 56, kGemmMoreRegisters = 104;
 constexpr int kGemmDealtRegisters = 128 * kGemmFewerRegisters + (kGemmThreads - 128) * kGemmMoreRegisters;
-constexpr int kGemmEpiWarps = 8;
+constexpr int kGemmEpiWarps = 16;
+constexpr int kGemmGroups = 4;                   // of four epilogue warps
+constexpr int kChunkCols = 16;                   // columns of D that a group finishes at a time
 constexpr int kGemmStages = 5;
 constexpr int kGemmK = 64;                       // depth of a block: 128 bytes of bf16
 constexpr uint32_t kGemmHalf = 128 * kGemmK * 2; // one CTA's operand of a block: 16 KB
@@ -44,9 +46,9 @@ constexpr uint32_t kGemmHalf = 128 * kGemmK * 2; // one CTA's operand of a block
 // addition off towards zero: relative error 4.7e-7 after 512 products, 1.5e-6 after 1536, 9e-6 after 8192.
 constexpr int kGemmChunk = 8;                    // blocks of 64 rows
 
-constexpr uint32_t kGemmStaging = 32768;         // one epilogue group's output boxes: two chunks of 16 KB
+constexpr uint32_t kGemmStaging = 16384;         // one epilogue group's output boxes: two chunks of 8 KB
 // alignment, operands, output boxes, barriers, [E + 1] offsets
-constexpr uint32_t kGemmSmem = 1024 + kGemmStages * 2 * kGemmHalf + 2 * kGemmStaging + 256 + 4 * (kExpertsMax + 1);
+constexpr uint32_t kGemmSmem = 1024 + kGemmStages * 2 * kGemmHalf + kGemmGroups * kGemmStaging + 256 + 4 * (kExpertsMax + 1);
 static_assert(kGemmSmem <= 227 * 1024, "shared memory of a CTA");
 
 struct GemmBars {
@@ -77,7 +79,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 // three bits, and those of i and 4 do not meet).
 __device__ __forceinline__ uint32_t pair_address(const uint8_t* boxes, int f) {
   const int odd = f & 1;
-  return smem_u32(boxes) + (f >> 6) * 4096 + sw128_offset(4 * odd, (f & 63) - odd);
+  return smem_u32(boxes) + (f >> 6) * 2048 + sw128_offset(4 * odd, (f & 63) - odd);
 }
 // One lane's values of rows `row` and row + 4 (x0, x4) to the boxes, with its neighbour's.
 __device__ __forceinline__ void put_pair(uint32_t at, int row, float x0, float x4, uint32_t pick) {
@@ -89,10 +91,10 @@ __device__ __forceinline__ void put_pair(uint32_t at, int row, float x0, float x
 __device__ __forceinline__ uint32_t pair_pick() { return (threadIdx.x & 1) ? 0x3276u : 0x5410u; }
 
 // One column of D a register; f: the lane's feature among the 128 of the boxes.
-__device__ __forceinline__ void put_chunk(uint8_t* boxes, int f, const float (&v)[32]) {
+__device__ __forceinline__ void put_chunk(uint8_t* boxes, int f, const float (&v)[kChunkCols]) {
   const uint32_t at = pair_address(boxes, f), pick = pair_pick();
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
+  for (int i = 0; i < kChunkCols / 2; ++i) {
     const int c = (i >> 2) * 8 + (i & 3);
     put_pair(at, c, v[c], v[c + 4], pick);
   }
@@ -102,10 +104,10 @@ __device__ __forceinline__ void put_chunk(uint8_t* boxes, int f, const float (&v
 // the lane's even feature, read for `rows` rows (none where the feature does not exist).
 template <bool kGated>
 __device__ __forceinline__ void load_residual(const ExpertLinearParams& l, const __nv_bfloat16* res, int rows,
-                                              uint32_t (&rv)[16]) {
+                                              uint32_t (&rv)[kChunkCols / 2]) {
   const int odd = threadIdx.x & 1, up = (threadIdx.x >> 4) & 1;
 #pragma unroll
-  for (int i = 0; i < (kGated ? 8 : 16); ++i) {
+  for (int i = 0; i < kChunkCols / (kGated ? 4 : 2); ++i) {
     const int c = kGated ? (i >> 1) * 8 + (i & 1) + 2 * up + 4 * odd : (i >> 2) * 8 + (i & 3) + 4 * odd;
     rv[i] = c < rows ? __ldg(reinterpret_cast<const uint32_t*>(res + c * static_cast<long long>(l.n_out))) : 0u;
   }
@@ -122,27 +124,27 @@ __device__ __forceinline__ void add_residual(float& x0, float& x4, uint32_t w) {
 // z (bias added) of a chunk to out, in shared memory, by whole warps. f: the lane's feature among the CTA's; rv: its
 // residual, when there is one.
 template <int kAct, bool kGated>
-__device__ __forceinline__ void put_forward(uint8_t* boxes, int f, float (&v)[32], bool residual,
-                                            const uint32_t (&rv)[16]) {
+__device__ __forceinline__ void put_forward(uint8_t* boxes, int f, float (&v)[kChunkCols], bool residual,
+                                            const uint32_t (&rv)[kChunkCols / 2]) {
   const uint32_t pick = pair_pick();
   uint32_t at = pair_address(boxes, f);
   if (!kGated) {
     if (kAct != SMOES_ACT_NONE) {
 #pragma unroll
-      for (int c = 0; c < 32; ++c) v[c] = act_value<kAct, true>(v[c]);
+      for (int c = 0; c < kChunkCols; ++c) v[c] = act_value<kAct, true>(v[c]);
     }
     if (residual) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) add_residual(v[(i >> 2) * 8 + (i & 3)], v[(i >> 2) * 8 + (i & 3) + 4], rv[i]);
+      for (int i = 0; i < kChunkCols / 2; ++i) add_residual(v[(i >> 2) * 8 + (i & 3)], v[(i >> 2) * 8 + (i & 3) + 4], rv[i]);
     }
     put_chunk(boxes, f, v);
     return;
   }
   // gated: lanes 0-15 hold g, 16-31 u; of columns c and c + 2 each half finishes one
   const int up = (threadIdx.x >> 4) & 1;
-  float y[16];                                   // columns 4 (i / 2) + i % 2 + 2 up
+  float y[kChunkCols / 2];                       // columns 4 (i / 2) + i % 2 + 2 up
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
+  for (int i = 0; i < kChunkCols / 2; ++i) {
     const int c = (i >> 1) * 4 + (i & 1);
     const float got = __shfl_xor_sync(0xffffffffu, up ? v[c] : v[c + 2], 16);
     const float g = up ? got : v[c], u = up ? v[c + 2] : got;
@@ -150,11 +152,11 @@ __device__ __forceinline__ void put_forward(uint8_t* boxes, int f, float (&v)[32
   }
   if (residual) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) add_residual(y[(i >> 1) * 4 + (i & 1)], y[(i >> 1) * 4 + (i & 1) + 2], rv[i]);
+    for (int i = 0; i < kChunkCols / 4; ++i) add_residual(y[(i >> 1) * 4 + (i & 1)], y[(i >> 1) * 4 + (i & 1) + 2], rv[i]);
   }
   at = (at ^ (up << 5)) + up * 256;              // the half's rows are two further down: the swizzle's bit of 2 with it
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < kChunkCols / 4; ++i) {
     const int a = (i >> 1) * 4 + (i & 1);
     put_pair(at, (i >> 1) * 8 + (i & 1), y[a], y[a + 2], pick);
   }
@@ -163,7 +165,7 @@ __device__ __forceinline__ void put_forward(uint8_t* boxes, int f, float (&v)[32
 // The group's staging between its four warps: they fill a chunk's half and arrive; warp 0 of the group waits for them and
 // hands the half to the copy engine. Before the next chunk but one goes into the same half, warp 0 has seen it read and
 // says so when it begins that chunk itself; so the others run up to a chunk ahead instead of meeting at every chunk.
-constexpr int kBarVote = 1, kBarFull = 3, kBarFree = 5;   // + group
+constexpr int kBarVote = 1, kBarFull = 1 + kGemmGroups, kBarFree = 1 + 2 * kGemmGroups;   // + group
 __device__ __forceinline__ void staging_acquire(int g, bool first_warp, bool issuer) {
   if (first_warp) {
     if (issuer) tma_store_wait_read<1>();        // all but the chunk before this one
@@ -201,8 +203,8 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
   uint8_t* sa = smem;
   uint8_t* sb = smem + kGemmStages * kGemmHalf;
   uint8_t* staging = smem + 2 * kGemmStages * kGemmHalf;
-  GemmBars& bars = *reinterpret_cast<GemmBars*>(staging + 2 * kGemmStaging);
-  int32_t* off = reinterpret_cast<int32_t*>(staging + 2 * kGemmStaging + 256);   // [E + 1] offsets
+  GemmBars& bars = *reinterpret_cast<GemmBars*>(staging + kGemmGroups * kGemmStaging);
+  int32_t* off = reinterpret_cast<int32_t*>(staging + kGemmGroups * kGemmStaging + 256);   // [E + 1] offsets
   const ExpertLinearParams& l = p.l;
   const int warp = warp_index(), lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
@@ -391,22 +393,22 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
           if (!l.accumulate) zero_weight_tile(l, t, 256, static_cast<int>(rank), warp - 4, kGemmEpiWarps);
           continue;
         }
-        float sum[4][32];
+        float sum[4][16];                        // columns 64 g + 16 c + i
 #pragma unroll
         for (int c = 0; c < 4; ++c)
 #pragma unroll
-          for (int i = 0; i < 32; ++i) sum[c][i] = 0.f;
+          for (int i = 0; i < 16; ++i) sum[c][i] = 0.f;
         for (int k0 = 0; k0 < t.blocks; k0 += kGemmChunk) {
           if (!warp_wait(&bars.acc_full[acc], aph, wc)) { ok = false; break; }
           tc_fence_after();
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
-            const int col = g * 128 + c * 32;
+            const int col = g * 64 + c * 16;
             if (col < t.cols) {
-              float v[32];
-              tmem_ld32(tmem + acc * 256 + col + lanes, v);
+              float v[16];
+              tmem_ld16(tmem + acc * 256 + col + lanes, v);
 #pragma unroll
-              for (int i = 0; i < 32; ++i) sum[c][i] += v[i];
+              for (int i = 0; i < 16; ++i) sum[c][i] += v[i];
             }
           }
           tc_fence_before();
@@ -414,18 +416,18 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
           if (lane == 0) mbar_arrive_peer(peer_smem(&bars.acc_empty[acc], 0));
           if (++acc == 2) { acc = 0; aph ^= 1; }
         }
-        // [32 rows of n_z][128 features] a chunk, to the copy engine, which leaves out what lies past n_z and n_in
+        // [16 rows of n_z][128 features] a chunk, to the copy engine, which leaves out what lies past n_z and n_in
         ok = named_bar_all(kBarVote + g, 128, ok);   // one answer for the group: its barriers below count all four warps
         if (!ok) break;
         const int i0 = t.m * 256 + static_cast<int>(rank) * 128;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          const int col = g * 128 + c * 32;
+          const int col = g * 64 + c * 16;
           if (col >= t.cols) break;
           float* box = reinterpret_cast<float*>(staging + g * kGemmStaging + buf * (kGemmStaging / 2));
           staging_acquire(g, q == 0, issuer);
 #pragma unroll
-          for (int j = 0; j < 32; ++j) box[j * 128 + 32 * q + lane] = sum[c][j];
+          for (int j = 0; j < 16; ++j) box[j * 128 + 32 * q + lane] = sum[c][j];
           fence_proxy_async_smem();
           staging_filled(g, q == 0, false);
           if (issuer && i0 < l.n_in) {
@@ -449,21 +451,21 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
         const long long ld = p.n_feat;
         float bias = 0.f;
         const __nv_bfloat16* res = static_cast<const __nv_bfloat16*>(l.residual) + f0 + (fl & ~1);
-        uint32_t rv[16];
+        uint32_t rv[kChunkCols / 2];
         if (kMode == kGemmForward && l.bias && f_in) bias = __ldg(l.bias + static_cast<long long>(t.e) * l.n_z + zf);
         // one answer for the group: its barriers below count all four warps
         ok = named_bar_all(kBarVote + g, 128, warp_wait(&bars.acc_full[acc], aph, wc));
         if (!ok) break;
         tc_fence_after();
-        const int chunks = (t.cols + 31) / 32;
-        for (int c = g; c < chunks; c += 2) {
-          const long long row = t.row0 + c * 32;
-          const int rows = min(32, t.cols - c * 32);
+        const int chunks = (t.cols + kChunkCols - 1) / kChunkCols;
+        for (int c = g; c < chunks; c += kGemmGroups) {
+          const long long row = t.row0 + c * kChunkCols;
+          const int rows = min(kChunkCols, t.cols - c * kChunkCols);
           if (kMode == kGemmForward && l.residual) load_residual<kGated>(l, res + row * ld, f_in ? rows : 0, rv);
           uint8_t* boxes = staging + g * kGemmStaging + buf * (kGemmStaging / 2);
-          float v[32];
-          tmem_ld32(tmem + acc * 256 + c * 32 + lanes, v);
-          if (c + 2 >= chunks) {                 // the accumulator's last use
+          float v[kChunkCols];
+          tmem_ld16(tmem + acc * 256 + c * kChunkCols + lanes, v);
+          if (c + kGemmGroups >= chunks) {                 // the accumulator's last use
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_peer(peer_smem(&bars.acc_empty[acc], 0));
@@ -471,34 +473,34 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
           staging_acquire(g, q == 0, issuer);
           if (kMode == kGemmForward) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] += bias;
-            if (l.pre) put_chunk(boxes + 8192, gated ? fl + (lane >> 4) * 64 : fl, v);
+            for (int j = 0; j < kChunkCols; ++j) v[j] += bias;
+            if (l.pre) put_chunk(boxes + 4096, gated ? fl + (lane >> 4) * 64 : fl, v);
             put_forward<kAct, kGated>(boxes, fl, v, l.residual != nullptr, rv);
           } else {
             put_chunk(boxes, fl, v);
           }
           fence_proxy_async_smem();
           const int n_out_boxes = width / 64;
-          const bool engine = rows == 32 && (whole || !gated);
+          const bool engine = rows == kChunkCols && (whole || !gated);
           staging_filled(g, q == 0, !engine);
           if (engine) {
             if (issuer) {
               for (int i = 0; i < n_out_boxes; ++i)
-                if (f0 + 64 * i < p.n_feat) tma_store_2d(&tmOut, boxes + i * 4096, f0 + 64 * i, static_cast<int>(row));
+                if (f0 + 64 * i < p.n_feat) tma_store_2d(&tmOut, boxes + i * 2048, f0 + 64 * i, static_cast<int>(row));
               if (kMode == kGemmForward && l.pre)
                 for (int i = 0; i < 2; ++i) {
                   const int x = gated ? f0 + i * l.n_out : f0 + 64 * i;
-                  if (x < l.n_z) tma_store_2d(&tmPre, boxes + 8192 + i * 4096, x, static_cast<int>(row));
+                  if (x < l.n_z) tma_store_2d(&tmPre, boxes + 4096 + i * 2048, x, static_cast<int>(row));
                 }
             }
           } else {
             for (int i = 0; i < n_out_boxes; ++i)
-              copy_box(boxes + i * 4096, static_cast<__nv_bfloat16*>(l.out) + row * ld + f0 + 64 * i, ld, rows,
+              copy_box(boxes + i * 2048, static_cast<__nv_bfloat16*>(l.out) + row * ld + f0 + 64 * i, ld, rows,
                        p.n_feat - f0 - 64 * i);
             if (kMode == kGemmForward && l.pre)
               for (int i = 0; i < 2; ++i) {
                 const int f = gated ? f0 : f0 + 64 * i;
-                copy_box(boxes + 8192 + i * 4096, static_cast<__nv_bfloat16*>(l.pre) + row * l.n_z + f + (gated ? i * l.n_out : 0),
+                copy_box(boxes + 4096 + i * 2048, static_cast<__nv_bfloat16*>(l.pre) + row * l.n_z + f + (gated ? i * l.n_out : 0),
                          l.n_z, rows, p.n_feat - f);
               }
           }
@@ -554,7 +556,7 @@ cudaError_t launch_expert_gemm(const ExpertLinearParams& l, ExpertGemmMode mode,
     const uint32_t box[2] = {64, 64};
     ok = encode_bf16(&a, l.X, 2, da, sta, box) && encode_bf16(&b, l.dZ, 2, db, stb, box);
     const uint64_t dout[3] = {ni, nz, E}, stout[2] = {ni * 4, ni * nz * 4};
-    const uint32_t boxout[3] = {128, 32, 1};
+    const uint32_t boxout[3] = {128, 16, 1};
     ok = ok && encode_f32(&out, l.dW, 3, dout, stout, boxout);
     b16 = pre = b;
   } else {
@@ -567,10 +569,10 @@ cudaError_t launch_expert_gemm(const ExpertLinearParams& l, ExpertGemmMode mode,
     ok = encode_bf16(&a, l.W, 3, da, sta, boxa) && encode_bf16(&b, rows, 2, db, stb, box) &&
          encode_bf16(&b16, rows, 2, db, stb, box16);
     const uint64_t nf = p.n_feat, dout[2] = {nf, R}, stout[1] = {nf * 2}, dpre[2] = {nz, R}, stpre[1] = {nz * 2};
-    const uint32_t box32[2] = {64, 32};
-    ok = ok && encode_bf16(&out, l.out, 2, dout, stout, box32);
+    const uint32_t box_out[2] = {64, kChunkCols};
+    ok = ok && encode_bf16(&out, l.out, 2, dout, stout, box_out);
     pre = out;
-    if (l.pre) ok = ok && encode_bf16(&pre, l.pre, 2, dpre, stpre, box32);
+    if (l.pre) ok = ok && encode_bf16(&pre, l.pre, 2, dpre, stpre, box_out);
   }
   if (!ok) return cudaErrorInvalidValue;
   // at most R / 256 + min(E, R) row tiles
