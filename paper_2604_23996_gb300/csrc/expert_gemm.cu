@@ -21,8 +21,6 @@
 // Roles of a CTA's warps: 0 producer, 1 MMA issuer (first CTA), 2 tensor memory and the clearing, 4-11
 // epilogue, in two groups that take alternate 32-column chunks. Two accumulators of 256 columns: the epilogue of a
 // tile runs under the next tile's products.
-#include <algorithm>
-
 #include "expert_gemm.cuh"
 #include "experts.cuh"
 #include "ptx.cuh"
@@ -234,7 +232,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
   cluster_sync();                                // both CTAs' barriers are ready before anything arrives on them
   tc_fence_after();
   RowTiles rt{};
-  if (kMode != kGemmGradW) rt = count_row_tiles(off, l.E, l.R, 256);
+  if (kMode != kGemmGradW) rt = count_row_tiles(off, l.E, l.R, p.tile_cols);
   const int n_total = kMode == kGemmGradW ? l.E * p.m_tiles * p.n_tiles : rt.total * p.m_tiles;   // tiles
   const uint32_t tmem = bars.tmem;
   const WaitCtx wc{&bars.abort, p.status, p.limit_ns};
@@ -246,7 +244,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     uint32_t ph = 0;
     bool ok = true;
     for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
-      const GemmTile t = gemm_tile<kMode, 256, kGemmK>(p, rt, off, tile);
+      const GemmTile t = gemm_tile<kMode, kGemmK>(p, rt, off, tile);
       const int half_n = gemm_n<kMode>(t.cols) / 2;
       for (int kb = 0; kb < t.blocks; ++kb) {
         if (!warp_wait(&bars.empty[st], ph ^ 1, wc)) { ok = false; break; }
@@ -312,7 +310,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     bool ok = true;
     constexpr bool kMajorA = kMode != kGemmForward, kMajorB = kMode == kGemmGradW;   // along M / N in memory
     for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
-      const GemmTile t = gemm_tile<kMode, 256, kGemmK>(p, rt, off, tile);
+      const GemmTile t = gemm_tile<kMode, kGemmK>(p, rt, off, tile);
       const uint32_t idesc = idesc_bf16(256, gemm_n<kMode>(t.cols), kMajorA, kMajorB);
       const int chunk = kMode == kGemmGradW ? kGemmChunk : t.blocks;
       for (int k0 = 0; ok && k0 < t.blocks; k0 += chunk) {
@@ -345,7 +343,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     int st = 0;
     uint32_t phases = 0;                         // bit s: parity of tail[s]
     for (int tile = pair; tile < n_total; tile += n_pairs) {
-      const GemmTile t = gemm_tile<kMode, 256, kGemmK>(p, rt, off, tile);
+      const GemmTile t = gemm_tile<kMode, kGemmK>(p, rt, off, tile);
       if (t.blocks == 0) continue;
       const int s = (st + t.blocks - 1) % kGemmStages;
       st = (st + t.blocks) % kGemmStages;
@@ -387,10 +385,10 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     uint32_t aph = 0;
     bool ok = true;
     for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
-      const GemmTile t = gemm_tile<kMode, 256, kGemmK>(p, rt, off, tile);
+      const GemmTile t = gemm_tile<kMode, kGemmK>(p, rt, off, tile);
       if constexpr (kMode == kGemmGradW) {
         if (t.blocks == 0) {                     // an expert without rows
-          if (!l.accumulate) zero_weight_tile(l, t, 256, static_cast<int>(rank), warp - 4, kGemmEpiWarps);
+          if (!l.accumulate) zero_weight_tile(l, t, static_cast<int>(rank), warp - 4, kGemmEpiWarps);
           continue;
         }
         float sum[4][16];                        // columns 64 g + 16 c + i
@@ -525,14 +523,14 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
 }
 
 template <int kMode, int kAct, bool kGated>
-cudaError_t launch(const ExpertGemmParams& p, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& b16,
-                   const CUtensorMap& out, const CUtensorMap& pre, long long tiles, int n_sms, cudaStream_t s) {
+cudaError_t launch(ExpertGemmParams& p, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& b16,
+                   const CUtensorMap& out, const CUtensorMap& pre, int n_sms, cudaStream_t s) {
   static GemmResidency held;
   int pairs = 0;
   const cudaError_t e = gemm_pairs(held, k_expert_gemm<kMode, kAct, kGated>, kGemmThreads, kGemmSmem,
                                    kMode == kGemmGradW ? kGemmDealtRegisters : 0, n_sms, &pairs);
   if (e != cudaSuccess) return e;
-  pairs = static_cast<int>(std::min<long long>(pairs, std::max(1ll, tiles)));
+  pairs = gemm_split(p, static_cast<ExpertGemmMode>(kMode), 256, kMode == kGemmGradW ? 128 : 64, pairs);
   return launch_pdl(k_expert_gemm<kMode, kAct, kGated>, dim3(2 * pairs), dim3(kGemmThreads), kGemmSmem, s, a, b, b16, out, pre, p);
 }
 
@@ -547,7 +545,6 @@ cudaError_t launch_expert_gemm(const ExpertLinearParams& l, ExpertGemmMode mode,
   p.n_feat = mode == kGemmForward ? l.n_out : l.n_in;
   const int per = mode == kGemmForward && l.gated ? 128 : 256;
   p.m_tiles = (p.n_feat + per - 1) / per;
-  p.n_tiles = (l.n_z + 255) / 256;
   const uint64_t R = static_cast<uint64_t>(l.R), ni = l.n_in, nz = l.n_z, E = l.E;
   CUtensorMap a, b, b16, out, pre;
   bool ok;
@@ -575,16 +572,14 @@ cudaError_t launch_expert_gemm(const ExpertLinearParams& l, ExpertGemmMode mode,
     if (l.pre) ok = ok && encode_bf16(&pre, l.pre, 2, dpre, stpre, box_out);
   }
   if (!ok) return cudaErrorInvalidValue;
-  // at most R / 256 + min(E, R) row tiles
-  const long long row_tiles = l.R / 256 + std::min<long long>(l.E, l.R);
   if (mode == kGemmForward)
     return with_act(l.act, [&](auto act) {
       constexpr int kAct = decltype(act)::value;
-      return l.gated ? launch<kGemmForward, kAct, true>(p, a, b, b16, out, pre, row_tiles * p.m_tiles, n_sms, s)
-                     : launch<kGemmForward, kAct, false>(p, a, b, b16, out, pre, row_tiles * p.m_tiles, n_sms, s);
+      return l.gated ? launch<kGemmForward, kAct, true>(p, a, b, b16, out, pre, n_sms, s)
+                     : launch<kGemmForward, kAct, false>(p, a, b, b16, out, pre, n_sms, s);
     });
-  if (mode == kGemmGradX) return launch<kGemmGradX, SMOES_ACT_NONE, false>(p, a, b, b16, out, pre, row_tiles * p.m_tiles, n_sms, s);
-  return launch<kGemmGradW, SMOES_ACT_NONE, false>(p, a, b, b16, out, pre, static_cast<long long>(l.E) * p.m_tiles * p.n_tiles, n_sms, s);
+  if (mode == kGemmGradX) return launch<kGemmGradX, SMOES_ACT_NONE, false>(p, a, b, b16, out, pre, n_sms, s);
+  return launch<kGemmGradW, SMOES_ACT_NONE, false>(p, a, b, b16, out, pre, n_sms, s);
 }
 
 }  // namespace smoes

@@ -18,8 +18,6 @@
 // Bound by shared memory: a block's 24 KB arrive, are read and written as 36 KB, and the products read 72 KB, 1220
 // clocks at 128 bytes each against 770 of the products. On the FMA units (128 x 128 a block of threads) 8192 x 512 x
 // 256 of 16 experts took 187 us for both gradients.
-#include <algorithm>
-
 #include "expert_gemm.cuh"
 #include "experts.cuh"
 #include "ptx.cuh"
@@ -134,7 +132,7 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
   cluster_sync();                                // both CTAs' barriers are ready before anything arrives on them
   tc_fence_after();
   RowTiles rt{};
-  if (kMode != kGemmGradW) rt = count_row_tiles(off, l.E, l.R, kF32Cols);
+  if (kMode != kGemmGradW) rt = count_row_tiles(off, l.E, l.R, p.tile_cols);
   const int n_total = kMode == kGemmGradW ? l.E * p.m_tiles * p.n_tiles : rt.total * p.m_tiles;   // tiles
   const uint32_t tmem = bars.tmem;               // accumulator b: h h at columns 256 b, the small products at 256 b + 128
   const WaitCtx wc{&bars.abort, p.status, p.limit_ns};
@@ -145,7 +143,7 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     uint32_t ph = 0;
     bool ok = true;
     for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
-      const GemmTile t = gemm_tile<kMode, kF32Cols, kF32K>(p, rt, off, tile);
+      const GemmTile t = gemm_tile<kMode, kF32K>(p, rt, off, tile);
       const int half_n = gemm_n<kMode>(t.cols) / 2;
       for (int kb = 0; kb < t.blocks; ++kb) {
         if (!warp_wait(&bars.raw_empty[st], ph ^ 1, wc)) { ok = false; break; }
@@ -190,7 +188,7 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     uint32_t ph = 0, aph = 0;
     bool ok = true;
     for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
-      const GemmTile t = gemm_tile<kMode, kF32Cols, kF32K>(p, rt, off, tile);
+      const GemmTile t = gemm_tile<kMode, kF32K>(p, rt, off, tile);
       const uint32_t idesc = idesc_bf16(256, gemm_n<kMode>(t.cols), kAcrossA, kAcrossB);
       for (int k0 = 0; ok && k0 < t.blocks; k0 += kF32Chunk) {
         if (!warp_wait(&bars.acc_empty[acc], aph ^ 1, wc)) { ok = false; break; }
@@ -322,7 +320,7 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     int tile = pair, k0 = 0;
     bool more = tile < n_total;
     GemmTile t{}, done{};                        // the chunk's tile; that of the chunk before
-    if (more) t = gemm_tile<kMode, kF32Cols, kF32K>(p, rt, off, tile);
+    if (more) t = gemm_tile<kMode, kF32K>(p, rt, off, tile);
     bool pending = false, pending_last = false;
     while (more || pending) {
       const int k1 = more ? min(k0 + kF32Chunk, t.blocks) : k0;
@@ -371,7 +369,7 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
       }
       if (pending && pending_last && done.blocks > 0) store(done);
       if (kMode == kGemmGradW && pending && done.blocks == 0 && !l.accumulate)   // an expert without rows
-        zero_weight_tile(l, done, kF32Cols, static_cast<int>(rank), warp - 4, kF32Warps);
+        zero_weight_tile(l, done, static_cast<int>(rank), warp - 4, kF32Warps);
       pending = more;
       pending_last = k1 == t.blocks;
       done = t;
@@ -380,7 +378,7 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         tile += n_pairs;
         k0 = 0;
         more = tile < n_total;
-        if (more) t = gemm_tile<kMode, kF32Cols, kF32K>(p, rt, off, tile);
+        if (more) t = gemm_tile<kMode, kF32K>(p, rt, off, tile);
       }
     }
     // every plane given back: no commit of the first CTA is still on its way to this one when it ends
@@ -401,13 +399,13 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
 }
 
 template <int kMode, int kAct, bool kGated>
-cudaError_t launch(const ExpertGemmParams& p, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& b16,
-                   long long tiles, int n_sms, cudaStream_t s) {
+cudaError_t launch(ExpertGemmParams& p, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& b16, int n_sms,
+                   cudaStream_t s) {
   static GemmResidency held;
   int pairs = 0;
   const cudaError_t e = gemm_pairs(held, k_expert_gemm_f32<kMode, kAct, kGated>, kF32Threads, kF32Smem, 0, n_sms, &pairs);
   if (e != cudaSuccess) return e;
-  pairs = static_cast<int>(std::min<long long>(pairs, std::max(1ll, tiles)));
+  pairs = gemm_split(p, static_cast<ExpertGemmMode>(kMode), kF32Cols, kMode == kGemmGradW ? kF32Cols : 32, pairs);
   return launch_pdl(k_expert_gemm_f32<kMode, kAct, kGated>, dim3(2 * pairs), dim3(kF32Threads), kF32Smem, s, a, b, b16, p);
 }
 
@@ -422,7 +420,6 @@ cudaError_t launch_expert_gemm_f32(const ExpertLinearParams& l, ExpertGemmMode m
   p.n_feat = mode == kGemmForward ? l.n_out : l.n_in;
   const int per = mode == kGemmForward && l.gated ? 128 : 256;
   p.m_tiles = (p.n_feat + per - 1) / per;
-  p.n_tiles = (l.n_z + kF32Cols - 1) / kF32Cols;
   const uint64_t R = static_cast<uint64_t>(l.R), ni = l.n_in, nz = l.n_z, E = l.E;
   CUtensorMap a, b, b16;
   bool ok;
@@ -442,16 +439,14 @@ cudaError_t launch_expert_gemm_f32(const ExpertLinearParams& l, ExpertGemmMode m
          encode_f32(&b, rows, 2, db, stb, boxb) && encode_f32(&b16, rows, 2, db, stb, box16);
   }
   if (!ok) return cudaErrorInvalidValue;
-  // at most R / 128 + min(E, R) row tiles
-  const long long tiles = (l.R / kF32Cols + std::min<long long>(l.E, l.R)) * p.m_tiles;
   if (mode == kGemmForward)
     return with_act(l.act, [&](auto act) {
       constexpr int kAct = decltype(act)::value;
-      return l.gated ? launch<kGemmForward, kAct, true>(p, a, b, b16, tiles, n_sms, s)
-                     : launch<kGemmForward, kAct, false>(p, a, b, b16, tiles, n_sms, s);
+      return l.gated ? launch<kGemmForward, kAct, true>(p, a, b, b16, n_sms, s)
+                     : launch<kGemmForward, kAct, false>(p, a, b, b16, n_sms, s);
     });
-  if (mode == kGemmGradX) return launch<kGemmGradX, SMOES_ACT_NONE, false>(p, a, b, b16, tiles, n_sms, s);
-  return launch<kGemmGradW, SMOES_ACT_NONE, false>(p, a, b, b16, static_cast<long long>(l.E) * p.m_tiles * p.n_tiles, n_sms, s);
+  if (mode == kGemmGradX) return launch<kGemmGradX, SMOES_ACT_NONE, false>(p, a, b, b16, n_sms, s);
+  return launch<kGemmGradW, SMOES_ACT_NONE, false>(p, a, b, b16, n_sms, s);
 }
 
 }  // namespace smoes

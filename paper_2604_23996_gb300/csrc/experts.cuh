@@ -76,6 +76,7 @@ struct ExpertGemmParams {
   ExpertLinearParams l;
   int n_feat;                // features along m: n_out, or n_in
   int m_tiles;
+  int tile_cols;             // rows of a tile (weights' gradient: columns of n_z)
   int n_tiles;               // tiles along n_z (weights' gradient)
   uint32_t* status;
   uint64_t limit_ns;
