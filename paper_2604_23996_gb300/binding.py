@@ -457,7 +457,8 @@ class Experts:
     expert and one selection (``E = k = 1``) is a dense layer and needs no sort. Tensors are contiguous, of the
     plan's type (weights of the top-k, biases and their gradients float32) and on the plan's device; a tensor
     that is not raises a ValueError before anything is launched. Results are new tensors unless an output is given.
-    Calls run on the stream given, or the current one of the plan's device. The methods call the library themselves:
+    Calls run on the stream given, or the current one of the plan's device; calls of one layer share its workspace, so
+    those on different streams are the caller's to order. The methods call the library themselves:
     a decoding step's calls are bound by their time on the host.
     """
 
@@ -496,10 +497,14 @@ class Experts:
                              f"wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
         return t.data_ptr()
 
-    def _new(self, t, shape, dtype):
-        """The output given, checked, or a new one."""
+    def _new(self, t, shape, dtype, stream):
+        """The output given, checked, or a new one; one made for another stream than the current one is kept by the
+        allocator until that stream is done with it."""
         if t is None:
-            return torch.empty(shape, dtype=dtype, device=self.device)
+            t = torch.empty(shape, dtype=dtype, device=self.device)
+            if stream is not None:
+                t.record_stream(stream)
+            return t
         self._in("output", t, shape, dtype)
         return t
 
@@ -517,7 +522,7 @@ class Experts:
         """Tokens [T, d] into expert order: [R, d]."""
         d = X.shape[-1]
         x = self._in("X", X, (self.T, d), self.dtype)
-        out = self._new(out, (self.R, d), self.dtype)
+        out = self._new(out, (self.R, d), self.dtype, stream)
         _check(_lib.smoes_expert_dispatch(self.plan, x, d, self.expert_offsets.data_ptr(), self.slot_row.data_ptr(),
                                           out.data_ptr(), self._stream(stream)), "smoes_expert_dispatch")
         return out
@@ -527,7 +532,7 @@ class Experts:
         d = dXs.shape[-1]
         dx = self._in("dXs", dXs, (self.R, d), self.dtype)
         res = self._in("residual", residual, (self.T, d), self.dtype)
-        out = self._new(out, (self.T, d), self.dtype)
+        out = self._new(out, (self.T, d), self.dtype, stream)
         _check(_lib.smoes_expert_dispatch_bwd(self.plan, dx, d, self.slot_row.data_ptr(), res, out.data_ptr(),
                                               self._stream(stream)), "smoes_expert_dispatch_bwd")
         return out
@@ -538,7 +543,7 @@ class Experts:
         ys = self._in("Ys", Ys, (self.R, d), self.dtype)
         w = self._in("topk_w", topk_w, (self.T, self.k), torch.float32)
         res = self._in("residual", residual, (self.T, d), self.dtype)
-        out = self._new(out, (self.T, d), self.dtype)
+        out = self._new(out, (self.T, d), self.dtype, stream)
         _check(_lib.smoes_expert_combine(self.plan, ys, d, w, self.slot_row.data_ptr(), res, out.data_ptr(),
                                          self._stream(stream)), "smoes_expert_combine")
         return out
@@ -549,8 +554,8 @@ class Experts:
         dy = self._in("dY", dY, (self.T, d), self.dtype)
         ys = self._in("Ys", Ys, (self.R, d), self.dtype)
         w = self._in("topk_w", topk_w, (self.T, self.k), torch.float32)
-        dYs = self._new(dYs, (self.R, d), self.dtype)
-        d_topk_w = self._new(d_topk_w, (self.T, self.k), torch.float32)
+        dYs = self._new(dYs, (self.R, d), self.dtype, stream)
+        d_topk_w = self._new(d_topk_w, (self.T, self.k), torch.float32, stream)
         _check(_lib.smoes_expert_combine_bwd(self.plan, dy, ys, d, w, self.expert_offsets.data_ptr(),
                                              self.slot_row.data_ptr(), dYs.data_ptr(), d_topk_w.data_ptr(),
                                              self._stream(stream)), "smoes_expert_combine_bwd")
@@ -568,9 +573,9 @@ class Experts:
         args = LinearArgs(self._in("X", X, (self.R, n_in), dt), self._in("W", W, (self.E, n_z, n_in), dt),
                           self._in("bias", bias, (self.E, n_z), torch.float32),
                           self._in("residual", residual, (self.R, n_out), dt), n_in, n_out, act, gated)
-        out = self._new(out, (self.R, n_out), dt)
+        out = self._new(out, (self.R, n_out), dt, stream)
         if save_pre or pre is not None:
-            pre = self._new(pre, (self.R, n_z), dt)
+            pre = self._new(pre, (self.R, n_z), dt, stream)
         _check(_lib.smoes_expert_linear(self.plan, args, self.expert_offsets.data_ptr(), out.data_ptr(), _ptr(pre),
                                         ws.data_ptr(), ws.numel(), self._stream(stream)), "smoes_expert_linear")
         return out, pre
@@ -583,7 +588,7 @@ class Experts:
         n_z = 2 * n_out if gated else n_out
         dout = self._in("dOut", dOut, (self.R, n_out), self.dtype)
         if bias_grad or db is not None:
-            db = self._new(db, (self.E, n_z), torch.float32)
+            db = self._new(db, (self.E, n_z), torch.float32, stream)
         if act == SMOES_ACT_NONE and not gated:
             z, dz, dZ = None, None, dOut
             if db is None:
@@ -592,7 +597,7 @@ class Experts:
             raise ValueError("pre: the pre-activations that linear saved are wanted")
         else:
             z = self._in("pre", pre, (self.R, n_z), self.dtype)
-            dZ = self._new(dZ, (self.R, n_z), self.dtype)
+            dZ = self._new(dZ, (self.R, n_z), self.dtype, stream)
             dz = dZ.data_ptr()
         ws = self.ws
         _check(_lib.smoes_expert_act_bwd(self.plan, dout, z, n_out, act, gated, self.expert_offsets.data_ptr(), dz,
@@ -608,8 +613,8 @@ class Experts:
         w = self._in("W", W, (self.E, n_z, n_in), self.dtype)
         if accumulate and dW is None:
             raise ValueError("dW: a tensor to accumulate into is wanted")
-        dX = self._new(dX, (self.R, n_in), self.dtype) if need_dX else None
-        dW = self._new(dW, (self.E, n_z, n_in), torch.float32) if need_dW else None
+        dX = self._new(dX, (self.R, n_in), self.dtype, stream) if need_dX else None
+        dW = self._new(dW, (self.E, n_z, n_in), torch.float32, stream) if need_dW else None
         ws = self.ws
         _check(_lib.smoes_expert_linear_bwd(self.plan, dz, x, w, n_in, n_z, self.expert_offsets.data_ptr(), _ptr(dX),
                                             _ptr(dW), accumulate, ws.data_ptr(), ws.numel(), self._stream(stream)),

@@ -243,15 +243,12 @@ __device__ __forceinline__ uint32_t peer_smem(const void* p, uint32_t rank) {
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
   return a;
 }
-// Arrivals on a barrier of either CTA (a cluster address). The plain forms order this CTA's own accesses
-// only: what the barriers of a pair hand over was written or read by the copy engine and the tensor cores,
-// which have their own fences. With cluster scope every block of a product waited for a fence in its producer
-// and ran at 1200 clocks instead of 520. The _release form is for shared memory that a warp wrote itself.
+// Arrivals on a barrier of either CTA (a cluster address). They order this CTA's own accesses only: what the
+// barriers of a pair hand over was written or read by the copy engine and the tensor cores, or by warps that
+// fenced it for the tensor cores of their own SM (fence_proxy_async_smem). With cluster scope every block of a
+// product waited for a fence in its producer and ran at 1200 clocks instead of 520.
 __device__ __forceinline__ void mbar_arrive_peer(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive_peer_release(uint32_t bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void mbar_arrive_expect_tx_peer(uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.relaxed.cluster.shared::cluster.b64 _, [%0], %1;"

@@ -376,6 +376,25 @@ def test_on_another_stream(bd):
         assert torch.equal(a, b)
 
 
+def test_on_a_stream_given_by_argument(bd):
+    """Outputs made by a call on another stream than the current one are not handed out again before it is done."""
+    lay = Layer(bd, 4096, 16, 4, torch.bfloat16, seed=10, max_width=512)
+    X, W = lay.normal(4096, 256), lay.normal(16, 512, 256, std=0.06)
+    idx = torch.from_numpy(lay.idx).cuda()
+    lay.ex.sort(idx)
+    want, _ = lay.ex.linear(lay.ex.dispatch(X), W, act=1, gated=True)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(5):
+        lay.ex.sort(idx, stream=side)
+        Xs = lay.ex.dispatch(X, stream=side)
+        got, _ = lay.ex.linear(Xs, W, act=1, gated=True, stream=side)
+        del Xs                                          # its memory is the side stream's until linear has read it
+        torch.full((16384, 256), 7.0, dtype=torch.bfloat16, device="cuda")
+        side.synchronize()
+        assert torch.equal(got, want)
+
+
 def test_offsets_past_32_bits(bd):
     """More than 2^31 elements in the rows: the last rows are the right ones."""
     T, E, k, d = 131072, 128, 8, 2056
