@@ -498,13 +498,12 @@ class Experts:
         return t.data_ptr()
 
     def _new(self, t, shape, dtype, stream):
-        """The output given, checked, or a new one; one made for another stream than the current one is kept by the
-        allocator until that stream is done with it."""
+        """The output given, checked, or a new one from the memory of the stream that the call runs on."""
         if t is None:
-            t = torch.empty(shape, dtype=dtype, device=self.device)
-            if stream is not None:
-                t.record_stream(stream)
-            return t
+            if stream is None:
+                return torch.empty(shape, dtype=dtype, device=self.device)
+            with torch.cuda.stream(stream):
+                return torch.empty(shape, dtype=dtype, device=self.device)
         self._in("output", t, shape, dtype)
         return t
 
