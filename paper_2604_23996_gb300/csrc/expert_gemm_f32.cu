@@ -73,15 +73,19 @@ __device__ __forceinline__ void split_store(const float4& v, uint8_t* h, uint8_t
 // the rows of the block, of which `depth` exist.
 template <bool kAcross, int kRows>
 __device__ __forceinline__ void split_word(const uint8_t* raw, uint8_t* planes, int u, int depth) {
-  float4 v = *reinterpret_cast<const float4*>(raw + u * 16);
+  float4 v;
   if (kAcross) {
+    v = *reinterpret_cast<const float4*>(raw + u * 16);
     const int k = u / (kRows / 4), c = u % (kRows / 4) * 4;
     if (k >= depth) v = make_float4(0.f, 0.f, 0.f, 0.f);
     constexpr uint32_t kPlane = kRows * kF32K * 2;
     uint8_t* at = planes + (c >> 6) * (kF32K * 128) + sw128_offset(k, c & 63);
     split_store(v, at, at + kPlane, at + 2 * kPlane);
   } else {
-    const int r = u >> 3, k = (u & 7) * 4;
+    // a warp's 4 rows are 0, 4, 1, 5 (or 2, 6, 3, 7) of eight: the words of a half warp's two rows lie in different banks
+    const int w = u >> 5, x = (u >> 3) & 3, k = (u & 7) * 4;
+    const int r = (w >> 1) * 8 + (w & 1) * 2 + (x & 1) * 4 + (x >> 1);
+    v = *reinterpret_cast<const float4*>(raw + r * (kF32K * 4) + k * 4);
     uint8_t* h = planes + sw128_offset(r, k);
     split_store(v, h, planes + sw128_offset(r, k + kF32K), h + kRows * 128);
   }
@@ -333,7 +337,7 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         for (int i = 0; i < 4; ++i) split_word<kAcrossA, 128>(ra, split_a + st * kSplitA, tid + 256 * i, depth);
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-          if (kAcrossB || 32 * i < gemm_n<kMode>(t.cols) / 2)   // (rows 32 i and on)
+          if (kAcrossB || 32 * i < gemm_n<kMode>(t.cols) / 2)   // (rows 32 i to 32 i + 31)
             split_word<kAcrossB, 64>(rb, split_b + st * kSplitB, tid + 256 * i, depth);
         fence_proxy_async_smem();
         __syncwarp();
