@@ -10,7 +10,7 @@
 // 3.38e38, which round to one, give NaN.
 //
 // A pair of CTAs forms 256 features by up to 128 rows, as in expert_gemm.cu. Roles of a CTA's warps: 0 copies fp32
-// blocks of 32 of the depth to shared memory, 1 issues the products (first CTA), 2 holds tensor memory, 4-11
+// blocks of 32 of the depth to shared memory, 1 issues the products (first CTA), 2 holds tensor memory, 4-19
 // split the blocks and, one 256-deep chunk behind, move the sums and store finished tiles.
 // A block's planes: along the depth 128-byte rows of [h | m] and [l | -]; across it one box of 32 depth rows
 // per plane and 64 features. Rows behind an expert's last one are cleared where they are split.
@@ -25,8 +25,8 @@
 namespace smoes {
 namespace {
 
-constexpr int kF32Threads = 384;
-constexpr int kF32Warps = 8;                     // splitting and epilogue
+constexpr int kF32Threads = 640;
+constexpr int kF32Warps = 16;                    // splitting and epilogue, in groups of four
 constexpr int kF32K = 32;                        // depth of a block
 constexpr int kF32Chunk = 8;                     // blocks between moves of the sums
 constexpr int kF32Cols = 128;
@@ -238,20 +238,19 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         for (int which = 0; which < (l.pre ? 2 : 1); ++which) {
           uint4* o = static_cast<uint4*>(which ? l.pre : l.out);
           const int words = (which ? l.n_z : p.n_feat) / 4;
-          for (long long i = end * words + static_cast<long long>(blockIdx.x) * 256 + tid; i < l.R * words;
-               i += static_cast<long long>(gridDim.x) * 256)
+          for (long long i = end * words + static_cast<long long>(blockIdx.x) * (32 * kF32Warps) + tid;
+               i < l.R * words; i += static_cast<long long>(gridDim.x) * (32 * kF32Warps))
             o[i] = make_uint4(0u, 0u, 0u, 0u);
         }
       }
     }
-    float sum[2][32];                            // columns 64 g + 32 c + j
+    float sum[32];                               // columns 32 g + j
 #pragma unroll
-    for (int c = 0; c < 2; ++c)
-#pragma unroll
-      for (int j = 0; j < 32; ++j) sum[c][j] = 0.f;
+    for (int j = 0; j < 32; ++j) sum[j] = 0.f;
 
     // the finished tile's sums to memory: lanes hold neighbouring features, a column is an output row (dW: a row of dW)
     auto store = [&](const GemmTile& t) {
+      const int cols = t.cols - g * 32;          // of this group's columns
       if constexpr (kMode == kGemmForward) {
         const int fl = kGated ? 16 * q + (lane & 15) : 32 * q + lane;
         const int f = (t.m * 2 + static_cast<int>(rank)) * (kGated ? 64 : 128) + fl;
@@ -259,62 +258,50 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         const int zf = f + (kGated ? up * l.n_out : 0);
         const bool in = f < p.n_feat;
         const float bias = l.bias && in ? __ldg(l.bias + static_cast<long long>(t.e) * l.n_z + zf) : 0.f;
-        const long long row = t.row0 + g * 64;
+        const long long row = t.row0 + g * 32;
         float* out = static_cast<float*>(l.out) + row * l.n_out + f;
         float* pre = static_cast<float*>(l.pre) + row * l.n_z + zf;
         const float* res = static_cast<const float*>(l.residual) + row * l.n_out + f;
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
+        for (int j = 0; j < 32; ++j) {
+          sum[j] += bias;
+          if (l.pre && in && j < cols) pre[static_cast<long long>(j) * l.n_z] = sum[j];
+        }
+        if (kGated) {                            // of two columns each half of the warp finishes one
+#pragma unroll
+          for (int j = 0; j < 32; j += 2) {
+            const float got = __shfl_xor_sync(0xffffffffu, up ? sum[j] : sum[j + 1], 16);
+            const float y = act_value<kAct, false>(up ? got : sum[j]) * (up ? sum[j + 1] : got);
+            if (in && j + up < cols) {
+              const long long at = static_cast<long long>(j + up) * l.n_out;
+              out[at] = l.residual ? y + __ldg(res + at) : y;
+            }
+          }
+        } else {
 #pragma unroll
           for (int j = 0; j < 32; ++j) {
-            sum[c][j] += bias;
-            const int col = c * 32 + j;
-            if (l.pre && in && g * 64 + col < t.cols) pre[static_cast<long long>(col) * l.n_z] = sum[c][j];
-          }
-          if (kGated) {                          // of two columns each half of the warp finishes one
-#pragma unroll
-            for (int j = 0; j < 32; j += 2) {
-              const float got = __shfl_xor_sync(0xffffffffu, up ? sum[c][j] : sum[c][j + 1], 16);
-              const float y = act_value<kAct, false>(up ? got : sum[c][j]) * (up ? sum[c][j + 1] : got);
-              const int col = c * 32 + j + up;
-              if (in && g * 64 + col < t.cols) {
-                const long long at = static_cast<long long>(col) * l.n_out;
-                out[at] = l.residual ? y + __ldg(res + at) : y;
-              }
-            }
-          } else {
-#pragma unroll
-            for (int j = 0; j < 32; ++j) {
-              const int col = c * 32 + j;
-              if (in && g * 64 + col < t.cols) {
-                const long long at = static_cast<long long>(col) * l.n_out;
-                const float y = act_value<kAct, false>(sum[c][j]);
-                out[at] = l.residual ? y + __ldg(res + at) : y;
-              }
+            if (in && j < cols) {
+              const long long at = static_cast<long long>(j) * l.n_out;
+              const float y = act_value<kAct, false>(sum[j]);
+              out[at] = l.residual ? y + __ldg(res + at) : y;
             }
           }
         }
       } else {
         const int f = t.m * 256 + static_cast<int>(rank) * 128 + 32 * q + lane;
         const long long row = kMode == kGemmGradW ? static_cast<long long>(t.e) * l.n_z + t.col0 : t.row0;
-        float* out = (kMode == kGemmGradW ? l.dW : static_cast<float*>(l.out)) + (row + g * 64) * l.n_in + f;
+        float* out = (kMode == kGemmGradW ? l.dW : static_cast<float*>(l.out)) + (row + g * 32) * l.n_in + f;
         const bool add = kMode == kGemmGradW && l.accumulate;
         if (f < l.n_in) {
-          const int cols = t.cols - g * 64;      // (a pointer that steps: 64 addresses at once do not fit the registers)
 #pragma unroll
-          for (int c = 0; c < 2; ++c)
-#pragma unroll
-            for (int j = 0; j < 32; ++j) {
-              if (c * 32 + j < cols) *out = add ? *out + sum[c][j] : sum[c][j];
-              out += l.n_in;
-              asm volatile("" : "+l"(out));
-            }
+          for (int j = 0; j < 32; ++j) {
+            if (j < cols) *out = add ? *out + sum[j] : sum[j];
+            out += l.n_in;
+          }
         }
       }
 #pragma unroll
-      for (int c = 0; c < 2; ++c)
-#pragma unroll
-        for (int j = 0; j < 32; ++j) sum[c][j] = 0.f;
+      for (int j = 0; j < 32; ++j) sum[j] = 0.f;
     };
 
     // a chunk is split, then the one before it drained (one place each: inlined twice the sums do not fit the registers)
@@ -334,11 +321,9 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         const uint8_t* ra = raw_a + raw * kRawA;
         const uint8_t* rb = raw_b + raw * kRawB;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) split_word<kAcrossA, 128>(ra, split_a + st * kSplitA, tid + 256 * i, depth);
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-          if (kAcrossB || 32 * i < gemm_n<kMode>(t.cols) / 2)   // (rows 32 i to 32 i + 31)
-            split_word<kAcrossB, 64>(rb, split_b + st * kSplitB, tid + 256 * i, depth);
+        for (int i = 0; i < 2; ++i) split_word<kAcrossA, 128>(ra, split_a + st * kSplitA, tid + 512 * i, depth);
+        if (kAcrossB || (warp - 4) * 4 < gemm_n<kMode>(t.cols) / 2)   // (two warps split eight rows)
+          split_word<kAcrossB, 64>(rb, split_b + st * kSplitB, tid, depth);
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) {
@@ -353,18 +338,14 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         ok = warp_wait(&bars.acc_full[acc], aph, wc);
         if (!ok) break;
         tc_fence_after();
+        if (g * 32 < done.cols) {
+          float v[32];
+          tmem_ld32(tmem + acc * 256 + 128 + g * 32 + lanes, v);
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const int col = g * 64 + c * 32;
-          if (col < done.cols) {
-            float v[32];
-            tmem_ld32(tmem + acc * 256 + 128 + col + lanes, v);
+          for (int j = 0; j < 32; ++j) sum[j] += v[j];
+          tmem_ld32(tmem + acc * 256 + g * 32 + lanes, v);
 #pragma unroll
-            for (int j = 0; j < 32; ++j) sum[c][j] += v[j];
-            tmem_ld32(tmem + acc * 256 + col + lanes, v);
-#pragma unroll
-            for (int j = 0; j < 32; ++j) sum[c][j] += v[j];
-          }
+          for (int j = 0; j < 32; ++j) sum[j] += v[j];
         }
         tc_fence_before();
         __syncwarp();
