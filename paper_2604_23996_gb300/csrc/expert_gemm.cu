@@ -18,9 +18,15 @@
 // stop at the 16 rows that hold the end, and a warp clears the rows behind it in shared memory before
 // they are issued (multiplying them by zero would let infinities of the next expert in).
 //
-// Roles of a CTA's warps: 0 producer, 1 MMA issuer (first CTA), 2 tensor memory and the clearing, 4-11
-// epilogue, in two groups that take alternate 32-column chunks. Two accumulators of 256 columns: the epilogue of a
-// tile runs under the next tile's products.
+// Roles of a CTA's warps: 0 producer, 1 MMA issuer (first CTA), 2 tensor memory and the clearing, 4-19
+// epilogue, in four groups that take 16-column chunks in turn (two groups on 32 columns: 131072 x 144 x 1024 of 64
+// experts with silu and pre 134 instead of 107 us). Two accumulators of 256 columns: the epilogue of a tile runs
+// under the next tile's products.
+//
+// Measured, equal experts, cold chip: 98304 x 2048 x 2048 of 64 experts 442 us forward and dX (1.87 PFLOP/s), 500 dW
+// (which writes 1.07 GB), 16384 x 8192 x 2048 282 us (1.95 PFLOP/s). A layer of this size runs at the power limit:
+// the same calls back to back take 10 to 15% longer. Otherwise bound by the products; small depths (n_in below 500 or so)
+// by the epilogue, few rows by the weights' bytes.
 #include "expert_gemm.cuh"
 #include "experts.cuh"
 #include "ptx.cuh"
@@ -29,11 +35,6 @@ namespace smoes {
 namespace {
 
 constexpr int kGemmThreads = 640;
-// dW: the launch's 384 x 168 registers dealt anew, 56 for the first four warps and 224 for the epilogue, whose
-// threads hold 128 sums each (128 x 56 + 256 x 224 = 64512, all of them). setmaxnreg.inc waits without a limit for
-// registers that the launch does not hold, so the launch is refused if the kernel was compiled to fewer.
-constexpr int kGemmFewerRegisters = 56, kGemmMoreRegisters = 104;
-constexpr int kGemmDealtRegisters = 128 * kGemmFewerRegisters + (kGemmThreads - 128) * kGemmMoreRegisters;
 constexpr int kGemmEpiWarps = 16;
 constexpr int kGemmGroups = 4;                   // of four epilogue warps
 constexpr int kChunkCols = 16;                   // columns of D that a group finishes at a time
@@ -64,13 +65,12 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// A chunk is 32 columns of D (a feature per lane, an output row per column) by a CTA's 128 features. It leaves
-// through shared memory as boxes of 64 features by 32 rows, 128 bytes a row in the copy engine's swizzle:
-// out's boxes (two, gated one), then at 8 KB those of pre (two; gated one of g and one of u). A lane rounds two columns
+// A chunk is 16 columns of D (a feature per lane, an output row per column) by a CTA's 128 features. It leaves
+// through shared memory as boxes of 64 features by 16 rows, 128 bytes a row in the copy engine's swizzle:
+// out's boxes (two, gated one), then at 4 KB those of pre (two; gated one of g and one of u). A lane rounds two columns
 // into one word, exchanges it with its neighbour and picks two neighbouring features of one row out of both; rows 4 (2,
 // 6) apart are written at a time, whose swizzled words lie in different banks. Stored from the lanes, 4 bytes
 // each, the 32-byte pieces of pre made dsmoe_vlm's gated layer take 557 us instead of 446 without pre.
-// Chunks are bound by issue slots: 131072 x 144 x 1024 of 64 experts with silu and pre took 19 instructions a value.
 
 // Shared addresses of a lane's words: its features f & ~1 and the next in box row 4 odd, with the row's swizzle;
 // word i of four rows c + i lies at (at ^ i << 4) + (c + i) * 128 (c a multiple of 8: the swizzle is the row's low
@@ -236,7 +236,6 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
   const int n_total = kMode == kGemmGradW ? l.E * p.m_tiles * p.n_tiles : rt.total * p.m_tiles;   // tiles
   const uint32_t tmem = bars.tmem;
   const WaitCtx wc{&bars.abort, p.status, p.limit_ns};
-  if (kMode == kGemmGradW && warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kGemmFewerRegisters));
 
   if (warp == 0) {
     // ------------------------------------------------------------------------------- producer
@@ -363,7 +362,6 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     }
   } else if (warp >= 4) {
     // ------------------------------------------------------------------------------- epilogue
-    if (kMode == kGemmGradW) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kGemmMoreRegisters));
     const int q = warp & 3, g = (warp - 4) >> 2;
     const uint32_t lanes = static_cast<uint32_t>(32 * q) << 16;
     if (kMode != kGemmGradW) {
@@ -527,8 +525,7 @@ cudaError_t launch(ExpertGemmParams& p, const CUtensorMap& a, const CUtensorMap&
                    const CUtensorMap& out, const CUtensorMap& pre, int n_sms, cudaStream_t s) {
   static GemmResidency held;
   int pairs = 0;
-  const cudaError_t e = gemm_pairs(held, k_expert_gemm<kMode, kAct, kGated>, kGemmThreads, kGemmSmem,
-                                   kMode == kGemmGradW ? kGemmDealtRegisters : 0, n_sms, &pairs);
+  const cudaError_t e = gemm_pairs(held, k_expert_gemm<kMode, kAct, kGated>, kGemmThreads, kGemmSmem, n_sms, &pairs);
   if (e != cudaSuccess) return e;
   pairs = gemm_split(p, static_cast<ExpertGemmMode>(kMode), 256, kMode == kGemmGradW ? 128 : 64, pairs);
   return launch_pdl(k_expert_gemm<kMode, kAct, kGated>, dim3(2 * pairs), dim3(kGemmThreads), kGemmSmem, s, a, b, b16, out, pre, p);

@@ -89,7 +89,7 @@ struct GemmResidency {
   int pairs[64] = {};
 };
 template <class K>
-cudaError_t gemm_pairs(GemmResidency& r, K kernel, int threads, uint32_t smem, int dealt_registers, int n_sms, int* out) {
+cudaError_t gemm_pairs(GemmResidency& r, K kernel, int threads, uint32_t smem, int n_sms, int* out) {
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
@@ -98,10 +98,6 @@ cudaError_t gemm_pairs(GemmResidency& r, K kernel, int threads, uint32_t smem, i
   if (r.pairs[dev] == 0) {
     e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
     if (e != cudaSuccess) return e;
-    cudaFuncAttributes fa;
-    e = cudaFuncGetAttributes(&fa, kernel);
-    if (e != cudaSuccess) return e;
-    if (fa.numRegs * threads < dealt_registers) return cudaErrorInvalidConfiguration;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(n_sms / 2 * 2);
     cfg.blockDim = dim3(threads);
