@@ -395,7 +395,8 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
 #pragma unroll
           for (int i = 0; i < 16; ++i) sum[c][i] = 0.f;
         for (int k0 = 0; k0 < t.blocks; k0 += kGemmChunk) {
-          if (!warp_wait(&bars.acc_full[acc], aph, wc)) { ok = false; break; }
+          ok = named_bar_all(kBarVote + g, 128, q != 0 || warp_wait(&bars.acc_full[acc], aph, wc));
+          if (!ok) break;
           tc_fence_after();
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
@@ -413,7 +414,6 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
           if (++acc == 2) { acc = 0; aph ^= 1; }
         }
         // [16 rows of n_z][128 features] a chunk, to the copy engine, which leaves out what lies past n_z and n_in
-        ok = named_bar_all(kBarVote + g, 128, ok);   // one answer for the group: its barriers below count all four warps
         if (!ok) break;
         const int i0 = t.m * 256 + static_cast<int>(rank) * 128;
 #pragma unroll
@@ -449,8 +449,8 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
         const __nv_bfloat16* res = static_cast<const __nv_bfloat16*>(l.residual) + f0 + (fl & ~1);
         uint32_t rv[kChunkCols / 2];
         if (kMode == kGemmForward && l.bias && f_in) bias = __ldg(l.bias + static_cast<long long>(t.e) * l.n_z + zf);
-        // one answer for the group: its barriers below count all four warps
-        ok = named_bar_all(kBarVote + g, 128, warp_wait(&bars.acc_full[acc], aph, wc));
+        // one warp of the group waits for the products, the others for it; one answer for all four
+        ok = named_bar_all(kBarVote + g, 128, q != 0 || warp_wait(&bars.acc_full[acc], aph, wc));
         if (!ok) break;
         tc_fence_after();
         const int chunks = (t.cols + kChunkCols - 1) / kChunkCols;
