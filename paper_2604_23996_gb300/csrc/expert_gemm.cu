@@ -232,19 +232,26 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
   cluster_sync();                                // both CTAs' barriers are ready before anything arrives on them
   tc_fence_after();
   RowTiles rt{};
-  if (kMode != kGemmGradW) rt = count_row_tiles(off, l.E, l.R, p.tile_cols);
+  if (kMode != kGemmGradW) rt = count_row_tiles(off, l.E, static_cast<int>(l.R), p.tile_shift);
   const int n_total = kMode == kGemmGradW ? l.E * p.m_tiles * p.n_tiles : rt.total * p.m_tiles;   // tiles
   const uint32_t tmem = bars.tmem;
   const WaitCtx wc{&bars.abort, p.status, p.limit_ns};
+  // the producer and the MMA issuer look a tile up once the first block of the one before it is on its way: at the
+  // tile's own beginning the tensor cores stood still meanwhile
+  auto tile_at = [&](int tile) {
+    return tile < n_total ? gemm_tile<kMode, kGemmK>(p, rt, off, tile) : GemmTile{};
+  };
 
   if (warp == 0) {
     // ------------------------------------------------------------------------------- producer
     int st = 0;
     uint32_t ph = 0;
     bool ok = true;
+    GemmTile next = tile_at(pair);
     for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
-      const GemmTile t = gemm_tile<kMode, kGemmK>(p, rt, off, tile);
+      const GemmTile t = next;
       const int half_n = gemm_n<kMode>(t.cols) / 2;
+      if (t.blocks == 0) next = tile_at(tile + n_pairs);
       for (int kb = 0; kb < t.blocks; ++kb) {
         if (!warp_wait(&bars.empty[st], ph ^ 1, wc)) { ok = false; break; }
         if (elect_one()) {
@@ -253,7 +260,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
           if (kMode == kGemmGradW) {
             const int boxes = half_n / 64;
             const uint32_t bytes = kGemmHalf + boxes * 8192u;
-            const int r0 = static_cast<int>(t.row0) + kb * kGemmK;
+            const int r0 = t.row0 + kb * kGemmK;
             uint32_t bar;
             if (kb == t.blocks - 1 && (t.last & 15)) {
               bar = smem_u32(&bars.tail[st]);
@@ -285,7 +292,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
               tma_load_3d_pair(a, &tmA, bar, i0, k0, t.e);
               tma_load_3d_pair(a + 8192, &tmA, bar, i0 + 64, k0, t.e);
             }
-            const int r0 = static_cast<int>(t.row0) + static_cast<int>(rank) * half_n;
+            const int r0 = t.row0 + static_cast<int>(rank) * half_n;
             if (half_n == 128) {
               tma_load_2d_pair(b, &tmB, bar, k0, r0);
             } else {
@@ -294,6 +301,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
           }
         }
         __syncwarp();
+        if (kb == 0) next = tile_at(tile + n_pairs);
         if (++st == kGemmStages) { st = 0; ph ^= 1; }
       }
     }
@@ -308,8 +316,10 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     uint32_t ph = 0, aph = 0;
     bool ok = true;
     constexpr bool kMajorA = kMode != kGemmForward, kMajorB = kMode == kGemmGradW;   // along M / N in memory
+    GemmTile next = tile_at(pair);
     for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
-      const GemmTile t = gemm_tile<kMode, kGemmK>(p, rt, off, tile);
+      const GemmTile t = next;
+      if (t.blocks == 0) next = tile_at(tile + n_pairs);
       const uint32_t idesc = idesc_bf16(256, gemm_n<kMode>(t.cols), kMajorA, kMajorB);
       const int chunk = kMode == kGemmGradW ? kGemmChunk : t.blocks;
       for (int k0 = 0; ok && k0 < t.blocks; k0 += chunk) {
@@ -332,6 +342,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
             if (kb == k1 - 1) umma_commit_pair(&bars.acc_full[acc]);
           }
           __syncwarp();
+          if (kb == 0) next = tile_at(tile + n_pairs);
           if (++st == kGemmStages) { st = 0; ph ^= 1; }
         }
         if (++acc == 2) { acc = 0; aph ^= 1; }
@@ -527,7 +538,7 @@ cudaError_t launch(ExpertGemmParams& p, const CUtensorMap& a, const CUtensorMap&
   int pairs = 0;
   const cudaError_t e = gemm_pairs(held, k_expert_gemm<kMode, kAct, kGated>, kGemmThreads, kGemmSmem, n_sms, &pairs);
   if (e != cudaSuccess) return e;
-  pairs = gemm_split(p, static_cast<ExpertGemmMode>(kMode), 256, kMode == kGemmGradW ? 128 : 64, pairs);
+  pairs = gemm_split(p, static_cast<ExpertGemmMode>(kMode), 8, kMode == kGemmGradW ? 7 : 6, pairs);
   return launch_pdl(k_expert_gemm<kMode, kAct, kGated>, dim3(2 * pairs), dim3(kGemmThreads), kGemmSmem, s, a, b, b16, out, pre, p);
 }
 

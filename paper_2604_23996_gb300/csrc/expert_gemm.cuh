@@ -7,10 +7,10 @@
 
 namespace smoes {
 
-// A tile: 256 features (along M) by up to tile_cols rows (along N; for dW n_in by n_z), blocks of kBlock along the depth.
+// A tile: 256 features (along M) by up to 2^tile_shift rows (along N; for dW n_in by n_z), blocks of kBlock along the depth.
 struct GemmTile {
   int e, m;                                      // expert, feature tile
-  long long row0;                                // first row (dW: the expert's first row)
+  int row0;                                      // first row (dW: the expert's first row)
   int cols;                                      // rows of the tile (dW: columns of n_z)
   int col0;                                      // dW: first column of n_z
   int blocks;                                    // blocks along the depth
@@ -22,26 +22,27 @@ template <int kMode, int kBlock>
 __device__ __forceinline__ GemmTile gemm_tile(const ExpertGemmParams& p, const RowTiles& rt, const int32_t* off,
                                               int tile) {
   GemmTile t;
+  const int R = static_cast<int>(p.l.R);
   if (kMode == kGemmGradW) {
     const int per = p.m_tiles * p.n_tiles;
     t.e = tile / per;
     const int in = tile - t.e * per;
     const int j = in / p.m_tiles;
     t.m = in - j * p.m_tiles;
-    t.col0 = j * p.tile_cols;
-    t.cols = min(p.tile_cols, p.l.n_z - t.col0);
-    t.row0 = expert_begin(off, t.e, p.l.R);
-    const long long rows = max(0ll, expert_begin(off, t.e + 1, p.l.R) - t.row0);
-    t.blocks = static_cast<int>((rows + kBlock - 1) / kBlock);
-    t.last = static_cast<int>(rows - static_cast<long long>(t.blocks - 1) * kBlock);
+    t.col0 = j << p.tile_shift;
+    t.cols = min(1 << p.tile_shift, p.l.n_z - t.col0);
+    t.row0 = expert_row(off, t.e, R);
+    const int rows = max(0, expert_row(off, t.e + 1, R) - t.row0);
+    t.blocks = (rows + kBlock - 1) / kBlock;
+    t.last = rows - (t.blocks - 1) * kBlock;
     return t;
   }
   const int r = tile / p.m_tiles;
   t.m = tile - r * p.m_tiles;
-  const RowTile row = find_row_tile(rt, off, p.l.E, p.l.R, p.tile_cols, r);
+  const RowTile row = find_row_tile(rt, off, p.l.E, R, p.tile_shift, r);
   t.e = row.e;
   t.row0 = row.row0;
-  t.cols = static_cast<int>(min(static_cast<long long>(p.tile_cols), row.row1 - row.row0));
+  t.cols = min(1 << p.tile_shift, row.row1 - row.row0);
   t.col0 = 0;
   t.last = kBlock;
   t.blocks = ((kMode == kGemmForward ? p.l.n_in : p.l.n_z) + kBlock - 1) / kBlock;
@@ -54,20 +55,21 @@ __device__ __forceinline__ int gemm_n(int cols) {
   return kMode == kGemmGradW ? (cols + 127) & ~127 : (cols + 31) & ~31;
 }
 
-// Chooses tile_cols and n_tiles of a launch and returns its pairs of CTAs. Tiles have the widest kind of columns, unless
+// Chooses tile_shift (between log2s narrowest and widest) and n_tiles of a launch and returns its pairs of CTAs. Tiles have the widest kind of columns, unless
 // all tiles of a narrower kind have a pair each: every tile's products then take less time in the one round that
 // there is. Measured, bf16: 256 x 2048 x 256 takes 14.5 us as one tile of 256 rows and 10.1 us as four of 64.
 inline int gemm_split(ExpertGemmParams& p, ExpertGemmMode mode, int widest, int narrowest, int pairs) {
   const ExpertLinearParams& l = p.l;
   long long tiles = 0;
-  for (int cols = narrowest; cols <= widest; cols *= 2) {
-    p.tile_cols = cols;
+  for (int shift = narrowest; shift <= widest; ++shift) {
+    const int cols = 1 << shift;
+    p.tile_shift = shift;
     p.n_tiles = (l.n_z + cols - 1) / cols;
     // at most R / cols + min(E, R) row tiles exist, whatever the offsets are
     tiles = mode == kGemmGradW ? static_cast<long long>(l.E) * p.n_tiles : l.R / cols + (l.R < l.E ? l.R : l.E);
     tiles *= p.m_tiles;
     if (tiles <= pairs) break;
-    if (cols == widest) return pairs;
+    if (shift == widest) return pairs;
   }
   return tiles < 1 ? 1 : static_cast<int>(tiles);
 }

@@ -30,7 +30,6 @@ constexpr int kF32Threads = 640;
 constexpr int kF32Warps = 16;                    // splitting and epilogue, in groups of four
 constexpr int kF32K = 32;                        // depth of a block
 constexpr int kF32Chunk = 8;                     // blocks between moves of the sums
-constexpr int kF32Cols = 128;
 // (five and two, with eight splitting warps: 351 instead of 312 us for 8192 x 2048 x 2048, 240 instead of 227 us for
 // 64 experts of few rows)
 constexpr int kRawStages = 3, kSplitStages = 3;
@@ -138,19 +137,26 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
   cluster_sync();                                // both CTAs' barriers are ready before anything arrives on them
   tc_fence_after();
   RowTiles rt{};
-  if (kMode != kGemmGradW) rt = count_row_tiles(off, l.E, l.R, p.tile_cols);
+  if (kMode != kGemmGradW) rt = count_row_tiles(off, l.E, static_cast<int>(l.R), p.tile_shift);
   const int n_total = kMode == kGemmGradW ? l.E * p.m_tiles * p.n_tiles : rt.total * p.m_tiles;   // tiles
   const uint32_t tmem = bars.tmem;               // accumulator b: h h at columns 256 b, the small products at 256 b + 128
   const WaitCtx wc{&bars.abort, p.status, p.limit_ns};
+  // the producer and the MMA issuer look a tile up once the first block of the one before it is on its way: at the
+  // tile's own beginning the tensor cores stood still meanwhile
+  auto tile_at = [&](int tile) {
+    return tile < n_total ? gemm_tile<kMode, kF32K>(p, rt, off, tile) : GemmTile{};
+  };
 
   if (warp == 0) {
     // ------------------------------------------------------------------------------- producer
     int st = 0;
     uint32_t ph = 0;
     bool ok = true;
+    GemmTile next = tile_at(pair);
     for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
-      const GemmTile t = gemm_tile<kMode, kF32K>(p, rt, off, tile);
+      const GemmTile t = next;
       const int half_n = gemm_n<kMode>(t.cols) / 2;
+      if (t.blocks == 0) next = tile_at(tile + n_pairs);
       for (int kb = 0; kb < t.blocks; ++kb) {
         if (!warp_wait(&bars.raw_empty[st], ph ^ 1, wc)) { ok = false; break; }
         if (elect_one()) {
@@ -162,7 +168,7 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
           mbar_arrive_expect_tx(&bars.raw_full[st], kRawA + (few ? half_n * (kF32K * 4) : kRawB));
           const int k0 = kb * kF32K, r = static_cast<int>(rank);
           if (kMode == kGemmGradW) {
-            const int r0 = static_cast<int>(t.row0) + k0;
+            const int r0 = t.row0 + k0;
             tma_load_2d_pair(a, &tmA, bar, t.m * 256 + r * 128, r0);
             tma_load_2d_pair(b, &tmB, bar, t.col0 + r * half_n, r0);
           } else {
@@ -176,7 +182,7 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
             } else {
               tma_load_3d_pair(a, &tmA, bar, k0, t.m * 256 + r * 128, t.e);
             }
-            const int r0 = static_cast<int>(t.row0) + r * half_n;
+            const int r0 = t.row0 + r * half_n;
             if (!few) {
               tma_load_2d_pair(b, &tmB, bar, k0, r0);
             } else {
@@ -185,6 +191,7 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
           }
         }
         __syncwarp();
+        if (kb == 0) next = tile_at(tile + n_pairs);
         if (++st == kRawStages) { st = 0; ph ^= 1; }
       }
     }
@@ -193,8 +200,10 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     int st = 0, acc = 0;
     uint32_t ph = 0, aph = 0;
     bool ok = true;
+    GemmTile next = tile_at(pair);
     for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
-      const GemmTile t = gemm_tile<kMode, kF32K>(p, rt, off, tile);
+      const GemmTile t = next;
+      if (t.blocks == 0) next = tile_at(tile + n_pairs);
       const uint32_t idesc = idesc_bf16(256, gemm_n<kMode>(t.cols), kAcrossA, kAcrossB);
       for (int k0 = 0; ok && k0 < t.blocks; k0 += kF32Chunk) {
         if (!warp_wait(&bars.acc_empty[acc], aph ^ 1, wc)) { ok = false; break; }
@@ -225,6 +234,7 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
             if (kb == k1 - 1) umma_commit_pair(&bars.acc_full[acc]);
           }
           __syncwarp();
+          if (kb == 0) next = tile_at(tile + n_pairs);
           if (++st == kSplitStages) { st = 0; ph ^= 1; }
         }
         if (++acc == 2) { acc = 0; aph ^= 1; }
@@ -392,7 +402,7 @@ cudaError_t launch(ExpertGemmParams& p, const CUtensorMap& a, const CUtensorMap&
   int pairs = 0;
   const cudaError_t e = gemm_pairs(held, k_expert_gemm_f32<kMode, kAct, kGated>, kF32Threads, kF32Smem, n_sms, &pairs);
   if (e != cudaSuccess) return e;
-  pairs = gemm_split(p, static_cast<ExpertGemmMode>(kMode), kF32Cols, kMode == kGemmGradW ? kF32Cols : 32, pairs);
+  pairs = gemm_split(p, static_cast<ExpertGemmMode>(kMode), 7, kMode == kGemmGradW ? 7 : 5, pairs);
   return launch_pdl(k_expert_gemm_f32<kMode, kAct, kGated>, dim3(2 * pairs), dim3(kF32Threads), kF32Smem, s, a, b, b16, p);
 }
 

@@ -76,7 +76,7 @@ struct ExpertGemmParams {
   ExpertLinearParams l;
   int n_feat;                // features along m: n_out, or n_in
   int m_tiles;
-  int tile_cols;             // rows of a tile (weights' gradient: columns of n_z)
+  int tile_shift;            // log2 of a tile's rows (weights' gradient: its columns of n_z)
   int n_tiles;               // tiles along n_z (weights' gradient)
   uint32_t* status;
   uint64_t limit_ns;
@@ -101,26 +101,29 @@ __device__ __forceinline__ long long expert_begin(const int32_t* off, int e, lon
   return o < 0 ? 0 : o > R ? R : o;
 }
 
-// Work over the experts' rows in tiles of BM rows, counted over the experts in order. Every warp that walks
-// the tiles keeps the count before every eighth expert in its lanes; `off` may be a copy in shared memory.
+// Work over the experts' rows in tiles of 2^shift rows, counted over the experts in order. Every warp that walks
+// the tiles keeps the count before every eighth expert in its lanes; `off` is a copy of the offsets in shared memory. (R is
+// at most 2^24; with 64-bit rows and a division by the tile the count and the search took some 2000 clocks a kernel and 600
+// a tile.)
 struct RowTile {
   int e;
-  long long row0, row1;      // the tile's first row, the expert's end
+  int row0, row1;            // the tile's first row, the expert's end
 };
 struct RowTiles {
   int before;                // lane l: tiles of the experts before 8 l
   int total;
 };
-__device__ __forceinline__ int row_tiles_of(const int32_t* off, int e, int E, long long R, int BM) {
+__device__ __forceinline__ int expert_row(const int32_t* off, int e, int R) { return min(max(off[e], 0), R); }
+__device__ __forceinline__ int row_tiles_of(const int32_t* off, int e, int E, int R, int shift) {
   if (e >= E) return 0;
-  const long long rows = expert_begin(off, e + 1, R) - expert_begin(off, e, R);
-  return rows > 0 ? static_cast<int>((rows + BM - 1) / BM) : 0;
+  const int rows = expert_row(off, e + 1, R) - expert_row(off, e, R);
+  return rows > 0 ? (rows + (1 << shift) - 1) >> shift : 0;
 }
-__device__ inline RowTiles count_row_tiles(const int32_t* off, int E, long long R, int BM) {
+__device__ inline RowTiles count_row_tiles(const int32_t* off, int E, int R, int shift) {
   const int lane = threadIdx.x & 31;
   int sum = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) sum += row_tiles_of(off, lane * 8 + i, E, R, BM);
+  for (int i = 0; i < 8; ++i) sum += row_tiles_of(off, lane * 8 + i, E, R, shift);
   int run = sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -130,12 +133,11 @@ __device__ inline RowTiles count_row_tiles(const int32_t* off, int E, long long 
   return RowTiles{run - sum, __shfl_sync(0xffffffffu, run, 31)};
 }
 // Tile 0 <= tile < total, by a whole warp.
-__device__ __forceinline__ RowTile find_row_tile(const RowTiles& t, const int32_t* off, int E, long long R, int BM,
-                                                 int tile) {
+__device__ __forceinline__ RowTile find_row_tile(const RowTiles& t, const int32_t* off, int E, int R, int shift, int tile) {
   const int lane = threadIdx.x & 31;
   const int q = 31 - __clz(__ballot_sync(0xffffffffu, t.before <= tile));   // the last group that starts at or before it
   const int in = tile - __shfl_sync(0xffffffffu, t.before, q);
-  const int n = lane < 8 ? row_tiles_of(off, q * 8 + lane, E, R, BM) : 0;
+  const int n = lane < 8 ? row_tiles_of(off, q * 8 + lane, E, R, shift) : 0;
   int run = n;
 #pragma unroll
   for (int o = 1; o < 8; o <<= 1) {
@@ -145,8 +147,8 @@ __device__ __forceinline__ RowTile find_row_tile(const RowTiles& t, const int32_
   const int src = __ffs(__ballot_sync(0xffffffffu, lane < 8 && in < run)) - 1;
   RowTile r;
   r.e = q * 8 + src;
-  r.row0 = expert_begin(off, r.e, R) + static_cast<long long>(in - __shfl_sync(0xffffffffu, run - n, src)) * BM;
-  r.row1 = expert_begin(off, r.e + 1, R);
+  r.row0 = expert_row(off, r.e, R) + ((in - __shfl_sync(0xffffffffu, run - n, src)) << shift);
+  r.row1 = expert_row(off, r.e + 1, R);
   return r;
 }
 
