@@ -421,6 +421,69 @@ def test_offsets_past_32_bits(bd):
     assert ((Y[-4096:].double() - want).abs() <= U_BF16 * want.abs() + 1e-5).all()
 
 
+def test_offsets_and_maps_of_another_make_stay_inside(bd):
+    """Offsets that run backwards or leave [0, R], rows out of range: every call keeps to its buffers (guard rows on both
+    sides of every output stay as they were) and returns."""
+    T, E, k, d = 300, 6, 2, 64
+    R = T * k
+    for dt, code in ((torch.bfloat16, bd.SMOES_BF16), (torch.float32, bd.SMOES_F32)):
+        ex = bd.Experts(T, E, k, dtype=code, max_width=128)
+        ex.expert_offsets.copy_(torch.tensor([40, -7, 2 ** 31 - 1, 3, 590, 100, 550], dtype=torch.int32))
+        ex.slot_row.copy_(torch.randint(-2 ** 31, 2 ** 31 - 1, (T, k), dtype=torch.int64).to(torch.int32))
+        ex.slot_row[:5] = torch.tensor([[0, R - 1], [R, -1], [R + 1, 7], [2 ** 31 - 1, -2 ** 31], [1, 2]], dtype=torch.int32)
+
+        def guarded(rows, width, dtype=dt):
+            whole = torch.full((rows + 64, width), 3.0, dtype=dtype, device="cuda")
+            return whole, whole[32:32 + rows]
+
+        x = lambda rows, width: torch.ones((rows, width), dtype=dt, device="cuda")  # noqa: E731
+        W = torch.ones((E, 128, d), dtype=dt, device="cuda")
+        w = torch.ones((T, k), device="cuda")
+        outs = [guarded(R, d), guarded(T, d), guarded(T, d), guarded(R, d), guarded(T, k * 2, torch.float32), guarded(R, 64),
+                guarded(R, 128), guarded(R, 128), guarded(E, 128, torch.float32), guarded(R, d), guarded(E * 128, d, torch.float32)]
+        o = [v for _, v in outs]
+        ex.dispatch(x(T, d), out=o[0])
+        ex.combine(x(R, d), w, out=o[1])
+        ex.dispatch_bwd(x(R, d), out=o[2])
+        dw = torch.empty((T, k), device="cuda")
+        ex.combine_bwd(x(T, d), x(R, d), w, dYs=o[3], d_topk_w=dw)
+        ex.linear(x(R, d), W, act=1, gated=True, out=o[5], pre=o[6])
+        ex.act_bwd(x(R, 64), x(R, 128), act=1, gated=True, dZ=o[7], db=o[8])
+        ex.linear_bwd(x(R, 128), x(R, d), W, dX=o[9], dW=o[10].view(E, 128, d))
+        torch.cuda.synchronize()
+        for whole, _ in outs:
+            assert (whole[:32] == 3).all() and (whole[-32:] == 3).all()
+        assert torch.isfinite(dw).all() and ex.device_status() == bd.SMOES_OK
+
+
+def test_captured_in_a_graph(bd):
+    """A layer's calls replayed as a CUDA graph on new tokens and selections give what the calls give."""
+    lay = Layer(bd, 700, 16, 4, torch.bfloat16, seed=11, max_width=256)
+    X, W = lay.normal(700, 256), lay.normal(16, 256, 256, std=0.06)
+    idx = torch.from_numpy(lay.idx).cuda()
+
+    def steps():
+        lay.ex.sort(idx)
+        Xs = lay.ex.dispatch(X)
+        h, pre = lay.ex.linear(Xs, W, act=2, gated=True, save_pre=True)
+        dZ, db = lay.ex.act_bwd(h, pre, act=2, gated=True, bias_grad=True)
+        dX, dW = lay.ex.linear_bwd(dZ, Xs, W)
+        return [lay.ex.dispatch_bwd(dX, residual=X), db, dW]
+
+    steps()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = steps()
+    X.copy_(lay.normal(700, 256))
+    idx.copy_((idx + 3) % 16)
+    graph.replay()
+    torch.cuda.synchronize()
+    got = [t.clone() for t in got]
+    for a, b in zip(got, steps()):
+        assert torch.equal(a, b)
+
+
 def test_no_tokens(bd):
     ex = bd.Experts(0, 8, 2, max_width=64)
     off, _, _ = ex.sort(torch.empty((0, 2), dtype=torch.int32, device="cuda"))
