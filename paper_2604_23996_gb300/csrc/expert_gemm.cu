@@ -38,7 +38,8 @@ constexpr int kGemmThreads = 640;
 constexpr int kGemmEpiWarps = 16;
 constexpr int kGemmGroups = 4;                   // of four epilogue warps
 constexpr int kChunkCols = 16;                   // columns of D that a group finishes at a time
-constexpr int kGemmStages = 5;
+constexpr int kGemmStagesMost = 8;
+constexpr uint32_t kGemmRing = 5 * 32768;        // operand stages: five of 256 columns, eight of 64
 constexpr int kGemmK = 64;                       // depth of a block: 128 bytes of bf16
 constexpr uint32_t kGemmHalf = 128 * kGemmK * 2; // one CTA's operand of a block: 16 KB
 // dW: rows summed by the tensor cores before the sum moves to fp32 registers. The tensor cores cut each
@@ -47,18 +48,19 @@ constexpr int kGemmChunk = 8;                    // blocks of 64 rows
 
 constexpr uint32_t kGemmStaging = 16384;         // one epilogue group's output boxes: two chunks of 8 KB
 // alignment, operands, output boxes, barriers, [E + 1] offsets
-constexpr uint32_t kGemmSmem = 1024 + kGemmStages * 2 * kGemmHalf + kGemmGroups * kGemmStaging + 256 + 4 * (kExpertsMax + 1);
+constexpr uint32_t kGemmSmem = 1024 + kGemmRing + kGemmGroups * kGemmStaging + kBarBytes + 4 * (kExpertsMax + 1);
 static_assert(kGemmSmem <= 227 * 1024, "shared memory of a CTA");
 
 struct GemmBars {
-  uint64_t full[kGemmStages];                    // operands of both CTAs (first CTA's)
-  uint64_t empty[kGemmStages];
-  uint64_t tail[kGemmStages];                    // this CTA's operands of an expert's last rows, to be cleared
+  uint64_t full[kGemmStagesMost];                    // operands of both CTAs (first CTA's)
+  uint64_t empty[kGemmStagesMost];
+  uint64_t tail[kGemmStagesMost];                    // this CTA's operands of an expert's last rows, to be cleared
   uint64_t acc_full[2], acc_empty[2];
   uint32_t tmem;
   int abort;
+  int before[33];                                // row tiles (count_row_tiles)
 };
-static_assert(sizeof(GemmBars) <= 256, "barriers");
+static_assert(sizeof(GemmBars) <= kBarBytes, "barriers");
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
@@ -110,13 +112,13 @@ __device__ __forceinline__ void load_residual(const ExpertLinearParams& l, const
     rv[i] = c < rows ? __ldg(reinterpret_cast<const uint32_t*>(res + c * static_cast<long long>(l.n_out))) : 0u;
   }
 }
-// Adds one of its words (and the neighbour's) to the lane's values of the two rows.
-__device__ __forceinline__ void add_residual(float& x0, float& x4, uint32_t w) {
+// Adds one of its words (and the neighbour's) to the lane's values of the two rows. half: 0x3244 in odd lanes, 0x1044
+// in even ones (the word's high or low half as the upper half of a float).
+__device__ __forceinline__ void add_residual(float& x0, float& x4, uint32_t w, uint32_t half) {
   const bool odd = threadIdx.x & 1;
   const uint32_t got = __shfl_xor_sync(0xffffffffu, w, 1);
-  const uint32_t w0 = odd ? got : w, w4 = odd ? w : got;
-  x0 += __uint_as_float(odd ? w0 & 0xffff0000u : w0 << 16);
-  x4 += __uint_as_float(odd ? w4 & 0xffff0000u : w4 << 16);
+  x0 += __uint_as_float(__byte_perm(odd ? got : w, 0u, half));
+  x4 += __uint_as_float(__byte_perm(odd ? w : got, 0u, half));
 }
 
 // z (bias added) of a chunk to out, in shared memory, by whole warps. f: the lane's feature among the CTA's; rv: its
@@ -124,7 +126,7 @@ __device__ __forceinline__ void add_residual(float& x0, float& x4, uint32_t w) {
 template <int kAct, bool kGated>
 __device__ __forceinline__ void put_forward(uint8_t* boxes, int f, float (&v)[kChunkCols], bool residual,
                                             const uint32_t (&rv)[kChunkCols / 2]) {
-  const uint32_t pick = pair_pick();
+  const uint32_t pick = pair_pick(), half = (threadIdx.x & 1) ? 0x3244u : 0x1044u;
   uint32_t at = pair_address(boxes, f);
   if (!kGated) {
     if (kAct != SMOES_ACT_NONE) {
@@ -133,7 +135,7 @@ __device__ __forceinline__ void put_forward(uint8_t* boxes, int f, float (&v)[kC
     }
     if (residual) {
 #pragma unroll
-      for (int i = 0; i < kChunkCols / 2; ++i) add_residual(v[(i >> 2) * 8 + (i & 3)], v[(i >> 2) * 8 + (i & 3) + 4], rv[i]);
+      for (int i = 0; i < kChunkCols / 2; ++i) add_residual(v[(i >> 2) * 8 + (i & 3)], v[(i >> 2) * 8 + (i & 3) + 4], rv[i], half);
     }
     put_chunk(boxes, f, v);
     return;
@@ -150,7 +152,7 @@ __device__ __forceinline__ void put_forward(uint8_t* boxes, int f, float (&v)[kC
   }
   if (residual) {
 #pragma unroll
-    for (int i = 0; i < kChunkCols / 4; ++i) add_residual(y[(i >> 1) * 4 + (i & 1)], y[(i >> 1) * 4 + (i & 1) + 2], rv[i]);
+    for (int i = 0; i < kChunkCols / 4; ++i) add_residual(y[(i >> 1) * 4 + (i & 1)], y[(i >> 1) * 4 + (i & 1) + 2], rv[i], half);
   }
   at = (at ^ (up << 5)) + up * 256;              // the half's rows are two further down: the swizzle's bit of 2 with it
 #pragma unroll
@@ -198,18 +200,22 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
               const __grid_constant__ CUtensorMap tmPre, const ExpertGemmParams p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  uint8_t* sa = smem;
-  uint8_t* sb = smem + kGemmStages * kGemmHalf;
-  uint8_t* staging = smem + 2 * kGemmStages * kGemmHalf;
+  uint8_t* staging = smem + kGemmRing;
   GemmBars& bars = *reinterpret_cast<GemmBars*>(staging + kGemmGroups * kGemmStaging);
-  int32_t* off = reinterpret_cast<int32_t*>(staging + kGemmGroups * kGemmStaging + 256);   // [E + 1] offsets
+  int32_t* off = reinterpret_cast<int32_t*>(staging + kGemmGroups * kGemmStaging + kBarBytes);   // [E + 1] offsets
   const ExpertLinearParams& l = p.l;
   const int warp = warp_index(), lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
   const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
 
+  // a stage: A's 128 features, then B's half of the widest tile; as many as fit
+  const uint32_t stage_bytes = kGemmHalf + (64u << p.tile_shift);
+  const int n_stages = min(kGemmStagesMost, static_cast<int>(kGemmRing / stage_bytes));
+  auto stage_a = [&](int s) { return smem + s * stage_bytes; };
+  auto stage_b = [&](int s) { return smem + s * stage_bytes + kGemmHalf; };
+
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kGemmStages; ++i) {
+    for (int i = 0; i < n_stages; ++i) {
       mbar_init(&bars.full[i], 2);
       mbar_init(&bars.empty[i], 1);
       mbar_init(&bars.tail[i], 1);
@@ -222,17 +228,21 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     fence_mbar_init();
     tma_prefetch_desc(&tmA);
     tma_prefetch_desc(&tmB);
+    tma_prefetch_desc(&tmB16);
+    tma_prefetch_desc(&tmOut);
+    if (kMode == kGemmForward) tma_prefetch_desc(&tmPre);
   }
   if (warp == 2) tmem_alloc_pair(&bars.tmem, 512);
   pdl_wait();
   pdl_trigger();
+  if (kMode != kGemmGradW && warp == 3) count_row_tiles(l.offsets, l.E, static_cast<int>(l.R), p.tile_shift, bars.before);
   for (int e = threadIdx.x; e <= l.E; e += kGemmThreads) off[e] = __ldg(l.offsets + e);
   tc_fence_before();
   __syncthreads();
   cluster_sync();                                // both CTAs' barriers are ready before anything arrives on them
   tc_fence_after();
   RowTiles rt{};
-  if (kMode != kGemmGradW) rt = count_row_tiles(off, l.E, static_cast<int>(l.R), p.tile_shift);
+  if (kMode != kGemmGradW) rt = RowTiles{bars.before[lane], bars.before[32]};
   const int n_total = kMode == kGemmGradW ? l.E * p.m_tiles * p.n_tiles : rt.total * p.m_tiles;   // tiles
   const uint32_t tmem = bars.tmem;
   const WaitCtx wc{&bars.abort, p.status, p.limit_ns};
@@ -255,8 +265,8 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
       for (int kb = 0; kb < t.blocks; ++kb) {
         if (!warp_wait(&bars.empty[st], ph ^ 1, wc)) { ok = false; break; }
         if (elect_one()) {
-          uint8_t* a = sa + st * kGemmHalf;
-          uint8_t* b = sb + st * kGemmHalf;
+          uint8_t* a = stage_a(st);
+          uint8_t* b = stage_b(st);
           if (kMode == kGemmGradW) {
             const int boxes = half_n / 64;
             const uint32_t bytes = kGemmHalf + boxes * 8192u;
@@ -302,13 +312,13 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
         }
         __syncwarp();
         if (kb == 0) next = tile_at(tile + n_pairs);
-        if (++st == kGemmStages) { st = 0; ph ^= 1; }
+        if (++st == n_stages) { st = 0; ph ^= 1; }
       }
     }
     // every stage given back: no commit of the first CTA is still on its way to this one when it ends
-    for (int i = 0; ok && i < kGemmStages; ++i) {
+    for (int i = 0; ok && i < n_stages; ++i) {
       ok = warp_wait(&bars.empty[st], ph ^ 1, wc);
-      if (++st == kGemmStages) { st = 0; ph ^= 1; }
+      if (++st == n_stages) { st = 0; ph ^= 1; }
     }
   } else if (warp == 1 && rank == 0) {
     // ----------------------------------------------------------------------------- MMA issuer
@@ -331,7 +341,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
           if (!warp_wait(&bars.full[st], ph, wc)) { ok = false; break; }
           tc_fence_after();
           if (elect_one()) {
-            const uint32_t a = smem_u32(sa + st * kGemmHalf), b = smem_u32(sb + st * kGemmHalf);
+            const uint32_t a = smem_u32(stage_a(st)), b = smem_u32(stage_b(st));
             const int steps = kMode == kGemmGradW && kb == t.blocks - 1 ? (t.last + 15) >> 4 : 4;
             for (int s = 0; s < steps; ++s) {
               const uint64_t da = kMajorA ? sdesc_sw128(a + s * 2048, 8192, 1024) : sdesc_sw128(a + s * 32, 16, 1024);
@@ -343,7 +353,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
           }
           __syncwarp();
           if (kb == 0) next = tile_at(tile + n_pairs);
-          if (++st == kGemmStages) { st = 0; ph ^= 1; }
+          if (++st == n_stages) { st = 0; ph ^= 1; }
         }
         if (++acc == 2) { acc = 0; aph ^= 1; }
       }
@@ -355,15 +365,15 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     for (int tile = pair; tile < n_total; tile += n_pairs) {
       const GemmTile t = gemm_tile<kMode, kGemmK>(p, rt, off, tile);
       if (t.blocks == 0) continue;
-      const int s = (st + t.blocks - 1) % kGemmStages;
-      st = (st + t.blocks) % kGemmStages;
+      const int s = (st + t.blocks - 1) % n_stages;
+      st = (st + t.blocks) % n_stages;
       if (!(t.last & 15)) continue;
       if (!warp_wait(&bars.tail[s], (phases >> s) & 1, wc)) break;
       phases ^= 1u << s;
       // rows [last, round_up(last, 16)) of every 64-column box, 8 lanes a row of 128 bytes. The next block's products
       // wait for this one: with cluster scope on the arrival below every ragged expert's tiles took 1.4 us longer.
       const int boxes = 2 + gemm_n<kMode>(t.cols) / 128;
-      uint8_t* box = lane < 16 ? sa + s * kGemmHalf + (lane >> 3) * 8192 : sb + s * kGemmHalf + ((lane >> 3) - 2) * 8192;
+      uint8_t* box = lane < 16 ? stage_a(s) + (lane >> 3) * 8192 : stage_b(s) + ((lane >> 3) - 2) * 8192;
       if ((lane >> 3) < boxes)
         for (int r = t.last; r & 15; ++r) *reinterpret_cast<uint4*>(box + r * 128 + (lane & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
       fence_proxy_async_smem();

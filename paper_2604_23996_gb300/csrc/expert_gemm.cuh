@@ -7,6 +7,8 @@
 
 namespace smoes {
 
+constexpr int kBarBytes = 384;                   // shared memory for a kernel's barriers and counts
+
 // A tile: 256 features (along M) by up to 2^tile_shift rows (along N; for dW n_in by n_z), blocks of kBlock along the depth.
 struct GemmTile {
   int e, m;                                      // expert, feature tile
@@ -55,9 +57,10 @@ __device__ __forceinline__ int gemm_n(int cols) {
   return kMode == kGemmGradW ? (cols + 127) & ~127 : (cols + 31) & ~31;
 }
 
-// Chooses tile_shift (between log2s narrowest and widest) and n_tiles of a launch and returns its pairs of CTAs. Tiles have the widest kind of columns, unless
-// all tiles of a narrower kind have a pair each: every tile's products then take less time in the one round that
-// there is. Measured, bf16: 256 x 2048 x 256 takes 14.5 us as one tile of 256 rows and 10.1 us as four of 64.
+// Chooses tile_shift (between the log2s narrowest and widest) and n_tiles of a launch and returns its pairs of CTAs. Tiles
+// have the widest kind of columns, unless all tiles of a narrower kind have a pair each (every tile's products then
+// take less time in the one round that there is) or no expert can have more rows (narrower stages, more of them).
+// Measured, bf16: 256 x 2048 x 256 takes 14.5 us as one tile of 256 rows and 10.1 us as four of 64.
 inline int gemm_split(ExpertGemmParams& p, ExpertGemmMode mode, int widest, int narrowest, int pairs) {
   const ExpertLinearParams& l = p.l;
   long long tiles = 0;
@@ -68,10 +71,9 @@ inline int gemm_split(ExpertGemmParams& p, ExpertGemmMode mode, int widest, int 
     // at most R / cols + min(E, R) row tiles exist, whatever the offsets are
     tiles = mode == kGemmGradW ? static_cast<long long>(l.E) * p.n_tiles : l.R / cols + (l.R < l.E ? l.R : l.E);
     tiles *= p.m_tiles;
-    if (tiles <= pairs) break;
-    if (shift == widest) return pairs;
+    if (tiles <= pairs || (mode != kGemmGradW && l.R <= cols)) break;
   }
-  return tiles < 1 ? 1 : static_cast<int>(tiles);
+  return tiles < 1 ? 1 : tiles < pairs ? static_cast<int>(tiles) : pairs;
 }
 
 // Zeros in a CTA's half of a tile of dW, by `warps` warps of which this is number w: a row of 128 features a warp at a

@@ -36,7 +36,7 @@ constexpr int kRawStages = 3, kSplitStages = 3;
 constexpr uint32_t kRawA = 128 * kF32K * 4, kRawB = 64 * kF32K * 4;     // one CTA's fp32 operands of a block
 constexpr uint32_t kSplitA = 2 * 128 * 128, kSplitB = 2 * 64 * 128;     // and their planes
 constexpr uint32_t kF32Smem =
-    1024 + kRawStages * (kRawA + kRawB) + kSplitStages * (kSplitA + kSplitB) + 256 + 4 * (kExpertsMax + 1);
+    1024 + kRawStages * (kRawA + kRawB) + kSplitStages * (kSplitA + kSplitB) + kBarBytes + 4 * (kExpertsMax + 1);
 static_assert(kF32Smem <= 227 * 1024, "shared memory of a CTA");
 
 struct F32Bars {
@@ -46,8 +46,9 @@ struct F32Bars {
   uint64_t acc_full[2], acc_empty[2];
   uint32_t tmem;
   int abort;
+  int before[33];                                // row tiles (count_row_tiles)
 };
-static_assert(sizeof(F32Bars) <= 256, "barriers");
+static_assert(sizeof(F32Bars) <= kBarBytes, "barriers");
 
 // Four values, split, to their places in the planes.
 __device__ __forceinline__ uint2 split_off(float (&x)[4]) {             // x becomes what is left
@@ -103,7 +104,7 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
   uint8_t* raw_a = split_b + kSplitStages * kSplitB;
   uint8_t* raw_b = raw_a + kRawStages * kRawA;
   F32Bars& bars = *reinterpret_cast<F32Bars*>(raw_b + kRawStages * kRawB);
-  int32_t* off = reinterpret_cast<int32_t*>(reinterpret_cast<uint8_t*>(&bars) + 256);   // [E + 1] offsets
+  int32_t* off = reinterpret_cast<int32_t*>(reinterpret_cast<uint8_t*>(&bars) + kBarBytes);   // [E + 1] offsets
   const ExpertLinearParams& l = p.l;
   const int warp = warp_index(), lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
@@ -127,17 +128,19 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     fence_mbar_init();
     tma_prefetch_desc(&tmA);
     tma_prefetch_desc(&tmB);
+    tma_prefetch_desc(&tmB16);
   }
   if (warp == 2) tmem_alloc_pair(&bars.tmem, 512);
   pdl_wait();
   pdl_trigger();
+  if (kMode != kGemmGradW && warp == 3) count_row_tiles(l.offsets, l.E, static_cast<int>(l.R), p.tile_shift, bars.before);
   for (int e = threadIdx.x; e <= l.E; e += kF32Threads) off[e] = __ldg(l.offsets + e);
   tc_fence_before();
   __syncthreads();
   cluster_sync();                                // both CTAs' barriers are ready before anything arrives on them
   tc_fence_after();
   RowTiles rt{};
-  if (kMode != kGemmGradW) rt = count_row_tiles(off, l.E, static_cast<int>(l.R), p.tile_shift);
+  if (kMode != kGemmGradW) rt = RowTiles{bars.before[lane], bars.before[32]};
   const int n_total = kMode == kGemmGradW ? l.E * p.m_tiles * p.n_tiles : rt.total * p.m_tiles;   // tiles
   const uint32_t tmem = bars.tmem;               // accumulator b: h h at columns 256 b, the small products at 256 b + 128
   const WaitCtx wc{&bars.abort, p.status, p.limit_ns};

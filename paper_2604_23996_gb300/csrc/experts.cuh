@@ -119,18 +119,23 @@ __device__ __forceinline__ int row_tiles_of(const int32_t* off, int e, int E, in
   const int rows = expert_row(off, e + 1, R) - expert_row(off, e, R);
   return rows > 0 ? (rows + (1 << shift) - 1) >> shift : 0;
 }
-__device__ inline RowTiles count_row_tiles(const int32_t* off, int E, int R, int shift) {
+// The counts, by one warp from the offsets in global memory: lane l's to before[l], the total to before[32].
+__device__ inline void count_row_tiles(const int32_t* offsets, int E, int R, int shift, int* before) {
   const int lane = threadIdx.x & 31;
+  int o[9];
+#pragma unroll
+  for (int i = 0; i < 9; ++i) o[i] = min(max(__ldg(offsets + min(lane * 8 + i, E)), 0), R);   // (past E: no rows)
   int sum = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) sum += row_tiles_of(off, lane * 8 + i, E, R, shift);
+  for (int i = 0; i < 8; ++i) sum += o[i + 1] > o[i] ? (o[i + 1] - o[i] + (1 << shift) - 1) >> shift : 0;
   int run = sum;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int v = __shfl_up_sync(0xffffffffu, run, o);
-    if (lane >= o) run += v;
+  for (int i = 1; i < 32; i <<= 1) {
+    const int v = __shfl_up_sync(0xffffffffu, run, i);
+    if (lane >= i) run += v;
   }
-  return RowTiles{run - sum, __shfl_sync(0xffffffffu, run, 31)};
+  before[lane] = run - sum;
+  if (lane == 31) before[32] = run;
 }
 // Tile 0 <= tile < total, by a whole warp.
 __device__ __forceinline__ RowTile find_row_tile(const RowTiles& t, const int32_t* off, int E, int R, int shift, int tile) {
@@ -219,28 +224,25 @@ template <bool kFast>
 __device__ __forceinline__ float sigmoid_of(float z) {
   return kFast ? fast_reciprocal(1.f + fast_exp2(-kLog2E * z)) : 1.f / (1.f + expf(-z));
 }
-// Phi(z) and phi(z), the normal distribution's function and density.
-template <bool kFast>
-__device__ __forceinline__ float normal_of(float z, float& density) {
-  if (!kFast) {
-    density = expf(-0.5f * z * z) * 0.39894228f;
-    return 0.5f * erfcf(z * -0.70710678f);
-  }
-  const float e = fast_exp2(-0.5f * kLog2E * z * z);
-  density = e * 0.39894228f;
+// The fast form's half - erfc(|z| / sqrt 2) / 2 (so that Phi = 0.5 +- it), and e^(-z^2 / 2).
+__device__ __forceinline__ float fast_half_erf(float z, float& e) {
+  const float w = z * 0.84932180f;                       // sqrt(log2(e) / 2)
+  e = fast_exp2(-w * w);
   const float t = fast_reciprocal(fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.f));
-  float q = fmaf(1.061405429f, t, -1.453152027f);        // erfc(|z| / sqrt 2) = t q(t) e^(-z^2 / 2)
-  q = fmaf(q, t, 1.421413741f);
-  q = fmaf(q, t, -0.284496736f);
-  q = fmaf(q, t, 0.254829592f);
-  const float half = 0.5f * q * t * e;
-  return z < 0.f ? half : 1.f - half;
+  float q = fmaf(0.5f * 1.061405429f, t, 0.5f * -1.453152027f);   // erfc(|z| / sqrt 2) / 2 = t q(t) e^(-z^2 / 2)
+  q = fmaf(q, t, 0.5f * 1.421413741f);
+  q = fmaf(q, t, 0.5f * -0.284496736f);
+  q = fmaf(q, t, 0.5f * 0.254829592f);
+  return fmaf(-q, t * e, 0.5f);
 }
 template <int kAct, bool kFast>
 __device__ __forceinline__ float act_value(float z) {
-  float density;
   if (kAct == SMOES_ACT_SILU) return kFast ? z * sigmoid_of<true>(z) : z / (1.f + expf(-z));
-  if (kAct == SMOES_ACT_GELU) return z * normal_of<kFast>(z, density);
+  if (kAct == SMOES_ACT_GELU) {
+    if (!kFast) return 0.5f * z * erfcf(z * -0.70710678f);
+    float e;
+    return fmaf(fabsf(z), fast_half_erf(z, e), 0.5f * z);
+  }
   return z;
 }
 template <int kAct, bool kFast>
@@ -250,10 +252,15 @@ __device__ __forceinline__ void act_value_slope(float z, float& value, float& sl
     value = z * s;
     slope = fmaf(value, 1.f - s, s);
   } else if (kAct == SMOES_ACT_GELU) {
-    float density;
-    const float n = normal_of<kFast>(z, density);
+    float e, n;                                          // e^(-z^2 / 2), Phi(z)
+    if (kFast) {
+      n = 0.5f + copysignf(fast_half_erf(z, e), z);
+    } else {
+      e = expf(-0.5f * z * z);
+      n = 0.5f * erfcf(z * -0.70710678f);
+    }
     value = z * n;
-    slope = fmaf(z, density, n);
+    slope = fmaf(z * 0.39894228f, e, n);
   } else {
     value = z;
     slope = 1.f;
