@@ -456,6 +456,42 @@ def test_offsets_and_maps_of_another_make_stay_inside(bd):
         assert torch.isfinite(dw).all() and ex.device_status() == bd.SMOES_OK
 
 
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+def test_both_gradients_at_once_are_complete_when_the_call_is(bd, dt):
+    """The two products of linear_bwd overlap on the GPU. What ran before is done when they write, and both are done when the
+    next kernel reads: one expert holds nearly all rows, so that dW takes far longer than dX; the outputs are poisoned right
+    before and read right after."""
+    lay = Layer(bd, 6000, 4, 1, dt, seed=12, route=[20, 5900, 0, 80])
+    dZ, X, W = lay.rows(128), lay.rows(64), lay.normal(4, 128, 64, std=0.1)
+    dX, dW = lay.ex.linear_bwd(dZ, X, W)
+    alone_x, _ = lay.ex.linear_bwd(dZ, X, W, need_dW=False)
+    _, alone_w = lay.ex.linear_bwd(dZ, X, W, need_dX=False)
+    torch.cuda.synchronize()
+    assert torch.equal(dX, alone_x) and torch.equal(dW, alone_w)
+    for _ in range(40):
+        dX.fill_(float("nan"))
+        dW.fill_(float("nan"))
+        lay.ex.linear_bwd(dZ, X, W, dX=dX, dW=dW)
+        got_w, got_x = dW.clone(), dX.clone()
+        assert torch.equal(got_w, alone_w) and torch.equal(got_x, alone_x)
+    # the activation's gradient and the sort before it, the layer below behind it, without a wait between
+    lay = Layer(bd, 3000, 16, 2, dt, seed=13, max_width=256)
+    X, W, idx = lay.normal(3000, 128), lay.normal(16, 256, 128, std=0.1), torch.from_numpy(lay.idx).cuda()
+
+    def steps():
+        lay.ex.sort(idx)
+        Xs = lay.ex.dispatch(X)
+        h, pre = lay.ex.linear(Xs, W, act=1, gated=True, save_pre=True)
+        dZ, db = lay.ex.act_bwd(h, pre, act=1, gated=True, bias_grad=True)
+        dX, dW = lay.ex.linear_bwd(dZ, Xs, W)
+        return lay.ex.dispatch_bwd(dX), dW, db
+
+    want = [t.clone() for t in steps()]
+    for _ in range(30):
+        for a, b in zip(steps(), want):
+            assert torch.equal(a, b)
+
+
 def test_captured_in_a_graph(bd):
     """A layer's calls replayed as a CUDA graph on new tokens and selections give what the calls give."""
     lay = Layer(bd, 700, 16, 4, torch.bfloat16, seed=11, max_width=256)
