@@ -11,14 +11,15 @@
 //
 // A pair of CTAs forms 256 features by up to 128 rows, as in expert_gemm.cu. Roles of a CTA's warps: 0 copies fp32
 // blocks of 32 of the depth to shared memory, 1 issues the products (first CTA), 2 holds tensor memory, 4-19
-// split the blocks and, one 256-deep chunk behind, move the sums and store finished tiles.
+// split the blocks, eight of them every other one, and, one 256-deep chunk behind, all move the sums and store
+// finished tiles.
 // A block's planes: along the depth 128-byte rows of [h | m] and [l | -]; across it one box of 32 depth rows
 // per plane and 64 features. Rows behind an expert's last one are cleared where they are split.
 //
 // Bound by shared memory: a block's 24 KB arrive, are read and written as 36 KB, and the products read 72 KB, 1220
-// clocks at 128 bytes each against 770 of the products. Measured: 32768 x 2048 x 2048 of 16 experts 261 TFLOP/s forward,
-// 279 dX, 269 dW; 8192 x 512 x 256 of 16 experts 35 us for both gradients, on the FMA units (128 x 128 a block of
-// threads) 187. Eight splitting warps instead of sixteen: 232, 267 and 233 TFLOP/s.
+// clocks at 128 bytes each against 770 of the products. Measured: 32768 x 2048 x 2048 of 16 experts 279 TFLOP/s forward,
+// 288 dX, 268 dW; 8192 x 512 x 256 of 16 experts 17 us dX and 16 us dW, on the FMA units (128 x 128 a block of
+// threads) 187 for both. Eight splitting warps instead of sixteen: 232, 267 and 233 TFLOP/s.
 #include "expert_gemm.cuh"
 #include "experts.cuh"
 #include "ptx.cuh"
@@ -27,28 +28,47 @@ namespace smoes {
 namespace {
 
 constexpr int kF32Threads = 640;
-constexpr int kF32Warps = 16;                    // splitting and epilogue, in groups of four
+constexpr int kF32Warps = 16;                    // splitting, and epilogue in groups of four
 constexpr int kF32K = 32;                        // depth of a block
 constexpr int kF32Chunk = 8;                     // blocks between moves of the sums
 // (five and two, with eight splitting warps: 351 instead of 312 us for 8192 x 2048 x 2048, 240 instead of 227 us for
 // 64 experts of few rows)
-constexpr int kRawStages = 3, kSplitStages = 3;
+// Blocks go to two halves of the splitting warps in turn: while one waits for its block's bytes and fences what it
+// wrote, the other splits (8192 x 2048 x 2048: 257 instead of 277 us forward, 250 instead of 255 dX, 283 instead of
+// 295 dW).
+constexpr int kTurns = 2, kSplitThreads = 32 * kF32Warps / kTurns;      // threads that split a block
+// A half sees every other use of a stage only, and by its parity could not tell a barrier's phase from the one two
+// before. Barriers are therefore kept for six blocks, two uses of each stage: every use of one of them has the same
+// half of the warps behind it, and the same in front.
+constexpr int kStages = 3, kBlockBars = kTurns * kStages;
 constexpr uint32_t kRawA = 128 * kF32K * 4, kRawB = 64 * kF32K * 4;     // one CTA's fp32 operands of a block
 constexpr uint32_t kSplitA = 2 * 128 * 128, kSplitB = 2 * 64 * 128;     // and their planes
 constexpr uint32_t kF32Smem =
-    1024 + kRawStages * (kRawA + kRawB) + kSplitStages * (kSplitA + kSplitB) + kBarBytes + 4 * (kExpertsMax + 1);
+    1024 + kStages * (kRawA + kRawB + kSplitA + kSplitB) + kBarBytes + 4 * (kExpertsMax + 1);
 static_assert(kF32Smem <= 227 * 1024, "shared memory of a CTA");
 
 struct F32Bars {
-  uint64_t raw_full[kRawStages], raw_empty[kRawStages];
-  uint64_t split_full[kSplitStages];               // planes of both CTAs (first CTA's)
-  uint64_t split_empty[kSplitStages];
+  uint64_t raw_full[kBlockBars], raw_empty[kBlockBars];
+  uint64_t split_full[kBlockBars];               // planes of both CTAs (first CTA's)
+  uint64_t split_empty[kBlockBars];
   uint64_t acc_full[2], acc_empty[2];
   uint32_t tmem;
   int abort;
   int before[33];                                // row tiles (count_row_tiles)
 };
 static_assert(sizeof(F32Bars) <= kBarBytes, "barriers");
+
+// A block's place in the ring: its barriers, and those of the block that had its stage before it.
+struct RingPlace {
+  int bar = 0;
+  uint32_t ph = 0;
+  __device__ __forceinline__ int stage() const { return bar < kStages ? bar : bar - kStages; }
+  __device__ __forceinline__ int before() const { return bar < kStages ? bar + kStages : bar - kStages; }
+  __device__ __forceinline__ uint32_t before_ph() const { return bar < kStages ? ph ^ 1 : ph; }
+  __device__ __forceinline__ void next() {
+    if (++bar == kBlockBars) { bar = 0; ph ^= 1; }
+  }
+};
 
 // Four values, split, to their places in the planes.
 __device__ __forceinline__ uint2 split_off(float (&x)[4]) {             // x becomes what is left
@@ -100,10 +120,10 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   uint8_t* split_a = smem;                       // [stage] each
-  uint8_t* split_b = split_a + kSplitStages * kSplitA;
-  uint8_t* raw_a = split_b + kSplitStages * kSplitB;
-  uint8_t* raw_b = raw_a + kRawStages * kRawA;
-  F32Bars& bars = *reinterpret_cast<F32Bars*>(raw_b + kRawStages * kRawB);
+  uint8_t* split_b = split_a + kStages * kSplitA;
+  uint8_t* raw_a = split_b + kStages * kSplitB;
+  uint8_t* raw_b = raw_a + kStages * kRawA;
+  F32Bars& bars = *reinterpret_cast<F32Bars*>(raw_b + kStages * kRawB);
   int32_t* off = reinterpret_cast<int32_t*>(reinterpret_cast<uint8_t*>(&bars) + kBarBytes);   // [E + 1] offsets
   const ExpertLinearParams& l = p.l;
   const int warp = warp_index(), lane = threadIdx.x & 31;
@@ -112,12 +132,10 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
   constexpr bool kAcrossA = kMode != kGemmForward, kAcrossB = kMode == kGemmGradW;   // the depth is not contiguous
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kRawStages; ++i) {
+    for (int i = 0; i < kBlockBars; ++i) {
       mbar_init(&bars.raw_full[i], 1);
-      mbar_init(&bars.raw_empty[i], kF32Warps);
-    }
-    for (int i = 0; i < kSplitStages; ++i) {
-      mbar_init(&bars.split_full[i], 2 * kF32Warps);
+      mbar_init(&bars.raw_empty[i], kF32Warps / kTurns);
+      mbar_init(&bars.split_full[i], 2 * kF32Warps / kTurns);   // (of both CTAs)
       mbar_init(&bars.split_empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -154,8 +172,7 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
 
   if (warp == 0) {
     // ------------------------------------------------------------------------------- producer
-    int st = 0;
-    uint32_t ph = 0;
+    RingPlace at;
     bool ok = true;
     GemmTile next = tile_at(pair);
     for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
@@ -163,14 +180,14 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
       const int half_n = gemm_n<kMode>(t.cols) / 2;
       if (t.blocks == 0) next = tile_at(tile + n_pairs);
       for (int kb = 0; kb < t.blocks; ++kb) {
-        if (!warp_wait(&bars.raw_empty[st], ph ^ 1, wc)) { ok = false; break; }
+        if (!warp_wait(&bars.raw_empty[at.before()], at.before_ph(), wc)) { ok = false; break; }
         if (elect_one()) {
-          uint8_t* a = raw_a + st * kRawA;
-          uint8_t* b = raw_b + st * kRawB;
-          const uint32_t bar = smem_u32(&bars.raw_full[st]);
+          uint8_t* a = raw_a + at.stage() * kRawA;
+          uint8_t* b = raw_b + at.stage() * kRawB;
+          const uint32_t bar = smem_u32(&bars.raw_full[at.bar]);
           // few rows: boxes of 16
           const bool few = kMode != kGemmGradW && half_n < 64;
-          mbar_arrive_expect_tx(&bars.raw_full[st], kRawA + (few ? half_n * (kF32K * 4) : kRawB));
+          mbar_arrive_expect_tx(&bars.raw_full[at.bar], kRawA + (few ? half_n * (kF32K * 4) : kRawB));
           const int k0 = kb * kF32K, r = static_cast<int>(rank);
           if (kMode == kGemmGradW) {
             const int r0 = t.row0 + k0;
@@ -197,13 +214,14 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         }
         __syncwarp();
         if (kb == 0) next = tile_at(tile + n_pairs);
-        if (++st == kRawStages) { st = 0; ph ^= 1; }
+        at.next();
       }
     }
   } else if (warp == 1 && rank == 0) {
     // ----------------------------------------------------------------------------- MMA issuer
-    int st = 0, acc = 0;
-    uint32_t ph = 0, aph = 0;
+    RingPlace at;
+    int acc = 0;
+    uint32_t aph = 0;
     bool ok = true;
     GemmTile next = tile_at(pair);
     for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
@@ -216,9 +234,10 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         const uint32_t d = tmem + acc * 256;
         const int k1 = min(k0 + kF32Chunk, t.blocks);
         for (int kb = k0; kb < k1; ++kb) {
-          if (!warp_wait(&bars.split_full[st], ph, wc)) { ok = false; break; }
+          if (!warp_wait(&bars.split_full[at.bar], at.ph, wc)) { ok = false; break; }
           tc_fence_after();
           if (elect_one()) {
+            const int st = at.stage();
             const uint32_t a = smem_u32(split_a + st * kSplitA), b = smem_u32(split_b + st * kSplitB);
             // plane 0 h, 1 m, 2 l; the products of planes (x, y) with x + y <= 2, small ones first
             constexpr int kX[6] = {2, 0, 1, 1, 0, 0}, kY[6] = {0, 2, 1, 0, 1, 0};
@@ -235,12 +254,12 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                 umma_bf16_pair(c == 5 ? d : d + 128, da, db, idesc, kb > k0 || s > 0 || (c > 0 && c < 5));
               }
             }
-            umma_commit_pair(&bars.split_empty[st]);
+            umma_commit_pair(&bars.split_empty[at.bar]);
             if (kb == k1 - 1) umma_commit_pair(&bars.acc_full[acc]);
           }
           __syncwarp();
           if (kb == 0) next = tile_at(tile + n_pairs);
-          if (++st == kSplitStages) { st = 0; ph ^= 1; }
+          at.next();
         }
         if (++acc == 2) { acc = 0; aph ^= 1; }
       }
@@ -322,8 +341,10 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     };
 
     // a chunk is split, then the one before it drained (one place each: inlined twice the sums do not fit the registers)
-    int st = 0, raw = 0, acc = 0;
-    uint32_t ph = 0, rph = 0, aph = 0;
+    const int turn = (warp - 4) / (kF32Warps / kTurns), part = tid & (kSplitThreads - 1);
+    RingPlace at;
+    int acc = 0;
+    uint32_t aph = 0;
     bool ok = true;
     int tile = pair, k0 = 0;
     bool more = tile < n_total;
@@ -332,23 +353,29 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     bool pending = false, pending_last = false;
     while (more || pending) {
       const int k1 = more ? min(k0 + kF32Chunk, t.blocks) : k0;
-      for (int kb = k0; kb < k1; ++kb) {
-        if (!warp_wait(&bars.raw_full[raw], rph, wc) || !warp_wait(&bars.split_empty[st], ph ^ 1, wc)) { ok = false; break; }
+      for (int kb = k0; kb < k1; ++kb, at.next()) {
+        if (at.bar % kTurns != turn) continue;
+        if (!warp_wait(&bars.raw_full[at.bar], at.ph, wc) ||
+            !warp_wait(&bars.split_empty[at.before()], at.before_ph(), wc)) { ok = false; break; }
+        const int st = at.stage();
         const int depth = kMode == kGemmGradW && kb == t.blocks - 1 ? t.last : kF32K;
-        const uint8_t* ra = raw_a + raw * kRawA;
-        const uint8_t* rb = raw_b + raw * kRawB;
+        const uint8_t* ra = raw_a + st * kRawA;
+        const uint8_t* rb = raw_b + st * kRawB;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) split_word<kAcrossA, 128>(ra, split_a + st * kSplitA, tid + 512 * i, depth);
-        if (kAcrossB || (warp - 4) * 4 < gemm_n<kMode>(t.cols) / 2)   // (two warps split eight rows)
-          split_word<kAcrossB, 64>(rb, split_b + st * kSplitB, tid, depth);
+        for (int i = 0; i < 2 * kTurns; ++i)
+          split_word<kAcrossA, 128>(ra, split_a + st * kSplitA, part + i * kSplitThreads, depth);
+#pragma unroll
+        for (int i = 0; i < kTurns; ++i) {
+          const int u = part + i * kSplitThreads;
+          if (kAcrossB || (u >> 6) * 8 < gemm_n<kMode>(t.cols) / 2)     // (two warps split eight rows)
+            split_word<kAcrossB, 64>(rb, split_b + st * kSplitB, u, depth);
+        }
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) {
-          mbar_arrive_peer(peer_smem(&bars.split_full[st], 0));
-          mbar_arrive(&bars.raw_empty[raw]);
+          mbar_arrive_peer(peer_smem(&bars.split_full[at.bar], 0));
+          mbar_arrive(&bars.raw_empty[at.bar]);
         }
-        if (++raw == kRawStages) { raw = 0; rph ^= 1; }
-        if (++st == kSplitStages) { st = 0; ph ^= 1; }
       }
       if (!ok) break;
       if (pending && done.blocks > 0) {
@@ -384,10 +411,9 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
       }
     }
     // every plane given back: no commit of the first CTA is still on its way to this one when it ends
-    for (int i = 0; ok && i < kSplitStages; ++i) {
-      ok = warp_wait(&bars.split_empty[st], ph ^ 1, wc);
-      if (++st == kSplitStages) { st = 0; ph ^= 1; }
-    }
+    // (each half those that it would wait for next)
+    for (int i = 0; ok && i < kStages; ++i, at.next())
+      if (at.bar % kTurns == turn) ok = warp_wait(&bars.split_empty[at.before()], at.before_ph(), wc);
   }
   __syncwarp();
   tc_fence_before();

@@ -492,6 +492,29 @@ def test_both_gradients_at_once_are_complete_when_the_call_is(bd, dt):
             assert torch.equal(a, b)
 
 
+def test_whole_numbers_come_out_exactly_call_after_call(bd):
+    """fp32 products of many short tiles: 72 experts with none to a few rows, a few hundred blocks of the ring each call. Whole
+    numbers up to 8 and sums below 2^17, so that every order of the sums gives the same bits; a block split too early or used
+    twice shows."""
+    for T, E, k, n_in, n_z, seed in ((4, 72, 4, 1024, 2048, 31), (45, 72, 4, 264, 520, 32), (1, 72, 1, 32, 8, 33)):
+        lay = Layer(bd, T, E, k, torch.float32, seed=seed, dropped=0.1)
+        whole = lambda *shape: torch.randint(-8, 9, shape, generator=lay.g, device="cuda").float()
+        X, W, dZ = whole(lay.ex.R, n_in), whole(E, n_z, n_in), whole(lay.ex.R, n_z)
+        want = torch.zeros(lay.ex.R, n_z, device="cuda", dtype=torch.float64)
+        want_x = torch.zeros(lay.ex.R, n_in, device="cuda", dtype=torch.float64)
+        want_w = torch.zeros(E, n_z, n_in, device="cuda", dtype=torch.float64)
+        for e in range(E):
+            a, b = int(lay.off[e]), int(lay.off[e + 1])
+            want[a:b] = X[a:b].double() @ W[e].double().T
+            want_x[a:b] = dZ[a:b].double() @ W[e].double()
+            want_w[e] = dZ[a:b].double().T @ X[a:b].double()
+        for _ in range(20):
+            out, _ = lay.ex.linear(X, W)
+            dX, dW = lay.ex.linear_bwd(dZ, X, W)
+            assert torch.equal(out.double(), want) and torch.equal(dX.double(), want_x)
+            assert torch.equal(dW.double(), want_w)
+
+
 def test_captured_in_a_graph(bd):
     """A layer's calls replayed as a CUDA graph on new tokens and selections give what the calls give."""
     lay = Layer(bd, 700, 16, 4, torch.bfloat16, seed=11, max_width=256)
