@@ -5,7 +5,8 @@
 // 32 x 16 bytes of columns, three blocks an SM and all of them resident: a row per warp, three rows' loads in flight.
 // Column sums stay in registers until the expert changes; then the eight warps' sums are added in order into the
 // partial of (range, expert), and a second small kernel adds each expert's partials in order. Ranges and experts
-// both only go up along the rows, so range + expert numbers the partials without gaps to search.
+// both only go up along the rows, so range + expert numbers the partials without gaps to search. No range is empty: the
+// second kernel adds every partial between an expert's first range and its last.
 //
 // Bound by HBM and by issue slots in about equal parts. A block per 32 rows, with the activation chosen at run time:
 // 57-61 us for 30035 x 704 gated (floor 31).
@@ -19,6 +20,10 @@ constexpr int kActThreads = 256;
 constexpr int kActWarps = kActThreads / 32;
 constexpr int kActRows = 3;                      // rows a warp has in flight
 
+// Ranges over n rows: the launch's, but a row each at least (its count is of the plan's rows; dropped selections have none).
+__device__ __forceinline__ int row_ranges(const ExpertActParams& p, long long n) {
+  return n < p.ranges ? static_cast<int>(n) : p.ranges;
+}
 // First row of range i of `ranges` over n rows.
 __device__ __forceinline__ long long range_begin(long long n, int ranges, int i) { return n * i / ranges; }
 
@@ -33,10 +38,10 @@ __global__ void __launch_bounds__(kActThreads, kActBlocksPerSm) k_act_bwd(const 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const long long n = expert_begin(p.offsets, p.E, p.R);
   if (!kSumsOnly) zero_rows(p.dZ, n, p.R, p.n_z / N);
-  const int segment = blockIdx.x / p.ranges, range = blockIdx.x - segment * p.ranges;
-  const long long end = range_begin(n, p.ranges, range + 1);
-  long long row = range_begin(n, p.ranges, range);
-  if (row >= end) return;
+  const int segment = blockIdx.x / p.ranges, range = blockIdx.x - segment * p.ranges, ranges = row_ranges(p, n);
+  if (range >= ranges) return;
+  const long long end = range_begin(n, ranges, range + 1);
+  long long row = range_begin(n, ranges, range);
   const int c0 = (segment * 32 + lane) * N;              // column of dOut (and of g or z)
   const bool in = c0 < p.n_out;
   const T* dout = static_cast<const T*>(p.dOut) + c0;
@@ -131,9 +136,10 @@ __global__ void __launch_bounds__(kActThreads) k_act_bias(const ExpertActParams 
   float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
   if (r0 < r1 && c < p.n_z) {
     // the range of row r: the last one that begins at or before it
-    int lo = static_cast<int>(r0 * p.ranges / n), hi = static_cast<int>((r1 - 1) * p.ranges / n);
-    while (lo + 1 < p.ranges && range_begin(n, p.ranges, lo + 1) <= r0) ++lo;
-    while (hi + 1 < p.ranges && range_begin(n, p.ranges, hi + 1) <= r1 - 1) ++hi;
+    const int ranges = row_ranges(p, n);
+    int lo = static_cast<int>(r0 * ranges / n), hi = static_cast<int>((r1 - 1) * ranges / n);
+    while (lo + 1 < ranges && range_begin(n, ranges, lo + 1) <= r0) ++lo;
+    while (hi + 1 < ranges && range_begin(n, ranges, hi + 1) <= r1 - 1) ++hi;
 #pragma unroll 8
     for (int i = lo + warp; i <= hi; i += kActWarps) {
       const float4 v = __ldcg(reinterpret_cast<const float4*>(p.part + static_cast<long long>(i + e) * p.n_z + c));
