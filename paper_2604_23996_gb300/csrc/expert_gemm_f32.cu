@@ -149,10 +149,8 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     tma_prefetch_desc(&tmB16);
   }
   if (warp == 2) tmem_alloc_pair(&bars.tmem, 512);
-  if (!p.beside) {
-    pdl_wait();
-    pdl_trigger();
-  }
+  pdl_wait();
+  pdl_trigger();
   if (kMode != kGemmGradW && warp == 3) count_row_tiles(l.offsets, l.E, static_cast<int>(l.R), p.tile_shift, bars.before);
   for (int e = threadIdx.x; e <= l.E; e += kF32Threads) off[e] = __ldg(l.offsets + e);
   tc_fence_before();
@@ -421,10 +419,6 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
   if (bars.abort && threadIdx.x == 0)            // copies and products in flight end long before this does
     for (int i = 0; i < 1000; ++i) __nanosleep(1000);
   __syncthreads();
-  if (p.beside) {                                // the kernel before has completed when this one does
-    pdl_wait();
-    pdl_trigger();
-  }
   cluster_sync();
   tc_fence_after();
   if (warp == 2) tmem_dealloc_pair(tmem, 512);
@@ -443,13 +437,12 @@ cudaError_t launch(ExpertGemmParams& p, const CUtensorMap& a, const CUtensorMap&
 
 }  // namespace
 
-cudaError_t launch_expert_gemm_f32(const ExpertLinearParams& l, ExpertGemmMode mode, bool beside, uint32_t* status,
+cudaError_t launch_expert_gemm_f32(const ExpertLinearParams& l, ExpertGemmMode mode, uint32_t* status,
                                    uint64_t limit_ns, int n_sms, cudaStream_t s) {
   ExpertGemmParams p{};
   p.l = l;
   p.status = status;
   p.limit_ns = limit_ns;
-  p.beside = beside ? 1 : 0;
   p.n_feat = mode == kGemmForward ? l.n_out : l.n_in;
   const int per = mode == kGemmForward && l.gated ? 128 : 256;
   p.m_tiles = (p.n_feat + per - 1) / per;

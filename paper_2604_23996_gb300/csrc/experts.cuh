@@ -80,17 +80,12 @@ struct ExpertGemmParams {
   int n_tiles;               // tiles along n_z (weights' gradient)
   uint32_t* status;
   uint64_t limit_ns;
-  int beside;                // nothing of the kernel launched just before is read or written here (see the launch)
 };
 
-// beside: the launch just before on the stream is the product of the other gradient. The kernel then begins while that one
-// still runs, on the SMs that it has left: every kernel before that one has completed when this one may start, and the
-// two share inputs alone. It waits for it before it ends, so that what follows on the stream finds both complete.
-// (8192 x 512 x 256 in fp32 of 16 unequal experts, both gradients: 45 us one after the other.)
-cudaError_t launch_expert_gemm(const ExpertLinearParams& p, ExpertGemmMode mode, bool beside, uint32_t* status,
-                               uint64_t limit_ns, int n_sms, cudaStream_t s);
-cudaError_t launch_expert_gemm_f32(const ExpertLinearParams& p, ExpertGemmMode mode, bool beside, uint32_t* status,
-                                   uint64_t limit_ns, int n_sms, cudaStream_t s);
+cudaError_t launch_expert_gemm(const ExpertLinearParams& p, ExpertGemmMode mode, uint32_t* status, uint64_t limit_ns,
+                               int n_sms, cudaStream_t s);
+cudaError_t launch_expert_gemm_f32(const ExpertLinearParams& p, ExpertGemmMode mode, uint32_t* status, uint64_t limit_ns,
+                                   int n_sms, cudaStream_t s);
 cudaError_t launch_expert_sort(const ExpertSortParams& p, cudaStream_t s);
 cudaError_t launch_expert_dispatch(const ExpertRowsParams& p, bool bf16, cudaStream_t s);
 cudaError_t launch_expert_combine(const ExpertRowsParams& p, bool bf16, cudaStream_t s);
