@@ -15,8 +15,10 @@
 // Ragged edges: rows of the next expert inside a tile are other columns of D and are not stored; features
 // past the expert's weights are zeros of the 3-d map (or the rows of u, not stored); a depth that ends
 // inside a block is zeros of both maps. For dW the depth is the expert's rows: the last block's products
-// stop at the 16 rows that hold the end, and a warp clears the rows behind it in shared memory before
-// they are issued (multiplying them by zero would let infinities of the next expert in).
+// stop at the 16 rows that hold the end, and a warp of each CTA clears the rows behind it in shared memory before
+// they are issued (multiplying them by zero would let infinities of the next expert in). The products of the first CTA
+// read what the second cleared: handed over at cluster scope, which takes about 1 us, and the tile's first block, so that
+// it passes under the products of the tile before.
 //
 // Roles of a CTA's warps: 0 producer, 1 MMA issuer (first CTA), 2 tensor memory and the clearing, 4-19
 // epilogue, in four groups that take 16-column chunks in turn (two groups on 32 columns: 131072 x 144 x 1024 of 64
@@ -270,9 +272,9 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
           if (kMode == kGemmGradW) {
             const int boxes = half_n / 64;
             const uint32_t bytes = kGemmHalf + boxes * 8192u;
-            const int r0 = t.row0 + kb * kGemmK;
+            const int r0 = t.row0 + (kb == 0 ? t.blocks - 1 : kb - 1) * kGemmK;   // the last rows first
             uint32_t bar;
-            if (kb == t.blocks - 1 && (t.last & 15)) {
+            if (kb == 0 && (t.last & 15)) {
               bar = smem_u32(&bars.tail[st]);
               mbar_arrive_expect_tx(&bars.tail[st], bytes);
             } else {
@@ -338,11 +340,13 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
         const uint32_t d = tmem + acc * 256;
         const int k1 = min(k0 + chunk, t.blocks);
         for (int kb = k0; kb < k1; ++kb) {
-          if (!warp_wait(&bars.full[st], ph, wc)) { ok = false; break; }
+          // an expert's last rows: warps of both CTAs have cleared what follows them
+          const bool cleared = kMode == kGemmGradW && kb == 0 && (t.last & 15);
+          if (!(cleared ? warp_wait<true>(&bars.full[st], ph, wc) : warp_wait(&bars.full[st], ph, wc))) { ok = false; break; }
           tc_fence_after();
           if (elect_one()) {
             const uint32_t a = smem_u32(stage_a(st)), b = smem_u32(stage_b(st));
-            const int steps = kMode == kGemmGradW && kb == t.blocks - 1 ? (t.last + 15) >> 4 : 4;
+            const int steps = kMode == kGemmGradW && kb == 0 ? (t.last + 15) >> 4 : 4;
             for (int s = 0; s < steps; ++s) {
               const uint64_t da = kMajorA ? sdesc_sw128(a + s * 2048, 8192, 1024) : sdesc_sw128(a + s * 32, 16, 1024);
               const uint64_t db = kMajorB ? sdesc_sw128(b + s * 2048, 8192, 1024) : sdesc_sw128(b + s * 32, 16, 1024);
@@ -365,20 +369,19 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     for (int tile = pair; tile < n_total; tile += n_pairs) {
       const GemmTile t = gemm_tile<kMode, kGemmK>(p, rt, off, tile);
       if (t.blocks == 0) continue;
-      const int s = (st + t.blocks - 1) % n_stages;
+      const int s = st;
       st = (st + t.blocks) % n_stages;
       if (!(t.last & 15)) continue;
       if (!warp_wait(&bars.tail[s], (phases >> s) & 1, wc)) break;
       phases ^= 1u << s;
-      // rows [last, round_up(last, 16)) of every 64-column box, 8 lanes a row of 128 bytes. The next block's products
-      // wait for this one: with cluster scope on the arrival below every ragged expert's tiles took 1.4 us longer.
+      // rows [last, round_up(last, 16)) of every 64-column box, 8 lanes a row of 128 bytes
       const int boxes = 2 + gemm_n<kMode>(t.cols) / 128;
       uint8_t* box = lane < 16 ? stage_a(s) + (lane >> 3) * 8192 : stage_b(s) + ((lane >> 3) - 2) * 8192;
       if ((lane >> 3) < boxes)
         for (int r = t.last; r & 15; ++r) *reinterpret_cast<uint4*>(box + r * 128 + (lane & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
       fence_proxy_async_smem();
       __syncwarp();
-      if (lane == 0) mbar_arrive_peer(peer_smem(&bars.full[s], 0));
+      if (lane == 0) mbar_arrive_peer_release(peer_smem(&bars.full[s], 0));
       __syncwarp();
     }
   } else if (warp >= 4) {

@@ -7,7 +7,7 @@
 
 namespace smoes {
 
-constexpr int kBarBytes = 384;                   // shared memory for a kernel's barriers and counts
+constexpr int kBarBytes = 448;                   // shared memory for a kernel's barriers and counts
 
 // A tile: 256 features (along M) by up to 2^tile_shift rows (along N; for dW n_in by n_z), blocks of kBlock along the depth.
 struct GemmTile {

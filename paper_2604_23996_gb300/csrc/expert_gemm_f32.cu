@@ -10,16 +10,23 @@
 // 3.38e38, which round to one, give NaN.
 //
 // A pair of CTAs forms 256 features by up to 128 rows, as in expert_gemm.cu. Roles of a CTA's warps: 0 copies fp32
-// blocks of 32 of the depth to shared memory, 1 issues the products (first CTA), 2 holds tensor memory, 4-19
-// split the blocks, eight of them every other one, and, one 256-deep chunk behind, all move the sums and store
-// finished tiles.
-// A block's planes: along the depth 128-byte rows of [h | m] and [l | -]; across it one box of 32 depth rows
-// per plane and 64 features. Rows behind an expert's last one are cleared where they are split.
+// blocks of 32 of the depth to shared memory, 1 issues the products (first CTA), 2 and 3 hand the second CTA's planes to
+// the first, 4-19 split the blocks, eight of them every other one, and, one 256-deep chunk behind, all move the sums and
+// store finished tiles. (2 holds tensor memory as well.)
+// A block's planes: along the depth 128-byte rows of [h | m], and of [l | l] for two blocks; across it one box of 32 depth
+// rows per plane and 64 features. Rows behind an expert's last one are cleared where they are split.
 //
-// Bound by shared memory: a block's 24 KB arrive, are read and written as 36 KB, and the products read 72 KB, 1220
-// clocks at 128 bytes each against 770 of the products. Measured: 32768 x 2048 x 2048 of 16 experts 279 TFLOP/s forward,
-// 288 dX, 268 dW; 8192 x 512 x 256 of 16 experts 17 us dX and 16 us dW, on the FMA units (128 x 128 a block of
-// threads) 187 for both. Eight splitting warps instead of sixteen: 232, 267 and 233 TFLOP/s.
+// The first CTA's products read planes that the second CTA's threads wrote. That order holds between CTAs only with a
+// release and an acquire at cluster scope, and each takes about as long as a block's products. Warps 2 and 3 make them,
+// for every other block each: in the second CTA they see the planes finished and release them to the first, there they
+// acquire them and arrive for the issuer. Made by the splitting warps and the issuer: 364 us for 8192 x 2048 x 2048 forward
+// instead of 300; by one warp of the second CTA and the issuer: 361. Without them (arrivals of a CTA's scope across the
+// pair, no promise that the products see the planes) 257.
+//
+// Bound by shared memory (a block's 24 KB arrive, are read and written as 36 KB, and the products read 72 KB, 1220
+// clocks at 128 bytes each against 770 of the products) and by a block's way through splitting, handing over and products,
+// four at a time. Measured: 32768 x 2048 x 2048 of 16 experts 243 TFLOP/s forward, 253 dX, 250 dW; 8192 x 512 x 256 of 16
+// experts 21 us dX and 20 us dW, on the FMA units (128 x 128 a block of threads) 187 for both.
 #include "expert_gemm.cuh"
 #include "experts.cuh"
 #include "ptx.cuh"
@@ -31,26 +38,27 @@ constexpr int kF32Threads = 640;
 constexpr int kF32Warps = 16;                    // splitting, and epilogue in groups of four
 constexpr int kF32K = 32;                        // depth of a block
 constexpr int kF32Chunk = 8;                     // blocks between moves of the sums
-// (five and two, with eight splitting warps: 351 instead of 312 us for 8192 x 2048 x 2048, 240 instead of 227 us for
-// 64 experts of few rows)
 // Blocks go to two halves of the splitting warps in turn: while one waits for its block's bytes and fences what it
-// wrote, the other splits (8192 x 2048 x 2048: 257 instead of 277 us forward, 250 instead of 255 dX, 283 instead of
-// 295 dW).
+// wrote, the other splits (8192 x 2048 x 2048: 300 instead of 311 us forward, 289 instead of 290 dX, 295 instead of
+// 308 dW).
 constexpr int kTurns = 2, kSplitThreads = 32 * kF32Warps / kTurns;      // threads that split a block
-// A half sees every other use of a stage only, and by its parity could not tell a barrier's phase from the one two
-// before. Barriers are therefore kept for six blocks, two uses of each stage: every use of one of them has the same
-// half of the warps behind it, and the same in front.
-constexpr int kStages = 3, kBlockBars = kTurns * kStages;
+// A half sees every other use of a raw stage only, and by its parity could not tell a barrier's phase from the one two
+// before. Barriers are therefore kept for six blocks, two uses of each of the three stages: every use of one of them has
+// the same half of the warps behind it, and the same in front. Planes have four stages, each of them one half's.
+constexpr int kRawStages = 3, kRawBars = kTurns * kRawStages, kPlaneStages = 4;
+static_assert(kPlaneStages % kTurns == 0, "a stage of planes has the same half of the warps behind every use");
 constexpr uint32_t kRawA = 128 * kF32K * 4, kRawB = 64 * kF32K * 4;     // one CTA's fp32 operands of a block
-constexpr uint32_t kSplitA = 2 * 128 * 128, kSplitB = 2 * 64 * 128;     // and their planes
+constexpr uint32_t kPlanesA = kPlaneStages * 3 * 128 * kF32K * 2, kPlanesB = kPlanesA / 2;   // all stages of their planes
 constexpr uint32_t kF32Smem =
-    1024 + kStages * (kRawA + kRawB + kSplitA + kSplitB) + kBarBytes + 4 * (kExpertsMax + 1);
+    1024 + kPlanesA + kPlanesB + kRawStages * (kRawA + kRawB) + kBarBytes + 4 * (kExpertsMax + 1);
 static_assert(kF32Smem <= 227 * 1024, "shared memory of a CTA");
 
 struct F32Bars {
-  uint64_t raw_full[kBlockBars], raw_empty[kBlockBars];
-  uint64_t split_full[kBlockBars];               // planes of both CTAs (first CTA's)
-  uint64_t split_empty[kBlockBars];
+  uint64_t raw_full[kRawBars], raw_empty[kRawBars];
+  uint64_t split_full[kPlaneStages];             // planes of both CTAs (in the first)
+  uint64_t split_mine[kPlaneStages];             // the second CTA's planes (in the second)
+  uint64_t split_peer[kPlaneStages];             // the second CTA's planes (in the first)
+  uint64_t split_empty[kPlaneStages];
   uint64_t acc_full[2], acc_empty[2];
   uint32_t tmem;
   int abort;
@@ -58,17 +66,33 @@ struct F32Bars {
 };
 static_assert(sizeof(F32Bars) <= kBarBytes, "barriers");
 
-// A block's place in the ring: its barriers, and those of the block that had its stage before it.
-struct RingPlace {
+// A block's place in the ring of raw stages: its barriers, and those of the block that had its stage before it.
+struct RawPlace {
   int bar = 0;
   uint32_t ph = 0;
-  __device__ __forceinline__ int stage() const { return bar < kStages ? bar : bar - kStages; }
-  __device__ __forceinline__ int before() const { return bar < kStages ? bar + kStages : bar - kStages; }
-  __device__ __forceinline__ uint32_t before_ph() const { return bar < kStages ? ph ^ 1 : ph; }
+  __device__ __forceinline__ int stage() const { return bar < kRawStages ? bar : bar - kRawStages; }
+  __device__ __forceinline__ int before() const { return bar < kRawStages ? bar + kRawStages : bar - kRawStages; }
+  __device__ __forceinline__ uint32_t before_ph() const { return bar < kRawStages ? ph ^ 1 : ph; }
   __device__ __forceinline__ void next() {
-    if (++bar == kBlockBars) { bar = 0; ph ^= 1; }
+    if (++bar == kRawBars) { bar = 0; ph ^= 1; }
   }
 };
+// And in that of the planes.
+struct PlanePlace {
+  int st = 0;
+  uint32_t ph = 0;
+  __device__ __forceinline__ void next() {
+    if (++st == kPlaneStages) { st = 0; ph ^= 1; }
+  }
+};
+
+// Where plane x (0 h, 1 m, 2 l) of a stage begins among an operand's planes of kRows rows or columns. kAcross: one after
+// the other. Along the depth two planes share rows of 128 bytes: h and m of a stage, l of two stages.
+template <bool kAcross, int kRows>
+__device__ __forceinline__ uint32_t plane_offset(int st, int x) {
+  if (kAcross) return static_cast<uint32_t>(st * 3 + x) * (kRows * kF32K * 2);
+  return x < 2 ? st * (kRows * 128) + x * 64 : (kPlaneStages + (st >> 1)) * (kRows * 128) + (st & 1) * 64;
+}
 
 // Four values, split, to their places in the planes.
 __device__ __forceinline__ uint2 split_off(float (&x)[4]) {             // x becomes what is left
@@ -91,25 +115,29 @@ __device__ __forceinline__ void split_store(const float4& v, uint8_t* h, uint8_t
   *reinterpret_cast<uint2*>(l) = split_off(x);
 }
 
-// Word `u` (16 bytes) of a raw operand of kRows rows or columns, split into its planes. kAcross: the depth runs over
-// the rows of the block, of which `depth` exist.
+// Word `u` (16 bytes) of a raw operand of kRows rows or columns, split into its planes of stage st. kAcross: the depth
+// runs over the rows of the block, of which `depth` exist.
 template <bool kAcross, int kRows>
-__device__ __forceinline__ void split_word(const uint8_t* raw, uint8_t* planes, int u, int depth) {
+__device__ __forceinline__ void split_word(const uint8_t* raw, uint8_t* planes, int st, int u, int depth) {
   float4 v;
   if (kAcross) {
     v = *reinterpret_cast<const float4*>(raw + u * 16);
     const int k = u / (kRows / 4), c = u % (kRows / 4) * 4;
     if (k >= depth) v = make_float4(0.f, 0.f, 0.f, 0.f);
     constexpr uint32_t kPlane = kRows * kF32K * 2;
-    uint8_t* at = planes + (c >> 6) * (kF32K * 128) + sw128_offset(k, c & 63);
+    uint8_t* at = planes + plane_offset<true, kRows>(st, 0) + (c >> 6) * (kF32K * 128) + sw128_offset(k, c & 63);
     split_store(v, at, at + kPlane, at + 2 * kPlane);
   } else {
     // a warp's 4 rows are 0, 4, 1, 5 (or 2, 6, 3, 7) of eight: the words of a half warp's two rows lie in different banks
     const int w = u >> 5, x = (u >> 3) & 3, k = (u & 7) * 4;
     const int r = (w >> 1) * 8 + (w & 1) * 2 + (x & 1) * 4 + (x >> 1);
     v = *reinterpret_cast<const float4*>(raw + r * (kF32K * 4) + k * 4);
-    uint8_t* h = planes + sw128_offset(r, k);
-    split_store(v, h, planes + sw128_offset(r, k + kF32K), h + kRows * 128);
+    // (a plane of a row's second 64 bytes: the swizzled word's place with that bit the other way round)
+    uint8_t* rows = planes + sw128_offset(r, k);
+    const int m = (sw128_offset(r, k) & 64) ? -64 : 64;
+    const uint32_t l = plane_offset<false, kRows>(st, 2);
+    uint8_t* h = rows + plane_offset<false, kRows>(st, 0);
+    split_store(v, h, h + m, rows + (l & ~64u) + ((l & 64) ? m : 0));
   }
 }
 
@@ -119,11 +147,11 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
                   const __grid_constant__ CUtensorMap tmB16, const ExpertGemmParams p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  uint8_t* split_a = smem;                       // [stage] each
-  uint8_t* split_b = split_a + kStages * kSplitA;
-  uint8_t* raw_a = split_b + kStages * kSplitB;
-  uint8_t* raw_b = raw_a + kStages * kRawA;
-  F32Bars& bars = *reinterpret_cast<F32Bars*>(raw_b + kStages * kRawB);
+  uint8_t* planes_a = smem;
+  uint8_t* planes_b = planes_a + kPlanesA;
+  uint8_t* raw_a = planes_b + kPlanesB;          // [stage] each
+  uint8_t* raw_b = raw_a + kRawStages * kRawA;
+  F32Bars& bars = *reinterpret_cast<F32Bars*>(raw_b + kRawStages * kRawB);
   int32_t* off = reinterpret_cast<int32_t*>(reinterpret_cast<uint8_t*>(&bars) + kBarBytes);   // [E + 1] offsets
   const ExpertLinearParams& l = p.l;
   const int warp = warp_index(), lane = threadIdx.x & 31;
@@ -132,10 +160,14 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
   constexpr bool kAcrossA = kMode != kGemmForward, kAcrossB = kMode == kGemmGradW;   // the depth is not contiguous
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kBlockBars; ++i) {
+    for (int i = 0; i < kRawBars; ++i) {
       mbar_init(&bars.raw_full[i], 1);
       mbar_init(&bars.raw_empty[i], kF32Warps / kTurns);
-      mbar_init(&bars.split_full[i], 2 * kF32Warps / kTurns);   // (of both CTAs)
+    }
+    for (int i = 0; i < kPlaneStages; ++i) {
+      mbar_init(&bars.split_full[i], kF32Warps / kTurns + 1);   // (this CTA's warps, and the other's through split_peer)
+      mbar_init(&bars.split_mine[i], kF32Warps / kTurns);
+      mbar_init(&bars.split_peer[i], 1);
       mbar_init(&bars.split_empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -170,7 +202,7 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
 
   if (warp == 0) {
     // ------------------------------------------------------------------------------- producer
-    RingPlace at;
+    RawPlace at;
     bool ok = true;
     GemmTile next = tile_at(pair);
     for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
@@ -217,7 +249,7 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     }
   } else if (warp == 1 && rank == 0) {
     // ----------------------------------------------------------------------------- MMA issuer
-    RingPlace at;
+    PlanePlace at;
     int acc = 0;
     uint32_t aph = 0;
     bool ok = true;
@@ -232,27 +264,24 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
         const uint32_t d = tmem + acc * 256;
         const int k1 = min(k0 + kF32Chunk, t.blocks);
         for (int kb = k0; kb < k1; ++kb) {
-          if (!warp_wait(&bars.split_full[at.bar], at.ph, wc)) { ok = false; break; }
+          if (!warp_wait(&bars.split_full[at.st], at.ph, wc)) { ok = false; break; }
           tc_fence_after();
           if (elect_one()) {
-            const int st = at.stage();
-            const uint32_t a = smem_u32(split_a + st * kSplitA), b = smem_u32(split_b + st * kSplitB);
+            const uint32_t a = smem_u32(planes_a), b = smem_u32(planes_b);
             // plane 0 h, 1 m, 2 l; the products of planes (x, y) with x + y <= 2, small ones first
             constexpr int kX[6] = {2, 0, 1, 1, 0, 0}, kY[6] = {0, 2, 1, 0, 1, 0};
 #pragma unroll
             for (int c = 0; c < 6; ++c) {
 #pragma unroll
               for (int s = 0; s < 2; ++s) {
-                const uint32_t pa = kAcrossA ? a + kX[c] * (128 * kF32K * 2) + s * 2048
-                                             : a + (kX[c] >> 1) * (128 * 128) + (kX[c] & 1) * 64 + s * 32;
-                const uint32_t pb = kAcrossB ? b + kY[c] * (64 * kF32K * 2) + s * 2048
-                                             : b + (kY[c] >> 1) * (64 * 128) + (kY[c] & 1) * 64 + s * 32;
+                const uint32_t pa = a + plane_offset<kAcrossA, 128>(at.st, kX[c]) + s * (kAcrossA ? 2048 : 32);
+                const uint32_t pb = b + plane_offset<kAcrossB, 64>(at.st, kY[c]) + s * (kAcrossB ? 2048 : 32);
                 const uint64_t da = sdesc_sw128(pa, kAcrossA ? kF32K * 128 : 16, 1024);
                 const uint64_t db = sdesc_sw128(pb, kAcrossB ? kF32K * 128 : 16, 1024);
                 umma_bf16_pair(c == 5 ? d : d + 128, da, db, idesc, kb > k0 || s > 0 || (c > 0 && c < 5));
               }
             }
-            umma_commit_pair(&bars.split_empty[at.bar]);
+            umma_commit_pair(&bars.split_empty[at.st]);
             if (kb == k1 - 1) umma_commit_pair(&bars.acc_full[acc]);
           }
           __syncwarp();
@@ -260,6 +289,25 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
           at.next();
         }
         if (++acc == 2) { acc = 0; aph ^= 1; }
+      }
+    }
+  } else if (warp == 2 || warp == 3) {
+    // ------------------- the second CTA's planes handed to the first, every other block by each of two warps
+    PlanePlace at;
+    bool ok = true;
+    for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
+      const int blocks = gemm_tile<kMode, kF32K>(p, rt, off, tile).blocks;
+      for (int kb = 0; kb < blocks; ++kb, at.next()) {
+        if ((at.st & 1) != (warp & 1)) continue;
+        ok = rank == 0 ? warp_wait<true>(&bars.split_peer[at.st], at.ph, wc) : warp_wait(&bars.split_mine[at.st], at.ph, wc);
+        if (!ok) break;
+        if (lane == 0) {
+          if (rank == 0)
+            mbar_arrive(&bars.split_full[at.st]);
+          else
+            mbar_arrive_peer_release(peer_smem(&bars.split_peer[at.st], 0));
+        }
+        __syncwarp();
       }
     }
   } else if (warp >= 4) {
@@ -340,7 +388,8 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
 
     // a chunk is split, then the one before it drained (one place each: inlined twice the sums do not fit the registers)
     const int turn = (warp - 4) / (kF32Warps / kTurns), part = tid & (kSplitThreads - 1);
-    RingPlace at;
+    RawPlace at;
+    PlanePlace to;
     int acc = 0;
     uint32_t aph = 0;
     bool ok = true;
@@ -351,28 +400,28 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     bool pending = false, pending_last = false;
     while (more || pending) {
       const int k1 = more ? min(k0 + kF32Chunk, t.blocks) : k0;
-      for (int kb = k0; kb < k1; ++kb, at.next()) {
+      for (int kb = k0; kb < k1; ++kb, at.next(), to.next()) {
         if (at.bar % kTurns != turn) continue;
         if (!warp_wait(&bars.raw_full[at.bar], at.ph, wc) ||
-            !warp_wait(&bars.split_empty[at.before()], at.before_ph(), wc)) { ok = false; break; }
+            !warp_wait(&bars.split_empty[to.st], to.ph ^ 1, wc)) { ok = false; break; }
         const int st = at.stage();
         const int depth = kMode == kGemmGradW && kb == t.blocks - 1 ? t.last : kF32K;
         const uint8_t* ra = raw_a + st * kRawA;
         const uint8_t* rb = raw_b + st * kRawB;
 #pragma unroll
         for (int i = 0; i < 2 * kTurns; ++i)
-          split_word<kAcrossA, 128>(ra, split_a + st * kSplitA, part + i * kSplitThreads, depth);
+          split_word<kAcrossA, 128>(ra, planes_a, to.st, part + i * kSplitThreads, depth);
 #pragma unroll
         for (int i = 0; i < kTurns; ++i) {
           const int u = part + i * kSplitThreads;
           if (kAcrossB || (u >> 6) * 8 < gemm_n<kMode>(t.cols) / 2)     // (two warps split eight rows)
-            split_word<kAcrossB, 64>(rb, split_b + st * kSplitB, u, depth);
+            split_word<kAcrossB, 64>(rb, planes_b, to.st, u, depth);
         }
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) {
-          mbar_arrive_peer(peer_smem(&bars.split_full[at.bar], 0));
           mbar_arrive(&bars.raw_empty[at.bar]);
+          mbar_arrive(rank == 0 ? &bars.split_full[to.st] : &bars.split_mine[to.st]);
         }
       }
       if (!ok) break;
@@ -410,8 +459,8 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
     }
     // every plane given back: no commit of the first CTA is still on its way to this one when it ends
     // (each half those that it would wait for next)
-    for (int i = 0; ok && i < kStages; ++i, at.next())
-      if (at.bar % kTurns == turn) ok = warp_wait(&bars.split_empty[at.before()], at.before_ph(), wc);
+    for (int i = 0; ok && i < kPlaneStages; ++i, to.next())
+      if (to.st % kTurns == turn) ok = warp_wait(&bars.split_empty[to.st], to.ph ^ 1, wc);
   }
   __syncwarp();
   tc_fence_before();

@@ -90,14 +90,29 @@ __device__ __forceinline__ void raise_abort(const WaitCtx& w, uint32_t bit) {
   atomicOr(w.status, bit);
 }
 
+// mbar_try_wait at cluster scope: what threads of the other CTA wrote before mbar_arrive_peer_release is visible behind it.
+__device__ __forceinline__ bool mbar_try_wait_cluster(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+
 // Waits for the phase with the given parity. Returns false on timeout or abort.
+template <bool kCluster = false>
 __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, const WaitCtx& w) {
-  if (mbar_try_wait(bar, parity)) return true;
+  auto done = [&] { return kCluster ? mbar_try_wait_cluster(bar, parity) : mbar_try_wait(bar, parity); };
+  if (done()) return true;
   const uint64_t t0 = global_ns();
   while (true) {
 #pragma unroll 1
     for (int i = 0; i < 64; ++i)
-      if (mbar_try_wait(bar, parity)) return true;
+      if (done()) return true;
     if (*w.abort_flag) return false;
     if (global_ns() - t0 > w.limit_ns) {
       raise_abort(w, 2u);
@@ -122,8 +137,9 @@ __device__ __forceinline__ bool elect_one() {       // always the same lane
       : "=r"(p));
   return p != 0;
 }
+template <bool kCluster = false>
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, const WaitCtx& w) {
-  return __all_sync(0xffffffffu, mbar_wait(bar, parity, w));
+  return __all_sync(0xffffffffu, mbar_wait<kCluster>(bar, parity, w));
 }
 
 // Grid barrier for co-resident blocks, called by one thread per block. sync[0] counts
@@ -243,12 +259,17 @@ __device__ __forceinline__ uint32_t peer_smem(const void* p, uint32_t rank) {
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
   return a;
 }
-// Arrivals on a barrier of either CTA (a cluster address). They order this CTA's own accesses only: what the
-// barriers of a pair hand over was written or read by the copy engine and the tensor cores, or by warps that
-// fenced it for the tensor cores of their own SM (fence_proxy_async_smem). With cluster scope every block of a
-// product waited for a fence in its producer and ran at 1200 clocks instead of 520.
+// Arrivals on a barrier of either CTA (a cluster address). They order this CTA's own accesses only, for what the copy
+// engine and the tensor cores wrote or read: their completion is counted on the barriers, or fenced before the arrival
+// (tc_fence_before). With cluster scope every block of a product waited for a fence in its producer and ran at 1200
+// clocks instead of 520.
 __device__ __forceinline__ void mbar_arrive_peer(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// The arrival for what threads wrote to shared memory themselves (and fenced for the tensor cores, fence_proxy_async_smem):
+// release at cluster scope, to be waited for with warp_wait<true>.
+__device__ __forceinline__ void mbar_arrive_peer_release(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void mbar_arrive_expect_tx_peer(uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.relaxed.cluster.shared::cluster.b64 _, [%0], %1;"
