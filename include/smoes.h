@@ -449,6 +449,11 @@ smoes_status smoes_expert_linear(smoes_experts plan, const smoes_linear_args* ar
 smoes_status smoes_expert_act_bwd(smoes_experts plan, const void* dOut, const void* pre, int n_out,
                                   int act, int gated, const int32_t* expert_offsets, void* dZ,
                                   float* db, void* ws, size_t ws_bytes, cudaStream_t stream);
+/* The same with the bias gradient accumulated: each expert's sum is added to what db (required) holds. */
+smoes_status smoes_expert_act_bwd_accumulate(smoes_experts plan, const void* dOut, const void* pre,
+                                             int n_out, int act, int gated,
+                                             const int32_t* expert_offsets, void* dZ, float* db,
+                                             void* ws, size_t ws_bytes, cudaStream_t stream);
 /* Gradients of the product: dX [R, n_in] = dZ W_e (dtype) and dW [E, n_z, n_in] float32 = sum over the
  *   expert's rows of dZ_r x_r^T, written, or accumulated into when accumulate_dW != 0 (an expert without
  *   rows: zeros, or left as it is). Either output may be NULL, and then W or X may be too. */

@@ -111,6 +111,7 @@ _sig = {
     "smoes_expert_combine_bwd": (_i, [_vp, _vp, _vp, _i, _vp, _vp, _vp, _vp, _vp, _vp]),
     "smoes_expert_linear": (_i, [_vp, C.POINTER(LinearArgs), _vp, _vp, _vp, _vp, _sz, _vp]),
     "smoes_expert_act_bwd": (_i, [_vp, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "smoes_expert_act_bwd_accumulate": (_i, [_vp, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _sz, _vp]),
     "smoes_expert_linear_bwd": (_i, [_vp, _vp, _vp, _vp, _i, _i, _vp, _vp, _vp, _i, _vp, _sz, _vp]),
     "smoes_attention_fwd": (_i, [_vp, C.POINTER(AttnArgs), _vp, _i, _vp, _vp, _vp, _sz, _vp]),
 }
@@ -580,12 +581,14 @@ class Experts:
         return out, pre
 
     def act_bwd(self, dOut, pre=None, act=SMOES_ACT_NONE, gated=False, bias_grad=False, dZ=None, db=None,
-                stream=None):
+                stream=None, accumulate=False):
         """Gradients of the pre-activations and of the bias: (dZ, db). Without an activation and not gated dZ is
-        dOut itself. db is None unless bias_grad (or a tensor to write) asks for it."""
+        dOut itself. db is None unless bias_grad (or a tensor to write) asks for it; accumulate adds to the given db."""
         n_out = dOut.shape[-1]
         n_z = 2 * n_out if gated else n_out
         dout = self._in("dOut", dOut, (self.R, n_out), self.dtype)
+        if accumulate and db is None:
+            raise ValueError("db: a tensor to accumulate into is wanted")
         if bias_grad or db is not None:
             db = self._new(db, (self.E, n_z), torch.float32, stream)
         if act == SMOES_ACT_NONE and not gated:
@@ -599,9 +602,9 @@ class Experts:
             dZ = self._new(dZ, (self.R, n_z), self.dtype, stream)
             dz = dZ.data_ptr()
         ws = self.ws
-        _check(_lib.smoes_expert_act_bwd(self.plan, dout, z, n_out, act, gated, self.expert_offsets.data_ptr(), dz,
-                                         _ptr(db), ws.data_ptr(), ws.numel(), self._stream(stream)),
-               "smoes_expert_act_bwd")
+        call = _lib.smoes_expert_act_bwd_accumulate if accumulate else _lib.smoes_expert_act_bwd
+        _check(call(self.plan, dout, z, n_out, act, gated, self.expert_offsets.data_ptr(), dz, _ptr(db), ws.data_ptr(),
+                    ws.numel(), self._stream(stream)), "smoes_expert_act_bwd")
         return dZ, db
 
     def linear_bwd(self, dZ, X, W, need_dX=True, need_dW=True, dX=None, dW=None, accumulate=False, stream=None):

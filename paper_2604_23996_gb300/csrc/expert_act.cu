@@ -159,7 +159,15 @@ __global__ void __launch_bounds__(kActThreads) k_act_bias(const ExpertActParams 
       a.z += v.z;
       a.w += v.w;
     }
-    *reinterpret_cast<float4*>(p.db + static_cast<long long>(e) * p.n_z + c) = a;
+    float4* db = reinterpret_cast<float4*>(p.db + static_cast<long long>(e) * p.n_z + c);
+    if (p.accumulate) {
+      const float4 v = *db;
+      a.x += v.x;
+      a.y += v.y;
+      a.z += v.z;
+      a.w += v.w;
+    }
+    *db = a;
   }
 }
 

@@ -64,6 +64,7 @@ struct ExpertActParams {
   const void* pre;
   void* dZ;
   float* db;
+  int accumulate;            // db is added to
   int ranges;                // row ranges: one block each and per segment of columns
   float* part;               // [ranges + E][n_z] (workspace)
 };

@@ -254,9 +254,9 @@ smoes_status smoes_expert_linear(smoes_experts P, const smoes_linear_args* args,
   return cuda_status(launch_product(P, p, kGemmForward, ws, stream));
 }
 
-smoes_status smoes_expert_act_bwd(smoes_experts P, const void* dOut, const void* pre, int n_out, int act, int gated,
-                                  const int32_t* expert_offsets, void* dZ, float* db, void* ws, size_t ws_bytes,
-                                  cudaStream_t stream) {
+static smoes_status act_bwd(smoes_experts P, const void* dOut, const void* pre, int n_out, int act, int gated,
+                            const int32_t* expert_offsets, void* dZ, float* db, bool accumulate, void* ws,
+                            size_t ws_bytes, cudaStream_t stream) {
   if (!P) return SMOES_ERR_INVALID_ARG;
   if (!known_act(act) || (gated != 0 && gated != 1)) return SMOES_ERR_INVALID_ARG;
   smoes_status st = check_ws(P, ws, ws_bytes);
@@ -269,7 +269,7 @@ smoes_status smoes_expert_act_bwd(smoes_experts P, const void* dOut, const void*
   if (plain ? (pre || dZ || !db) : false) return SMOES_ERR_INVALID_ARG;
   if (!aligned16(db)) return SMOES_ERR_ALIGNMENT;
   if (P->R == 0)
-    return db ? cuda_status(cudaMemsetAsync(db, 0, sizeof(float) * P->desc.E * n_z, stream)) : SMOES_OK;
+    return db && !accumulate ? cuda_status(cudaMemsetAsync(db, 0, sizeof(float) * P->desc.E * n_z, stream)) : SMOES_OK;
   st = check_given(dOut, expert_offsets);
   if (st == SMOES_OK && !plain) st = check_given(pre, dZ);
   if (st == SMOES_OK) st = check_aligned(dOut, pre, expert_offsets, dZ);
@@ -286,8 +286,22 @@ smoes_status smoes_expert_act_bwd(smoes_experts P, const void* dOut, const void*
   p.pre = pre;
   p.dZ = dZ;
   p.db = db;
+  p.accumulate = accumulate ? 1 : 0;
   p.part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + P->part);
   return cuda_status(launch_expert_act_bwd(p, P->desc.dtype == SMOES_BF16, P->n_sms, stream));
+}
+
+smoes_status smoes_expert_act_bwd(smoes_experts P, const void* dOut, const void* pre, int n_out, int act, int gated,
+                                  const int32_t* expert_offsets, void* dZ, float* db, void* ws, size_t ws_bytes,
+                                  cudaStream_t stream) {
+  return act_bwd(P, dOut, pre, n_out, act, gated, expert_offsets, dZ, db, false, ws, ws_bytes, stream);
+}
+
+smoes_status smoes_expert_act_bwd_accumulate(smoes_experts P, const void* dOut, const void* pre, int n_out, int act,
+                                             int gated, const int32_t* expert_offsets, void* dZ, float* db, void* ws,
+                                             size_t ws_bytes, cudaStream_t stream) {
+  if (!db) return SMOES_ERR_INVALID_ARG;
+  return act_bwd(P, dOut, pre, n_out, act, gated, expert_offsets, dZ, db, true, ws, ws_bytes, stream);
 }
 
 smoes_status smoes_expert_linear_bwd(smoes_experts P, const void* dZ, const void* X, const void* W, int n_in, int n_z,

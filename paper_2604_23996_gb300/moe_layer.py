@@ -47,14 +47,15 @@ class MoELayer:
 
     def backward(self, dY, loss_scale=1.0, accumulate=False):
         """Gradient of <dY, Y> + loss_scale * L_MI: returns dX [T, d], fills dW_gate, dW_up, dW_down (and db_up,
-        db_down)."""
+        db_down), or adds to all of them."""
         r, ex = self.router, self.experts
         X, W_gate, W_up, W_down, M, Xs, pre, H, Ys = self.saved
         dYs, d_topk_w = ex.combine_bwd(dY, Ys, r.topk_w)
         if self.biases:
-            ex.act_bwd(dYs, db=self.db_down)
+            ex.act_bwd(dYs, db=self.db_down, accumulate=accumulate)
         dH, _ = ex.linear_bwd(dYs, H, W_down, dW=self.dW_down, accumulate=accumulate)
-        dZ, _ = ex.act_bwd(dH, pre, act=bd.SMOES_ACT_SILU, gated=True, db=self.db_up)
+        dZ, _ = ex.act_bwd(dH, pre, act=bd.SMOES_ACT_SILU, gated=True, db=self.db_up,
+                           accumulate=accumulate and self.biases)
         dXs, _ = ex.linear_bwd(dZ, Xs, W_up, dW=self.dW_up, accumulate=accumulate)
         dX = torch.empty_like(X)
         r.backward(X, W_gate, M, self.dW_gate, dX=dX, loss_scale=loss_scale, d_topk_w=d_topk_w, accumulate=accumulate)

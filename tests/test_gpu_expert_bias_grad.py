@@ -56,3 +56,25 @@ def test_bias_gradient_of_a_few_rows_of_one_expert(bd, n):  # noqa: F811
     lay.n = n
     lay.ex.sort(torch.from_numpy(idx).cuda())
     check(lay, 8, 1, False)
+
+
+@pytest.mark.parametrize("act,gated", [(0, False), (1, True), (2, False)])
+def test_bias_gradient_accumulated(bd, act, gated):  # noqa: F811
+    """What db held, plus the gradient in one addition: the same bits as that addition by itself."""
+    lay = Layer(bd, 500, 12, 4, torch.bfloat16, seed=act, dropped=0.2, max_width=144)
+    n_z = 144 if gated else 72
+    dOut, z = lay.rows(72), lay.rows(n_z) if act or gated else None
+    dZ, db = lay.ex.act_bwd(dOut, z, act=act, gated=gated, bias_grad=True)
+    base = lay.normal(12, n_z, dtype=torch.float32)
+    acc = base.clone()
+    dZ2, got = lay.ex.act_bwd(dOut, z, act=act, gated=gated, db=acc, accumulate=True)
+    assert got is acc and torch.equal(acc, base + db) and torch.equal(dZ2[:lay.n], dZ[:lay.n])
+    with pytest.raises(ValueError):
+        lay.ex.act_bwd(dOut, z, act=act, gated=gated, bias_grad=True, accumulate=True)
+
+
+def test_bias_gradient_accumulated_without_tokens(bd):  # noqa: F811
+    ex = bd.Experts(0, 3, 2, max_width=64)
+    db = torch.full((3, 64), 5.0, device="cuda")
+    ex.act_bwd(torch.empty((0, 64), dtype=torch.bfloat16, device="cuda"), db=db, accumulate=True)
+    assert (db == 5).all()
