@@ -20,14 +20,23 @@ class MoELayer:
     """Router and experts of one layer for batches of ``T`` tokens.
 
     ``W_gate`` [E, d], ``W_up`` [E, 2 f, d] (g's rows, then u's) and ``W_down`` [E, d, f] are the caller's, of the
-    plan's type; ``b_up`` [E, 2 f] and ``b_down`` [E, d] float32 are optional. The gradients' buffers are kept
-    (float32), written by every backward or accumulated into.
+    plan's type; ``b_up`` [E, 2 f] and ``b_down`` [E, d] float32 are optional (``biases``: their gradients are formed).
+    The gradients' buffers are kept (float32), written by every backward or accumulated into.
+
+    ``router`` and ``experts`` hold the results of the last forward. A backward belongs to the last forward in training,
+    whatever was evaluated since, and can be repeated.
     """
+
+    # what the backward reads of the router's and the experts' own buffers, which the next forward writes again
+    _STATE = (("router", "ws"), ("router", "topk_idx"), ("router", "topk_w"), ("router", "M"),
+              ("experts", "expert_offsets"), ("experts", "row_slot"), ("experts", "slot_row"))
 
     def __init__(self, T, d, f, E, k, n_bins, sample_offsets, expert_bin, dtype=bd.SMOES_BF16, device="cuda", biases=False):
         self.router = bd.Router(T, d, E, k, n_bins, sample_offsets, expert_bin, dtype, device=device)
         self.experts = bd.Experts(T, E, k, dtype, max_width=max(2 * f, d) if biases else 0, device=device)
         self.biases = biases
+        self.saved = None                              # tensors of the last forward in training
+        self.kept = None                               # and copies of _STATE, once another forward has followed it
         new = lambda *shape: torch.zeros(shape, dtype=torch.float32, device=device)  # noqa: E731
         self.dW_gate, self.dW_up, self.dW_down = new(E, d), new(E, 2 * f, d), new(E, d, f)
         self.db_up, self.db_down = (new(E, 2 * f), new(E, d)) if biases else (None, None)
@@ -36,20 +45,43 @@ class MoELayer:
         """X [T, d] -> Y [T, d] = X + sum over the chosen experts. ``training`` keeps what the backward reads. The MI
         loss is in ``router.loss``."""
         r, ex = self.router, self.experts
+        if training:
+            self.saved = self.kept = None
+        elif self.saved is not None and self.kept is None:
+            self.kept = [getattr(getattr(self, owner), name).clone() for owner, name in self._STATE]
         r.forward(X, W_gate, M_in=M_in, mu=mu, var=var, tau=tau, bin_prob=False)
         ex.sort(r.topk_idx)
         Xs = ex.dispatch(X)
         H, pre = ex.linear(Xs, W_up, bias=b_up, act=bd.SMOES_ACT_SILU, gated=True, save_pre=training)
         Ys, _ = ex.linear(H, W_down, bias=b_down)
         if training:
-            self.saved = (X, W_gate, W_up, W_down, M_in if M_in is not None else r.M, Xs, pre, H, Ys)
+            self.saved = (X, W_gate, W_up, W_down, M_in, Xs, pre, H, Ys)
         return ex.combine(Ys, r.topk_w, residual=X)
 
     def backward(self, dY, loss_scale=1.0, accumulate=False):
-        """Gradient of <dY, Y> + loss_scale * L_MI: returns dX [T, d], fills dW_gate, dW_up, dW_down (and db_up,
-        db_down), or adds to all of them."""
+        """Gradient of <dY, Y> + loss_scale * L_MI of the last forward in training: returns dX [T, d], fills dW_gate,
+        dW_up, dW_down (and db_up, db_down), or adds to all of them."""
+        if self.saved is None:
+            raise RuntimeError("backward: no forward in training to go back through")
+        if self.kept is None:
+            return self._backward(dY, loss_scale, accumulate)
+        self._exchange()
+        try:
+            return self._backward(dY, loss_scale, accumulate)
+        finally:
+            self._exchange()
+
+    def _exchange(self):
+        """The kept buffers in the place of the present ones, or back."""
+        for i, (owner, name) in enumerate(self._STATE):
+            owner = getattr(self, owner)
+            present = getattr(owner, name)
+            setattr(owner, name, self.kept[i])
+            self.kept[i] = present
+
+    def _backward(self, dY, loss_scale, accumulate):
         r, ex = self.router, self.experts
-        X, W_gate, W_up, W_down, M, Xs, pre, H, Ys = self.saved
+        X, W_gate, W_up, W_down, M_in, Xs, pre, H, Ys = self.saved
         dYs, d_topk_w = ex.combine_bwd(dY, Ys, r.topk_w)
         if self.biases:
             ex.act_bwd(dYs, db=self.db_down, accumulate=accumulate)
@@ -58,7 +90,8 @@ class MoELayer:
                            accumulate=accumulate and self.biases)
         dXs, _ = ex.linear_bwd(dZ, Xs, W_up, dW=self.dW_up, accumulate=accumulate)
         dX = torch.empty_like(X)
-        r.backward(X, W_gate, M, self.dW_gate, dX=dX, loss_scale=loss_scale, d_topk_w=d_topk_w, accumulate=accumulate)
+        r.backward(X, W_gate, M_in if M_in is not None else r.M, self.dW_gate, dX=dX, loss_scale=loss_scale,
+                   d_topk_w=d_topk_w, accumulate=accumulate)
         # the router's part and the residual stream's join the experts'
         dX += dY
         return ex.dispatch_bwd(dXs, residual=dX)

@@ -54,3 +54,62 @@ def test_gradients_of_two_batches_add_up(dt):
     c.layer.backward(batches[1][1], accumulate=True)
     for name, got in c.gradients().items():
         assert torch.equal(got, alone[0][name] + alone[1][name]), name
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("between", [1, 3])
+def test_a_forward_between_leaves_the_backward_as_it_is(dt, between):
+    """Other tokens evaluated between a training forward and its backward: the gradients are the same bits as without."""
+    c = Case(dt)
+    X, dY = c.normal(T, d), c.normal(T, d)
+    c.forward(X)
+    want_x = c.layer.backward(dY, loss_scale=0.5)
+    want = c.gradients()
+    Y = c.forward(X)
+    for _ in range(between):
+        other = c.normal(T, d)
+        got = c.forward(other, training=False)
+        assert torch.isfinite(got).all() and not torch.equal(got, Y)
+    evaluated = c.layer.router.topk_idx.clone(), c.layer.router.loss.clone()
+    assert torch.equal(c.layer.backward(dY, loss_scale=0.5), want_x)
+    for name, got in c.gradients().items():
+        assert torch.equal(got, want[name]), name
+    # the router's results stay those of the last forward; a backward can be repeated; the next step is its own
+    assert torch.equal(c.layer.router.topk_idx, evaluated[0]) and torch.equal(c.layer.router.loss, evaluated[1])
+    assert torch.equal(c.layer.backward(dY, loss_scale=0.5), want_x)
+    again = c.forward(X)
+    assert torch.equal(again, Y) and torch.equal(c.layer.backward(dY, loss_scale=0.5), want_x)
+    assert c.layer.router.device_status()[0] == c.layer.experts.device_status() == c.bd.SMOES_OK
+
+
+def test_an_evaluation_gives_what_it_gives_alone():
+    c = Case(torch.bfloat16)
+    X, other = c.normal(T, d), c.normal(T, d)
+    want = c.forward(other, training=False)
+    c.forward(X)
+    assert torch.equal(c.forward(other, training=False), want)
+
+
+def test_the_backward_is_that_of_the_last_training_forward():
+    c = Case(torch.float32)
+    X1, X2, dY = c.normal(T, d), c.normal(T, d), c.normal(T, d)
+    c.forward(X2)
+    want = c.layer.backward(dY)
+    c.forward(X1)
+    c.forward(X1, training=False)
+    c.forward(X2)
+    assert torch.equal(c.layer.backward(dY), want)
+
+
+def test_a_backward_without_a_training_forward_is_refused():
+    c = Case(torch.bfloat16)
+    dY = c.normal(T, d)
+    with pytest.raises(RuntimeError):
+        c.layer.backward(dY)
+    c.forward(c.normal(T, d), training=False)
+    with pytest.raises(RuntimeError):
+        c.layer.backward(dY)
+    with pytest.raises(c.bd.SmoesError):
+        c.forward(None)
+    with pytest.raises(RuntimeError):
+        c.layer.backward(dY)
