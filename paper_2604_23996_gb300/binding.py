@@ -458,19 +458,25 @@ class Experts:
     expert and one selection (``E = k = 1``) is a dense layer and needs no sort. Tensors are contiguous, of the
     plan's type (weights of the top-k, biases and their gradients float32) and on the plan's device; a tensor
     that is not raises a ValueError before anything is launched. Results are new tensors unless an output is given.
-    Calls run on the stream given, or the current one of the plan's device; calls of one layer share its workspace, so
-    those on different streams are the caller's to order. The methods call the library themselves:
-    a decoding step's calls are bound by their time on the host.
+    The plan's device is the current one when the layer is made, and has to be the current one at every call (a
+    ValueError otherwise: the library's launches go to the current device). Calls run on the stream given, or the
+    current one; calls of one layer share its workspace, so those on different streams are the caller's to order. The
+    methods call the library themselves: a decoding step's calls are bound by their time on the host.
     """
 
     def __init__(self, T, E, k, dtype=SMOES_BF16, max_width=0, device="cuda"):
+        self.plan = None
+        device = torch.device(device)
+        if device.type != "cuda":
+            raise ValueError(f"device: a GPU is wanted, got {device}")
+        self._index = torch.cuda.current_device() if device.index is None else device.index
+        self.check_device()
         code, self.plan = smoes_experts_create(T, E, k, dtype, max_width)
         _check(code, "smoes_experts_create")
         self.T, self.E, self.k, self.R = T, E, k, T * k
         self.dtype = torch.bfloat16 if dtype == SMOES_BF16 else torch.float32
         self.ws = torch.empty(smoes_experts_workspace_bytes(self.plan), dtype=torch.uint8, device=device)
         self.device = self.ws.device
-        self._index = self.device.index
         _check(smoes_experts_workspace_init(self.plan, self.ws), "smoes_experts_workspace_init")
         self.expert_offsets = torch.zeros(E + 1, dtype=torch.int32, device=device)
         self.row_slot = torch.full((self.R,), -1, dtype=torch.int32, device=device)
@@ -486,8 +492,20 @@ class Experts:
         except Exception:
             pass
 
+    def check_device(self):
+        """A ValueError if the plan's device is not the current one."""
+        current = torch._C._cuda_getDevice()
+        if current != self._index:
+            raise ValueError(f"device: the layer is on cuda:{self._index}, the current device is cuda:{current}")
+
     def _stream(self, stream):
-        return torch._C._cuda_getCurrentRawStream(self._index) if stream is None else stream.cuda_stream
+        """The handle of the stream that a call is about to be launched on."""
+        self.check_device()
+        if stream is None:
+            return torch._C._cuda_getCurrentRawStream(self._index)
+        if stream.device_index != self._index:
+            raise ValueError(f"stream: one of cuda:{self._index} is wanted, got one of cuda:{stream.device_index}")
+        return stream.cuda_stream
 
     def _in(self, name, t, shape, dtype):
         """Address of one checked argument; None stays None."""
@@ -624,6 +642,4 @@ class Experts:
         return dX, dW
 
     def device_status(self, stream=None):
-        if stream is None:
-            stream = torch.cuda.current_stream(self._index)
-        return smoes_experts_read_status(self.plan, self.ws, stream)
+        return _lib.smoes_experts_read_status(self.plan, self.ws.data_ptr(), self._stream(stream))

@@ -32,8 +32,8 @@ class MoELayer:
               ("experts", "expert_offsets"), ("experts", "row_slot"), ("experts", "slot_row"))
 
     def __init__(self, T, d, f, E, k, n_bins, sample_offsets, expert_bin, dtype=bd.SMOES_BF16, device="cuda", biases=False):
-        self.router = bd.Router(T, d, E, k, n_bins, sample_offsets, expert_bin, dtype, device=device)
         self.experts = bd.Experts(T, E, k, dtype, max_width=max(2 * f, d) if biases else 0, device=device)
+        self.router = bd.Router(T, d, E, k, n_bins, sample_offsets, expert_bin, dtype, device=device)
         self.biases = biases
         self.saved = None                              # tensors of the last forward in training
         self.kept = None                               # and copies of _STATE, once another forward has followed it
@@ -45,6 +45,7 @@ class MoELayer:
         """X [T, d] -> Y [T, d] = X + sum over the chosen experts. ``training`` keeps what the backward reads. The MI
         loss is in ``router.loss``."""
         r, ex = self.router, self.experts
+        ex.check_device()
         if training:
             self.saved = self.kept = None
         elif self.saved is not None and self.kept is None:
