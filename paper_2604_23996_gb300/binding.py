@@ -601,10 +601,13 @@ class Experts:
     def act_bwd(self, dOut, pre=None, act=SMOES_ACT_NONE, gated=False, bias_grad=False, dZ=None, db=None,
                 stream=None, accumulate=False):
         """Gradients of the pre-activations and of the bias: (dZ, db). Without an activation and not gated dZ is
-        dOut itself. db is None unless bias_grad (or a tensor to write) asks for it; accumulate adds to the given db."""
+        dOut itself (and not given). db is None unless bias_grad (or a tensor to write) asks for it; accumulate adds to
+        the given db."""
         n_out = dOut.shape[-1]
         n_z = 2 * n_out if gated else n_out
         dout = self._in("dOut", dOut, (self.R, n_out), self.dtype)
+        if dZ is not None and act == SMOES_ACT_NONE and not gated:
+            raise ValueError("dZ: without an activation and not gated it is dOut, and none is written")
         if accumulate and db is None:
             raise ValueError("db: a tensor to accumulate into is wanted")
         if bias_grad or db is not None:
