@@ -286,8 +286,8 @@ def smoes_adaptive_bins(plan, expert_counts, beta, C_bar, expert_bin, f_spec=Non
                                     _p(f_spec), _stream(stream))
 
 
-# The expert layer's calls take addresses as plain integers (a layer of a few tokens takes less time on the
-# GPU than the marshalling of its arguments).
+# The expert layer's calls are made by ``Experts``, with addresses as plain integers (a layer of a few tokens takes less
+# time on the GPU than the marshalling of its arguments). What a plan needs besides:
 
 def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
@@ -319,53 +319,6 @@ def smoes_experts_workspace_init(plan, ws, stream=None) -> int:
 
 def smoes_experts_set_wait_limit(plan, limit_ns: int) -> int:
     return _lib.smoes_experts_set_wait_limit(plan, int(limit_ns))
-
-
-def smoes_experts_read_status(plan, ws, stream=None) -> int:
-    return _lib.smoes_experts_read_status(plan, _ptr(ws), _raw(stream))
-
-
-def smoes_expert_sort(plan, topk_idx, expert_offsets, row_slot, slot_row, ws, stream=None) -> int:
-    return _lib.smoes_expert_sort(plan, _ptr(topk_idx), _ptr(expert_offsets), _ptr(row_slot), _ptr(slot_row),
-                                  _ptr(ws), ws.numel() * ws.element_size(), _raw(stream))
-
-
-def smoes_expert_dispatch(plan, X, d, expert_offsets, slot_row, Xs, stream=None) -> int:
-    return _lib.smoes_expert_dispatch(plan, _ptr(X), int(d), _ptr(expert_offsets), _ptr(slot_row), _ptr(Xs),
-                                      _raw(stream))
-
-
-def smoes_expert_dispatch_bwd(plan, dXs, d, slot_row, residual, dX, stream=None) -> int:
-    return _lib.smoes_expert_dispatch_bwd(plan, _ptr(dXs), int(d), _ptr(slot_row), _ptr(residual), _ptr(dX),
-                                          _raw(stream))
-
-
-def smoes_expert_combine(plan, Ys, d, topk_w, slot_row, residual, Y, stream=None) -> int:
-    return _lib.smoes_expert_combine(plan, _ptr(Ys), int(d), _ptr(topk_w), _ptr(slot_row), _ptr(residual), _ptr(Y),
-                                     _raw(stream))
-
-
-def smoes_expert_combine_bwd(plan, dY, Ys, d, topk_w, expert_offsets, slot_row, dYs, d_topk_w, stream=None) -> int:
-    return _lib.smoes_expert_combine_bwd(plan, _ptr(dY), _ptr(Ys), int(d), _ptr(topk_w), _ptr(expert_offsets), _ptr(slot_row),
-                                         _ptr(dYs), _ptr(d_topk_w), _raw(stream))
-
-
-def smoes_expert_linear(plan, X, W, bias, residual, n_in, n_out, act, gated, expert_offsets, out, pre, ws,
-                        stream=None) -> int:
-    args = LinearArgs(_ptr(X), _ptr(W), _ptr(bias), _ptr(residual), int(n_in), int(n_out), int(act), int(gated))
-    return _lib.smoes_expert_linear(plan, C.byref(args), _ptr(expert_offsets), _ptr(out), _ptr(pre), _ptr(ws),
-                                    ws.numel() * ws.element_size(), _raw(stream))
-
-
-def smoes_expert_act_bwd(plan, dOut, pre, n_out, act, gated, expert_offsets, dZ, db, ws, stream=None) -> int:
-    return _lib.smoes_expert_act_bwd(plan, _ptr(dOut), _ptr(pre), int(n_out), int(act), int(gated), _ptr(expert_offsets),
-                                     _ptr(dZ), _ptr(db), _ptr(ws), ws.numel() * ws.element_size(), _raw(stream))
-
-
-def smoes_expert_linear_bwd(plan, dZ, X, W, n_in, n_z, expert_offsets, dX, dW, accumulate_dW, ws, stream=None) -> int:
-    return _lib.smoes_expert_linear_bwd(plan, _ptr(dZ), _ptr(X), _ptr(W), int(n_in), int(n_z), _ptr(expert_offsets), _ptr(dX),
-                                        _ptr(dW), int(accumulate_dW), _ptr(ws), ws.numel() * ws.element_size(),
-                                        _raw(stream))
 
 
 # ----------------------------------------------------------------------------- convenience
