@@ -358,12 +358,14 @@ smoes_status smoes_bin_permute_noalloc(smoes_plan plan, const int32_t* topk_idx,
  * from expert_offsets[E] to R belong to no expert, and every call that writes rows writes zeros
  * there. Offsets and maps that were not made by smoes_expert_sort are kept inside [0, R] by the
  * kernels. The conventions at the head of this file hold: dense row-major device arrays, 16-byte
- * aligned, asynchronous on the given stream, nothing allocated. Outputs do not overlap inputs.
+ * aligned, asynchronous on the given stream, nothing allocated. Outputs do not overlap inputs. Calls run on
+ * the current device, which is the one that was current when the plan was created.
  * Widths are multiples of 8 on SMOES_BF16 plans and of 4 on SMOES_F32 plans (rows of whole 16-byte
  * words), at most 2^20. "dtype" below is the plan's type; everything is summed in float32. Rows and weights of
  * other experts do not reach an expert's results, whatever they hold. On SMOES_F32 plans the products
  * of (11) are formed on the tensor cores from three bf16 parts of each value, to float32 accuracy; an
- * infinity, or a magnitude above 3.38e38, in X, W or dZ gives NaN there. */
+ * infinity, or a magnitude above 3.38e38, in X, W or dZ gives NaN there, and of magnitudes below 2^-107
+ * what falls below 2^-133 is lost. */
 typedef struct smoes_experts_s* smoes_experts;
 
 /* T tokens (0..2^20), E experts (1..256), k selections a token (1..16). E = k = 1 is a dense layer,

@@ -8,8 +8,8 @@
 // both only go up along the rows, so range + expert numbers the partials without gaps to search. No range is empty: the
 // second kernel adds every partial between an expert's first range and its last.
 //
-// Bound by HBM and by issue slots in about equal parts. A block per 32 rows, with the activation chosen at run time:
-// 57-61 us for 30035 x 704 gated (floor 31).
+// Bound by HBM and by issue slots in about equal parts. 30035 x 704 gated: 40 us in bf16 (floor 31; a block per 32 rows, with
+// the activation chosen at run time, 57-61), 74 in fp32 with CUDA's accurate functions (floor 62).
 #include "experts.cuh"
 #include "ptx.cuh"
 

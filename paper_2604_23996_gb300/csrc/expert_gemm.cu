@@ -25,8 +25,8 @@
 // experts with silu and pre 134 instead of 107 us). Two accumulators of 256 columns: the epilogue of a tile runs
 // under the next tile's products.
 //
-// Measured, equal experts, before the power limit sets in: 98304 x 2048 x 2048 of 64 experts 442 us forward and dX
-// (1.87 PFLOP/s), 500 dW (which writes 1.07 GB), 16384 x 8192 x 2048 282 us (1.95 PFLOP/s). A layer of this size runs
+// Measured, equal experts, before the power limit sets in: 98304 x 2048 x 2048 of 64 experts 447 us forward and dX
+// (1.84 PFLOP/s), 520 dW (which writes 1.07 GB), 16384 x 8192 x 2048 282 us (1.95 PFLOP/s). A layer of this size runs
 // at the power limit: the same calls back to back take 10 to 15% longer. Otherwise bound by the products; small depths
 // (n_in below 500 or so) by the epilogue, few rows by the weights' bytes.
 #include "expert_gemm.cuh"
