@@ -464,6 +464,38 @@ smoes_status smoes_expert_linear_bwd(smoes_experts plan, const void* dZ, const v
                                      float* dW, int accumulate_dW, void* ws, size_t ws_bytes,
                                      cudaStream_t stream);
 
+/* -------------------------------------------------------------------------------- layer norm
+ * (12) The norm in front of the router and the experts, with the residual stream's sum:
+ *     s = X + residual,  mean = sum_j s_j / d,  rstd = 1 / sqrt(sum_j (s_j - mean)^2 / d + eps),
+ *     Y = (s - mean) rstd w + b.
+ * The conventions at the head of this file hold. A plan (smoes_norm) has T tokens (0..2^20) of d features
+ * (d % 8 == 0, at most 16384 of SMOES_BF16 and 8192 of SMOES_F32), and eps >= 0. Outputs do not overlap inputs. */
+typedef struct smoes_norm_s* smoes_norm;
+typedef struct {
+  int T, d;
+  smoes_dtype dtype;                   /* X, residual, S, Y, dY and dX                             */
+  float eps;
+} smoes_norm_desc;
+
+smoes_status smoes_norm_create(const smoes_norm_desc* desc, smoes_norm* out);
+void smoes_norm_destroy(smoes_norm plan);
+/* Workspace of smoes_norm_bwd's sums over the tokens; needs no initialisation, holds nothing between calls. */
+size_t smoes_norm_workspace_bytes(smoes_norm plan);
+/*   X, residual [T, d]; residual and S (both or neither): S [T, d] = X + residual, rounded to dtype, and the norm is
+ *   of the rounded sum. w [d] float32, b [d] float32 or NULL. mean, rstd [T] float32, or NULL for both. */
+smoes_status smoes_norm_fwd(smoes_norm plan, const void* X, const void* residual, const float* w,
+                            const float* b, void* S, void* Y, float* mean, float* rstd,
+                            cudaStream_t stream);
+/* Gradients. S: what was normed (the forward's S, or X without a residual), with its mean and rstd.
+ *   dX [T, d] = residual + the gradient of <dY, Y> by S (residual [T, d]: the gradient that reached the stream another
+ *   way, or NULL); dX is the gradient of X and of the forward's residual alike. dw [d], db [d] float32: sums over the
+ *   tokens in a fixed order (bitwise reproducible), written, or added to when accumulate != 0; each may be NULL, and
+ *   ws too without both. */
+smoes_status smoes_norm_bwd(smoes_norm plan, const void* dY, const void* S, const float* mean,
+                            const float* rstd, const float* w, const void* residual, void* dX,
+                            float* dw, float* db, int accumulate, void* ws, size_t ws_bytes,
+                            cudaStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

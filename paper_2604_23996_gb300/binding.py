@@ -75,6 +75,10 @@ class LinearArgs(C.Structure):
                 ("n_in", C.c_int), ("n_out", C.c_int), ("act", C.c_int), ("gated", C.c_int)]
 
 
+class NormDesc(C.Structure):
+    _fields_ = [("T", C.c_int), ("d", C.c_int), ("dtype", C.c_int), ("eps", C.c_float)]
+
+
 _vp, _i, _f, _sz = C.c_void_p, C.c_int, C.c_float, C.c_size_t
 _sig = {
     "smoes_plan_create": (_i, [C.POINTER(RouterDesc), C.POINTER(_vp)]),
@@ -113,6 +117,11 @@ _sig = {
     "smoes_expert_act_bwd": (_i, [_vp, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _sz, _vp]),
     "smoes_expert_act_bwd_accumulate": (_i, [_vp, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _sz, _vp]),
     "smoes_expert_linear_bwd": (_i, [_vp, _vp, _vp, _vp, _i, _i, _vp, _vp, _vp, _i, _vp, _sz, _vp]),
+    "smoes_norm_create": (_i, [C.POINTER(NormDesc), C.POINTER(_vp)]),
+    "smoes_norm_destroy": (None, [_vp]),
+    "smoes_norm_workspace_bytes": (_sz, [_vp]),
+    "smoes_norm_fwd": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "smoes_norm_bwd": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _vp, _sz, _vp]),
     "smoes_attention_fwd": (_i, [_vp, C.POINTER(AttnArgs), _vp, _i, _vp, _vp, _vp, _sz, _vp]),
 }
 for _name, (_res, _args) in _sig.items():
@@ -404,52 +413,25 @@ class Router:
         return code, n_absent
 
 
-class Experts:
-    """The expert layer behind a router: one plan, its workspace and the maps of its last ``sort``.
+class _Calls:
+    """Checked arguments, outputs and streams of a plan that belongs to one device (``_index``, ``device``)."""
 
-    ``T`` tokens of ``k`` selections over ``E`` experts give ``R = T * k`` rows in expert order. A layer of one
-    expert and one selection (``E = k = 1``) is a dense layer and needs no sort. Tensors are contiguous, of the
-    plan's type (weights of the top-k, biases and their gradients float32) and on the plan's device; a tensor
-    that is not raises a ValueError before anything is launched. Results are new tensors unless an output is given.
-    The plan's device is the current one when the layer is made, and has to be the current one at every call (a
-    ValueError otherwise: the library's launches go to the current device). Calls run on the stream given, or the
-    current one; calls of one layer share its workspace, so those on different streams are the caller's to order. The
-    methods call the library themselves: a decoding step's calls are bound by their time on the host.
-    """
+    _what = "layer"
 
-    def __init__(self, T, E, k, dtype=SMOES_BF16, max_width=0, device="cuda"):
-        self.plan = None
+    def _on(self, device):
+        """Takes the device of the constructor: a GPU, the current one."""
         device = torch.device(device)
         if device.type != "cuda":
             raise ValueError(f"device: a GPU is wanted, got {device}")
         self._index = torch.cuda.current_device() if device.index is None else device.index
         self.check_device()
-        code, self.plan = smoes_experts_create(T, E, k, dtype, max_width)
-        _check(code, "smoes_experts_create")
-        self.T, self.E, self.k, self.R = T, E, k, T * k
-        self.dtype = torch.bfloat16 if dtype == SMOES_BF16 else torch.float32
-        self.ws = torch.empty(smoes_experts_workspace_bytes(self.plan), dtype=torch.uint8, device=device)
-        self.device = self.ws.device
-        _check(smoes_experts_workspace_init(self.plan, self.ws), "smoes_experts_workspace_init")
-        self.expert_offsets = torch.zeros(E + 1, dtype=torch.int32, device=device)
-        self.row_slot = torch.full((self.R,), -1, dtype=torch.int32, device=device)
-        self.slot_row = torch.full((T, k), -1, dtype=torch.int32, device=device)
-        if E == 1 and k == 1:                          # every token is a row of the one expert
-            self.expert_offsets[1:].fill_(T)
-            torch.arange(T, out=self.row_slot)
-            torch.arange(T, out=self.slot_row.view(-1))
-
-    def __del__(self):
-        try:
-            smoes_experts_destroy(self.plan)
-        except Exception:
-            pass
+        return device
 
     def check_device(self):
         """A ValueError if the plan's device is not the current one."""
         current = torch._C._cuda_getDevice()
         if current != self._index:
-            raise ValueError(f"device: the layer is on cuda:{self._index}, the current device is cuda:{current}")
+            raise ValueError(f"device: the {self._what} is on cuda:{self._index}, the current device is cuda:{current}")
 
     def _stream(self, stream):
         """The handle of the stream that a call is about to be launched on."""
@@ -478,6 +460,44 @@ class Experts:
                 return torch.empty(shape, dtype=dtype, device=self.device)
         self._in("output", t, shape, dtype)
         return t
+
+
+class Experts(_Calls):
+    """The expert layer behind a router: one plan, its workspace and the maps of its last ``sort``.
+
+    ``T`` tokens of ``k`` selections over ``E`` experts give ``R = T * k`` rows in expert order. A layer of one
+    expert and one selection (``E = k = 1``) is a dense layer and needs no sort. Tensors are contiguous, of the
+    plan's type (weights of the top-k, biases and their gradients float32) and on the plan's device; a tensor
+    that is not raises a ValueError before anything is launched. Results are new tensors unless an output is given.
+    The plan's device is the current one when the layer is made, and has to be the current one at every call (a
+    ValueError otherwise: the library's launches go to the current device). Calls run on the stream given, or the
+    current one; calls of one layer share its workspace, so those on different streams are the caller's to order. The
+    methods call the library themselves: a decoding step's calls are bound by their time on the host.
+    """
+
+    def __init__(self, T, E, k, dtype=SMOES_BF16, max_width=0, device="cuda"):
+        self.plan = None
+        device = self._on(device)
+        code, self.plan = smoes_experts_create(T, E, k, dtype, max_width)
+        _check(code, "smoes_experts_create")
+        self.T, self.E, self.k, self.R = T, E, k, T * k
+        self.dtype = torch.bfloat16 if dtype == SMOES_BF16 else torch.float32
+        self.ws = torch.empty(smoes_experts_workspace_bytes(self.plan), dtype=torch.uint8, device=device)
+        self.device = self.ws.device
+        _check(smoes_experts_workspace_init(self.plan, self.ws), "smoes_experts_workspace_init")
+        self.expert_offsets = torch.zeros(E + 1, dtype=torch.int32, device=device)
+        self.row_slot = torch.full((self.R,), -1, dtype=torch.int32, device=device)
+        self.slot_row = torch.full((T, k), -1, dtype=torch.int32, device=device)
+        if E == 1 and k == 1:                          # every token is a row of the one expert
+            self.expert_offsets[1:].fill_(T)
+            torch.arange(T, out=self.row_slot)
+            torch.arange(T, out=self.slot_row.view(-1))
+
+    def __del__(self):
+        try:
+            smoes_experts_destroy(self.plan)
+        except Exception:
+            pass
 
     def sort(self, topk_idx, stream=None):
         """Selections [T, k] int32 (negative: takes no part) into expert order; fills and returns
@@ -599,3 +619,69 @@ class Experts:
 
     def device_status(self, stream=None):
         return _lib.smoes_experts_read_status(self.plan, self.ws.data_ptr(), self._stream(stream))
+
+
+class LayerNorm(_Calls):
+    """The layer norm in front of a router and its experts, for batches of ``T`` tokens of ``d`` features.
+
+    Tensors are contiguous, of the plan's type (weight, bias, statistics and their gradients float32) and on the plan's
+    device, which has to be the current one at every call, as for ``Experts``. Nothing is kept from one call for the
+    next: the backward is given what the forward returned. Backwards on different streams share the workspace, and are
+    the caller's to order.
+    """
+
+    _what = "norm"
+
+    def __init__(self, T, d, dtype=SMOES_BF16, eps=1e-5, device="cuda"):
+        self.plan = None
+        device = self._on(device)
+        plan = C.c_void_p()
+        _check(_lib.smoes_norm_create(NormDesc(T, d, dtype, eps), plan), "smoes_norm_create")
+        self.plan = plan
+        self.T, self.d = T, d
+        self.dtype = torch.bfloat16 if dtype == SMOES_BF16 else torch.float32
+        self.ws = torch.empty(_lib.smoes_norm_workspace_bytes(plan), dtype=torch.uint8, device=device)
+        self.device = self.ws.device
+
+    def __del__(self):
+        try:
+            _lib.smoes_norm_destroy(self.plan)
+        except Exception:
+            pass
+
+    def forward(self, X, w, b=None, residual=None, stats=True, out=None, sum_out=None, stream=None):
+        """Norm of X [T, d], or of the residual stream S = X + residual: returns (Y, S, mean, rstd), what ``backward``
+        reads. S is X without a residual; mean and rstd [T] are None without ``stats``."""
+        shape, dt, f32 = (self.T, self.d), self.dtype, torch.float32
+        x, r = self._in("X", X, shape, dt), self._in("residual", residual, shape, dt)
+        wp, bp = self._in("w", w, (self.d,), f32), self._in("b", b, (self.d,), f32)
+        raw = self._stream(stream)
+        if residual is None and sum_out is not None:
+            raise ValueError("sum_out: without a residual the sum is X, and none is written")
+        S = X if residual is None else self._new(sum_out, shape, dt, stream)
+        out = self._new(out, shape, dt, stream)
+        mean = rstd = None
+        if stats:
+            both = self._new(None, (2, (self.T + 3) // 4 * 4), f32, stream)
+            mean, rstd = both[0, :self.T], both[1, :self.T]
+        _check(_lib.smoes_norm_fwd(self.plan, x, r, wp, bp, None if residual is None else S.data_ptr(), out.data_ptr(),
+                                   _ptr(mean), _ptr(rstd), raw), "smoes_norm_fwd")
+        return out, S, mean, rstd
+
+    def backward(self, dY, S, mean, rstd, w, residual=None, need_dw=True, need_db=True, dX=None, dw=None, db=None,
+                 accumulate=False, stream=None):
+        """(dX, dw, db) from the forward's S, mean and rstd; ``residual`` [T, d], the stream's own gradient, joins dX.
+        accumulate adds to the dw and db that are given."""
+        shape, dt, f32 = (self.T, self.d), self.dtype, torch.float32
+        dy, s, r = self._in("dY", dY, shape, dt), self._in("S", S, shape, dt), self._in("residual", residual, shape, dt)
+        m, q = self._in("mean", mean, (self.T,), f32), self._in("rstd", rstd, (self.T,), f32)
+        wp = self._in("w", w, (self.d,), f32)
+        raw = self._stream(stream)
+        if accumulate and ((need_dw and dw is None) or (need_db and db is None)):
+            raise ValueError("dw, db: tensors to accumulate into are wanted")
+        dX = self._new(dX, shape, dt, stream)
+        dw = self._new(dw, (self.d,), f32, stream) if need_dw else None
+        db = self._new(db, (self.d,), f32, stream) if need_db else None
+        _check(_lib.smoes_norm_bwd(self.plan, dy, s, m, q, wp, r, dX.data_ptr(), _ptr(dw), _ptr(db), accumulate,
+                                   self.ws.data_ptr(), self.ws.numel(), raw), "smoes_norm_bwd")
+        return dX, dw, db
