@@ -277,6 +277,26 @@ smoes_status smoes_bin_balance(smoes_plan plan, const int32_t* topk_idx, float l
                                float* loss_bal, float* f_e, float* P_e, void* ws, size_t ws_bytes,
                                cudaStream_t stream);
 
+/* (7b) Expert-level load-balance loss of the last forward on ws, per sample (per_sample = 1, B samples) or over the
+ *   batch (0, B = 1), the usual companion of a top-k router (the paper balances bins, (7)):
+ *     L = 1/B sum_s sum_e f_se P_se,  f_se = E C_se / sum_e' C_se',  P_se = 1/n_s sum_j g_je,
+ *   over the n_s tokens j of sample s that select anything: C_se of their selections are of expert e, g is the dense
+ *   gate (softmax, or s / sum s of a SMOES_GATE_SIGMOID plan). topk_idx [T, k]: the forward's, in which selections may
+ *   be set to a negative number (dropped ones, padding tokens), as for smoes_expert_sort; they and those >= E are not
+ *   counted, and a sample without any adds nothing. loss [1] float32 = L; counts [B, E] int32 = C or NULL; d_gate
+ *   [B, E] float32 or NULL = the gradient of loss_scale * L by g_je (f constant), the same for all n_s tokens of a
+ *   sample, for smoes_router_bwd_gates. Sums are fp32 in a fixed order (bitwise reproducible). */
+smoes_status smoes_expert_balance(smoes_plan plan, const int32_t* topk_idx, int per_sample, float loss_scale,
+                                  float* loss, int32_t* counts, float* d_gate, void* ws, size_t ws_bytes,
+                                  cudaStream_t stream);
+/* smoes_router_bwd with a gradient of the gate values besides: d_gate [n_samples, E] float32, the same for all tokens of
+ *   a sample (per_sample = 1), or [E], for all tokens (0); NULL for none. It reaches the tokens that have a selection in
+ *   [0, E) in topk_idx, as smoes_expert_balance counts them. */
+smoes_status smoes_router_bwd_gates(smoes_plan plan, const void* X, const void* W, const float* M,
+                                    const int32_t* topk_idx, const float* d_topk_w, const float* d_gate,
+                                    int per_sample, float loss_scale, float* dW, int accumulate_dW, void* dX,
+                                    float* dlogits, void* ws, size_t ws_bytes, cudaStream_t stream);
+
 /* (4) Bin-grouped permutation with de-duplicated dispatch (Sec. 4.5, "DeDup").
  *   One entry per unique (token, bin) pair, ordered by bin ascending then token ascending.
  *   topk_idx [T, k] int32 in [0, E). home [T] int32 in [0, n_bins) or NULL for the contiguous

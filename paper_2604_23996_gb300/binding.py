@@ -96,6 +96,8 @@ _sig = {
                                       _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz,
                                       _vp]),
     "smoes_router_bwd": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _f, _vp, _i, _vp, _vp, _vp, _sz, _vp]),
+    "smoes_router_bwd_gates": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _f, _vp, _i, _vp, _vp, _vp, _sz, _vp]),
+    "smoes_expert_balance": (_i, [_vp, _vp, _i, _f, _vp, _vp, _vp, _vp, _sz, _vp]),
     "smoes_bin_permute": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
     "smoes_bin_permute_noalloc": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
     "smoes_gaussian_stats_update": (_i, [_vp, _vp, _vp, C.c_double, _vp, _vp, _vp, _vp, _vp, _vp,
@@ -249,6 +251,19 @@ def smoes_router_bwd(plan, X, W, M, topk_idx, d_topk_w, loss_scale, dW, accumula
                                  _stream(stream))
 
 
+def smoes_router_bwd_gates(plan, X, W, M, topk_idx, d_topk_w, d_gate, per_sample, loss_scale, dW, accumulate_dW, dX,
+                           dlogits, ws, stream=None) -> int:
+    """smoes_router_bwd with a gradient of the gate values, [n_samples, E] (per_sample) or [1, E]."""
+    return _lib.smoes_router_bwd_gates(plan, _p(X), _p(W), _p(M), _p(topk_idx), _p(d_topk_w), _p(d_gate),
+                                       int(per_sample), float(loss_scale), _p(dW), int(accumulate_dW), _p(dX),
+                                       _p(dlogits), _p(ws), ws.numel() * ws.element_size(), _stream(stream))
+
+
+def smoes_expert_balance(plan, topk_idx, per_sample, loss_scale, loss, counts, d_gate, ws, stream=None) -> int:
+    return _lib.smoes_expert_balance(plan, _p(topk_idx), int(per_sample), float(loss_scale), _p(loss), _p(counts),
+                                     _p(d_gate), _p(ws), ws.numel() * ws.element_size(), _stream(stream))
+
+
 def smoes_bin_permute(plan, topk_idx, home, is_vision, bin_offsets, perm_token, perm_mask,
                       dispatch, expert_counts, ws, stream=None) -> int:
     return _lib.smoes_bin_permute(plan, _p(topk_idx), _p(home), _p(is_vision), _p(bin_offsets),
@@ -392,10 +407,47 @@ class Router:
         _check(code, "smoes_router_fwd_permute")
 
     def backward(self, X, W, M, dW, dX=None, dlogits=None, loss_scale=1.0, d_topk_w=None,
-                 accumulate=False, stream=None):
-        code = smoes_router_bwd(self.plan, X, W, M, self.topk_idx, d_topk_w, loss_scale, dW,
-                                accumulate, dX, dlogits, self.ws, stream)
-        _check(code, "smoes_router_bwd")
+                 accumulate=False, stream=None, d_gate=None, topk_idx=None):
+        """d_gate: what ``expert_balance`` returned, [B, E] or [1, E]; topk_idx: the forward's with dropped selections."""
+        idx = self.topk_idx if topk_idx is None else topk_idx
+        if d_gate is None:
+            code = smoes_router_bwd(self.plan, X, W, M, idx, d_topk_w, loss_scale, dW,
+                                    accumulate, dX, dlogits, self.ws, stream)
+            _check(code, "smoes_router_bwd")
+            return
+        self._table("d_gate", d_gate, torch.float32, d_gate.shape[0] if d_gate.dim() == 2 else -1)
+        self._table("topk_idx", idx, torch.int32, self.T, self.k)
+        code = smoes_router_bwd_gates(self.plan, X, W, M, idx, d_topk_w, d_gate, self.B != 1 and len(d_gate) == self.B,
+                                      loss_scale, dW, accumulate, dX, dlogits, self.ws, stream)
+        _check(code, "smoes_router_bwd_gates")
+
+    def _table(self, name, t, dtype, rows, cols=None):
+        """A ValueError if t is not a contiguous [rows, cols] tensor of this type (cols: E; rows of experts: 1 or B)."""
+        wrong = cols is None and rows not in (1, self.B)
+        if wrong or t.dtype is not dtype or t.shape != (rows, cols or self.E) or not t.is_contiguous() or t.device != self.ws.device:
+            raise ValueError(f"{name}: a contiguous {dtype} tensor of {f'1 or {self.B}' if cols is None else rows} rows of "
+                             f"{cols or self.E} on {self.ws.device} is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
+
+    def expert_balance(self, topk_idx=None, per_sample=True, loss_scale=1.0, loss=None, counts=None, d_gate=None,
+                       stream=None):
+        """Expert-level load-balance loss of the last forward, per sample or over the batch: returns (loss [1], counts
+        [B or 1, E] int32, d_gate [B or 1, E]); ``backward`` takes d_gate, the gradient of loss_scale times the loss.
+        topk_idx: the forward's with dropped selections set to a negative number (to be given to ``backward`` too)."""
+        idx, rows = self.topk_idx if topk_idx is None else topk_idx, self.B if per_sample else 1
+        self._table("topk_idx", idx, torch.int32, self.T, self.k)
+        out = []
+        for name, t, dtype, cols in (("loss", loss, torch.float32, 0), ("counts", counts, torch.int32, self.E),
+                                     ("d_gate", d_gate, torch.float32, self.E)):
+            if t is None:
+                with torch.cuda.stream(stream):         # (no change where it is None)
+                    t = torch.empty((rows, cols) if cols else 1, dtype=dtype, device=self.ws.device)
+            elif cols:
+                self._table(name, t, dtype, rows)
+            elif t.dtype is not dtype or t.shape != (1,) or t.device != self.ws.device:
+                raise ValueError(f"loss: a float32 tensor of one value on {self.ws.device} is wanted")
+            out.append(t)
+        _check(smoes_expert_balance(self.plan, idx, per_sample, loss_scale, *out, self.ws, stream), "smoes_expert_balance")
+        return tuple(out)
 
     def permute(self, is_vision=None, home=None, topk_idx=None, stream=None):
         code = smoes_bin_permute(self.plan, self.topk_idx if topk_idx is None else topk_idx, home,

@@ -26,7 +26,7 @@ struct Layout {
   size_t status, sample_ticket, loss_ticket, offsets, token_sample, expert_bin, expert_slot,
       piece_base, sample_pieces, pieces, mi32, tabs, gsave, ginv, dw_part, dz_img, perm, attn_ticket, attn_part,
       gcoef, perm_sync, fperm, stat_part, stat_nvis, stat_n0, f32_part, tile_ticket, bal_flag,
-      bal_f, bal_a, bal_h, bal_s, bal_u, gmmcoef;
+      bal_f, bal_a, bal_h, bal_s, bal_u, gmmcoef, ebal_ticket, ebal_base, ebal_h, ebal_c, ebal_n, ebal_loss;
   size_t header_bytes;   // [0, header_bytes) is cleared by smoes_workspace_init
   size_t total;
 };
@@ -49,7 +49,8 @@ struct smoes_plan_s {
   bool contig_bins = false;
   uint64_t limit_ns = kWaitLimitNs;   // bounded device waits
   bool balance_armed = false;         // smoes_bin_balance enqueued since the last forward
-  std::vector<int32_t> offsets, expert_bin, expert_slot, token_sample, piece_base, sample_pieces;
+  int ebal_len = 32;                  // expert-level balance: tokens of a block's run
+  std::vector<int32_t> offsets, expert_bin, expert_slot, token_sample, piece_base, sample_pieces, ebal_base;
   Layout L{};
 };
 
@@ -383,6 +384,12 @@ smoes_status smoes_plan_create(const smoes_router_desc* desc, smoes_plan* out) {
   }
   P->perm_nblocks = std::max(1, perm_blocks(T, d.k));
 
+  // expert-level balance: about one run of tokens per SM, cut at the samples
+  P->ebal_len = std::max(32, (T + P->n_sms - 1) / P->n_sms);
+  P->ebal_base.assign(B + 1, 0);
+  for (int i = 0; i < B; ++i)
+    P->ebal_base[i + 1] = P->ebal_base[i] + (P->offsets[i + 1] - P->offsets[i] + P->ebal_len - 1) / P->ebal_len;
+
   // workspace layout
   Layout& L = P->L;
   size_t o = 0;
@@ -394,6 +401,7 @@ smoes_status smoes_plan_create(const smoes_router_desc* desc, smoes_plan* out) {
   L.perm_sync = take(sizeof(uint32_t) * 4);
   L.tile_ticket = take(sizeof(uint32_t) * static_cast<size_t>(std::max(P->n_groups, 1)));
   L.bal_flag = take(sizeof(uint32_t) * 4);
+  L.ebal_ticket = take(sizeof(uint32_t) * (static_cast<size_t>(B) + 2));   // per sample, then the losses'
   L.header_bytes = o;
   L.offsets = take(sizeof(int32_t) * (B + 1));
   L.token_sample = take(sizeof(int32_t) * std::max(T, 1));
@@ -424,6 +432,12 @@ smoes_status smoes_plan_create(const smoes_router_desc* desc, smoes_plan* out) {
   L.bal_h = take(sizeof(float) * static_cast<size_t>(P->bal_blocks) * E);
   L.bal_s = take(sizeof(int32_t) * static_cast<size_t>(P->bal_blocks) * E);
   L.bal_u = take(sizeof(int32_t) * static_cast<size_t>(P->bal_blocks) * K);
+  const size_t ebal_rows = 2 * static_cast<size_t>(T / P->ebal_len + 1);
+  L.ebal_base = take(sizeof(int32_t) * (B + 1));
+  L.ebal_h = take(sizeof(float) * ebal_rows * E);
+  L.ebal_c = take(sizeof(int32_t) * ebal_rows * E);
+  L.ebal_n = take(sizeof(int32_t) * ebal_rows);
+  L.ebal_loss = take(sizeof(float) * std::max(B, 1));
   L.f32_part = take(d.dtype == SMOES_F32 ? sizeof(float) * static_cast<size_t>(P->n_groups) *
                                                f32_chunks(d.d) * (E + 1) * 128 : 0);
   L.total = o;
@@ -459,6 +473,7 @@ smoes_status smoes_workspace_init(smoes_plan P, void* ws, size_t ws_bytes, cudaS
   up(L.expert_slot, P->expert_slot, E);
   up(L.piece_base, P->piece_base, P->n_groups + 1);
   up(L.sample_pieces, P->sample_pieces, B + 1);
+  up(L.ebal_base, P->ebal_base, B + 1);
   if (e == cudaSuccess) e = cudaStreamSynchronize(stream);   // host vectors must outlive the copies
   return cuda_status(e);
 }
@@ -684,6 +699,14 @@ smoes_status smoes_router_bwd(smoes_plan P, const void* X, const void* W, const 
                               const int32_t* topk_idx, const float* d_topk_w, float loss_scale,
                               float* dW, int accumulate_dW, void* dX, float* dlogits, void* ws,
                               size_t ws_bytes, cudaStream_t stream) {
+  return smoes_router_bwd_gates(P, X, W, M, topk_idx, d_topk_w, nullptr, 0, loss_scale, dW, accumulate_dW, dX, dlogits,
+                                ws, ws_bytes, stream);
+}
+
+smoes_status smoes_router_bwd_gates(smoes_plan P, const void* X, const void* W, const float* M,
+                                    const int32_t* topk_idx, const float* d_topk_w, const float* d_gate,
+                                    int per_sample, float loss_scale, float* dW, int accumulate_dW, void* dX,
+                                    float* dlogits, void* ws, size_t ws_bytes, cudaStream_t stream) {
   if (!P) return SMOES_ERR_INVALID_ARG;
   smoes_status st = check_ws(P, ws, ws_bytes);
   if (st != SMOES_OK) return st;
@@ -694,7 +717,8 @@ smoes_status smoes_router_bwd(smoes_plan P, const void* X, const void* W, const 
     return cuda_status(cudaMemsetAsync(dW, 0, sizeof(float) * static_cast<size_t>(d.E) * d.d, stream));
   }
   if (!X || !W || !M) return SMOES_ERR_INVALID_ARG;
-  if ((d_topk_w || d.mi_topk_mask) && !topk_idx) return SMOES_ERR_INVALID_ARG;
+  if ((d_topk_w || d_gate || d.mi_topk_mask) && !topk_idx) return SMOES_ERR_INVALID_ARG;
+  if (d_gate && !aligned16(d_gate)) return SMOES_ERR_ALIGNMENT;
   if (!aligned16(X) || !aligned16(W) || !aligned16(M) || !aligned16(dW) || (dX && !aligned16(dX)))
     return SMOES_ERR_ALIGNMENT;
   if (d.dtype == SMOES_BF16 && d.E > 128) return SMOES_ERR_UNSUPPORTED;
@@ -719,6 +743,8 @@ smoes_status smoes_router_bwd(smoes_plan P, const void* X, const void* W, const 
   p.n_tiles = P->bwd_tiles;
   p.limit_ns = P->limit_ns;
   p.balance_armed = P->balance_armed ? 1 : 0;
+  p.d_gate = d_gate;
+  p.d_gate_stride = per_sample ? d.E : 0;
   p.n_sms = P->n_sms;
   cudaError_t e;
   if (d.dtype == SMOES_BF16) {
@@ -856,6 +882,49 @@ smoes_status smoes_bin_balance(smoes_plan P, const int32_t* topk_idx, float loss
   const smoes_status r = cuda_status(launch_bin_balance(p, stream));
   if (r == SMOES_OK) P->balance_armed = true;
   return r;
+}
+
+smoes_status smoes_expert_balance(smoes_plan P, const int32_t* topk_idx, int per_sample, float loss_scale, float* loss,
+                                  int32_t* counts, float* d_gate, void* ws, size_t ws_bytes, cudaStream_t stream) {
+  if (!P || !loss || (per_sample != 0 && per_sample != 1)) return SMOES_ERR_INVALID_ARG;
+  smoes_status st = check_ws(P, ws, ws_bytes);
+  if (st != SMOES_OK) return st;
+  const smoes_router_desc& d = P->desc;
+  if ((counts && !aligned16(counts)) || (d_gate && !aligned16(d_gate))) return SMOES_ERR_ALIGNMENT;
+  if (d.T == 0) {
+    cudaError_t e = cudaMemsetAsync(loss, 0, sizeof(float), stream);
+    for (void* a : {static_cast<void*>(counts), static_cast<void*>(d_gate)})
+      if (a && !per_sample && e == cudaSuccess) e = cudaMemsetAsync(a, 0, 4 * static_cast<size_t>(d.E), stream);
+    return cuda_status(e);
+  }
+  if (!topk_idx) return SMOES_ERR_INVALID_ARG;
+  if (!aligned16(topk_idx)) return SMOES_ERR_ALIGNMENT;
+  uint8_t* b = static_cast<uint8_t*>(ws);
+  const WsView v = make_view(P, ws);
+  ExpertBalanceParams p{};
+  p.T = d.T;
+  p.E = d.E;
+  p.k = d.k;
+  p.B = per_sample ? d.n_samples : 1;
+  p.len = P->ebal_len;
+  p.per_sample = per_sample;
+  p.gsave = v.gsave;
+  p.ginv = v.ginv;
+  p.topk_idx = topk_idx;
+  p.offsets = v.offsets;
+  p.base = reinterpret_cast<const int32_t*>(b + P->L.ebal_base);
+  p.scale = loss_scale;
+  p.part_h = reinterpret_cast<float*>(b + P->L.ebal_h);
+  p.part_c = reinterpret_cast<int32_t*>(b + P->L.ebal_c);
+  p.part_n = reinterpret_cast<int32_t*>(b + P->L.ebal_n);
+  p.sample_loss = reinterpret_cast<float*>(b + P->L.ebal_loss);
+  p.ticket = reinterpret_cast<uint32_t*>(b + P->L.ebal_ticket);
+  p.loss_ticket = p.ticket + d.n_samples;
+  p.loss = loss;
+  p.counts = counts;
+  p.d_gate = d_gate;
+  const int blocks = per_sample ? P->ebal_base[d.n_samples] : (d.T + P->ebal_len - 1) / P->ebal_len;
+  return cuda_status(launch_expert_balance(p, blocks, stream));
 }
 
 smoes_status smoes_adaptive_bins(smoes_plan P, const int32_t* expert_counts, double beta,

@@ -157,6 +157,33 @@ __device__ __forceinline__ void add_balance_grad(const BwdParams& p, const TopkS
   }
 }
 
+// Whether the token of a GS-lane group has a selection in [0, E), from its slots.
+template <int GS>
+__device__ __forceinline__ bool takes_part(const BwdParams& p, const TopkSlots<GS>& u) {
+  int any = 0;
+#pragma unroll
+  for (int i = 0; i < TopkSlots<GS>::kPer; ++i) any |= u.idx[i] >= 0 && u.idx[i] < p.dm.E;
+#pragma unroll
+  for (int o = 1; o < GS; o <<= 1) any |= __shfl_xor_sync(0xffffffffu, any, o);
+  return any != 0;
+}
+
+// Gradient t of the gate values at one token's logits, added to dz: dz_e += fac_e g_e (t_e - sum_e' g_e' t_e'), the sum
+// over the token's GS-lane group.
+template <int GS, int N>
+__device__ __forceinline__ void add_gate_grad(const float (&g)[N], const float (&t)[N], const float (&fac)[N], bool on,
+                                              float (&dz)[N]) {
+  float part = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) part = fmaf(g[i], t[i], part);
+#pragma unroll
+  for (int o = 1; o < GS; o <<= 1) part += __shfl_xor_sync(0xffffffffu, part, o);
+  if (on) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) dz[i] = fmaf(fac[i] * g[i], t[i] - part, dz[i]);
+  }
+}
+
 // MI gradient at one token's logits for the thread's N experts (a GS-lane group holds the token):
 //   dz_e = scale fac_e w_e (u_e - sum_e' w_e' u_e'),
 // with w the gate values that enter eq. (12) (the dense gate g, or with the top-k mask g on the
@@ -213,7 +240,7 @@ __device__ __forceinline__ void mi_grad(const BwdParams& p, int j, bool valid, c
 // tokens, waited for them and then for the coefficients stopped for each. small_hidden step with
 // upstream gradients (32768 tokens, E = 64): 106.5 -> 101.4 us; large_fine unchanged. kUp: an upstream gradient of the top-k weights is present (its slots stay out of the
 // register budget otherwise).
-template <int TPT, bool kUp, bool kBal, bool kVar>
+template <int TPT, bool kUp, bool kBal, bool kVar, bool kGates>
 __global__ void __launch_bounds__(256) k_dz_prep(const BwdParams p) {
   pdl_wait();                                         // scores and tables of the forward
   pdl_trigger();
@@ -272,11 +299,14 @@ __global__ void __launch_bounds__(256) k_dz_prep(const BwdParams p) {
       in.m = __ldg(reinterpret_cast<const float2*>(p.M) + j);
       in.smp = __ldg(p.ws.token_sample + j);
     }
-    if (kUp || bal) load_slots<TPT, kUp>(p, j, j < dm.T, c, in.slots);
+    if (kUp || kGates || bal) load_slots<TPT, kUp>(p, j, j < dm.T, c, in.slots);
   };
   // coefficients (a, b, h) of the thread's two bins for sample held (-1: none yet)
   int held = -1;
   float ca[2] = {0.f, 0.f}, cb[2] = {0.f, 0.f}, ch[2] = {0.f, 0.f};
+  // the gradient of the gate values, of row t_row (-1: none yet)
+  int t_row = -1;
+  float te[8];
 
   const int n_it = ((p.n_tiles - static_cast<int>(blockIdx.x) + static_cast<int>(gridDim.x) - 1) / static_cast<int>(gridDim.x)) * kIt;
   auto token = [&](int it) { return (static_cast<int>(blockIdx.x) + it / kIt * static_cast<int>(gridDim.x)) * kBwdBT + it % kIt * kGroups + grp; };
@@ -327,6 +357,15 @@ __global__ void __launch_bounds__(256) k_dz_prep(const BwdParams p) {
     mi_grad<TPT, 8, kVar>(p, j, valid, eidx, raw, g, u, fac, dz);
     if (kUp) add_upstream<TPT, 8>(p, in.slots, eidx, g, fac, kVar && dm.gate, dz);
     if (kBal && bal) add_balance_grad<TPT, 8>(p, in.slots, g, be, fe, fac, dz);
+    if (kGates) {
+      const int row = in.smp * p.d_gate_stride;
+      if (row != t_row) {
+        t_row = row;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) te[i] = e0 + i < E ? __ldg(p.d_gate + row + e0 + i) : 0.f;
+      }
+      add_gate_grad<TPT, 8>(g, te, fac, takes_part<TPT>(p, in.slots), dz);
+    }
     if (valid && p.dlogits) {
       float* dl = p.dlogits + static_cast<size_t>(j) * E;
       if (vec) {
@@ -721,7 +760,7 @@ k_router_bwd_f32(const BwdParams p) {
     const bool has_up = p.d_topk_w != nullptr;
     const bool bal = p.topk_idx && __ldcg(p.ws.bal_flag) != 0u;   // the balance term (eq. 16); block-uniform
     if (has_up) load_slots<4, true>(p, j, valid, qd, slots);
-    else if (bal) load_slots<4, false>(p, j, valid, qd, slots);
+    else if (bal || p.d_gate) load_slots<4, false>(p, j, valid, qd, slots);
     const float* g = p.ws.gsave + static_cast<size_t>(valid ? j : 0) * E;
     const float ginv = valid ? p.ws.ginv[j] : 0.f;
     // the token's 4-thread group holds experts qd, qd + 4, ...
@@ -744,6 +783,12 @@ k_router_bwd_f32(const BwdParams p) {
 #pragma unroll
       for (int i = 0; i < NQ; ++i) fq[i] = bq[i] >= 0 ? p.ws.bal_f[eidx[i]] : 0.f;
       add_balance_grad<4, NQ>(p, slots, gq, bq, fq, fac, dzv);
+    }
+    if (p.d_gate) {
+      const float* t = p.d_gate + static_cast<size_t>(valid ? p.ws.token_sample[j] : 0) * p.d_gate_stride;
+#pragma unroll
+      for (int i = 0; i < NQ; ++i) fq[i] = eidx[i] >= 0 ? __ldg(t + eidx[i]) : 0.f;
+      add_gate_grad<4, NQ>(gq, fq, fac, takes_part<4>(p, slots), dzv);
     }
 #pragma unroll
     for (int i = 0; i < EB / 4; ++i) {
@@ -876,17 +921,20 @@ cudaError_t launch_dz_prep(const BwdParams& p, cudaStream_t s) {
   // holds two or three of them and starts the rest as those end; a grid of just what it holds was no
   // better (131072 x 1024, E = 64, upstream gradient 127.3 -> 125.4 us; 65536 x 1024, E = 128 94.5 -> 96.0).
   const int blocks = p.n_tiles < 4 * p.n_sms ? p.n_tiles : 4 * p.n_sms;
-  // the upstream-gradient and balance variants keep their tables out of the common kernel's
+  // the upstream-gradient, balance and gate-gradient variants keep their tables out of the common kernel's
   // registers; the balance variant still checks the arming flag on the device
-  const bool up = p.d_topk_w != nullptr, bal = p.balance_armed != 0;
+  const bool up = p.d_topk_w != nullptr, bal = p.balance_armed != 0, gates = p.d_gate != nullptr;
   const bool var = p.dm.gate != 0 || p.dm.mask != 0;      // sigmoid gate or top-k-masked g
   auto pick = [&](auto tpt) {
     constexpr int TPT = decltype(tpt)::value;
-    if (var)
-      return up ? (bal ? k_dz_prep<TPT, true, true, true> : k_dz_prep<TPT, true, false, true>)
-                : (bal ? k_dz_prep<TPT, false, true, true> : k_dz_prep<TPT, false, false, true>);
-    return up ? (bal ? k_dz_prep<TPT, true, true, false> : k_dz_prep<TPT, true, false, false>)
-              : (bal ? k_dz_prep<TPT, false, true, false> : k_dz_prep<TPT, false, false, false>);
+    auto with = [](bool on, auto&& f) { return on ? f(std::true_type()) : f(std::false_type()); };
+    return with(up, [&](auto u) {
+      return with(bal, [&](auto ba) {
+        return with(var, [&](auto v) {
+          return with(gates, [&](auto ga) { return k_dz_prep<TPT, u.value, ba.value, v.value, ga.value>; });
+        });
+      });
+    });
   };
   if (E_pad == 64) return launch_pdl(pick(std::integral_constant<int, 8>()), dim3(blocks), dim3(256), 0, s, p);
   if (E_pad == 128) return launch_pdl(pick(std::integral_constant<int, 16>()), dim3(blocks), dim3(256), 0, s, p);

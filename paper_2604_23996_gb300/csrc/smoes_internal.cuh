@@ -129,6 +129,8 @@ struct BwdParams {
   int n_tiles;               // token tiles
   uint64_t limit_ns;
   int balance_armed;         // host's view: smoes_bin_balance was called since the last forward
+  const float* d_gate;       // gradient of the gate values by sample or batch, or null
+  int d_gate_stride;         // E (a row per sample) or 0
   int n_sms;
 };
 
@@ -237,6 +239,27 @@ struct BalParams {
   float* P_out;              // [E] or null
 };
 
+// Expert-level load-balance loss over runs of at most `len` tokens of a sample (or of the batch, B = 1): partials of the
+// runs of samples that have several, tickets (zero between calls), the samples' losses.
+struct ExpertBalanceParams {
+  int T, E, k, B, len, per_sample;
+  const float* gsave;
+  const float* ginv;
+  const int32_t* topk_idx;
+  const int32_t* offsets;    // [B+1] tokens of a sample
+  const int32_t* base;       // [B+1] runs of the samples before
+  float scale;
+  float* part_h;             // [2 (T / len + 1)][E]
+  int32_t* part_c;
+  int32_t* part_n;
+  float* sample_loss;        // [B]
+  uint32_t* ticket;          // [B]
+  uint32_t* loss_ticket;
+  float* loss;
+  int32_t* counts;           // [B, E] or null
+  float* d_gate;             // [B, E] or null
+};
+
 // Momentum-adaptive binning (eqs. 10-11).
 struct BinsParams {
   int E, N_B;
@@ -321,6 +344,7 @@ cudaError_t launch_gauss_coef(const float* mu, const float* var, int d, int dcoe
 cudaError_t launch_stats_update(const StatsParams& p, bool bf16, cudaStream_t s);
 cudaError_t launch_adaptive_bins(const BinsParams& p, cudaStream_t s);
 cudaError_t launch_bin_balance(const BalParams& p, cudaStream_t s);
+cudaError_t launch_expert_balance(const ExpertBalanceParams& p, int blocks, cudaStream_t s);
 // Attention forward with the vision score as one more value column (eqs. 2-4), grouped-query
 // heads: K and V have Hkv heads, query head h reads key/value head h / (H / Hkv). O [B, H, S, hd]
 // bf16, M as for the mass-only kernel.
