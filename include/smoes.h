@@ -484,6 +484,41 @@ smoes_status smoes_expert_linear_bwd(smoes_experts plan, const void* dZ, const v
                                      float* dW, int accumulate_dW, void* ws, size_t ws_bytes,
                                      cudaStream_t stream);
 
+/* ------------------------------------------------------------------------ microscaled 4-bit values
+ * (13) Values in 4 bits with a scale for every 32 consecutive ones of a row (the MXFP4 format): codes [rows, n / 2] bytes, the
+ *   even value of a pair in the low half; scales [rows, n / 32] bytes, 2^(byte - 127), byte 255 NaN. A code's low three bits
+ *   are the sizes 0, 0.5, 1, 1.5, 2, 3, 4, 6, its fourth the sign. n % 32 == 0 (32..2^20), up to 2^31 rows; X [rows, n] of
+ *   `dtype`. Arrays as at the head of this file; no plan, no workspace; on the current device.
+ *   Quantisation: byte - 127 = max(floor(log2 max |x|) - 2, -127) of the 32; a value over the scale goes to the nearest size,
+ *   a tie to the even code, above 6 to 6. 32 values with a NaN or an infinity among them get the byte 255 and the codes 0. */
+smoes_status smoes_mx_quantise(const void* X, smoes_dtype dtype, long long rows, int n, uint8_t* codes,
+                               uint8_t* scales, cudaStream_t stream);
+/* The values back, rounded to dtype (those that smoes_mx_quantise made are exact in both types). */
+smoes_status smoes_mx_dequantise(const uint8_t* codes, const uint8_t* scales, long long rows, int n,
+                                 smoes_dtype dtype, void* X, cudaStream_t stream);
+/* (14) smoes_expert_dispatch with quantised rows: X [T, d] (dtype of the plan) -> codes [R, d / 2] and scales
+ *   [R, d / 32] in expert order; zeros in the rows of no expert. */
+smoes_status smoes_expert_dispatch_mx(smoes_experts plan, const void* X, int d, const int32_t* expert_offsets,
+                                      const int32_t* slot_row, uint8_t* codes, uint8_t* scales,
+                                      cudaStream_t stream);
+/* (15) smoes_expert_linear of quantised rows and weights, for serving: X [R, n_in] and W [E, n_z, n_in] as codes and
+ *   scales, n_in % 32 == 0, bias [E, n_z] float32 or NULL, residual and out [R, n_out] bf16. Plans of SMOES_BF16 (others
+ *   return SMOES_ERR_UNSUPPORTED). Products are exact, their sums float32. */
+typedef struct {
+  const uint8_t* X;
+  const uint8_t* X_scales;
+  const uint8_t* W;
+  const uint8_t* W_scales;
+  const float* bias;
+  const void* residual;
+  int n_in, n_out;
+  int act;                             /* smoes_act */
+  int gated;
+} smoes_linear_mx_args;
+smoes_status smoes_expert_linear_mx(smoes_experts plan, const smoes_linear_mx_args* args,
+                                    const int32_t* expert_offsets, void* out, void* ws, size_t ws_bytes,
+                                    cudaStream_t stream);
+
 /* -------------------------------------------------------------------------------- layer norm
  * (12) The norm in front of the router and the experts, with the residual stream's sum:
  *     s = X + residual,  mean = sum_j s_j / d,  rstd = 1 / sqrt(sum_j (s_j - mean)^2 / d + eps),

@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import numpy as np
 import torch
@@ -75,6 +75,12 @@ class LinearArgs(C.Structure):
                 ("n_in", C.c_int), ("n_out", C.c_int), ("act", C.c_int), ("gated", C.c_int)]
 
 
+class LinearMxArgs(C.Structure):
+    _fields_ = [("X", C.c_void_p), ("X_scales", C.c_void_p), ("W", C.c_void_p), ("W_scales", C.c_void_p),
+                ("bias", C.c_void_p), ("residual", C.c_void_p), ("n_in", C.c_int), ("n_out", C.c_int), ("act", C.c_int),
+                ("gated", C.c_int)]
+
+
 class NormDesc(C.Structure):
     _fields_ = [("T", C.c_int), ("d", C.c_int), ("dtype", C.c_int), ("eps", C.c_float)]
 
@@ -119,6 +125,10 @@ _sig = {
     "smoes_expert_act_bwd": (_i, [_vp, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _sz, _vp]),
     "smoes_expert_act_bwd_accumulate": (_i, [_vp, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _sz, _vp]),
     "smoes_expert_linear_bwd": (_i, [_vp, _vp, _vp, _vp, _i, _i, _vp, _vp, _vp, _i, _vp, _sz, _vp]),
+    "smoes_mx_quantise": (_i, [_vp, _i, C.c_longlong, _i, _vp, _vp, _vp]),
+    "smoes_mx_dequantise": (_i, [_vp, _vp, C.c_longlong, _i, _i, _vp, _vp]),
+    "smoes_expert_dispatch_mx": (_i, [_vp, _vp, _i, _vp, _vp, _vp, _vp, _vp]),
+    "smoes_expert_linear_mx": (_i, [_vp, C.POINTER(LinearMxArgs), _vp, _vp, _vp, _sz, _vp]),
     "smoes_norm_create": (_i, [C.POINTER(NormDesc), C.POINTER(_vp)]),
     "smoes_norm_destroy": (None, [_vp]),
     "smoes_norm_workspace_bytes": (_sz, [_vp]),
@@ -343,6 +353,70 @@ def smoes_experts_workspace_init(plan, ws, stream=None) -> int:
 
 def smoes_experts_set_wait_limit(plan, limit_ns: int) -> int:
     return _lib.smoes_experts_set_wait_limit(plan, int(limit_ns))
+
+
+# ---------------------------------------------------------------- microscaled 4-bit values
+
+class Mx(NamedTuple):
+    """Values in 4 bits with a scale for every 32 of the last dimension: codes [..., n / 2] and scales [..., n / 32], uint8."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+
+
+def _mx_stream(t, stream):
+    """The stream's handle for a call without a plan: the tensors' device has to be the current one, and the stream's."""
+    index = t.get_device()                              # (-1 on the host)
+    if index < 0 or index != torch._C._cuda_getDevice() or (stream is not None and stream.device_index != index):
+        raise ValueError(f"device: a tensor of the current GPU, and a stream of it, are wanted, got one of {t.device}")
+    return torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+
+
+def _mx_checked(name, x, shape, index):
+    """Addresses of the codes and scales of an Mx that stands for [*shape]."""
+    codes, scales = x
+    lead, n = tuple(shape[:-1]), shape[-1]
+    for t, want in ((codes, lead + (n // 2,)), (scales, lead + (n // 32,))):
+        if t.dtype is not torch.uint8 or t.shape != want or not t.is_contiguous() or t.get_device() != index:
+            raise ValueError(f"{name}: contiguous uint8 codes {lead + (n // 2,)} and scales {lead + (n // 32,)} on cuda:{index} "
+                             f"are wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return codes.data_ptr(), scales.data_ptr()
+
+
+def mx_quantise(X, out=None, stream=None) -> Mx:
+    """X [..., n] (bf16 or float32, contiguous, n a multiple of 32) in 4 bits."""
+    if X.dtype not in (torch.bfloat16, torch.float32) or X.dim() < 1 or X.shape[-1] % 32 or X.shape[-1] == 0 or not X.is_contiguous():
+        raise ValueError(f"X: a contiguous bf16 or float32 tensor with a last dimension of 32s is wanted, got {X.dtype} {tuple(X.shape)}")
+    raw, n, lead = _mx_stream(X, stream), X.shape[-1], X.shape[:-1]
+    if out is None:
+        with torch.cuda.stream(stream):                 # (no change where it is None)
+            out = Mx(torch.empty(lead + (n // 2,), dtype=torch.uint8, device=X.device),
+                     torch.empty(lead + (n // 32,), dtype=torch.uint8, device=X.device))
+    q, s = _mx_checked("out", out, X.shape, X.get_device())
+    _check(_lib.smoes_mx_quantise(X.data_ptr(), SMOES_BF16 if X.dtype is torch.bfloat16 else SMOES_F32, X.numel() // n, n, q, s, raw),
+           "smoes_mx_quantise")
+    return Mx(*out)
+
+
+def mx_dequantise(x, dtype=torch.bfloat16, out=None, stream=None) -> torch.Tensor:
+    """The values of an Mx, in bf16 or float32."""
+    codes = x[0]
+    if codes.dim() < 1 or codes.shape[-1] % 16 or codes.shape[-1] == 0:
+        raise ValueError(f"codes: a last dimension of 16s is wanted, got {tuple(codes.shape)}")
+    raw, n = _mx_stream(codes, stream), 2 * codes.shape[-1]
+    shape = codes.shape[:-1] + (n,)
+    q, s = _mx_checked("x", x, shape, codes.get_device())
+    if out is not None:
+        dtype = out.dtype
+        if out.shape != shape or not out.is_contiguous() or out.device != codes.device:
+            raise ValueError(f"out: a contiguous tensor of shape {tuple(shape)} on {codes.device} is wanted")
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"dtype: bf16 or float32 is wanted, got {dtype}")
+    if out is None:
+        with torch.cuda.stream(stream):
+            out = torch.empty(shape, dtype=dtype, device=codes.device)
+    _check(_lib.smoes_mx_dequantise(q, s, codes.numel() * 2 // n, n, SMOES_BF16 if dtype is torch.bfloat16 else SMOES_F32,
+                                    out.data_ptr(), raw), "smoes_mx_dequantise")
+    return out
 
 
 # ----------------------------------------------------------------------------- convenience
@@ -668,6 +742,39 @@ class Experts(_Calls):
                                             _ptr(dW), accumulate, ws.data_ptr(), ws.numel(), self._stream(stream)),
                "smoes_expert_linear_bwd")
         return dX, dW
+
+    def dispatch_mx(self, X, out=None, stream=None):
+        """Tokens [T, d] into expert order, quantised to 4 bits: an Mx of [R, d]."""
+        d = X.shape[-1]
+        if d % 32:
+            raise ValueError(f"X: a width of 32s is wanted, got {d}")
+        x = self._in("X", X, (self.T, d), self.dtype)
+        u8 = torch.uint8
+        codes, scales = (None, None) if out is None else out
+        codes, scales = self._new(codes, (self.R, d // 2), u8, stream), self._new(scales, (self.R, d // 32), u8, stream)
+        _check(_lib.smoes_expert_dispatch_mx(self.plan, x, d, self.expert_offsets.data_ptr(), self.slot_row.data_ptr(),
+                                             codes.data_ptr(), scales.data_ptr(), self._stream(stream)),
+               "smoes_expert_dispatch_mx")
+        return Mx(codes, scales)
+
+    def linear_mx(self, X, W, bias=None, act=SMOES_ACT_NONE, gated=False, residual=None, out=None, stream=None):
+        """``linear`` of quantised rows (an Mx of [R, n_in] in expert order) and weights (an Mx of [E, n_z, n_in]), in bf16
+        and for serving: no pre-activations are saved. Returns out."""
+        n_z, n_in = W[0].shape[-2], 2 * W[0].shape[-1]
+        n_out = n_z // 2 if gated else n_z
+        if gated and n_z % 2:
+            raise ValueError(f"W: a gated layer has an even number of rows, got {n_z}")
+        if n_in % 32:
+            raise ValueError(f"W: a width of 32s is wanted, got {n_in}")
+        x = _mx_checked("X", X, (self.R, n_in), self._index)
+        w = _mx_checked("W", W, (self.E, n_z, n_in), self._index)
+        args = LinearMxArgs(*x, *w, self._in("bias", bias, (self.E, n_z), torch.float32),
+                            self._in("residual", residual, (self.R, n_out), self.dtype), n_in, n_out, act, gated)
+        out = self._new(out, (self.R, n_out), self.dtype, stream)
+        ws = self.ws
+        _check(_lib.smoes_expert_linear_mx(self.plan, args, self.expert_offsets.data_ptr(), out.data_ptr(), ws.data_ptr(),
+                                           ws.numel(), self._stream(stream)), "smoes_expert_linear_mx")
+        return out
 
     def device_status(self, stream=None):
         return _lib.smoes_experts_read_status(self.plan, self.ws.data_ptr(), self._stream(stream))

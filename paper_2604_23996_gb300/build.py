@@ -20,7 +20,7 @@ LIB = os.path.join(LIBDIR, "libsmoes.so")
 SOURCES = ["api.cu", "router_fwd.cu", "router_fwd_var.cu", "router_bwd.cu", "bin_permute.cu",
            "gauss_score.cu", "gmm_score.cu", "gauss_stats.cu", "bin_balance.cu", "expert_balance.cu", "attn_mass.cu",
            "attn_fwd.cu", "experts_api.cu", "expert_sort.cu", "expert_rows.cu", "expert_gemm.cu",
-           "expert_gemm_f32.cu", "expert_act.cu", "layer_norm.cu"]
+           "expert_gemm_f32.cu", "expert_act.cu", "expert_mx.cu", "mx.cu", "layer_norm.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-I" + INCLUDE, "-I" + CSRC]
 

@@ -272,6 +272,10 @@ bool smoes::encode_f32(CUtensorMap* m, const void* ptr, int rank, const uint64_t
                        const uint32_t* box) {
   return encode_tiled(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, CU_TENSOR_MAP_SWIZZLE_NONE, ptr, rank, dims, strides, box);
 }
+bool smoes::encode_u8(CUtensorMap* m, const void* ptr, int rank, const uint64_t* dims, const uint64_t* strides,
+                      const uint32_t* box) {
+  return encode_tiled(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, CU_TENSOR_MAP_SWIZZLE_128B, ptr, rank, dims, strides, box);
+}
 
 extern "C" {
 

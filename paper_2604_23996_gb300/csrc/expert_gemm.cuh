@@ -41,7 +41,7 @@ __device__ __forceinline__ GemmTile gemm_tile(const ExpertGemmParams& p, const R
   }
   const int r = tile / p.m_tiles;
   t.m = tile - r * p.m_tiles;
-  const RowTile row = find_row_tile(rt, off, p.l.E, R, p.tile_shift, r);
+  const RowTile row = find_row_tile(rt, off, p.l.E, R, ShiftRows{p.tile_shift}, r);
   t.e = row.e;
   t.row0 = row.row0;
   t.cols = min(1 << p.tile_shift, row.row1 - row.row0);

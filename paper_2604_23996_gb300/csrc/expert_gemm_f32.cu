@@ -183,7 +183,7 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
   if (warp == 2) tmem_alloc_pair(&bars.tmem, 512);
   pdl_wait();
   pdl_trigger();
-  if (kMode != kGemmGradW && warp == 3) count_row_tiles(l.offsets, l.E, static_cast<int>(l.R), p.tile_shift, bars.before);
+  if (kMode != kGemmGradW && warp == 3) count_row_tiles(l.offsets, l.E, static_cast<int>(l.R), ShiftRows{p.tile_shift}, bars.before);
   for (int e = threadIdx.x; e <= l.E; e += kF32Threads) off[e] = __ldg(l.offsets + e);
   tc_fence_before();
   __syncthreads();

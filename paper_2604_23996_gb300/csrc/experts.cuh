@@ -87,6 +87,21 @@ cudaError_t launch_expert_gemm(const ExpertLinearParams& p, ExpertGemmMode mode,
                                int n_sms, cudaStream_t s);
 cudaError_t launch_expert_gemm_f32(const ExpertLinearParams& p, ExpertGemmMode mode, uint32_t* status, uint64_t limit_ns,
                                    int n_sms, cudaStream_t s);
+// The forward's product of microscaled 4-bit rows and weights (l.X and l.W hold the pairs of codes; expert_mx.cu).
+struct ExpertMxParams {
+  ExpertLinearParams l;
+  const uint8_t* x_scale;    // [R, n_in / 32]
+  const uint8_t* w_scale;    // [E, n_z, n_in / 32]
+  int m_tiles;
+  int tile_rows;
+  uint32_t* status;
+  uint64_t limit_ns;
+};
+cudaError_t launch_expert_mx(ExpertMxParams p, int n_sms, cudaStream_t s);   // fills m_tiles and tile_rows
+cudaError_t launch_mx_quantise(const void* X, bool bf16, long long values, uint8_t* q, uint8_t* scale, cudaStream_t s);
+cudaError_t launch_mx_dequantise(const uint8_t* q, const uint8_t* scale, long long values, bool bf16, void* X, cudaStream_t s);
+// rows_out: the pairs of codes, scale: [R, d / 32]
+cudaError_t launch_expert_dispatch_mx(const ExpertRowsParams& p, bool bf16, uint8_t* scale, cudaStream_t s);
 cudaError_t launch_expert_sort(const ExpertSortParams& p, cudaStream_t s);
 cudaError_t launch_expert_dispatch(const ExpertRowsParams& p, bool bf16, cudaStream_t s);
 cudaError_t launch_expert_combine(const ExpertRowsParams& p, bool bf16, cudaStream_t s);
@@ -102,7 +117,7 @@ __device__ __forceinline__ long long expert_begin(const int32_t* off, int e, lon
   return o < 0 ? 0 : o > R ? R : o;
 }
 
-// Work over the experts' rows in tiles of 2^shift rows, counted over the experts in order. Every warp that walks
+// Work over the experts' rows in tiles of some number of rows, counted over the experts in order. Every warp that walks
 // the tiles keeps the count before every eighth expert in its lanes; `off` is a copy of the offsets in shared memory. (R is
 // at most 2^24; with 64-bit rows and a division by the tile the count and the search took some 2000 clocks a kernel and 600
 // a tile.)
@@ -115,20 +130,29 @@ struct RowTiles {
   int total;
 };
 __device__ __forceinline__ int expert_row(const int32_t* off, int e, int R) { return min(max(off[e], 0), R); }
-__device__ __forceinline__ int row_tiles_of(const int32_t* off, int e, int E, int R, int shift) {
-  if (e >= E) return 0;
-  const int rows = expert_row(off, e + 1, R) - expert_row(off, e, R);
-  return rows > 0 ? (rows + (1 << shift) - 1) >> shift : 0;
-}
+// The rows of a tile: a power of two, or any number.
+struct ShiftRows {
+  int shift;
+  __device__ __forceinline__ int tiles(int rows) const { return rows > 0 ? (rows + (1 << shift) - 1) >> shift : 0; }
+  __device__ __forceinline__ int first(int tile) const { return tile << shift; }
+};
+struct AnyRows {
+  int n;
+  __device__ __forceinline__ int tiles(int rows) const {
+    return rows > 0 ? static_cast<int>(static_cast<unsigned>(rows + n - 1) / static_cast<unsigned>(n)) : 0;
+  }
+  __device__ __forceinline__ int first(int tile) const { return tile * n; }
+};
 // The counts, by one warp from the offsets in global memory: lane l's to before[l], the total to before[32].
-__device__ inline void count_row_tiles(const int32_t* offsets, int E, int R, int shift, int* before) {
+template <class Rows>
+__device__ inline void count_row_tiles(const int32_t* offsets, int E, int R, Rows of, int* before) {
   const int lane = threadIdx.x & 31;
   int o[9];
 #pragma unroll
   for (int i = 0; i < 9; ++i) o[i] = min(max(__ldg(offsets + min(lane * 8 + i, E)), 0), R);   // (past E: no rows)
   int sum = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) sum += o[i + 1] > o[i] ? (o[i + 1] - o[i] + (1 << shift) - 1) >> shift : 0;
+  for (int i = 0; i < 8; ++i) sum += of.tiles(o[i + 1] - o[i]);
   int run = sum;
 #pragma unroll
   for (int i = 1; i < 32; i <<= 1) {
@@ -139,11 +163,13 @@ __device__ inline void count_row_tiles(const int32_t* offsets, int E, int R, int
   if (lane == 31) before[32] = run;
 }
 // Tile 0 <= tile < total, by a whole warp.
-__device__ __forceinline__ RowTile find_row_tile(const RowTiles& t, const int32_t* off, int E, int R, int shift, int tile) {
+template <class Rows>
+__device__ __forceinline__ RowTile find_row_tile(const RowTiles& t, const int32_t* off, int E, int R, Rows of, int tile) {
   const int lane = threadIdx.x & 31;
   const int q = 31 - __clz(__ballot_sync(0xffffffffu, t.before <= tile));   // the last group that starts at or before it
   const int in = tile - __shfl_sync(0xffffffffu, t.before, q);
-  const int n = lane < 8 ? row_tiles_of(off, q * 8 + lane, E, R, shift) : 0;
+  const int mine = q * 8 + lane;
+  const int n = lane < 8 && mine < E ? of.tiles(expert_row(off, mine + 1, R) - expert_row(off, mine, R)) : 0;
   int run = n;
 #pragma unroll
   for (int o = 1; o < 8; o <<= 1) {
@@ -153,7 +179,7 @@ __device__ __forceinline__ RowTile find_row_tile(const RowTiles& t, const int32_
   const int src = __ffs(__ballot_sync(0xffffffffu, lane < 8 && in < run)) - 1;
   RowTile r;
   r.e = q * 8 + src;
-  r.row0 = expert_row(off, r.e, R) + ((in - __shfl_sync(0xffffffffu, run - n, src)) << shift);
+  r.row0 = expert_row(off, r.e, R) + of.first(in - __shfl_sync(0xffffffffu, run - n, src));
   r.row1 = expert_row(off, r.e + 1, R);
   return r;
 }

@@ -344,4 +344,78 @@ smoes_status smoes_expert_linear_bwd(smoes_experts P, const void* dZ, const void
   return cuda_status(e);
 }
 
+static smoes_status check_mx(smoes_dtype dtype, long long rows, int n) {
+  if ((dtype != SMOES_F32 && dtype != SMOES_BF16) || rows < 0 || n < 32 || n % 32 != 0) return SMOES_ERR_INVALID_ARG;
+  return rows > (1ll << 31) || n > kExpertWidthMax ? SMOES_ERR_UNSUPPORTED : SMOES_OK;
+}
+
+smoes_status smoes_mx_quantise(const void* X, smoes_dtype dtype, long long rows, int n, uint8_t* codes, uint8_t* scales,
+                               cudaStream_t stream) {
+  smoes_status st = check_mx(dtype, rows, n);
+  if (st != SMOES_OK || rows == 0) return st;
+  st = check_given(X, codes, scales);
+  if (st == SMOES_OK) st = check_aligned(X, codes, scales);
+  return st != SMOES_OK ? st : cuda_status(launch_mx_quantise(X, dtype == SMOES_BF16, rows * n, codes, scales, stream));
+}
+
+smoes_status smoes_mx_dequantise(const uint8_t* codes, const uint8_t* scales, long long rows, int n, smoes_dtype dtype,
+                                 void* X, cudaStream_t stream) {
+  smoes_status st = check_mx(dtype, rows, n);
+  if (st != SMOES_OK || rows == 0) return st;
+  st = check_given(codes, scales, X);
+  if (st == SMOES_OK) st = check_aligned(codes, scales, X);
+  return st != SMOES_OK ? st : cuda_status(launch_mx_dequantise(codes, scales, rows * n, dtype == SMOES_BF16, X, stream));
+}
+
+smoes_status smoes_expert_dispatch_mx(smoes_experts P, const void* X, int d, const int32_t* expert_offsets,
+                                      const int32_t* slot_row, uint8_t* codes, uint8_t* scales, cudaStream_t stream) {
+  if (!P) return SMOES_ERR_INVALID_ARG;
+  smoes_status st = check_mx(P->desc.dtype, P->R, d);
+  if (st != SMOES_OK || P->R == 0) return st;
+  st = check_given(X, expert_offsets, slot_row, codes, scales);
+  if (st == SMOES_OK) st = check_aligned(X, expert_offsets, slot_row, codes, scales);
+  if (st != SMOES_OK) return st;
+  ExpertRowsParams p = rows_params(P, d);
+  p.offsets = expert_offsets;
+  p.slot_row = slot_row;
+  p.tokens = X;
+  p.rows_out = codes;
+  return cuda_status(launch_expert_dispatch_mx(p, P->desc.dtype == SMOES_BF16, scales, stream));
+}
+
+smoes_status smoes_expert_linear_mx(smoes_experts P, const smoes_linear_mx_args* args, const int32_t* expert_offsets,
+                                    void* out, void* ws, size_t ws_bytes, cudaStream_t stream) {
+  if (!P || !args) return SMOES_ERR_INVALID_ARG;
+  const smoes_linear_mx_args& a = *args;
+  if (!known_act(a.act) || (a.gated != 0 && a.gated != 1)) return SMOES_ERR_INVALID_ARG;
+  if (P->desc.dtype != SMOES_BF16) return SMOES_ERR_UNSUPPORTED;
+  smoes_status st = check_ws(P, ws, ws_bytes);
+  if (st == SMOES_OK) st = check_mx(P->desc.dtype, P->R, a.n_in);
+  if (st == SMOES_OK) st = check_width(P, a.n_out);
+  if (st == SMOES_OK) st = check_width(P, static_cast<long long>(a.n_out) * (a.gated ? 2 : 1));
+  if (st != SMOES_OK || P->R == 0) return st;
+  st = check_given(a.X, a.X_scales, a.W, a.W_scales, expert_offsets, out);
+  if (st == SMOES_OK) st = check_aligned(a.X, a.X_scales, a.W, a.W_scales, a.bias, a.residual, expert_offsets, out);
+  if (st != SMOES_OK) return st;
+  ExpertMxParams p{};
+  p.l.E = P->desc.E;
+  p.l.n_in = a.n_in;
+  p.l.n_out = a.n_out;
+  p.l.n_z = a.n_out * (a.gated ? 2 : 1);
+  p.l.act = a.act;
+  p.l.gated = a.gated;
+  p.l.R = P->R;
+  p.l.offsets = expert_offsets;
+  p.l.X = a.X;
+  p.l.W = a.W;
+  p.l.bias = a.bias;
+  p.l.residual = a.residual;
+  p.l.out = out;
+  p.x_scale = a.X_scales;
+  p.w_scale = a.W_scales;
+  p.status = static_cast<uint32_t*>(ws);
+  p.limit_ns = P->limit_ns;
+  return cuda_status(launch_expert_mx(p, P->n_sms, stream));
+}
+
 }  // extern "C"

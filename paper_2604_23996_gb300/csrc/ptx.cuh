@@ -207,6 +207,13 @@ __device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* map, u
       ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(x), "r"(y)
       : "memory");
 }
+__device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, uint64_t* bar, int x, int y, int z) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%3, %4, %5}], [%2];"
+      ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z)
+      : "memory");
+}
 // Contiguous bulk copy global -> shared (16-byte aligned addresses, size a multiple of 16),
 // completion counted (bytes) on `bar`.
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
@@ -346,6 +353,23 @@ __device__ __forceinline__ void umma_bf16(uint32_t d_tmem, uint64_t a_desc, uint
       ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
+// D[tmem] (+)= A[smem] * B[smem] of 4-bit values in blocks of 32 with a power-of-two scale each, f32 accumulate; the
+// scales lie in tensor memory (tmem_copy_scales).
+__device__ __forceinline__ void umma_mx4(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                         uint32_t a_scales, uint32_t b_scales, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %6, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(a_scales), "r"(b_scales), "r"(accumulate)
+      : "memory");
+}
+// 32 rows of 16 bytes of shared memory to 4 columns of tensor memory, the same for each quarter of its lanes. Row l holds
+// the scale words of rows l, l + 32, l + 64 and l + 96 of an operand; a word's bytes are the scales of four blocks along the
+// depth. Runs in order with the products that the same thread issues.
+__device__ __forceinline__ void tmem_copy_scales(uint32_t taddr, uint64_t desc) {
+  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
 // Arrives once on `bar` when every tcgen05.mma issued so far by this thread has completed.
 __device__ __forceinline__ void umma_commit(uint64_t* bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];"
@@ -470,6 +494,23 @@ __host__ __device__ constexpr uint32_t idesc_bf16(int M, int N, bool a_mn_major,
          | ((b_mn_major ? 1u : 0u) << 16)           // B major-ness
          | (static_cast<uint32_t>(N >> 3) << 17)    // N / 8
          | (static_cast<uint32_t>(M >> 4) << 24);   // M / 16
+}
+
+// Instruction descriptor, 4-bit (e2m1) operands along K in memory, f32 accumulation; part: which half of the scale words
+// (the scales of 64 of the depth) the product takes.
+__host__ __device__ constexpr uint32_t idesc_mx4(int M, int N, int part) {
+  return (static_cast<uint32_t>(2 * part) << 4)     // B's scales: first byte
+         | (1u << 7)                                // A format: e2m1
+         | (1u << 10)                               // B format: e2m1
+         | (static_cast<uint32_t>(N >> 3) << 17)    // N / 8
+         | (1u << 23)                               // scales: powers of two (ue8m0)
+         | (static_cast<uint32_t>(M >> 4) << 24)    // M / 16
+         | (static_cast<uint32_t>(2 * part) << 29); // A's scales: first byte
+}
+
+// Descriptor of 32 rows of 16 bytes without a swizzle: 8-row groups 128 bytes apart.
+__device__ __forceinline__ uint64_t sdesc_scales(uint32_t saddr) {
+  return static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4) | static_cast<uint64_t>(128u >> 4) << 32 | static_cast<uint64_t>(1) << 46;
 }
 
 // Byte offset of element (row, col) inside a 128-byte-swizzled tile of 16-bit elements whose
