@@ -6,6 +6,7 @@ module fails loudly when the library has not been built: there is no fallback pa
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from typing import NamedTuple, Optional
@@ -269,11 +270,6 @@ def smoes_router_bwd_gates(plan, X, W, M, topk_idx, d_topk_w, d_gate, per_sample
                                        _p(dlogits), _p(ws), ws.numel() * ws.element_size(), _stream(stream))
 
 
-def smoes_expert_balance(plan, topk_idx, per_sample, loss_scale, loss, counts, d_gate, ws, stream=None) -> int:
-    return _lib.smoes_expert_balance(plan, _p(topk_idx), int(per_sample), float(loss_scale), _p(loss), _p(counts),
-                                     _p(d_gate), _p(ws), ws.numel() * ws.element_size(), _stream(stream))
-
-
 def smoes_bin_permute(plan, topk_idx, home, is_vision, bin_offsets, perm_token, perm_mask,
                       dispatch, expert_counts, ws, stream=None) -> int:
     return _lib.smoes_bin_permute(plan, _p(topk_idx), _p(home), _p(is_vision), _p(bin_offsets),
@@ -388,13 +384,14 @@ def mx_quantise(X, out=None, stream=None) -> Mx:
         raise ValueError(f"X: a contiguous bf16 or float32 tensor with a last dimension of 32s is wanted, got {X.dtype} {tuple(X.shape)}")
     raw, n, lead = _mx_stream(X, stream), X.shape[-1], X.shape[:-1]
     if out is None:
-        with torch.cuda.stream(stream):                 # (no change where it is None)
-            out = Mx(torch.empty(lead + (n // 2,), dtype=torch.uint8, device=X.device),
-                     torch.empty(lead + (n // 32,), dtype=torch.uint8, device=X.device))
-    q, s = _mx_checked("out", out, X.shape, X.get_device())
+        with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+            out = Mx(X.new_empty(lead + (n // 2,), dtype=torch.uint8), X.new_empty(lead + (n // 32,), dtype=torch.uint8))
+        q, s = out.codes.data_ptr(), out.scales.data_ptr()
+    else:
+        q, s = _mx_checked("out", out, X.shape, X.get_device())
     _check(_lib.smoes_mx_quantise(X.data_ptr(), SMOES_BF16 if X.dtype is torch.bfloat16 else SMOES_F32, X.numel() // n, n, q, s, raw),
            "smoes_mx_quantise")
-    return Mx(*out)
+    return out
 
 
 def mx_dequantise(x, dtype=torch.bfloat16, out=None, stream=None) -> torch.Tensor:
@@ -412,8 +409,8 @@ def mx_dequantise(x, dtype=torch.bfloat16, out=None, stream=None) -> torch.Tenso
     if dtype not in (torch.bfloat16, torch.float32):
         raise ValueError(f"dtype: bf16 or float32 is wanted, got {dtype}")
     if out is None:
-        with torch.cuda.stream(stream):
-            out = torch.empty(shape, dtype=dtype, device=codes.device)
+        with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+            out = codes.new_empty(shape, dtype=dtype)
     _check(_lib.smoes_mx_dequantise(q, s, codes.numel() * 2 // n, n, SMOES_BF16 if dtype is torch.bfloat16 else SMOES_F32,
                                     out.data_ptr(), raw), "smoes_mx_dequantise")
     return out
@@ -489,39 +486,38 @@ class Router:
                                     accumulate, dX, dlogits, self.ws, stream)
             _check(code, "smoes_router_bwd")
             return
-        self._table("d_gate", d_gate, torch.float32, d_gate.shape[0] if d_gate.dim() == 2 else -1)
-        self._table("topk_idx", idx, torch.int32, self.T, self.k)
+        self._table("d_gate", d_gate, torch.float32, (1, self.E), (self.B, self.E))
+        self._table("topk_idx", idx, torch.int32, (self.T, self.k))
         code = smoes_router_bwd_gates(self.plan, X, W, M, idx, d_topk_w, d_gate, self.B != 1 and len(d_gate) == self.B,
                                       loss_scale, dW, accumulate, dX, dlogits, self.ws, stream)
         _check(code, "smoes_router_bwd_gates")
 
-    def _table(self, name, t, dtype, rows, cols=None):
-        """A ValueError if t is not a contiguous [rows, cols] tensor of this type (cols: E; rows of experts: 1 or B)."""
-        wrong = cols is None and rows not in (1, self.B)
-        if wrong or t.dtype is not dtype or t.shape != (rows, cols or self.E) or not t.is_contiguous() or t.device != self.ws.device:
-            raise ValueError(f"{name}: a contiguous {dtype} tensor of {f'1 or {self.B}' if cols is None else rows} rows of "
-                             f"{cols or self.E} on {self.ws.device} is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    def _table(self, name, t, dtype, *shapes):
+        """Address of a contiguous tensor of this type and one of the shapes on the workspace's device; a ValueError otherwise."""
+        if t.dtype is not dtype or t.shape not in shapes or not t.is_contiguous() or t.get_device() != self.ws.get_device():
+            raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {' or '.join(map(str, shapes))} on {self.ws.device} is "
+                             f"wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        return t.data_ptr()
 
     def expert_balance(self, topk_idx=None, per_sample=True, loss_scale=1.0, loss=None, counts=None, d_gate=None,
                        stream=None):
         """Expert-level load-balance loss of the last forward, per sample or over the batch: returns (loss [1], counts
         [B or 1, E] int32, d_gate [B or 1, E]); ``backward`` takes d_gate, the gradient of loss_scale times the loss.
         topk_idx: the forward's with dropped selections set to a negative number (to be given to ``backward`` too)."""
-        idx, rows = self.topk_idx if topk_idx is None else topk_idx, self.B if per_sample else 1
-        self._table("topk_idx", idx, torch.int32, self.T, self.k)
-        out = []
-        for name, t, dtype, cols in (("loss", loss, torch.float32, 0), ("counts", counts, torch.int32, self.E),
-                                     ("d_gate", d_gate, torch.float32, self.E)):
-            if t is None:
-                with torch.cuda.stream(stream):         # (no change where it is None)
-                    t = torch.empty((rows, cols) if cols else 1, dtype=dtype, device=self.ws.device)
-            elif cols:
-                self._table(name, t, dtype, rows)
-            elif t.dtype is not dtype or t.shape != (1,) or t.device != self.ws.device:
-                raise ValueError(f"loss: a float32 tensor of one value on {self.ws.device} is wanted")
-            out.append(t)
-        _check(smoes_expert_balance(self.plan, idx, per_sample, loss_scale, *out, self.ws, stream), "smoes_expert_balance")
-        return tuple(out)
+        f32, i32, shape, ws = torch.float32, torch.int32, (self.B if per_sample else 1, self.E), self.ws
+        idx = self._table("topk_idx", self.topk_idx if topk_idx is None else topk_idx, i32, (self.T, self.k))
+        index = ws.get_device()
+        if index != torch._C._cuda_getDevice() or (stream is not None and stream.device_index != index):
+            raise ValueError(f"device: the router is on cuda:{index}; the current device, and a stream given, have to be too")
+        with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+            loss = torch.empty(1, dtype=f32, device=ws.device) if loss is None else loss
+            counts = torch.empty(shape, dtype=i32, device=ws.device) if counts is None else counts
+            d_gate = torch.empty(shape, dtype=f32, device=ws.device) if d_gate is None else d_gate
+        _check(_lib.smoes_expert_balance(
+            self.plan, idx, per_sample, loss_scale, self._table("loss", loss, f32, (1,)), self._table("counts", counts, i32, shape),
+            self._table("d_gate", d_gate, f32, shape), ws.data_ptr(), ws.numel(),
+            torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream), "smoes_expert_balance")
+        return loss, counts, d_gate
 
     def permute(self, is_vision=None, home=None, topk_idx=None, stream=None):
         code = smoes_bin_permute(self.plan, self.topk_idx if topk_idx is None else topk_idx, home,
@@ -819,10 +815,7 @@ class LayerNorm(_Calls):
             raise ValueError("sum_out: without a residual the sum is X, and none is written")
         S = X if residual is None else self._new(sum_out, shape, dt, stream)
         out = self._new(out, shape, dt, stream)
-        mean = rstd = None
-        if stats:
-            both = self._new(None, (2, (self.T + 3) // 4 * 4), f32, stream)
-            mean, rstd = both[0, :self.T], both[1, :self.T]
+        mean, rstd = (self._new(None, (self.T,), f32, stream), self._new(None, (self.T,), f32, stream)) if stats else (None, None)
         _check(_lib.smoes_norm_fwd(self.plan, x, r, wp, bp, None if residual is None else S.data_ptr(), out.data_ptr(),
                                    _ptr(mean), _ptr(rstd), raw), "smoes_norm_fwd")
         return out, S, mean, rstd

@@ -166,11 +166,13 @@ __global__ void __launch_bounds__(kThreads) k_norm_fwd(const NormParams p) {
   }
 }
 
-// kRows rows of a group of kTpr threads are in flight at a time.
-template <class T, int kTpr, int kWords, int kRows, int kThreads>
-__global__ void __launch_bounds__(kThreads, kThreads <= 256 ? 2 : 1) k_norm_bwd(const NormParams p) {
+// A round of a block is kRows rows of each of its groups of kTpr threads; the next round's rows are on their way while the
+// block works on this one's. Blocks of 1024 threads have 64 registers each and neither fetch ahead nor keep the weight (kLean).
+template <class T, int kTpr, int kWords, int kRows, int kThreads, int kBlocks>
+__global__ void __launch_bounds__(kThreads, kBlocks) k_norm_bwd(const NormParams p) {
   constexpr int N = Pack<T>::N;
   constexpr int kGroups = kThreads / kTpr;
+  constexpr bool kLean = kThreads > 512;
   __shared__ float scratch[2][kThreads / 32 * 2 * kRows];
   extern __shared__ float join[];                // [kGroups][2][kTpr * kWords * N] where there are more groups than one
   pdl_wait();
@@ -178,48 +180,68 @@ __global__ void __launch_bounds__(kThreads, kThreads <= 256 ? 2 : 1) k_norm_bwd(
   const int c = threadIdx.x % kTpr, grp = threadIdx.x / kTpr;
   const int r0 = static_cast<int>(static_cast<long long>(blockIdx.x) * p.T / gridDim.x);
   const int r1 = static_cast<int>(static_cast<long long>(blockIdx.x + 1) * p.T / gridDim.x);
-  float dw[kWords][N], db[kWords][N], w[kWords][N];
+  float dw[kWords][N], db[kWords][N], held[kWords][N];
+  auto weight = [&](int u, float (&w)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = 0.f;
+    if (c + u * kTpr < p.words) load_floats<N>(p.w + (c + u * kTpr) * N, w);
+  };
 #pragma unroll
   for (int u = 0; u < kWords; ++u) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) dw[u][i] = db[u][i] = w[u][i] = 0.f;
-    if (c + u * kTpr < p.words) load_floats<N>(p.w + (c + u * kTpr) * N, w[u]);
+    for (int i = 0; i < N; ++i) dw[u][i] = db[u][i] = 0.f;
+    if (!kLean) weight(u, held[u]);
   }
-  int turn = 0;
-  for (int base = r0; base < r1; base += kGroups * kRows, turn ^= 1) {
-    uint4 dy[kRows][kWords], x[kRows][kWords];
+  struct In {
+    uint4 dy[kRows][kWords], x[kRows][kWords], ds[kRows][kWords];
     float mean[kRows], rstd[kRows];
+  };
+  auto load = [&](int base, In& in) {
 #pragma unroll
     for (int q = 0; q < kRows; ++q) {
       const int t = base + q * kGroups + grp;
       const bool row = t < r1;
-      mean[q] = row ? __ldg(p.mean + t) : 0.f;
-      rstd[q] = row ? __ldg(p.rstd + t) : 0.f;
+      in.mean[q] = row ? __ldg(p.mean + t) : 0.f;
+      in.rstd[q] = row ? __ldg(p.rstd + t) : 0.f;
 #pragma unroll
       for (int u = 0; u < kWords; ++u) {
         const int i = c + u * kTpr;
-        dy[q][u] = x[q][u] = make_uint4(0u, 0u, 0u, 0u);
+        const long long at = static_cast<long long>(t) * p.words + i;
+        in.dy[q][u] = in.x[q][u] = in.ds[q][u] = make_uint4(0u, 0u, 0u, 0u);
         if (row && i < p.words) {
-          dy[q][u] = __ldg(static_cast<const uint4*>(p.dY) + static_cast<long long>(t) * p.words + i);
-          x[q][u] = __ldg(static_cast<const uint4*>(p.X) + static_cast<long long>(t) * p.words + i);
+          in.dy[q][u] = __ldg(static_cast<const uint4*>(p.dY) + at);
+          in.x[q][u] = __ldg(static_cast<const uint4*>(p.X) + at);
+          if (!kLean && p.residual) in.ds[q][u] = __ldg(static_cast<const uint4*>(p.residual) + at);
         }
       }
     }
+  };
+  constexpr int kStep = kGroups * kRows;
+  int turn = 0;
+  In nx;
+  if (!kLean) load(r0, nx);
+#pragma unroll 1
+  for (int base = r0; base < r1; base += kStep, turn ^= 1) {
+    if (kLean) load(base, nx);
+    const In in = nx;
+    if (!kLean && base + kStep < r1) load(base + kStep, nx);
     float sums[2 * kRows];
 #pragma unroll
     for (int q = 0; q < kRows; ++q) {
       float a0 = 0.f, a1 = 0.f;
 #pragma unroll
       for (int u = 0; u < kWords; ++u) {
-        float g[N], h[N];
-        Pack<T>::unpack(dy[q][u], g);
-        Pack<T>::unpack(x[q][u], h);
+        float g[N], h[N], w[N];
+        if (kLean) weight(u, w);
+        Pack<T>::unpack(in.dy[q][u], g);
+        Pack<T>::unpack(in.x[q][u], h);
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-          h[j] = (h[j] - mean[q]) * rstd[q];
+          if (!kLean) w[j] = held[u][j];
+          h[j] = (h[j] - in.mean[q]) * in.rstd[q];
           dw[u][j] = fmaf(g[j], h[j], dw[u][j]);
           db[u][j] += g[j];
-          const float a = g[j] * w[u][j];
+          const float a = g[j] * w[j];
           a0 += a;
           a1 = fmaf(a, h[j], a1);
         }
@@ -238,14 +260,16 @@ __global__ void __launch_bounds__(kThreads, kThreads <= 256 ? 2 : 1) k_norm_bwd(
         const int i = c + u * kTpr;
         if (i < p.words) {
           const long long at = static_cast<long long>(t) * p.words + i;
-          float g[N], h[N], ds[N];
-          Pack<T>::unpack(dy[q][u], g);
-          Pack<T>::unpack(x[q][u], h);
-          Pack<T>::unpack(p.residual ? __ldg(static_cast<const uint4*>(p.residual) + at) : make_uint4(0u, 0u, 0u, 0u), ds);
+          float g[N], h[N], ds[N], w[N];
+          if (kLean) weight(u, w);
+          Pack<T>::unpack(in.dy[q][u], g);
+          Pack<T>::unpack(in.x[q][u], h);
+          Pack<T>::unpack(!kLean ? in.ds[q][u] : p.residual ? __ldg(static_cast<const uint4*>(p.residual) + at) : make_uint4(0u, 0u, 0u, 0u), ds);
 #pragma unroll
           for (int j = 0; j < N; ++j) {
-            const float hj = (h[j] - mean[q]) * rstd[q];
-            g[j] = fmaf(rstd[q], fmaf(g[j], w[u][j], -ma) - hj * mah, ds[j]);
+            if (!kLean) w[j] = held[u][j];
+            const float hj = (h[j] - in.mean[q]) * in.rstd[q];
+            g[j] = fmaf(in.rstd[q], fmaf(g[j], w[j], -ma) - hj * mah, ds[j]);
           }
           static_cast<uint4*>(p.Y)[at] = Pack<T>::pack(g);
         }
@@ -285,20 +309,27 @@ __global__ void __launch_bounds__(kThreads, kThreads <= 256 ? 2 : 1) k_norm_bwd(
   }
 }
 
-// dw and db from the blocks' partials: eight slices of the blocks, each added in order, then the slices in order.
-constexpr int kSumSlices = 8, kSumCols = 32;
+// dw and db from the blocks' partials: 32 slices of the blocks, each added in order, then the slices four by eight.
+constexpr int kSumSlices = 32, kSumCols = 8;
+
+__device__ __forceinline__ void add4(float4& a, const float4& v) {
+  a.x += v.x;
+  a.y += v.y;
+  a.z += v.z;
+  a.w += v.w;
+}
 
 __global__ void __launch_bounds__(kSumSlices * kSumCols) k_norm_sum(const NormParams p) {
   __shared__ float4 slice[kSumSlices][kSumCols];
   pdl_wait();
   pdl_trigger();
   const int col = threadIdx.x % kSumCols, sl = threadIdx.x / kSumCols;
-  const int n = p.d / 2;                         // float4 columns of [dw | db]
+  const int n = p.d / 2;                         // float4 columns of [dw | db], a multiple of 4
   const int i = blockIdx.x * kSumCols + col;
   const int b0 = sl * p.blocks / kSumSlices, b1 = (sl + 1) * p.blocks / kSumSlices;
   float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
   if (i < n) {
-    constexpr int kU = 8;
+    constexpr int kU = 10;                       // all of a slice in flight (304 blocks)
     for (int b = b0; b < b1; b += kU) {
       float4 v[kU];
 #pragma unroll
@@ -307,40 +338,36 @@ __global__ void __launch_bounds__(kSumSlices * kSumCols) k_norm_sum(const NormPa
         if (b + u < b1) v[u] = __ldcg(reinterpret_cast<const float4*>(p.part) + static_cast<long long>(b + u) * n + i);
       }
 #pragma unroll
-      for (int u = 0; u < kU; ++u) {
-        a.x += v[u].x;
-        a.y += v[u].y;
-        a.z += v[u].z;
-        a.w += v[u].w;
-      }
+      for (int u = 0; u < kU; ++u) add4(a, v[u]);
     }
   }
   slice[sl][col] = a;
   __syncthreads();
+  if (sl < 4) {
+    a = slice[sl * 8][col];
+#pragma unroll
+    for (int q = 1; q < 8; ++q) add4(a, slice[sl * 8 + q][col]);
+  }
+  __syncthreads();
+  if (sl < 4) slice[sl][col] = a;
+  __syncthreads();
   if (sl != 0 || i >= n) return;
 #pragma unroll
-  for (int q = 1; q < kSumSlices; ++q) {
-    const float4 v = slice[q][col];
-    a.x += v.x;
-    a.y += v.y;
-    a.z += v.z;
-    a.w += v.w;
-  }
+  for (int q = 1; q < 4; ++q) add4(a, slice[q][col]);
   float* to = i < p.d / 4 ? p.dw : p.db;
   if (!to) return;
   float4* out = reinterpret_cast<float4*>(to) + (i < p.d / 4 ? i : i - p.d / 4);
   if (p.accumulate) {
     const float4 o = *out;
-    a.x += o.x;
-    a.y += o.y;
-    a.z += o.z;
-    a.w += o.w;
+    a = make_float4(a.x + o.x, a.y + o.y, a.z + o.z, a.w + o.w);
   }
   *out = a;
 }
 
-// Blocks of the backward: what the device holds at once, fewer where a block would have less than one round of rows.
-int norm_blocks(int n_sms, int T) { return std::max(1, std::min(3 * n_sms, (T + 3) / 4)); }
+// Blocks of the backward: what the device holds at once (with three or four per SM the second round is a short one: 16384 x 2048
+// 53.4 and 47.6 us instead of 44.7), fewer where the partials would weigh against the rows (4091 x 512 in fp32 with the sums over
+// the blocks: 8.6 us with one block per SM, 9.7 with two).
+int norm_blocks(int n_sms, int T) { return T >= 32 * n_sms ? 2 * n_sms : std::max(1, std::min(n_sms, (T + 7) / 8)); }
 
 template <class T, int kTpr, int kWords, int kThreads>
 cudaError_t forward(const NormParams& p, cudaStream_t s) {
@@ -358,10 +385,10 @@ cudaError_t launch_forward(const NormParams& p, int n_sms, cudaStream_t s) {
   return forward<T, 256, 8, 256>(p, s);
 }
 
-template <class T, int kTpr, int kWords, int kRows, int kThreads>
+template <class T, int kTpr, int kWords, int kRows, int kThreads, int kBlocks = 2>
 cudaError_t backward(NormParams p, cudaStream_t s) {
   const size_t smem = kThreads > kTpr ? sizeof(float) * 2 * (kThreads / kTpr) * kTpr * kWords * Pack<T>::N : 0;
-  return launch_pdl(k_norm_bwd<T, kTpr, kWords, kRows, kThreads>, dim3(p.blocks), dim3(kThreads), smem, s, p);
+  return launch_pdl(k_norm_bwd<T, kTpr, kWords, kRows, kThreads, kBlocks>, dim3(p.blocks), dim3(kThreads), smem, s, p);
 }
 
 template <class T>
@@ -370,10 +397,10 @@ cudaError_t launch_backward(const NormParams& p, cudaStream_t s) {
   if (p.words <= 32) return backward<T, 32, 1, 2, 256>(p, s);
   if (p.words <= 64) return backward<T, 64, 1, 2, 256>(p, s);
   if (p.words <= 128) return backward<T, 128, 1, 2, 256>(p, s);
-  if (p.words <= 256) return backward<T, 256, 1, 2, 256>(p, s);
+  if (p.words <= 256) return backward<T, 128, 2, 1, 256>(p, s);
   if (p.words <= 512) return backward<T, 256, 2, 1, 256>(p, s);
-  if (p.words <= 1024) return backward<T, 512, 2, 1, 512>(p, s);
-  return backward<T, 1024, 2, 1, 1024>(p, s);
+  if (p.words <= 1024) return backward<T, 512, 2, 1, 512, 1>(p, s);
+  return backward<T, 1024, 2, 1, 1024, 1>(p, s);
 }
 
 bool aligned(const void* a) { return (reinterpret_cast<uintptr_t>(a) & 15u) == 0; }
