@@ -274,7 +274,8 @@ bool smoes::encode_f32(CUtensorMap* m, const void* ptr, int rank, const uint64_t
 }
 bool smoes::encode_u8(CUtensorMap* m, const void* ptr, int rank, const uint64_t* dims, const uint64_t* strides,
                       const uint32_t* box) {
-  return encode_tiled(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, CU_TENSOR_MAP_SWIZZLE_128B, ptr, rank, dims, strides, box);
+  const CUtensorMapSwizzle swizzle = box[0] == 32 ? CU_TENSOR_MAP_SWIZZLE_32B : CU_TENSOR_MAP_SWIZZLE_128B;
+  return encode_tiled(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, swizzle, ptr, rank, dims, strides, box);
 }
 
 extern "C" {

@@ -2,13 +2,18 @@
 // rows:  z = W_e x_r + b_e,  out = act(z) (or act(g) u of z = [g | u]) + residual, out in bf16.
 //
 // Both operands hold pairs of e2m1 codes along the depth and a power-of-two scale for every 32 of it; the tensor cores
-// multiply by both scales. A CTA forms a tile of 128 features (along M) by up to kRowsMost rows (along N), in blocks of
-// 256 of the depth: 128 bytes a row, in the copy engine's swizzle, as for 64 bf16 values.
+// multiply by both scales. A pair of CTAs forms a tile of 256 features (along M, 128 in each CTA) by up to kRowsMost rows (along
+// N), in blocks of 256 of the depth: 128 bytes a row, in the copy engine's swizzle, as for 64 bf16 values. Each CTA loads its half
+// of both operands; the first CTA issues the products of both. (One CTA a tile of 128 x 192 read every operand byte of the
+// tile for itself: 98304 x 2048 x 2048 took 190 us without an epilogue, at 15.5 TB/s from L2.)
 //
-// Scales lie in memory as they are given, [rows][n_in / 32] bytes. The tensor cores want them in tensor memory, in lane
-// r % 32 and column r / 32 of row r, with four blocks' bytes in a word. A warp loads the 8 bytes of a block of 256 of four rows
-// 32 apart a lane, writes their words side by side (16 bytes a lane: no bank conflicts) and hands them to the MMA issuer, which
-// copies them to tensor memory ahead of the products.
+// Scales lie in memory as they are given, [rows][n_in / 32] bytes. The tensor cores want them in tensor memory: of a CTA's own
+// features, and of all of the tile's rows in both CTAs. The 32 bytes of four blocks of every row (a round) come to shared memory
+// by the copy engine, or where rows are not whole 16-byte words by two copying warps; four warps of each CTA, one for each
+// quarter of its tensor memory's lanes, read four rows 32 apart a lane and store a block's words to one of four sets of
+// columns, which the MMA issuer waits for and gives back. (Not kept, 98304 x 2048 x 2048 gated: words through shared memory
+// and the tensor cores' own copy, the second CTA's released at cluster scope, 1 us a block: 237 us; the storing warps copying
+// for themselves, 1000 clocks a round: 231 us.)
 //
 // Ragged edges and gated layers are those of expert_gemm.cu: rows of the next expert inside a tile are other columns of
 // D and are not stored; features past the expert's weights and a depth that ends inside a block are zeros of the maps (their scales
@@ -22,25 +27,33 @@ namespace smoes {
 namespace {
 
 constexpr int kMxScaleWarps = 4;
-constexpr int kMxEpi = 2 + kMxScaleWarps;        // first epilogue warp; 0 producer, 1 MMA issuer, then the scales' warps
+constexpr int kMxCopyWarps = 2;
+constexpr int kMxCopy = 2 + kMxScaleWarps;       // 0 producer, 1 MMA issuer, then the scales' warps
+constexpr int kMxEpi = kMxCopy + kMxCopyWarps;   // first epilogue warp
 constexpr int kMxEpiWarps = 4 * kGemmGroups;
 constexpr int kMxGemmThreads = 32 * (kMxEpi + kMxEpiWarps);
 constexpr int kMxBlock = 256;                    // depth of a block: 128 bytes
 constexpr int kMxA = 128 * 128;                  // a block's bytes of the features
-constexpr int kRowsMost = 192;
+constexpr int kRowsMost = 208;                   // (two accumulators and the scales fill the 512 columns)
 constexpr int kMxStagesMost = 8;
-constexpr uint32_t kMxRing = 4 * (kMxA + kRowsMost * 128);
-constexpr uint32_t kMxScaleStage = 2 * 512 + 2 * 1024;   // of the features and of up to 256 rows: two words each
+constexpr uint32_t kMxRing = 5 * (kMxA + kRowsMost * 64);
+constexpr int kMxSets = 4;                       // blocks' scales in tensor memory
+constexpr uint32_t kMxSetCols = 24;              // two words of 4 columns of the features and 8 of the rows
+constexpr uint32_t kMxScaleCols = 2 * kRowsMost; // behind the accumulators
+constexpr int kMxGroups = 4 + (kRowsMost + 31) / 32;     // of 32 features or rows
+constexpr int kMxRound = 4;                      // blocks whose scales are copied at a time: 32 bytes a row
+constexpr int kMxSlots = 3;
+constexpr uint32_t kMxSlot = kMxGroups * 32 * 32;
 constexpr uint32_t kMxStaging = 8192;            // one epilogue group's output boxes: two chunks
-constexpr uint32_t kMxSmem = 1024 + kMxRing + kMxStagesMost * kMxScaleStage + kGemmGroups * kMxStaging + kBarBytes + 4 * (kExpertsMax + 1);
+constexpr uint32_t kMxSmem = 1024 + kMxRing + kMxSlots * kMxSlot + kGemmGroups * kMxStaging + kBarBytes + 4 * (kExpertsMax + 1);
+static_assert(kMxScaleCols + kMxSets * kMxSetCols <= 512, "tensor memory");
 static_assert(kMxSmem <= 227 * 1024, "shared memory of a CTA");
-constexpr uint32_t kMxScaleCols = 2 * kRowsMost;  // tensor memory: two accumulators, then two blocks' scales
-constexpr uint32_t kMxScaleSet = 24;             // 2 words x 4 columns of the features, 2 x 8 of the rows
-
 struct MxBars {
-  uint64_t full[kMxStagesMost];                  // the operands
-  uint64_t scales[kMxStagesMost];                // their scales
+  uint64_t full[kMxStagesMost];                  // operands of both CTAs (first CTA's)
   uint64_t empty[kMxStagesMost];
+  uint64_t scales[kMxSets];                      // scales of both CTAs (first CTA's)
+  uint64_t scales_empty[kMxSets];
+  uint64_t slot_full[kMxSlots], slot_empty[kMxSlots];
   uint64_t acc_full[2], acc_empty[2];
   uint32_t tmem;
   int abort;
@@ -48,60 +61,97 @@ struct MxBars {
 };
 static_assert(sizeof(MxBars) <= kBarBytes, "barriers");
 
-// Bytes [at, at + 8) of a row of n scales; what lies past the row is 0.
-__device__ __forceinline__ uint2 load_scales(const uint8_t* row, int at, int n) {
-  if (row == nullptr || at >= n) return make_uint2(0u, 0u);
-  if ((n & 7) == 0) return __ldg(reinterpret_cast<const uint2*>(row + at));
-  uint32_t w[2] = {0u, 0u};
+// Bytes [at, at + 16) of a row of n scales to shared memory, zeros for what lies past the row (row null: for all of them).
+// Rows of whole 16, 8 or 4 bytes are copied; others (n_in not a multiple of 128) are put together from the aligned words that
+// hold them.
+__device__ __forceinline__ void fetch_scales(uint32_t dst, const uint8_t* row, int at, int n, const uint8_t* any) {
+  const int there = row == nullptr ? 0 : min(max(n - at, 0), 16);
+  const uint8_t* src = there > 0 ? row + at : any;
+  if ((n & 15) == 0) {
+    cp_async<16>(dst, src, there);
+  } else if ((n & 7) == 0) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (at + i < n) w[i >> 2] |= static_cast<uint32_t>(__ldg(row + at + i)) << (8 * (i & 3));
-  return make_uint2(w[0], w[1]);
+    for (int i = 0; i < 16; i += 8) cp_async<8>(dst + i, there > i ? src + i : any, min(max(there - i, 0), 8));
+  } else if ((n & 3) == 0) {
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) cp_async<4>(dst + i, there > i ? src + i : any, min(max(there - i, 0), 4));
+  } else {
+    const int skew = static_cast<int>(reinterpret_cast<uintptr_t>(src) & 3u);
+    const uint32_t* words = reinterpret_cast<const uint32_t*>(src - skew);
+    uint32_t w[5], out[4];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) w[i] = 4 * i < skew + there ? __ldg(words + i) : 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int left = there - 4 * i;            // bytes of this word that the row has
+      out[i] = __funnelshift_r(w[i], w[i + 1], 8 * skew);
+      if (left < 4) out[i] &= left > 0 ? (1u << (8 * left)) - 1u : 0u;
+    }
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(out[0]), "r"(out[1]), "r"(out[2]), "r"(out[3]) : "memory");
+  }
+}
+// Shared address of half h (16 bytes) of row r in a slot; the halves of every other four rows change places (bank conflicts).
+__device__ __forceinline__ uint32_t scale_at(uint32_t slot, int r, int h) {
+  return slot + static_cast<uint32_t>(r) * 32u + static_cast<uint32_t>((h ^ (r >> 2)) & 1) * 16u;
 }
 
 template <int kAct, bool kGated>
-__global__ void __launch_bounds__(kMxGemmThreads, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMxGemmThreads, 1)
 k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
-            const __grid_constant__ CUtensorMap tmOut, const ExpertMxParams p) {
+            const __grid_constant__ CUtensorMap tmB16, const __grid_constant__ CUtensorMap tmScaleA,
+            const __grid_constant__ CUtensorMap tmScaleB, const __grid_constant__ CUtensorMap tmOut, const ExpertMxParams p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   uint8_t* scale_ring = smem + kMxRing;
-  uint8_t* staging = scale_ring + kMxStagesMost * kMxScaleStage;
+  uint8_t* staging = scale_ring + kMxSlots * kMxSlot;
   MxBars& bars = *reinterpret_cast<MxBars*>(staging + kGemmGroups * kMxStaging);
   int32_t* off = reinterpret_cast<int32_t*>(staging + kGemmGroups * kMxStaging + kBarBytes);   // [E + 1] offsets
   const ExpertLinearParams& l = p.l;
   const int warp = warp_index(), lane = threadIdx.x & 31;
   const int R = static_cast<int>(l.R);
+  const uint32_t rank = cluster_rank();
+  const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
   const AnyRows rows_of{p.tile_rows};
-  const uint32_t stage_bytes = kMxA + static_cast<uint32_t>(p.tile_rows) * 128u;
+  // a stage: the CTA's 128 features, then its half of the widest tile
+  const uint32_t stage_bytes = kMxA + static_cast<uint32_t>(p.tile_rows) * 64u;
   const int n_stages = min(kMxStagesMost, static_cast<int>(kMxRing / stage_bytes));
   auto stage_a = [&](int s) { return smem + s * stage_bytes; };
   auto stage_b = [&](int s) { return smem + s * stage_bytes + kMxA; };
-  auto stage_scales = [&](int s) { return scale_ring + s * kMxScaleStage; };
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < n_stages; ++i) {
-      mbar_init(&bars.full[i], 1);
-      mbar_init(&bars.scales[i], 1);
+      mbar_init(&bars.full[i], 2);
       mbar_init(&bars.empty[i], 1);
+    }
+    for (int i = 0; i < kMxSets; ++i) {
+      mbar_init(&bars.scales[i], 2 * kMxScaleWarps);
+      mbar_init(&bars.scales_empty[i], 1);
+    }
+    for (int i = 0; i < kMxSlots; ++i) {
+      mbar_init(&bars.slot_full[i], p.scale_maps ? 1 : 32 * kMxCopyWarps);
+      mbar_init(&bars.slot_empty[i], kMxScaleWarps);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&bars.acc_full[i], 1);
-      mbar_init(&bars.acc_empty[i], kMxEpiWarps);
+      mbar_init(&bars.acc_empty[i], 2 * kMxEpiWarps);
     }
     bars.abort = 0;
     fence_mbar_init();
     tma_prefetch_desc(&tmA);
     tma_prefetch_desc(&tmB);
+    tma_prefetch_desc(&tmB16);
+    tma_prefetch_desc(&tmScaleA);
+    tma_prefetch_desc(&tmScaleB);
     tma_prefetch_desc(&tmOut);
   }
-  if (warp == 2) tmem_alloc(&bars.tmem, 512);
+  if (warp == 2) tmem_alloc_pair(&bars.tmem, 512);
   pdl_wait();
   pdl_trigger();
   if (warp == 3) count_row_tiles(l.offsets, l.E, R, rows_of, bars.before);
   for (int e = threadIdx.x; e <= l.E; e += kMxGemmThreads) off[e] = __ldg(l.offsets + e);
   tc_fence_before();
   __syncthreads();
+  cluster_sync();                                // both CTAs' barriers are ready before anything arrives on them
   tc_fence_after();
   const RowTiles rt{bars.before[lane], bars.before[32]};
   const int n_total = rt.total * p.m_tiles;
@@ -129,120 +179,175 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
     int st = 0;
     uint32_t ph = 0;
     bool ok = true;
-    Tile next = tile_at(blockIdx.x);
-    for (int tile = blockIdx.x; ok && tile < n_total; tile += gridDim.x) {
+    Tile next = tile_at(pair);
+    for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
       const Tile t = next;
-      const int n = (t.rows + 31) & ~31;
+      const int half = min((t.rows + 31) & ~31, p.tile_rows) / 2;
       for (int kb = 0; kb < blocks; ++kb) {
         if (!warp_wait(&bars.empty[st], ph ^ 1, wc)) { ok = false; break; }
         if (elect_one()) {
           uint8_t* a = stage_a(st);
           uint8_t* b = stage_b(st);
-          mbar_arrive_expect_tx(&bars.full[st], kMxA + n * 128u);
+          const uint32_t bar = peer_smem(&bars.full[st], 0);
+          mbar_arrive_expect_tx_peer(bar, kMxA + half * 128u);
           const int x = kb * 128;
           if (kGated) {
-            const int f0 = t.m * 64;
+            const int f0 = t.m * 128 + static_cast<int>(rank) * 64;
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-              tma_load_3d(a + i * 2048, &tmA, &bars.full[st], x, (i & 1) * l.n_out + f0 + (i >> 1) * 16, t.e);
+              tma_load_3d_pair(a + i * 2048, &tmA, bar, x, (i & 1) * l.n_out + f0 + (i >> 1) * 16, t.e);
           } else {
-            tma_load_3d(a, &tmA, &bars.full[st], x, t.m * 128, t.e);
+            tma_load_3d_pair(a, &tmA, bar, x, t.m * 256 + static_cast<int>(rank) * 128, t.e);
           }
-          for (int i = 0; i < n; i += 32) tma_load_2d(b + i * 128, &tmB, &bars.full[st], x, t.row0 + i);
+          const int r0 = t.row0 + static_cast<int>(rank) * half;
+          if (2 * half == p.tile_rows) {
+            tma_load_2d_pair(b, &tmB, bar, x, r0);
+          } else {
+            for (int i = 0; i < half; i += 16) tma_load_2d_pair(b + i * 128, &tmB16, bar, x, r0 + i);
+          }
         }
         __syncwarp();
-        if (kb == 0) next = tile_at(tile + gridDim.x);
+        if (kb == 0) next = tile_at(tile + n_pairs);
         if (++st == n_stages) { st = 0; ph ^= 1; }
       }
     }
-    for (int i = 0; ok && i < n_stages; ++i) {   // every stage given back: no copy or product is in flight at the end
+    // every stage given back: no commit of the first CTA is still on its way to this one when it ends
+    for (int i = 0; ok && i < n_stages; ++i) {
       ok = warp_wait(&bars.empty[st], ph ^ 1, wc);
       if (++st == n_stages) { st = 0; ph ^= 1; }
     }
-  } else if (warp == 1) {
+  } else if (warp == 1 && rank == 0) {
     // ----------------------------------------------------------------------------- MMA issuer
     int st = 0, acc = 0, set = 0;
-    uint32_t ph = 0, aph = 0;
+    uint32_t ph = 0, aph = 0, sph = 0;
     bool ok = true;
-    Tile next = tile_at(blockIdx.x);
-    for (int tile = blockIdx.x; ok && tile < n_total; tile += gridDim.x) {
+    Tile next = tile_at(pair);
+    for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
       const Tile t = next;
-      const int n = (t.rows + 31) & ~31;
+      const int n = min((t.rows + 31) & ~31, p.tile_rows);
       if (!warp_wait(&bars.acc_empty[acc], aph ^ 1, wc)) break;
       tc_fence_after();
       const uint32_t d = tmem + acc * kRowsMost;
       for (int kb = 0; kb < blocks; ++kb) {
-        if (!warp_wait(&bars.full[st], ph, wc) || !warp_wait(&bars.scales[st], ph, wc)) { ok = false; break; }
+        if (!warp_wait(&bars.scales[set], sph, wc) || !warp_wait(&bars.full[st], ph, wc)) { ok = false; break; }
         tc_fence_after();
         if (elect_one()) {
-          const uint32_t a = smem_u32(stage_a(st)), b = smem_u32(stage_b(st)), sc = smem_u32(stage_scales(st));
-          const uint32_t sa = tmem + kMxScaleCols + set * kMxScaleSet, sb = sa + 8;
-#pragma unroll
-          for (int w = 0; w < 2; ++w) {
-            tmem_copy_scales(sa + 4 * w, sdesc_scales(sc + 512 * w));
-            tmem_copy_scales(sb + 8 * w, sdesc_scales(sc + 1024 + 1024 * w));
-            if (n > 128) tmem_copy_scales(sb + 8 * w + 4, sdesc_scales(sc + 1024 + 1024 * w + 512));
-          }
+          const uint32_t a = smem_u32(stage_a(st)), b = smem_u32(stage_b(st));
+          const uint32_t sa = tmem + kMxScaleCols + set * kMxSetCols;
 #pragma unroll
           for (int s = 0; s < 4; ++s)              // 64 of the depth an instruction
-            umma_mx4(d, sdesc_sw128(a + s * 32, 16, 1024), sdesc_sw128(b + s * 32, 16, 1024), idesc_mx4(128, n, s & 1),
-                     sa + 4 * (s >> 1), sb + 8 * (s >> 1), kb > 0 || s > 0);
-          umma_commit(&bars.empty[st]);
-          if (kb == blocks - 1) umma_commit(&bars.acc_full[acc]);
+            umma_mx4_pair(d, sdesc_sw128(a + s * 32, 16, 1024), sdesc_sw128(b + s * 32, 16, 1024), idesc_mx4(256, n, s & 1),
+                          sa + 12 * (s >> 1), sa + 12 * (s >> 1) + 4, kb > 0 || s > 0);
+          umma_commit_pair(&bars.empty[st]);
+          umma_commit_pair(&bars.scales_empty[set]);
+          if (kb == blocks - 1) umma_commit_pair(&bars.acc_full[acc]);
         }
         __syncwarp();
-        if (kb == 0) next = tile_at(tile + gridDim.x);
-        set ^= 1;
+        if (kb == 0) next = tile_at(tile + n_pairs);
+        if (++set == kMxSets) { set = 0; sph ^= 1; }
         if (++st == n_stages) { st = 0; ph ^= 1; }
       }
       if (++acc == 2) { acc = 0; aph ^= 1; }
     }
-  } else if (warp < kMxEpi) {
-    // ------------------------------------------------------------------------------- scales
-    const int n_scales = l.n_in / 32;
-    int st = 0, turn = warp - 2;                 // blocks until this warp's next one
-    uint32_t ph = 0;
+  } else if (warp >= 2 && warp < kMxCopy) {
+    // ------------------------------------------------------------------- scales to tensor memory
+    const uint32_t slots = smem_u32(scale_ring);
+    const uint32_t cols = tmem + (static_cast<uint32_t>(32 * (warp & 3)) << 16) + kMxScaleCols;
+    int slot = 0, set = 0;
+    uint32_t lph = 0, sph = 0;
     bool ok = true;
-    for (int tile = blockIdx.x; ok && tile < n_total; tile += gridDim.x) {
-      const Tile t = tile_at(tile);
-      const int groups = (t.rows + 31) >> 5;
-      const uint8_t* row[4 + kRowsMost / 32];    // of the lane's features and rows
+    for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
+      for (int k0 = 0; ok && k0 < blocks; k0 += kMxRound) {
+        ok = warp_wait(&bars.slot_full[slot], lph, wc);
+        const uint32_t from = slots + slot * kMxSlot;
+        for (int h = 0; ok && h < 2 && k0 + 2 * h < blocks; ++h) {
+          uint32_t v[kMxGroups][4];              // lane's row of each group, two blocks' words
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int r = g * 32 + lane;
-        const int f = kGated ? ((r >> 4) & 1) * l.n_out + t.m * 64 + (r >> 5) * 16 + (r & 15) : t.m * 128 + r;
-        row[g] = f < l.n_z ? p.w_scale + (static_cast<long long>(t.e) * l.n_z + f) * n_scales : nullptr;
-      }
+          for (int g = 0; g < kMxGroups; ++g)
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(v[g][0]), "=r"(v[g][1]), "=r"(v[g][2]), "=r"(v[g][3]) : "r"(scale_at(from, g * 32 + lane, h)));
 #pragma unroll
-      for (int g = 0; g < kRowsMost / 32; ++g) {
-        const int r = t.row0 + g * 32 + lane;
-        row[4 + g] = g < groups && r < R ? p.x_scale + static_cast<long long>(r) * n_scales : nullptr;
-      }
-      for (int kb = 0; kb < blocks; ++kb) {
-        if (turn == 0) {
-          uint2 v[4 + kRowsMost / 32];
+          for (int b = 0; b < 2; ++b) {
+            if (!ok || k0 + 2 * h + b >= blocks) break;
+            ok = warp_wait(&bars.scales_empty[set], sph ^ 1, wc);
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t to = cols + set * kMxSetCols;
 #pragma unroll
-          for (int g = 0; g < 4 + kRowsMost / 32; ++g) v[g] = load_scales(row[g], kb * 8, n_scales);
-          if (!warp_wait(&bars.empty[st], ph ^ 1, wc)) { ok = false; break; }
-          uint4* out = reinterpret_cast<uint4*>(stage_scales(st)) + lane;   // 512 bytes a word of 128 rows
-          out[0] = make_uint4(v[0].x, v[1].x, v[2].x, v[3].x);
-          out[32] = make_uint4(v[0].y, v[1].y, v[2].y, v[3].y);
-          out[64] = make_uint4(v[4].x, v[5].x, v[6].x, v[7].x);
-          out[128] = make_uint4(v[4].y, v[5].y, v[6].y, v[7].y);
-          if (groups > 4) {
-            out[96] = make_uint4(v[8].x, v[9].x, 0u, 0u);
-            out[160] = make_uint4(v[8].y, v[9].y, 0u, 0u);
+            for (int q = 0; q < 2; ++q) {
+              tmem_st4(to + 12 * q, v[0][2 * b + q], v[1][2 * b + q], v[2][2 * b + q], v[3][2 * b + q]);
+              tmem_st8(to + 12 * q + 4, v[4][2 * b + q], v[5][2 * b + q], v[6][2 * b + q], v[7][2 * b + q], v[8][2 * b + q],
+                       v[9][2 * b + q], v[10][2 * b + q], 0u);
+            }
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_peer(peer_smem(&bars.scales[set], 0));
+            __syncwarp();
+            if (++set == kMxSets) { set = 0; sph ^= 1; }
           }
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&bars.scales[st]);
-          turn = kMxScaleWarps;
         }
-        --turn;
-        if (++st == n_stages) { st = 0; ph ^= 1; }
+        if (lane == 0) mbar_arrive(&bars.slot_empty[slot]);   // (every lane's words have arrived: the warp stored them)
+        if (++slot == kMxSlots) { slot = 0; lph ^= 1; }
       }
     }
-  } else {
+    for (int i = 0; ok && i < kMxSets; ++i) {    // every set given back, as the producer's stages
+      ok = warp_wait(&bars.scales_empty[set], sph ^ 1, wc);
+      if (++set == kMxSets) { set = 0; sph ^= 1; }
+    }
+  } else if (warp >= kMxCopy && warp < kMxEpi && (warp == kMxCopy || !p.scale_maps)) {
+    // ------------------------------------------------------------------- scales to shared memory
+    const int n_scales = l.n_in / 32;
+    int slot = 0;
+    uint32_t lph = 0;
+    bool ok = true;
+    Tile next = tile_at(pair);
+    for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
+      const Tile t = next;
+      const int f0 = t.m * (kGated ? 128 : 256) + static_cast<int>(rank) * (kGated ? 64 : 128);
+      for (int k0 = 0; k0 < blocks; k0 += kMxRound) {
+        if (!warp_wait(&bars.slot_empty[slot], lph ^ 1, wc)) { ok = false; break; }
+        uint8_t* to = scale_ring + slot * kMxSlot;
+        if (p.scale_maps) {
+          if (elect_one()) {
+            uint64_t* bar = &bars.slot_full[slot];
+            mbar_arrive_expect_tx(bar, (128 + p.tile_rows) * 32u);
+            if (kGated) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) tma_load_3d(to + i * 512, &tmScaleA, bar, k0 * 8, (i & 1) * l.n_out + f0 + (i >> 1) * 16, t.e);
+            } else {
+              tma_load_3d(to, &tmScaleA, bar, k0 * 8, f0, t.e);
+            }
+            tma_load_2d(to + 4096, &tmScaleB, bar, k0 * 8, t.row0);
+          }
+        } else {
+          const int units = 8 + (t.rows + 15) / 16;   // 16 rows each, two lanes a row: the features', the rows'
+#pragma unroll 2
+          for (int u = warp - kMxCopy; u < units; u += kMxCopyWarps) {
+            const int r = u * 16 + (lane >> 1);
+            const uint8_t* row = nullptr;
+            if (u < 8) {
+              const int f = kGated ? ((r >> 4) & 1) * l.n_out + f0 + (r >> 5) * 16 + (r & 15) : f0 + r;
+              if (f < l.n_z) row = p.w_scale + (static_cast<long long>(t.e) * l.n_z + f) * n_scales;
+            } else if (t.row0 + r - 128 < R) {
+              row = p.x_scale + static_cast<long long>(t.row0 + r - 128) * n_scales;
+            }
+            fetch_scales(scale_at(smem_u32(to), r, lane & 1), row, k0 * 8 + (lane & 1) * 16, n_scales, p.w_scale);
+          }
+          if ((n_scales & 3) == 0) cp_async_arrive(&bars.slot_full[slot]); else mbar_arrive(&bars.slot_full[slot]);
+        }
+        __syncwarp();
+        if (k0 == 0) next = tile_at(tile + n_pairs);
+        if (++slot == kMxSlots) { slot = 0; lph ^= 1; }
+      }
+    }
+    cp_async_wait_all();
+    if (p.scale_maps)                            // no copy is in flight at the end
+      for (int i = 0; ok && i < kMxSlots; ++i) {
+        ok = warp_wait(&bars.slot_empty[slot], lph ^ 1, wc);
+        if (++slot == kMxSlots) { slot = 0; lph ^= 1; }
+      }
+  } else if (warp >= kMxEpi) {
     // ------------------------------------------------------------------------------- epilogue
     const int q = warp & 3, g = (warp - kMxEpi) >> 2;
     const uint32_t lanes = static_cast<uint32_t>(32 * q) << 16;
@@ -261,9 +366,9 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
     const bool issuer = lead && elect_one();
     int buf = 0, acc = 0;
     uint32_t aph = 0;
-    for (int tile = blockIdx.x; tile < n_total; tile += gridDim.x) {
+    for (int tile = pair; tile < n_total; tile += n_pairs) {
       const Tile t = tile_at(tile);
-      const int f0 = t.m * width;
+      const int f0 = (t.m * 2 + static_cast<int>(rank)) * width;
       const int zf = f0 + fl + (kGated ? (lane >> 4) * l.n_out : 0);
       const bool f_in = f0 + fl < l.n_out;
       const bool whole = f0 + width <= l.n_out;
@@ -285,7 +390,7 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
         if (c + kGemmGroups >= chunks) {           // the accumulator's last use
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(&bars.acc_empty[acc]);
+          if (lane == 0) mbar_arrive_peer(peer_smem(&bars.acc_empty[acc], 0));
         }
         staging_acquire(g, lead, issuer);
 #pragma unroll
@@ -306,7 +411,7 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
         if (issuer) tma_store_commit();            // (every chunk is a group, an empty one too: staging_acquire counts them)
         buf ^= 1;
       }
-      if (chunks <= g && lane == 0) mbar_arrive(&bars.acc_empty[acc]);
+      if (chunks <= g && lane == 0) mbar_arrive_peer(peer_smem(&bars.acc_empty[acc], 0));
       if (++acc == 2) { acc = 0; aph ^= 1; }
     }
     if (issuer) tma_store_wait_all<0>();
@@ -317,39 +422,67 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
   if (bars.abort && threadIdx.x == 0)            // copies and products in flight end long before this does
     for (int i = 0; i < 1000; ++i) __nanosleep(1000);
   __syncthreads();
+  cluster_sync();
   tc_fence_after();
-  if (warp == 2) tmem_dealloc(tmem, 512);
+  if (warp == 2) tmem_dealloc_pair(tmem, 512);
 }
 
 template <int kAct, bool kGated>
-cudaError_t launch(const ExpertMxParams& p, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& out, int n_sms,
-                   cudaStream_t s) {
-  auto kernel = k_expert_mx<kAct, kGated>;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kMxSmem));
+cudaError_t launch(ExpertMxParams& p, const CUtensorMap& a, const CUtensorMap& b16, const CUtensorMap& scale_a,
+                   const CUtensorMap& out, int n_sms, cudaStream_t s) {
+  static GemmResidency held;
+  int pairs = 0;
+  const cudaError_t e = gemm_pairs(held, k_expert_mx<kAct, kGated>, kMxGemmThreads, kMxSmem, n_sms, &pairs);
   if (e != cudaSuccess) return e;
+  // Rows of a tile: the widest, unless all tiles of a narrower kind have a pair each or no expert has more rows (narrower
+  // stages, more of them), as for the bf16 products.
   const ExpertLinearParams& l = p.l;
-  long long tiles = (l.R / p.tile_rows + (l.R < l.E ? l.R : l.E)) * p.m_tiles;   // at most, whatever the offsets are
-  const int grid = tiles < 1 ? 1 : tiles < n_sms ? static_cast<int>(tiles) : n_sms;
-  return launch_pdl(kernel, dim3(grid), dim3(kMxGemmThreads), kMxSmem, s, a, b, out, p);
+  long long tiles = 0;
+  for (int rows : {32, 64, 128, kRowsMost}) {
+    p.tile_rows = rows;
+    tiles = (l.R / rows + (l.R < l.E ? l.R : l.E)) * p.m_tiles;   // at most, whatever the offsets are
+    if (tiles <= pairs || l.R <= rows) break;
+  }
+  const uint64_t bytes = l.n_in / 2, db[2] = {bytes, static_cast<uint64_t>(l.R)}, stb[1] = {bytes};
+  const uint32_t box[2] = {128, static_cast<uint32_t>(p.tile_rows) / 2};
+  CUtensorMap b, scale_b;
+  if (!encode_u8(&b, l.X, 2, db, stb, box)) return cudaErrorInvalidValue;
+  scale_b = b;
+  if (p.scale_maps) {
+    const uint64_t n = l.n_in / 32, ds[2] = {n, static_cast<uint64_t>(l.R)}, sts[1] = {n};
+    const uint32_t boxs[2] = {32, static_cast<uint32_t>(p.tile_rows)};
+    if (!encode_u8(&scale_b, p.x_scale, 2, ds, sts, boxs)) return cudaErrorInvalidValue;
+  }
+  pairs = tiles < 1 ? 1 : tiles < pairs ? static_cast<int>(tiles) : pairs;
+  return launch_pdl(k_expert_mx<kAct, kGated>, dim3(2 * pairs), dim3(kMxGemmThreads), kMxSmem, s, a, b, b16, scale_a, scale_b, out, p);
 }
 
 }  // namespace
 
 cudaError_t launch_expert_mx(ExpertMxParams p, int n_sms, cudaStream_t s) {
   const ExpertLinearParams& l = p.l;
-  const int per = l.gated ? 64 : 128;
+  const int per = l.gated ? 128 : 256;
   p.m_tiles = (l.n_out + per - 1) / per;
-  p.tile_rows = l.R <= 32 * static_cast<long long>(l.E) ? 32 : l.R <= 96 * static_cast<long long>(l.E) ? 96 : kRowsMost;
   const uint64_t R = static_cast<uint64_t>(l.R), bytes = l.n_in / 2, nz = l.n_z, E = l.E, no = l.n_out;
   const uint64_t da[3] = {bytes, nz, E}, sta[2] = {bytes, bytes * nz}, db[2] = {bytes, R}, stb[1] = {bytes};
-  const uint32_t boxa[3] = {128, l.gated ? 16u : 128u, 1}, boxb[2] = {128, 32}, box_out[2] = {64, kChunkCols};
+  const uint32_t boxa[3] = {128, l.gated ? 16u : 128u, 1}, box16[2] = {128, 16}, box_out[2] = {64, kChunkCols};
   const uint64_t dout[2] = {no, R}, stout[1] = {no * 2};
-  CUtensorMap a, b, out;
-  if (!encode_u8(&a, l.W, 3, da, sta, boxa) || !encode_u8(&b, l.X, 2, db, stb, boxb) || !encode_bf16(&out, l.out, 2, dout, stout, box_out))
+  CUtensorMap a, b16, out;
+  if (!encode_u8(&a, l.W, 3, da, sta, boxa) || !encode_u8(&b16, l.X, 2, db, stb, box16) ||
+      !encode_bf16(&out, l.out, 2, dout, stout, box_out))
     return cudaErrorInvalidValue;
+  // rows of scales of whole 16-byte words: the copy engine's
+  p.scale_maps = l.n_in % 512 == 0;
+  CUtensorMap scale_a = a;
+  if (p.scale_maps) {
+    const uint64_t n = l.n_in / 32, ds[3] = {n, nz, E}, sts[2] = {n, n * nz};
+    const uint32_t boxs[3] = {32, l.gated ? 16u : 128u, 1};
+    if (!encode_u8(&scale_a, p.w_scale, 3, ds, sts, boxs)) return cudaErrorInvalidValue;
+  }
   return with_act(l.act, [&](auto act) {
     constexpr int kAct = decltype(act)::value;
-    return l.gated ? launch<kAct, true>(p, a, b, out, n_sms, s) : launch<kAct, false>(p, a, b, out, n_sms, s);
+    return l.gated ? launch<kAct, true>(p, a, b16, scale_a, out, n_sms, s)
+                   : launch<kAct, false>(p, a, b16, scale_a, out, n_sms, s);
   });
 }
 

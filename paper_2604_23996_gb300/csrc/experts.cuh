@@ -94,10 +94,11 @@ struct ExpertMxParams {
   const uint8_t* w_scale;    // [E, n_z, n_in / 32]
   int m_tiles;
   int tile_rows;
+  int scale_maps;            // the copy engine brings the scales
   uint32_t* status;
   uint64_t limit_ns;
 };
-cudaError_t launch_expert_mx(ExpertMxParams p, int n_sms, cudaStream_t s);   // fills m_tiles and tile_rows
+cudaError_t launch_expert_mx(ExpertMxParams p, int n_sms, cudaStream_t s);   // fills the tiles and scale_maps
 cudaError_t launch_mx_quantise(const void* X, bool bf16, long long values, uint8_t* q, uint8_t* scale, cudaStream_t s);
 cudaError_t launch_mx_dequantise(const uint8_t* q, const uint8_t* scale, long long values, bool bf16, void* X, cudaStream_t s);
 // rows_out: the pairs of codes, scale: [R, d / 32]

@@ -222,6 +222,16 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
       ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(smem_u32(bar))
       : "memory");
 }
+// kBytes (4, 8 or 16, both addresses multiples of it) global -> shared, the last kBytes - `there` of them zeros;
+// cp_async_arrive: the thread's arrival on `bar` once its copies are done.
+template <int kBytes>
+__device__ __forceinline__ void cp_async(uint32_t dst, const void* src, int there) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(kBytes), "r"(there) : "memory");
+}
+__device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 // 2-D tiled store shared -> global (bulk group). Coordinates are non-negative.
 __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, const void* src, int x, int y) {
   asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];"
@@ -353,23 +363,6 @@ __device__ __forceinline__ void umma_bf16(uint32_t d_tmem, uint64_t a_desc, uint
       ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-// D[tmem] (+)= A[smem] * B[smem] of 4-bit values in blocks of 32 with a power-of-two scale each, f32 accumulate; the
-// scales lie in tensor memory (tmem_copy_scales).
-__device__ __forceinline__ void umma_mx4(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
-                                         uint32_t a_scales, uint32_t b_scales, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %6, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(a_scales), "r"(b_scales), "r"(accumulate)
-      : "memory");
-}
-// 32 rows of 16 bytes of shared memory to 4 columns of tensor memory, the same for each quarter of its lanes. Row l holds
-// the scale words of rows l, l + 32, l + 64 and l + 96 of an operand; a word's bytes are the scales of four blocks along the
-// depth. Runs in order with the products that the same thread issues.
-__device__ __forceinline__ void tmem_copy_scales(uint32_t taddr, uint64_t desc) {
-  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
-}
 // Arrives once on `bar` when every tcgen05.mma issued so far by this thread has completed.
 __device__ __forceinline__ void umma_commit(uint64_t* bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];"
@@ -398,6 +391,18 @@ __device__ __forceinline__ void umma_bf16_pair(uint32_t d_tmem, uint64_t a_desc,
       ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
+// 4-bit values in blocks of 32 with a power-of-two scale each, by a pair of CTAs. The scales lie in tensor memory, the same in
+// each quarter of the lanes: row r's word in lane r % 32 and column r / 32, its bytes the scales of four blocks along the depth;
+// those of its own 128 rows of A, and of all of B's rows, in each CTA.
+__device__ __forceinline__ void umma_mx4_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                              uint32_t a_scales, uint32_t b_scales, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %6, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(a_scales), "r"(b_scales), "r"(accumulate)
+      : "memory");
+}
 __device__ __forceinline__ void umma_commit_pair(uint64_t* bar) {
   asm volatile(
       "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
@@ -405,6 +410,20 @@ __device__ __forceinline__ void umma_commit_pair(uint64_t* bar) {
 }
 __device__ __forceinline__ void tmem_ld_wait() {
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+
+// Words to 4 or 8 columns of the warp's 32 lanes; tmem_st_wait: what the warp stored is there.
+__device__ __forceinline__ void tmem_st4(uint32_t taddr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};"
+               ::"r"(taddr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t e,
+                                         uint32_t f, uint32_t g, uint32_t h) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"r"(taddr), "r"(a), "r"(b), "r"(c), "r"(d), "r"(e), "r"(f), "r"(g), "r"(h) : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() {
+  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
 
 // tcgen05.ld is .sync.aligned: the whole warp must execute it converged. Lanes leave bounded
@@ -506,11 +525,6 @@ __host__ __device__ constexpr uint32_t idesc_mx4(int M, int N, int part) {
          | (1u << 23)                               // scales: powers of two (ue8m0)
          | (static_cast<uint32_t>(M >> 4) << 24)    // M / 16
          | (static_cast<uint32_t>(2 * part) << 29); // A's scales: first byte
-}
-
-// Descriptor of 32 rows of 16 bytes without a swizzle: 8-row groups 128 bytes apart.
-__device__ __forceinline__ uint64_t sdesc_scales(uint32_t saddr) {
-  return static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4) | static_cast<uint64_t>(128u >> 4) << 32 | static_cast<uint64_t>(1) << 46;
 }
 
 // Byte offset of element (row, col) inside a 128-byte-swizzled tile of 16-bit elements whose
