@@ -44,7 +44,8 @@ constexpr int kMxGroups = 4 + (kRowsMost + 31) / 32;     // of 32 features or ro
 constexpr int kMxRound = 4;                      // blocks whose scales are copied at a time: 32 bytes a row
 constexpr int kMxSlots = 3;
 constexpr uint32_t kMxSlot = kMxGroups * 32 * 32;
-constexpr uint32_t kMxStaging = 8192;            // one epilogue group's output boxes: two chunks
+constexpr int kMxChunk = 32;                     // rows that an epilogue group finishes at a time
+constexpr uint32_t kMxStaging = 8192;            // one group's output boxes of 64 features by 32 rows: two, gated two chunks of one
 constexpr uint32_t kMxSmem = 1024 + kMxRing + kMxSlots * kMxSlot + kGemmGroups * kMxStaging + kBarBytes + 4 * (kExpertsMax + 1);
 static_assert(kMxScaleCols + kMxSets * kMxSetCols <= 512, "tensor memory");
 static_assert(kMxSmem <= 227 * 1024, "shared memory of a CTA");
@@ -99,7 +100,8 @@ template <int kAct, bool kGated>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMxGemmThreads, 1)
 k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
             const __grid_constant__ CUtensorMap tmB16, const __grid_constant__ CUtensorMap tmScaleA,
-            const __grid_constant__ CUtensorMap tmScaleB, const __grid_constant__ CUtensorMap tmOut, const ExpertMxParams p) {
+            const __grid_constant__ CUtensorMap tmScaleB, const __grid_constant__ CUtensorMap tmOut,
+            const __grid_constant__ CUtensorMap tmOut16, const ExpertMxParams p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   uint8_t* scale_ring = smem + kMxRing;
@@ -143,6 +145,7 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
     tma_prefetch_desc(&tmScaleA);
     tma_prefetch_desc(&tmScaleB);
     tma_prefetch_desc(&tmOut);
+    tma_prefetch_desc(&tmOut16);
   }
   if (warp == 2) tmem_alloc_pair(&bars.tmem, 512);
   pdl_wait();
@@ -260,32 +263,27 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
       for (int k0 = 0; ok && k0 < blocks; k0 += kMxRound) {
         ok = warp_wait(&bars.slot_full[slot], lph, wc);
         const uint32_t from = slots + slot * kMxSlot;
-        for (int h = 0; ok && h < 2 && k0 + 2 * h < blocks; ++h) {
-          uint32_t v[kMxGroups][4];              // lane's row of each group, two blocks' words
+        for (int b = 0; ok && b < kMxRound && k0 + b < blocks; ++b) {
+          uint32_t v[kMxGroups][2];              // lane's row of each group, a block's words
 #pragma unroll
           for (int g = 0; g < kMxGroups; ++g)
-            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
-                         : "=r"(v[g][0]), "=r"(v[g][1]), "=r"(v[g][2]), "=r"(v[g][3]) : "r"(scale_at(from, g * 32 + lane, h)));
+            asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v[g][0]), "=r"(v[g][1])
+                         : "r"(scale_at(from, g * 32 + lane, b >> 1) + 8 * (b & 1)));
+          ok = warp_wait(&bars.scales_empty[set], sph ^ 1, wc);
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t to = cols + set * kMxSetCols;
 #pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            if (!ok || k0 + 2 * h + b >= blocks) break;
-            ok = warp_wait(&bars.scales_empty[set], sph ^ 1, wc);
-            if (!ok) break;
-            tc_fence_after();
-            const uint32_t to = cols + set * kMxSetCols;
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-              tmem_st4(to + 12 * q, v[0][2 * b + q], v[1][2 * b + q], v[2][2 * b + q], v[3][2 * b + q]);
-              tmem_st8(to + 12 * q + 4, v[4][2 * b + q], v[5][2 * b + q], v[6][2 * b + q], v[7][2 * b + q], v[8][2 * b + q],
-                       v[9][2 * b + q], v[10][2 * b + q], 0u);
-            }
-            tmem_st_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_peer(peer_smem(&bars.scales[set], 0));
-            __syncwarp();
-            if (++set == kMxSets) { set = 0; sph ^= 1; }
+          for (int w = 0; w < 2; ++w) {
+            tmem_st4(to + 12 * w, v[0][w], v[1][w], v[2][w], v[3][w]);
+            tmem_st8(to + 12 * w + 4, v[4][w], v[5][w], v[6][w], v[7][w], v[8][w], v[9][w], v[10][w], 0u);
           }
+          tmem_st_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_peer(peer_smem(&bars.scales[set], 0));
+          __syncwarp();
+          if (++set == kMxSets) { set = 0; sph ^= 1; }
         }
         if (lane == 0) mbar_arrive(&bars.slot_empty[slot]);   // (every lane's words have arrived: the warp stored them)
         if (++slot == kMxSlots) { slot = 0; lph ^= 1; }
@@ -361,55 +359,105 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
            i += static_cast<long long>(gridDim.x) * (32 * kMxEpiWarps))
         o[i] = make_uint4(0u, 0u, 0u, 0u);
     }
+    // A warp's features are two times 16 (gated: 16, as g and as u). A 16-lane load gives a thread two neighbouring rows of
+    // features lane / 4 and 8 further on; rounded and packed they are stored transposed, 8 features (16 bytes) of a row at a time.
+    constexpr int kHalves = kGated ? 1 : 2;
     const int width = kGated ? 64 : 128;
-    const int fl = kGated ? 16 * q + (lane & 15) : 32 * q + lane;
+    const int fw = kGated ? 16 * q : 32 * q;     // the warp's first feature among the CTA's
+    const uint32_t st_row = static_cast<uint32_t>(lane & 7);
+    const uint32_t st_at = static_cast<uint32_t>(fw >> 6) * 4096u + (static_cast<uint32_t>(lane >> 4) * 8u + st_row) * 128u;
+    const uint32_t st_chunk = static_cast<uint32_t>((fw & 63) >> 3) + static_cast<uint32_t>((lane >> 3) & 1);
     const bool issuer = lead && elect_one();
     int buf = 0, acc = 0;
     uint32_t aph = 0;
     for (int tile = pair; tile < n_total; tile += n_pairs) {
       const Tile t = tile_at(tile);
       const int f0 = (t.m * 2 + static_cast<int>(rank)) * width;
-      const int zf = f0 + fl + (kGated ? (lane >> 4) * l.n_out : 0);
-      const bool f_in = f0 + fl < l.n_out;
       const bool whole = f0 + width <= l.n_out;
       const long long ld = l.n_out;
-      float bias = 0.f;
-      const __nv_bfloat16* res = static_cast<const __nv_bfloat16*>(l.residual) + f0 + (fl & ~1);
-      uint32_t rv[kChunkCols / 2];
-      if (l.bias && f_in) bias = __ldg(l.bias + static_cast<long long>(t.e) * l.n_z + zf);
+      float bias[2][2] = {{0.f, 0.f}, {0.f, 0.f}};   // non-gated: of the halves; gated: of g and of u
+      if (l.bias) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int f = f0 + fw + (kGated ? 0 : 16 * h) + 8 * i + (lane >> 2);
+            if (f < l.n_out) bias[h][i] = __ldg(l.bias + static_cast<long long>(t.e) * l.n_z + f + (kGated ? h * l.n_out : 0));
+          }
+      }
       if (!named_bar_all(kBarVote + g, 128, !lead || warp_wait(&bars.acc_full[acc], aph, wc))) break;
       tc_fence_after();
-      const int chunks = (t.rows + kChunkCols - 1) / kChunkCols;
+      const int chunks = (t.rows + kMxChunk - 1) / kMxChunk;
       for (int c = g; c < chunks; c += kGemmGroups) {
-        const long long row = t.row0 + c * kChunkCols;
-        const int rows = min(kChunkCols, t.rows - c * kChunkCols);
-        if (l.residual) load_residual<kGated>(l, res + row * ld, f_in ? rows : 0, rv);
-        uint8_t* boxes = staging + g * kMxStaging + buf * (kMxStaging / 2);
-        float v[kChunkCols];
-        tmem_ld16(tmem + acc * kRowsMost + c * kChunkCols + lanes, v);
-        if (c + kGemmGroups >= chunks) {           // the accumulator's last use
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive_peer(peer_smem(&bars.acc_empty[acc], 0));
-        }
-        staging_acquire(g, lead, issuer);
+        const long long row = t.row0 + c * kMxChunk;
+        const int rows = min(kMxChunk, t.rows - c * kMxChunk);
+        uint8_t* boxes = staging + g * kMxStaging + (kGated ? buf * 4096 : 0);
+        const uint32_t from = tmem + acc * kRowsMost + c * kMxChunk + lanes;
 #pragma unroll
-        for (int j = 0; j < kChunkCols; ++j) v[j] += bias;
-        put_forward<kAct, kGated>(boxes, fl, v, l.residual != nullptr, rv);
+        for (int h = 0; h < kHalves; ++h) {
+          // the residual's words, transposed as the accumulators are: [rows 8 n][features 8 i]
+          uint32_t rv[4][2];
+          if (l.residual) {
+            const int f = f0 + fw + 16 * h + 2 * (lane & 3);
+            const __nv_bfloat16* res = static_cast<const __nv_bfloat16*>(l.residual) + (row + (lane >> 2)) * ld + f;
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+#pragma unroll
+              for (int i = 0; i < 2; ++i)
+                rv[n][i] = 8 * n + (lane >> 2) < rows && f + 8 * i < l.n_out
+                               ? __ldg(reinterpret_cast<const uint32_t*>(res + 8 * n * ld + 8 * i)) : 0u;
+          }
+          float v[16];                           // [rows 8 n][features 8 i][two rows]
+          tmem_ld_16x256b_x4(from + (static_cast<uint32_t>(16 * h) << 16), v);
+          if (kGated) {
+            float u[16];
+            tmem_ld_16x256b_x4(from + (16u << 16), u);
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+              v[j] = act_value<kAct, true>(v[j] + bias[0][(j >> 1) & 1]) * (u[j] + bias[1][(j >> 1) & 1]);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) v[j] = act_value<kAct, true>(v[j] + bias[h][(j >> 1) & 1]);
+          }
+          if (h == kHalves - 1 && c + kGemmGroups >= chunks) {   // the accumulator's last use
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_peer(peer_smem(&bars.acc_empty[acc], 0));
+          }
+          if (l.residual) {
+            __syncwarp();
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                const uint32_t w = transpose_8x8(rv[n][i]);
+                v[4 * n + 2 * i] += __uint_as_float(w << 16);
+                v[4 * n + 2 * i + 1] += __uint_as_float(w & 0xffff0000u);
+              }
+          }
+          if (h == 0) staging_acquire<kGated ? 2 : 1>(g, lead, issuer);
+          __syncwarp();
+          const uint32_t at = smem_u32(boxes) + st_at + (((st_chunk + 2u * h) ^ st_row) << 4);
+#pragma unroll
+          for (int n = 0; n < 2; ++n)            // 16 rows
+            stmatrix_x4_trans(at + 2048u * n, pack_bf16(v[8 * n], v[8 * n + 1]), pack_bf16(v[8 * n + 2], v[8 * n + 3]),
+                              pack_bf16(v[8 * n + 4], v[8 * n + 5]), pack_bf16(v[8 * n + 6], v[8 * n + 7]));
+        }
         fence_proxy_async_smem();
-        const bool engine = rows == kChunkCols && (whole || !kGated);
+        const bool engine = (rows == kMxChunk || rows == 16) && (whole || !kGated);
         staging_filled(g, lead, !engine);
         if (engine) {
           if (issuer)
             for (int i = 0; i < width / 64; ++i)
-              if (f0 + 64 * i < l.n_out) tma_store_2d(&tmOut, boxes + i * 2048, f0 + 64 * i, static_cast<int>(row));
+              if (f0 + 64 * i < l.n_out)
+                tma_store_2d(rows == 16 ? &tmOut16 : &tmOut, boxes + i * 4096, f0 + 64 * i, static_cast<int>(row));
         } else {
           for (int i = 0; i < width / 64; ++i)
-            copy_box(boxes + i * 2048, static_cast<__nv_bfloat16*>(l.out) + row * ld + f0 + 64 * i, ld, rows, l.n_out - f0 - 64 * i,
+            copy_box(boxes + i * 4096, static_cast<__nv_bfloat16*>(l.out) + row * ld + f0 + 64 * i, ld, rows, l.n_out - f0 - 64 * i,
                      et & 127);
         }
         if (issuer) tma_store_commit();            // (every chunk is a group, an empty one too: staging_acquire counts them)
-        buf ^= 1;
+        if (kGated) buf ^= 1;
       }
       if (chunks <= g && lane == 0) mbar_arrive_peer(peer_smem(&bars.acc_empty[acc], 0));
       if (++acc == 2) { acc = 0; aph ^= 1; }
@@ -429,7 +477,7 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
 
 template <int kAct, bool kGated>
 cudaError_t launch(ExpertMxParams& p, const CUtensorMap& a, const CUtensorMap& b16, const CUtensorMap& scale_a,
-                   const CUtensorMap& out, int n_sms, cudaStream_t s) {
+                   const CUtensorMap& out, const CUtensorMap& out16, int n_sms, cudaStream_t s) {
   static GemmResidency held;
   int pairs = 0;
   const cudaError_t e = gemm_pairs(held, k_expert_mx<kAct, kGated>, kMxGemmThreads, kMxSmem, n_sms, &pairs);
@@ -454,7 +502,8 @@ cudaError_t launch(ExpertMxParams& p, const CUtensorMap& a, const CUtensorMap& b
     if (!encode_u8(&scale_b, p.x_scale, 2, ds, sts, boxs)) return cudaErrorInvalidValue;
   }
   pairs = tiles < 1 ? 1 : tiles < pairs ? static_cast<int>(tiles) : pairs;
-  return launch_pdl(k_expert_mx<kAct, kGated>, dim3(2 * pairs), dim3(kMxGemmThreads), kMxSmem, s, a, b, b16, scale_a, scale_b, out, p);
+  return launch_pdl(k_expert_mx<kAct, kGated>, dim3(2 * pairs), dim3(kMxGemmThreads), kMxSmem, s, a, b, b16, scale_a, scale_b, out,
+                    out16, p);
 }
 
 }  // namespace
@@ -465,11 +514,11 @@ cudaError_t launch_expert_mx(ExpertMxParams p, int n_sms, cudaStream_t s) {
   p.m_tiles = (l.n_out + per - 1) / per;
   const uint64_t R = static_cast<uint64_t>(l.R), bytes = l.n_in / 2, nz = l.n_z, E = l.E, no = l.n_out;
   const uint64_t da[3] = {bytes, nz, E}, sta[2] = {bytes, bytes * nz}, db[2] = {bytes, R}, stb[1] = {bytes};
-  const uint32_t boxa[3] = {128, l.gated ? 16u : 128u, 1}, box16[2] = {128, 16}, box_out[2] = {64, kChunkCols};
+  const uint32_t boxa[3] = {128, l.gated ? 16u : 128u, 1}, box16[2] = {128, 16}, box_out[2] = {64, kMxChunk}, box_out16[2] = {64, 16};
   const uint64_t dout[2] = {no, R}, stout[1] = {no * 2};
-  CUtensorMap a, b16, out;
+  CUtensorMap a, b16, out, out16;
   if (!encode_u8(&a, l.W, 3, da, sta, boxa) || !encode_u8(&b16, l.X, 2, db, stb, box16) ||
-      !encode_bf16(&out, l.out, 2, dout, stout, box_out))
+      !encode_bf16(&out, l.out, 2, dout, stout, box_out) || !encode_bf16(&out16, l.out, 2, dout, stout, box_out16))
     return cudaErrorInvalidValue;
   // rows of scales of whole 16-byte words: the copy engine's
   p.scale_maps = l.n_in % 512 == 0;
@@ -481,8 +530,8 @@ cudaError_t launch_expert_mx(ExpertMxParams p, int n_sms, cudaStream_t s) {
   }
   return with_act(l.act, [&](auto act) {
     constexpr int kAct = decltype(act)::value;
-    return l.gated ? launch<kAct, true>(p, a, b16, scale_a, out, n_sms, s)
-                   : launch<kAct, false>(p, a, b16, scale_a, out, n_sms, s);
+    return l.gated ? launch<kAct, true>(p, a, b16, scale_a, out, out16, n_sms, s)
+                   : launch<kAct, false>(p, a, b16, scale_a, out, out16, n_sms, s);
   });
 }
 
