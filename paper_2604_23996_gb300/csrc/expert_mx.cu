@@ -18,6 +18,8 @@
 // Ragged edges and gated layers are those of expert_gemm.cu: rows of the next expert inside a tile are other columns of
 // D and are not stored; features past the expert's weights and a depth that ends inside a block are zeros of the maps (their scales
 // are set to 2^-127, so no NaN scale meets a zero).
+#include <type_traits>
+
 #include "expert_epilogue.cuh"
 #include "expert_gemm.cuh"
 #include "experts.cuh"
@@ -62,33 +64,41 @@ struct MxBars {
 };
 static_assert(sizeof(MxBars) <= kBarBytes, "barriers");
 
-// Bytes [at, at + 16) of a row of n scales to shared memory, zeros for what lies past the row (row null: for all of them).
-// Rows of whole 16, 8 or 4 bytes are copied; others (n_in not a multiple of 128) are put together from the aligned words that
-// hold them.
-__device__ __forceinline__ void fetch_scales(uint32_t dst, const uint8_t* row, int at, int n, const uint8_t* any) {
-  const int there = row == nullptr ? 0 : min(max(n - at, 0), 16);
-  const uint8_t* src = there > 0 ? row + at : any;
-  if ((n & 15) == 0) {
-    cp_async<16>(dst, src, there);
-  } else if ((n & 7) == 0) {
+// 16 scale bytes of each of kUnits rows, `step` bytes apart, to shared memory 1024 bytes apart; the first there[i] of them, zeros
+// behind. Whole words of kBytes are copied; with kBytes = 0 (rows of no whole 4-byte words) they are put together from the aligned
+// words that hold them. any: an aligned address that may be read.
+template <int kBytes, int kUnits>
+__device__ __forceinline__ void fetch_scales(uint32_t dst, const uint8_t* src, long long step, const int (&there)[kUnits],
+                                             const uint8_t* any) {
+  if constexpr (kBytes > 0) {
 #pragma unroll
-    for (int i = 0; i < 16; i += 8) cp_async<8>(dst + i, there > i ? src + i : any, min(max(there - i, 0), 8));
-  } else if ((n & 3) == 0) {
+    for (int i = 0; i < kUnits; ++i)
 #pragma unroll
-    for (int i = 0; i < 16; i += 4) cp_async<4>(dst + i, there > i ? src + i : any, min(max(there - i, 0), 4));
+      for (int j = 0; j < 16; j += kBytes)
+        cp_async<kBytes>(dst + 1024 * i + j, there[i] > j ? src + i * step + j : any, min(max(there[i] - j, 0), kBytes));
   } else {
-    const int skew = static_cast<int>(reinterpret_cast<uintptr_t>(src) & 3u);
-    const uint32_t* words = reinterpret_cast<const uint32_t*>(src - skew);
-    uint32_t w[5], out[4];
+    uint32_t w[kUnits][5];
+    int skew[kUnits];
 #pragma unroll
-    for (int i = 0; i < 5; ++i) w[i] = 4 * i < skew + there ? __ldg(words + i) : 0u;
+    for (int i = 0; i < kUnits; ++i) {
+      const uint8_t* p = src + i * step;
+      skew[i] = static_cast<int>(reinterpret_cast<uintptr_t>(p) & 3u);
+      const uint32_t* words = reinterpret_cast<const uint32_t*>(p - skew[i]);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int left = there - 4 * i;            // bytes of this word that the row has
-      out[i] = __funnelshift_r(w[i], w[i + 1], 8 * skew);
-      if (left < 4) out[i] &= left > 0 ? (1u << (8 * left)) - 1u : 0u;
+      for (int j = 0; j < 5; ++j) w[i][j] = there[i] > 0 && 4 * j < skew[i] + there[i] ? __ldg(words + j) : 0u;
     }
-    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(out[0]), "r"(out[1]), "r"(out[2]), "r"(out[3]) : "memory");
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+      uint32_t out[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int left = there[i] - 4 * j;       // bytes of this word that the row has
+        out[j] = __funnelshift_r(w[i][j], w[i][j + 1], 8 * skew[i]);
+        if (left < 4) out[j] &= left > 0 ? (1u << (8 * left)) - 1u : 0u;
+      }
+      asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};"
+                   ::"r"(dst + 1024 * i), "r"(out[0]), "r"(out[1]), "r"(out[2]), "r"(out[3]) : "memory");
+    }
   }
 }
 // Shared address of half h (16 bytes) of row r in a slot; the halves of every other four rows change places (bank conflicts).
@@ -319,19 +329,30 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
             tma_load_2d(to + 4096, &tmScaleB, bar, k0 * 8, t.row0);
           }
         } else {
-          const int units = 8 + (t.rows + 15) / 16;   // 16 rows each, two lanes a row: the features', the rows'
-#pragma unroll 2
-          for (int u = warp - kMxCopy; u < units; u += kMxCopyWarps) {
-            const int r = u * 16 + (lane >> 1);
-            const uint8_t* row = nullptr;
-            if (u < 8) {
-              const int f = kGated ? ((r >> 4) & 1) * l.n_out + f0 + (r >> 5) * 16 + (r & 15) : f0 + r;
-              if (f < l.n_z) row = p.w_scale + (static_cast<long long>(t.e) * l.n_z + f) * n_scales;
-            } else if (t.row0 + r - 128 < R) {
-              row = p.x_scale + static_cast<long long>(t.row0 + r - 128) * n_scales;
-            }
-            fetch_scales(scale_at(smem_u32(to), r, lane & 1), row, k0 * 8 + (lane & 1) * 16, n_scales, p.w_scale);
+          // sixteen rows at a time, two lanes a row, the warps in turn: the features' (gated: one warp g's, the other
+          // u's, as the operand has them), then the rows'
+          const int w = warp - kMxCopy, r = 16 * w + (lane >> 1);
+          const int at = k0 * 8 + (lane & 1) * 16, there = min(max(n_scales - at, 0), 16);
+          const int f = kGated ? w * l.n_out + f0 + (lane >> 1) : f0 + r, f_step = kGated ? 16 : 32;
+          const uint32_t dst = scale_at(smem_u32(to), r, lane & 1);
+          int have_a[4], have_b[4], have_c[3];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            have_a[i] = f + i * f_step < l.n_z ? there : 0;
+            have_b[i] = 16 * w + 32 * i < t.rows && t.row0 + r + 32 * i < R ? there : 0;
+            if (i < 3) have_c[i] = 16 * w + 32 * (i + 4) < t.rows && t.row0 + r + 32 * (i + 4) < R ? there : 0;
           }
+          const uint8_t* a = p.w_scale + (static_cast<long long>(t.e) * l.n_z + f) * n_scales + at;
+          const uint8_t* b = p.x_scale + static_cast<long long>(t.row0 + r) * n_scales + at;
+          const long long n = n_scales;
+          auto fetch = [&](auto bytes) {
+            fetch_scales<decltype(bytes)::value, 4>(dst, a, f_step * n, have_a, p.w_scale);
+            fetch_scales<decltype(bytes)::value, 4>(dst + 4096, b, 32 * n, have_b, p.w_scale);
+            if (t.rows > 128) fetch_scales<decltype(bytes)::value, 3>(dst + 8192, b + 128 * n, 32 * n, have_c, p.w_scale);
+          };
+          if ((n_scales & 7) == 0) fetch(std::integral_constant<int, 8>());
+          else if ((n_scales & 3) == 0) fetch(std::integral_constant<int, 4>());
+          else fetch(std::integral_constant<int, 0>());
           if ((n_scales & 3) == 0) cp_async_arrive(&bars.slot_full[slot]); else mbar_arrive(&bars.slot_full[slot]);
         }
         __syncwarp();
