@@ -30,8 +30,9 @@ namespace {
 
 constexpr int kMxScaleWarps = 4;
 constexpr int kMxCopyWarps = 2;
-constexpr int kMxCopy = 2 + kMxScaleWarps;       // 0 producer, 1 MMA issuer, then the scales' warps
-constexpr int kMxEpi = kMxCopy + kMxCopyWarps;   // first epilogue warp
+constexpr int kMxCopy = 2 + kMxScaleWarps;       // 0 producer of the features, 1 MMA issuer, then the scales' warps
+constexpr int kMxRows = kMxCopy + kMxCopyWarps;  // producer of the rows
+constexpr int kMxEpi = kMxRows + 1;              // first epilogue warp
 constexpr int kMxEpiWarps = 4 * kGemmGroups;
 constexpr int kMxGemmThreads = 32 * (kMxEpi + kMxEpiWarps);
 constexpr int kMxBlock = 256;                    // depth of a block: 128 bytes
@@ -123,7 +124,7 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
   const int R = static_cast<int>(l.R);
   const uint32_t rank = cluster_rank();
   const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
-  const AnyRows rows_of{p.tile_rows};
+  const AnyRows rows_of = p.rows_of;
   // a stage: the CTA's 128 features, then its half of the widest tile
   const uint32_t stage_bytes = kMxA + static_cast<uint32_t>(p.tile_rows) * 64u;
   const int n_stages = min(kMxStagesMost, static_cast<int>(kMxRing / stage_bytes));
@@ -132,7 +133,7 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < n_stages; ++i) {
-      mbar_init(&bars.full[i], 2);
+      mbar_init(&bars.full[i], 4);
       mbar_init(&bars.empty[i], 1);
     }
     for (int i = 0; i < kMxSets; ++i) {
@@ -171,56 +172,93 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
   const int blocks = (l.n_in + kMxBlock - 1) / kMxBlock;
   const uint32_t tmem = bars.tmem;
   const WaitCtx wc{&bars.abort, p.status, p.limit_ns};
+  // The pair's tiles in turn, looked up by a whole warp: most are of the same expert as the one before or of one of the
+  // next few; only farther ones are searched for.
   struct Tile {
     int e, m, row0, rows;
+    int r, before, tiles;                        // row tile; those of the experts before e, and of e
   };
-  auto tile_at = [&](int tile) {
-    Tile t{0, 0, 0, 0};
-    if (tile < n_total) {
-      const int r = tile / p.m_tiles;
-      t.m = tile - r * p.m_tiles;
-      const RowTile row = find_row_tile(rt, off, l.E, R, rows_of, r);
-      t.e = row.e;
-      t.row0 = row.row0;
-      t.rows = min(p.tile_rows, row.row1 - row.row0);
+  auto settle = [&](Tile& t) {
+    const int start = expert_row(off, t.e, R);
+    t.row0 = start + rows_of.first(t.r - t.before);
+    t.rows = min(p.tile_rows, expert_row(off, t.e + 1, R) - t.row0);
+  };
+  auto search = [&](Tile& t) {
+    const RowTile row = find_row_tile(rt, off, l.E, R, rows_of, t.r);
+    t.e = row.e;
+    t.before = row.before;
+    t.tiles = row.tiles;
+  };
+  auto first_tile = [&] {
+    Tile t{};
+    if (pair < n_total) {
+      t.r = pair / p.m_tiles;
+      t.m = pair - t.r * p.m_tiles;
+      search(t);
+      settle(t);
     }
     return t;
   };
+  const int step_r = n_pairs / p.m_tiles, step_m = n_pairs - step_r * p.m_tiles;
+  auto tile_after = [&](Tile t) {
+    t.r += step_r;
+    t.m += step_m;
+    if (t.m >= p.m_tiles) {
+      t.m -= p.m_tiles;
+      ++t.r;
+    }
+    if (t.r >= rt.total) return t;
+    for (int i = 0; t.r >= t.before + t.tiles; ++i) {
+      if (i == 3) {
+        search(t);
+        break;
+      }
+      t.before += t.tiles;
+      ++t.e;
+      t.tiles = rows_of.tiles(expert_row(off, t.e + 1, R) - expert_row(off, t.e, R));
+    }
+    settle(t);
+    return t;
+  };
 
-  if (warp == 0) {
-    // ------------------------------------------------------------------------------- producer
+  if (warp == 0 || warp == kMxRows) {
+    // ------------------------------------------------------------------------------- producers
+    const bool rows = warp == kMxRows;
     int st = 0;
     uint32_t ph = 0;
     bool ok = true;
-    Tile next = tile_at(pair);
+    Tile next = first_tile();
     for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
       const Tile t = next;
       const int half = min((t.rows + 31) & ~31, p.tile_rows) / 2;
+      const int r0 = t.row0 + static_cast<int>(rank) * half;
+      const int f0 = t.m * (kGated ? 128 : 256) + static_cast<int>(rank) * (kGated ? 64 : 128);
       for (int kb = 0; kb < blocks; ++kb) {
         if (!warp_wait(&bars.empty[st], ph ^ 1, wc)) { ok = false; break; }
         if (elect_one()) {
-          uint8_t* a = stage_a(st);
-          uint8_t* b = stage_b(st);
           const uint32_t bar = peer_smem(&bars.full[st], 0);
-          mbar_arrive_expect_tx_peer(bar, kMxA + half * 128u);
           const int x = kb * 128;
-          if (kGated) {
-            const int f0 = t.m * 128 + static_cast<int>(rank) * 64;
+          if (!rows) {
+            uint8_t* a = stage_a(st);
+            mbar_arrive_expect_tx_peer(bar, kMxA);
+            if (kGated) {                        // 16 features of g, the same of u, the next 16 ...
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-              tma_load_3d_pair(a + i * 2048, &tmA, bar, x, (i & 1) * l.n_out + f0 + (i >> 1) * 16, t.e);
+              for (int i = 0; i < 4; ++i) tma_load_4d_pair(a + i * 4096, &tmA, bar, x, f0 + 16 * i, 0, t.e);
+            } else {
+              tma_load_4d_pair(a, &tmA, bar, x, f0, 0, t.e);
+            }
           } else {
-            tma_load_3d_pair(a, &tmA, bar, x, t.m * 256 + static_cast<int>(rank) * 128, t.e);
-          }
-          const int r0 = t.row0 + static_cast<int>(rank) * half;
-          if (2 * half == p.tile_rows) {
-            tma_load_2d_pair(b, &tmB, bar, x, r0);
-          } else {
-            for (int i = 0; i < half; i += 16) tma_load_2d_pair(b + i * 128, &tmB16, bar, x, r0 + i);
+            uint8_t* b = stage_b(st);
+            mbar_arrive_expect_tx_peer(bar, half * 128u);
+            if (2 * half == p.tile_rows) {
+              tma_load_2d_pair(b, &tmB, bar, x, r0);
+            } else {
+              for (int i = 0; i < half; i += 16) tma_load_2d_pair(b + i * 128, &tmB16, bar, x, r0 + i);
+            }
           }
         }
         __syncwarp();
-        if (kb == 0) next = tile_at(tile + n_pairs);
+        if (kb == 0) next = tile_after(t);
         if (++st == n_stages) { st = 0; ph ^= 1; }
       }
     }
@@ -234,7 +272,7 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
     int st = 0, acc = 0, set = 0;
     uint32_t ph = 0, aph = 0, sph = 0;
     bool ok = true;
-    Tile next = tile_at(pair);
+    Tile next = first_tile();
     for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
       const Tile t = next;
       const int n = min((t.rows + 31) & ~31, p.tile_rows);
@@ -256,7 +294,7 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
           if (kb == blocks - 1) umma_commit_pair(&bars.acc_full[acc]);
         }
         __syncwarp();
-        if (kb == 0) next = tile_at(tile + n_pairs);
+        if (kb == 0) next = tile_after(t);
         if (++set == kMxSets) { set = 0; sph ^= 1; }
         if (++st == n_stages) { st = 0; ph ^= 1; }
       }
@@ -303,13 +341,13 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
       ok = warp_wait(&bars.scales_empty[set], sph ^ 1, wc);
       if (++set == kMxSets) { set = 0; sph ^= 1; }
     }
-  } else if (warp >= kMxCopy && warp < kMxEpi && (warp == kMxCopy || !p.scale_maps)) {
+  } else if (warp >= kMxCopy && warp < kMxRows && (warp == kMxCopy || !p.scale_maps)) {
     // ------------------------------------------------------------------- scales to shared memory
     const int n_scales = l.n_in / 32;
     int slot = 0;
     uint32_t lph = 0;
     bool ok = true;
-    Tile next = tile_at(pair);
+    Tile next = first_tile();
     for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
       const Tile t = next;
       const int f0 = t.m * (kGated ? 128 : 256) + static_cast<int>(rank) * (kGated ? 64 : 128);
@@ -322,9 +360,9 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
             mbar_arrive_expect_tx(bar, (128 + p.tile_rows) * 32u);
             if (kGated) {
 #pragma unroll
-              for (int i = 0; i < 8; ++i) tma_load_3d(to + i * 512, &tmScaleA, bar, k0 * 8, (i & 1) * l.n_out + f0 + (i >> 1) * 16, t.e);
+              for (int i = 0; i < 4; ++i) tma_load_4d(to + i * 1024, &tmScaleA, bar, k0 * 8, f0 + 16 * i, 0, t.e);
             } else {
-              tma_load_3d(to, &tmScaleA, bar, k0 * 8, f0, t.e);
+              tma_load_4d(to, &tmScaleA, bar, k0 * 8, f0, 0, t.e);
             }
             tma_load_2d(to + 4096, &tmScaleB, bar, k0 * 8, t.row0);
           }
@@ -356,7 +394,7 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
           if ((n_scales & 3) == 0) cp_async_arrive(&bars.slot_full[slot]); else mbar_arrive(&bars.slot_full[slot]);
         }
         __syncwarp();
-        if (k0 == 0) next = tile_at(tile + n_pairs);
+        if (k0 == 0) next = tile_after(t);
         if (++slot == kMxSlots) { slot = 0; lph ^= 1; }
       }
     }
@@ -391,8 +429,8 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
     const bool issuer = lead && elect_one();
     int buf = 0, acc = 0;
     uint32_t aph = 0;
-    for (int tile = pair; tile < n_total; tile += n_pairs) {
-      const Tile t = tile_at(tile);
+    Tile t = first_tile();
+    for (int tile = pair; tile < n_total; tile += n_pairs, t = tile_after(t)) {
       const int f0 = (t.m * 2 + static_cast<int>(rank)) * width;
       const bool whole = f0 + width <= l.n_out;
       const long long ld = l.n_out;
@@ -512,6 +550,7 @@ cudaError_t launch(ExpertMxParams& p, const CUtensorMap& a, const CUtensorMap& b
     tiles = (l.R / rows + (l.R < l.E ? l.R : l.E)) * p.m_tiles;   // at most, whatever the offsets are
     if (tiles <= pairs || l.R <= rows) break;
   }
+  p.rows_of = AnyRows::of(p.tile_rows);
   const uint64_t bytes = l.n_in / 2, db[2] = {bytes, static_cast<uint64_t>(l.R)}, stb[1] = {bytes};
   const uint32_t box[2] = {128, static_cast<uint32_t>(p.tile_rows) / 2};
   CUtensorMap b, scale_b;
@@ -534,20 +573,21 @@ cudaError_t launch_expert_mx(ExpertMxParams p, int n_sms, cudaStream_t s) {
   const int per = l.gated ? 128 : 256;
   p.m_tiles = (l.n_out + per - 1) / per;
   const uint64_t R = static_cast<uint64_t>(l.R), bytes = l.n_in / 2, nz = l.n_z, E = l.E, no = l.n_out;
-  const uint64_t da[3] = {bytes, nz, E}, sta[2] = {bytes, bytes * nz}, db[2] = {bytes, R}, stb[1] = {bytes};
-  const uint32_t boxa[3] = {128, l.gated ? 16u : 128u, 1}, box16[2] = {128, 16}, box_out[2] = {64, kMxChunk}, box_out16[2] = {64, 16};
+  // the weights as [E][g, u][n_out] (one of the two where there is no gate)
+  const uint64_t parts = l.gated ? 2 : 1, da[4] = {bytes, no, parts, E}, sta[3] = {bytes, bytes * no, bytes * nz}, db[2] = {bytes, R}, stb[1] = {bytes};
+  const uint32_t rows_a = l.gated ? 16 : 128, boxa[4] = {128, rows_a, static_cast<uint32_t>(parts), 1}, box16[2] = {128, 16}, box_out[2] = {64, kMxChunk}, box_out16[2] = {64, 16};
   const uint64_t dout[2] = {no, R}, stout[1] = {no * 2};
   CUtensorMap a, b16, out, out16;
-  if (!encode_u8(&a, l.W, 3, da, sta, boxa) || !encode_u8(&b16, l.X, 2, db, stb, box16) ||
+  if (!encode_u8(&a, l.W, 4, da, sta, boxa) || !encode_u8(&b16, l.X, 2, db, stb, box16) ||
       !encode_bf16(&out, l.out, 2, dout, stout, box_out) || !encode_bf16(&out16, l.out, 2, dout, stout, box_out16))
     return cudaErrorInvalidValue;
   // rows of scales of whole 16-byte words: the copy engine's
   p.scale_maps = l.n_in % 512 == 0;
   CUtensorMap scale_a = a;
   if (p.scale_maps) {
-    const uint64_t n = l.n_in / 32, ds[3] = {n, nz, E}, sts[2] = {n, n * nz};
-    const uint32_t boxs[3] = {32, l.gated ? 16u : 128u, 1};
-    if (!encode_u8(&scale_a, p.w_scale, 3, ds, sts, boxs)) return cudaErrorInvalidValue;
+    const uint64_t n = l.n_in / 32, ds[4] = {n, no, parts, E}, sts[3] = {n, n * no, n * nz};
+    const uint32_t boxs[4] = {32, rows_a, static_cast<uint32_t>(parts), 1};
+    if (!encode_u8(&scale_a, p.w_scale, 4, ds, sts, boxs)) return cudaErrorInvalidValue;
   }
   return with_act(l.act, [&](auto act) {
     constexpr int kAct = decltype(act)::value;

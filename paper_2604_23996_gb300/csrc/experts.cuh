@@ -87,6 +87,19 @@ cudaError_t launch_expert_gemm(const ExpertLinearParams& p, ExpertGemmMode mode,
                                int n_sms, cudaStream_t s);
 cudaError_t launch_expert_gemm_f32(const ExpertLinearParams& p, ExpertGemmMode mode, uint32_t* status, uint64_t limit_ns,
                                    int n_sms, cudaStream_t s);
+// The rows of a tile: a power of two, or any number.
+struct ShiftRows {
+  int shift;
+  __device__ __forceinline__ int tiles(int rows) const { return rows > 0 ? (rows + (1 << shift) - 1) >> shift : 0; }
+  __device__ __forceinline__ int first(int tile) const { return tile << shift; }
+};
+struct AnyRows {
+  int n;
+  uint32_t inv;                                  // ceil(2^32 / n): exact for fewer than 2^32 / n rows, 2^24 for n up to 255
+  static AnyRows of(int n) { return AnyRows{n, static_cast<uint32_t>(((1ull << 32) + n - 1) / n)}; }
+  __device__ __forceinline__ int tiles(int rows) const { return rows > 0 ? __umulhi(rows + n - 1, inv) : 0; }
+  __device__ __forceinline__ int first(int tile) const { return tile * n; }
+};
 // The forward's product of microscaled 4-bit rows and weights (l.X and l.W hold the pairs of codes; expert_mx.cu).
 struct ExpertMxParams {
   ExpertLinearParams l;
@@ -94,6 +107,7 @@ struct ExpertMxParams {
   const uint8_t* w_scale;    // [E, n_z, n_in / 32]
   int m_tiles;
   int tile_rows;
+  AnyRows rows_of;           // tile_rows
   int scale_maps;            // the copy engine brings the scales
   uint32_t* status;
   uint64_t limit_ns;
@@ -125,25 +139,13 @@ __device__ __forceinline__ long long expert_begin(const int32_t* off, int e, lon
 struct RowTile {
   int e;
   int row0, row1;            // the tile's first row, the expert's end
+  int before, tiles;         // tiles of the experts before, and of this one
 };
 struct RowTiles {
   int before;                // lane l: tiles of the experts before 8 l
   int total;
 };
 __device__ __forceinline__ int expert_row(const int32_t* off, int e, int R) { return min(max(off[e], 0), R); }
-// The rows of a tile: a power of two, or any number.
-struct ShiftRows {
-  int shift;
-  __device__ __forceinline__ int tiles(int rows) const { return rows > 0 ? (rows + (1 << shift) - 1) >> shift : 0; }
-  __device__ __forceinline__ int first(int tile) const { return tile << shift; }
-};
-struct AnyRows {
-  int n;
-  __device__ __forceinline__ int tiles(int rows) const {
-    return rows > 0 ? static_cast<int>(static_cast<unsigned>(rows + n - 1) / static_cast<unsigned>(n)) : 0;
-  }
-  __device__ __forceinline__ int first(int tile) const { return tile * n; }
-};
 // The counts, by one warp from the offsets in global memory: lane l's to before[l], the total to before[32].
 template <class Rows>
 __device__ inline void count_row_tiles(const int32_t* offsets, int E, int R, Rows of, int* before) {
@@ -180,6 +182,8 @@ __device__ __forceinline__ RowTile find_row_tile(const RowTiles& t, const int32_
   const int src = __ffs(__ballot_sync(0xffffffffu, lane < 8 && in < run)) - 1;
   RowTile r;
   r.e = q * 8 + src;
+  r.before = __shfl_sync(0xffffffffu, t.before, q) + __shfl_sync(0xffffffffu, run - n, src);
+  r.tiles = __shfl_sync(0xffffffffu, n, src);
   r.row0 = expert_row(off, r.e, R) + of.first(in - __shfl_sync(0xffffffffu, run - n, src));
   r.row1 = expert_row(off, r.e + 1, R);
   return r;
