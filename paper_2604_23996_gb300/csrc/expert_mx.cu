@@ -53,10 +53,8 @@ constexpr uint32_t kMxSmem = 1024 + kMxRing + kMxSlots * kMxSlot + kGemmGroups *
 static_assert(kMxScaleCols + kMxSets * kMxSetCols <= 512, "tensor memory");
 static_assert(kMxSmem <= 227 * 1024, "shared memory of a CTA");
 struct MxBars {
-  uint64_t full[kMxStagesMost];                  // operands of both CTAs (first CTA's)
+  uint64_t full[kMxStagesMost];                  // operands and scales of both CTAs (first CTA's)
   uint64_t empty[kMxStagesMost];
-  uint64_t scales[kMxSets];                      // scales of both CTAs (first CTA's)
-  uint64_t scales_empty[kMxSets];
   uint64_t slot_full[kMxSlots], slot_empty[kMxSlots];
   uint64_t acc_full[2], acc_empty[2];
   uint32_t tmem;
@@ -64,6 +62,7 @@ struct MxBars {
   int before[33];
 };
 static_assert(sizeof(MxBars) <= kBarBytes, "barriers");
+static_assert(kMxRing / (kMxA + kRowsMost * 64) > kMxSets, "a block's scales arrive after the stage's block before is done");
 
 // 16 scale bytes of each of kUnits rows, `step` bytes apart, to shared memory 1024 bytes apart; the first there[i] of them, zeros
 // behind. Whole words of kBytes are copied; with kBytes = 0 (rows of no whole 4-byte words) they are put together from the aligned
@@ -107,6 +106,47 @@ __device__ __forceinline__ uint32_t scale_at(uint32_t slot, int r, int h) {
   return slot + static_cast<uint32_t>(r) * 32u + static_cast<uint32_t>((h ^ (r >> 2)) & 1) * 16u;
 }
 
+// The epilogue's sums and products go two at a time (f32x2): of the instructions that an SM issues under dsmoe_vlm's gated layer
+// half were its epilogue's.
+__device__ __forceinline__ void add_bias(float (&v)[16], const float (&bias)[2]) {
+#pragma unroll
+  for (int j = 0; j < 16; j += 2) {
+    const float b = bias[(j >> 1) & 1];
+    const uint64_t s = fadd2(pack2(v[j], v[j + 1]), pack2(b, b));
+    v[j] = lo2(s);
+    v[j + 1] = hi2(s);
+  }
+}
+// act(v) in place.
+template <int kAct>
+__device__ __forceinline__ void activate(float (&v)[16]) {
+#pragma unroll
+  for (int j = 0; j < 16; j += 2) {
+    if (kAct == SMOES_ACT_SILU) {
+      const uint64_t z = pack2(v[j], v[j + 1]);
+      const uint64_t w = fmul2(z, pack2(-kLog2E, -kLog2E));
+      const uint64_t e = fadd2(pack2(fast_exp2(lo2(w)), fast_exp2(hi2(w))), pack2(1.f, 1.f));
+      const uint64_t y = fmul2(z, pack2(fast_reciprocal(lo2(e)), fast_reciprocal(hi2(e))));
+      v[j] = lo2(y);
+      v[j + 1] = hi2(y);
+    } else {
+      v[j] = act_value<kAct, true>(v[j]);
+      v[j + 1] = act_value<kAct, true>(v[j + 1]);
+    }
+  }
+}
+// act(v) u in place.
+template <int kAct>
+__device__ __forceinline__ void gate(float (&v)[16], const float (&u)[16]) {
+  if (kAct != SMOES_ACT_NONE) activate<kAct>(v);
+#pragma unroll
+  for (int j = 0; j < 16; j += 2) {
+    const uint64_t y = fmul2(pack2(v[j], v[j + 1]), pack2(u[j], u[j + 1]));
+    v[j] = lo2(y);
+    v[j + 1] = hi2(y);
+  }
+}
+
 template <int kAct, bool kGated>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMxGemmThreads, 1)
 k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
@@ -133,12 +173,8 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < n_stages; ++i) {
-      mbar_init(&bars.full[i], 4);
+      mbar_init(&bars.full[i], 1 + 2 * kMxScaleWarps);
       mbar_init(&bars.empty[i], 1);
-    }
-    for (int i = 0; i < kMxSets; ++i) {
-      mbar_init(&bars.scales[i], 2 * kMxScaleWarps);
-      mbar_init(&bars.scales_empty[i], 1);
     }
     for (int i = 0; i < kMxSlots; ++i) {
       mbar_init(&bars.slot_full[i], p.scale_maps ? 1 : 32 * kMxCopyWarps);
@@ -240,7 +276,8 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
           const int x = kb * 128;
           if (!rows) {
             uint8_t* a = stage_a(st);
-            mbar_arrive_expect_tx_peer(bar, kMxA);
+            // the first CTA expects the bytes of both (the second one's may come before: the phase waits for this arrival)
+            if (rank == 0) mbar_arrive_expect_tx(&bars.full[st], 2 * kMxA + half * 256u);
             if (kGated) {                        // 16 features of g, the same of u, the next 16 ...
 #pragma unroll
               for (int i = 0; i < 4; ++i) tma_load_4d_pair(a + i * 4096, &tmA, bar, x, f0 + 16 * i, 0, t.e);
@@ -249,7 +286,6 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
             }
           } else {
             uint8_t* b = stage_b(st);
-            mbar_arrive_expect_tx_peer(bar, half * 128u);
             if (2 * half == p.tile_rows) {
               tma_load_2d_pair(b, &tmB, bar, x, r0);
             } else {
@@ -270,32 +306,34 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
   } else if (warp == 1 && rank == 0) {
     // ----------------------------------------------------------------------------- MMA issuer
     int st = 0, acc = 0, set = 0;
-    uint32_t ph = 0, aph = 0, sph = 0;
+    uint32_t ph = 0, aph = 0;
     bool ok = true;
+    const uint64_t a0 = sdesc_sw128(smem_u32(stage_a(0)), 16, 1024), b0 = sdesc_sw128(smem_u32(stage_b(0)), 16, 1024);
     Tile next = first_tile();
     for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
       const Tile t = next;
       const int n = min((t.rows + 31) & ~31, p.tile_rows);
+      const uint32_t id0 = idesc_mx4(256, n, 0), id1 = idesc_mx4(256, n, 1);
       if (!warp_wait(&bars.acc_empty[acc], aph ^ 1, wc)) break;
       tc_fence_after();
       const uint32_t d = tmem + acc * kRowsMost;
       for (int kb = 0; kb < blocks; ++kb) {
-        if (!warp_wait(&bars.scales[set], sph, wc) || !warp_wait(&bars.full[st], ph, wc)) { ok = false; break; }
+        if (!warp_wait(&bars.full[st], ph, wc)) { ok = false; break; }
         tc_fence_after();
         if (elect_one()) {
-          const uint32_t a = smem_u32(stage_a(st)), b = smem_u32(stage_b(st));
+          const uint64_t at = (st * stage_bytes) >> 4, da = a0 + at, db = b0 + at;
           const uint32_t sa = tmem + kMxScaleCols + set * kMxSetCols;
-#pragma unroll
-          for (int s = 0; s < 4; ++s)              // 64 of the depth an instruction
-            umma_mx4_pair(d, sdesc_sw128(a + s * 32, 16, 1024), sdesc_sw128(b + s * 32, 16, 1024), idesc_mx4(256, n, s & 1),
-                          sa + 12 * (s >> 1), sa + 12 * (s >> 1) + 4, kb > 0 || s > 0);
+          // 64 of the depth an instruction: 32 bytes of each row, one half of a scale word
+          umma_mx4_pair(d, da, db, id0, sa, sa + 4, kb > 0);
+          umma_mx4_pair(d, da + 2, db + 2, id1, sa, sa + 4, 1u);
+          umma_mx4_pair(d, da + 4, db + 4, id0, sa + 12, sa + 16, 1u);
+          umma_mx4_pair(d, da + 6, db + 6, id1, sa + 12, sa + 16, 1u);
           umma_commit_pair(&bars.empty[st]);
-          umma_commit_pair(&bars.scales_empty[set]);
           if (kb == blocks - 1) umma_commit_pair(&bars.acc_full[acc]);
         }
         __syncwarp();
         if (kb == 0) next = tile_after(t);
-        if (++set == kMxSets) { set = 0; sph ^= 1; }
+        set = (set + 1) % kMxSets;
         if (++st == n_stages) { st = 0; ph ^= 1; }
       }
       if (++acc == 2) { acc = 0; aph ^= 1; }
@@ -304,8 +342,10 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
     // ------------------------------------------------------------------- scales to tensor memory
     const uint32_t slots = smem_u32(scale_ring);
     const uint32_t cols = tmem + (static_cast<uint32_t>(32 * (warp & 3)) << 16) + kMxScaleCols;
-    int slot = 0, set = 0;
-    uint32_t lph = 0, sph = 0;
+    // A set is stored to once the products of the block kMxSets before are done (its stage's `empty`), and the store arrives at
+    // the `full` of the block's own stage: with more stages than sets its phase before is over.
+    int slot = 0, set = 0, st = 0, old = 0, stored = 0;
+    uint32_t lph = 0, oph = 0;
     bool ok = true;
     for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
       for (int k0 = 0; ok && k0 < blocks; k0 += kMxRound) {
@@ -317,9 +357,14 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
           for (int g = 0; g < kMxGroups; ++g)
             asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v[g][0]), "=r"(v[g][1])
                          : "r"(scale_at(from, g * 32 + lane, b >> 1) + 8 * (b & 1)));
-          ok = warp_wait(&bars.scales_empty[set], sph ^ 1, wc);
-          if (!ok) break;
-          tc_fence_after();
+          if (stored < kMxSets) {
+            ++stored;
+          } else {
+            ok = warp_wait(&bars.empty[old], oph, wc);
+            if (!ok) break;
+            tc_fence_after();
+            if (++old == n_stages) { old = 0; oph ^= 1; }
+          }
           const uint32_t to = cols + set * kMxSetCols;
 #pragma unroll
           for (int w = 0; w < 2; ++w) {
@@ -329,17 +374,14 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
           tmem_st_wait();
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive_peer(peer_smem(&bars.scales[set], 0));
+          if (lane == 0) mbar_arrive_peer(peer_smem(&bars.full[st], 0));
           __syncwarp();
-          if (++set == kMxSets) { set = 0; sph ^= 1; }
+          set = (set + 1) % kMxSets;
+          if (++st == n_stages) st = 0;
         }
         if (lane == 0) mbar_arrive(&bars.slot_empty[slot]);   // (every lane's words have arrived: the warp stored them)
         if (++slot == kMxSlots) { slot = 0; lph ^= 1; }
       }
-    }
-    for (int i = 0; ok && i < kMxSets; ++i) {    // every set given back, as the producer's stages
-      ok = warp_wait(&bars.scales_empty[set], sph ^ 1, wc);
-      if (++set == kMxSets) { set = 0; sph ^= 1; }
     }
   } else if (warp >= kMxCopy && warp < kMxRows && (warp == kMxCopy || !p.scale_maps)) {
     // ------------------------------------------------------------------- scales to shared memory
@@ -468,15 +510,14 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
           }
           float v[16];                           // [rows 8 n][features 8 i][two rows]
           tmem_ld_16x256b_x4(from + (static_cast<uint32_t>(16 * h) << 16), v);
+          if (l.bias) add_bias(v, bias[h]);
           if (kGated) {
             float u[16];
             tmem_ld_16x256b_x4(from + (16u << 16), u);
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-              v[j] = act_value<kAct, true>(v[j] + bias[0][(j >> 1) & 1]) * (u[j] + bias[1][(j >> 1) & 1]);
-          } else {
-#pragma unroll
-            for (int j = 0; j < 16; ++j) v[j] = act_value<kAct, true>(v[j] + bias[h][(j >> 1) & 1]);
+            if (l.bias) add_bias(u, bias[1]);
+            gate<kAct>(v, u);
+          } else if (kAct != SMOES_ACT_NONE) {
+            activate<kAct>(v);
           }
           if (h == kHalves - 1 && c + kGemmGroups >= chunks) {   // the accumulator's last use
             tc_fence_before();
