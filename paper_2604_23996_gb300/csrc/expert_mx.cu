@@ -49,19 +49,29 @@ constexpr int kMxSlots = 3;
 constexpr uint32_t kMxSlot = kMxGroups * 32 * 32;
 constexpr int kMxChunk = 32;                     // rows that an epilogue group finishes at a time
 constexpr uint32_t kMxStaging = 8192;            // one group's output boxes of 64 features by 32 rows: two, gated two chunks of one
-constexpr uint32_t kMxSmem = 1024 + kMxRing + kMxSlots * kMxSlot + kGemmGroups * kMxStaging + kBarBytes + 4 * (kExpertsMax + 1);
+constexpr uint32_t kMxBarBytes = 1024;
+constexpr uint32_t kMxSmem = 1024 + kMxRing + kMxSlots * kMxSlot + kGemmGroups * kMxStaging + kMxBarBytes + 4 * (kExpertsMax + 1);
 static_assert(kMxScaleCols + kMxSets * kMxSetCols <= 512, "tensor memory");
 static_assert(kMxSmem <= 227 * 1024, "shared memory of a CTA");
+// The pair's tiles for the epilogue, written by the rows' producer. It is at most the stages, two accumulators and the tile it
+// looks up ahead of the epilogue: fewer than kMxNotes tiles, so no note is written over before it is read.
+constexpr int kMxNotes = 16;
+struct alignas(16) MxNote {
+  int e, m, row0, rows;
+};
+
 struct MxBars {
   uint64_t full[kMxStagesMost];                  // operands and scales of both CTAs (first CTA's)
   uint64_t empty[kMxStagesMost];
   uint64_t slot_full[kMxSlots], slot_empty[kMxSlots];
   uint64_t acc_full[2], acc_empty[2];
+  uint64_t note_full[kMxNotes];
   uint32_t tmem;
   int abort;
   int before[33];
+  MxNote notes[kMxNotes];
 };
-static_assert(sizeof(MxBars) <= kBarBytes, "barriers");
+static_assert(sizeof(MxBars) <= kMxBarBytes && kMxStagesMost + 4 < kMxNotes, "barriers");
 static_assert(kMxRing / (kMxA + kRowsMost * 64) > kMxSets, "a block's scales arrive after the stage's block before is done");
 
 // 16 scale bytes of each of kUnits rows, `step` bytes apart, to shared memory 1024 bytes apart; the first there[i] of them, zeros
@@ -158,7 +168,7 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
   uint8_t* scale_ring = smem + kMxRing;
   uint8_t* staging = scale_ring + kMxSlots * kMxSlot;
   MxBars& bars = *reinterpret_cast<MxBars*>(staging + kGemmGroups * kMxStaging);
-  int32_t* off = reinterpret_cast<int32_t*>(staging + kGemmGroups * kMxStaging + kBarBytes);   // [E + 1] offsets
+  int32_t* off = reinterpret_cast<int32_t*>(staging + kGemmGroups * kMxStaging + kMxBarBytes);   // [E + 1] offsets
   const ExpertLinearParams& l = p.l;
   const int warp = warp_index(), lane = threadIdx.x & 31;
   const int R = static_cast<int>(l.R);
@@ -184,6 +194,7 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
       mbar_init(&bars.acc_full[i], 1);
       mbar_init(&bars.acc_empty[i], 2 * kMxEpiWarps);
     }
+    for (int i = 0; i < kMxNotes; ++i) mbar_init(&bars.note_full[i], 1);
     bars.abort = 0;
     fence_mbar_init();
     tma_prefetch_desc(&tmA);
@@ -260,12 +271,17 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
   if (warp == 0 || warp == kMxRows) {
     // ------------------------------------------------------------------------------- producers
     const bool rows = warp == kMxRows;
-    int st = 0;
+    int st = 0, note = 0;
     uint32_t ph = 0;
     bool ok = true;
     Tile next = first_tile();
     for (int tile = pair; ok && tile < n_total; tile += n_pairs) {
       const Tile t = next;
+      if (rows && lane == 0) {
+        bars.notes[note] = MxNote{t.e, t.m, t.row0, t.rows};
+        mbar_arrive(&bars.note_full[note]);
+      }
+      note = (note + 1) % kMxNotes;
       const int half = min((t.rows + 31) & ~31, p.tile_rows) / 2;
       const int r0 = t.row0 + static_cast<int>(rank) * half;
       const int f0 = t.m * (kGated ? 128 : 256) + static_cast<int>(rank) * (kGated ? 64 : 128);
@@ -366,11 +382,9 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
             if (++old == n_stages) { old = 0; oph ^= 1; }
           }
           const uint32_t to = cols + set * kMxSetCols;
-#pragma unroll
-          for (int w = 0; w < 2; ++w) {
-            tmem_st4(to + 12 * w, v[0][w], v[1][w], v[2][w], v[3][w]);
-            tmem_st8(to + 12 * w + 4, v[4][w], v[5][w], v[6][w], v[7][w], v[8][w], v[9][w], v[10][w], 0u);
-          }
+          tmem_st16(to, {v[0][0], v[1][0], v[2][0], v[3][0], v[4][0], v[5][0], v[6][0], v[7][0], v[8][0], v[9][0], v[10][0], 0u,
+                         v[0][1], v[1][1], v[2][1], v[3][1]});
+          tmem_st8(to + 16, v[4][1], v[5][1], v[6][1], v[7][1], v[8][1], v[9][1], v[10][1], 0u);
           tmem_st_wait();
           tc_fence_before();
           __syncwarp();
@@ -471,8 +485,9 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
     const bool issuer = lead && elect_one();
     int buf = 0, acc = 0;
     uint32_t aph = 0;
-    Tile t = first_tile();
-    for (int tile = pair; tile < n_total; tile += n_pairs, t = tile_after(t)) {
+    for (int tile = pair, i = 0; tile < n_total; tile += n_pairs, ++i) {
+      const bool told = warp_wait(&bars.note_full[i % kMxNotes], (i / kMxNotes) & 1, wc);
+      const MxNote t = told ? bars.notes[i % kMxNotes] : MxNote{};
       const int f0 = (t.m * 2 + static_cast<int>(rank)) * width;
       const bool whole = f0 + width <= l.n_out;
       const long long ld = l.n_out;
@@ -486,7 +501,8 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
             if (f < l.n_out) bias[h][i] = __ldg(l.bias + static_cast<long long>(t.e) * l.n_z + f + (kGated ? h * l.n_out : 0));
           }
       }
-      if (!named_bar_all(kBarVote + g, 128, !lead || warp_wait(&bars.acc_full[acc], aph, wc))) break;
+      // one answer for the group: a warp whose wait ran out takes the others along
+      if (!named_bar_all(kBarVote + g, 128, told && (!lead || warp_wait(&bars.acc_full[acc], aph, wc)))) break;
       tc_fence_after();
       const int chunks = (t.rows + kMxChunk - 1) / kMxChunk;
       for (int c = g; c < chunks; c += kGemmGroups) {
@@ -496,6 +512,9 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
         const uint32_t from = tmem + acc * kRowsMost + c * kMxChunk + lanes;
 #pragma unroll
         for (int h = 0; h < kHalves; ++h) {
+          uint32_t raw[kGated ? 2 : 1][16];      // gated: g and u; [rows 8 n][features 8 i][two rows]
+          tmem_ld_16x256b_x4(from + (static_cast<uint32_t>(16 * h) << 16), raw[0]);
+          if constexpr (kGated) tmem_ld_16x256b_x4(from + (16u << 16), raw[1]);
           // the residual's words, transposed as the accumulators are: [rows 8 n][features 8 i]
           uint32_t rv[4][2];
           if (l.residual) {
@@ -508,24 +527,28 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
                 rv[n][i] = 8 * n + (lane >> 2) < rows && f + 8 * i < l.n_out
                                ? __ldg(reinterpret_cast<const uint32_t*>(res + 8 * n * ld + 8 * i)) : 0u;
           }
-          float v[16];                           // [rows 8 n][features 8 i][two rows]
-          tmem_ld_16x256b_x4(from + (static_cast<uint32_t>(16 * h) << 16), v);
-          if (l.bias) add_bias(v, bias[h]);
-          if (kGated) {
-            float u[16];
-            tmem_ld_16x256b_x4(from + (16u << 16), u);
-            if (l.bias) add_bias(u, bias[1]);
-            gate<kAct>(v, u);
-          } else if (kAct != SMOES_ACT_NONE) {
-            activate<kAct>(v);
-          }
+          tmem_ld_ready(raw[0]);
+          if constexpr (kGated) tmem_ld_ready(raw[1]);
           if (h == kHalves - 1 && c + kGemmGroups >= chunks) {   // the accumulator's last use
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_peer(peer_smem(&bars.acc_empty[acc], 0));
           }
+          float v[16];
+#pragma unroll
+          for (int j = 0; j < 16; ++j) v[j] = __uint_as_float(raw[0][j]);
+          if (l.bias) add_bias(v, bias[h]);
+          if constexpr (kGated) {
+            float u[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) u[j] = __uint_as_float(raw[1][j]);
+            if (l.bias) add_bias(u, bias[1]);
+            gate<kAct>(v, u);
+          } else if (kAct != SMOES_ACT_NONE) {
+            activate<kAct>(v);
+          }
+          __syncwarp();
           if (l.residual) {
-            __syncwarp();
 #pragma unroll
             for (int n = 0; n < 4; ++n)
 #pragma unroll
