@@ -26,7 +26,7 @@ struct Layout {
   size_t status, sample_ticket, loss_ticket, offsets, token_sample, expert_bin, expert_slot,
       piece_base, sample_pieces, pieces, mi32, tabs, gsave, ginv, dw_part, dz_img, perm, attn_ticket, attn_part,
       gcoef, perm_sync, fperm, stat_part, stat_nvis, stat_n0, f32_part, tile_ticket, bal_flag,
-      bal_f, bal_a, bal_h, bal_s, bal_u, gmmcoef, ebal_ticket, ebal_base, ebal_h, ebal_c, ebal_n, ebal_loss;
+      bal_f, bal_a, bal_h, bal_s, bal_u, gmmcoef, ebal_ticket, ebal_base, ebal_part, ebal_n, ebal_loss;
   size_t header_bytes;   // [0, header_bytes) is cleared by smoes_workspace_init
   size_t total;
 };
@@ -437,10 +437,9 @@ smoes_status smoes_plan_create(const smoes_router_desc* desc, smoes_plan* out) {
   L.bal_h = take(sizeof(float) * static_cast<size_t>(P->bal_blocks) * E);
   L.bal_s = take(sizeof(int32_t) * static_cast<size_t>(P->bal_blocks) * E);
   L.bal_u = take(sizeof(int32_t) * static_cast<size_t>(P->bal_blocks) * K);
-  const size_t ebal_rows = 2 * static_cast<size_t>(T / P->ebal_len + 1);
+  const size_t ebal_rows = 2 * static_cast<size_t>(T / P->ebal_len + 1) + 32;   // with up to 32 samples a row per run
   L.ebal_base = take(sizeof(int32_t) * (B + 1));
-  L.ebal_h = take(sizeof(float) * ebal_rows * E);
-  L.ebal_c = take(sizeof(int32_t) * ebal_rows * E);
+  L.ebal_part = take(sizeof(uint2) * ebal_rows * E);
   L.ebal_n = take(sizeof(int32_t) * ebal_rows);
   L.ebal_loss = take(sizeof(float) * std::max(B, 1));
   L.f32_part = take(d.dtype == SMOES_F32 ? sizeof(float) * static_cast<size_t>(P->n_groups) *
@@ -919,8 +918,7 @@ smoes_status smoes_expert_balance(smoes_plan P, const int32_t* topk_idx, int per
   p.offsets = v.offsets;
   p.base = reinterpret_cast<const int32_t*>(b + P->L.ebal_base);
   p.scale = loss_scale;
-  p.part_h = reinterpret_cast<float*>(b + P->L.ebal_h);
-  p.part_c = reinterpret_cast<int32_t*>(b + P->L.ebal_c);
+  p.part = reinterpret_cast<uint2*>(b + P->L.ebal_part);
   p.part_n = reinterpret_cast<int32_t*>(b + P->L.ebal_n);
   p.sample_loss = reinterpret_cast<float*>(b + P->L.ebal_loss);
   p.ticket = reinterpret_cast<uint32_t*>(b + P->L.ebal_ticket);

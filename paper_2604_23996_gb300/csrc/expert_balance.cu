@@ -7,10 +7,11 @@
 // so the gradient leaves as a table [B, E] that the backward reads per sample.
 //
 // A block takes a run of at most `len` tokens of one sample, a warp a token at a time (lane l holds experts l, l + 32,
-// ...), kR tokens with their loads in flight. Runs of a longer sample leave partials, and the block that finishes last
-// adds them in order (a ticket per sample); the block that finishes the last sample adds the samples' losses. The sums
-// are fp32 in a fixed order, whichever block makes them. Bound by the gate values' bytes; small batches by the latency
-// of one launch and the hand-over between the blocks.
+// ...), kR tokens at work and kR on their way. Runs of a sample that has several leave partials. Up to kFewSamples samples are
+// finished by the block that arrives last of all, a warp a sample; with more of them each by the last of its own blocks, and
+// the losses are added by the one that finishes the last sample. The sums are fp32 in a fixed order, whichever block makes
+// them. Bound by the gate values' bytes (131072 x 128: %LARGE% us for 10.6 us of HBM); small batches by the latency of a launch, two
+// reads and one hand-over between the blocks.
 #include "device_common.cuh"
 #include "ptx.cuh"
 #include "smoes_internal.cuh"
@@ -20,6 +21,15 @@ namespace {
 
 constexpr int kR = 4;
 constexpr int kCols = 128;                          // experts at most
+constexpr int kFewSamples = 32;                   // (the workspace has a row for each beside those of whole runs)
+
+// An arrival that hands over what the block wrote, and takes what the blocks before it handed over (thread 0, between two
+// block barriers).
+__device__ __forceinline__ uint32_t arrive(uint32_t* ticket) {
+  uint32_t old;
+  asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(old) : "l"(ticket) : "memory");
+  return old;
+}
 
 // The sum over the block of one value per thread, by thread 0's warp; the same order every time.
 __device__ __forceinline__ float block_sum(float v, float* scratch) {
@@ -36,11 +46,21 @@ template <int PL, int kThreads>
 __global__ void __launch_bounds__(kThreads) k_expert_balance(const ExpertBalanceParams p) {
   constexpr int kWarps = kThreads / 32;
   constexpr int kSlices = kThreads / kCols;
-  __shared__ float hs[kWarps][PL * 32];
+  // the warps' sums, then (behind a barrier) those of the samples or of the slices of one
+  union Sums {
+    float hs[kWarps][PL * 32];
+    struct {
+      float h[kFewSamples][kCols];
+      int c[kFewSamples][kCols];
+    } few;
+    struct {
+      float h[kSlices][kCols];
+      int c[kSlices][kCols];
+    } slices;
+  };
+  __shared__ Sums sums;
   __shared__ int cs[PL * 32];
-  __shared__ int ns;
-  __shared__ float h_sl[kSlices][kCols];
-  __shared__ int c_sl[kSlices][kCols], n_sl[kSlices];
+  __shared__ int ns, N_s[kFewSamples];
   __shared__ float scratch[32];
   __shared__ int last;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -69,57 +89,149 @@ __global__ void __launch_bounds__(kThreads) k_expert_balance(const ExpertBalance
 #pragma unroll
   for (int i = 0; i < PL; ++i) h[i] = 0.f;
   int n = 0;
-  for (int j0 = r0 + warp; j0 < r1; j0 += kR * kWarps) {
+  struct In {
     float g[kR][PL], inv[kR];
     int sel[kR];
+  };
+  auto load = [&](int j0, In& in) {
 #pragma unroll
     for (int r = 0; r < kR; ++r) {
       const int j = j0 + r * kWarps;
-      const bool in = j < r1;
+      const bool there = j < r1;
 #pragma unroll
       for (int i = 0; i < PL; ++i) {
         const int e = lane + 32 * i;
-        g[r][i] = in && e < E ? __ldcg(p.gsave + static_cast<size_t>(j) * E + e) : 0.f;
+        in.g[r][i] = there && e < E ? __ldcg(p.gsave + static_cast<size_t>(j) * E + e) : 0.f;
       }
-      inv[r] = in ? __ldcg(p.ginv + j) : 0.f;
-      sel[r] = in && lane < k ? __ldg(p.topk_idx + static_cast<size_t>(j) * k + lane) : -1;
+      in.inv[r] = there ? __ldcg(p.ginv + j) : 0.f;
+      in.sel[r] = there && lane < k ? __ldg(p.topk_idx + static_cast<size_t>(j) * k + lane) : -1;
     }
+  };
+  In nx;
+  load(r0 + warp, nx);
+#pragma unroll 1
+  for (int j0 = r0 + warp; j0 < r1; j0 += kR * kWarps) {
+    const In in = nx;
+    if (j0 + kR * kWarps < r1) load(j0 + kR * kWarps, nx);
 #pragma unroll
     for (int r = 0; r < kR; ++r) {
-      const bool ok = sel[r] >= 0 && sel[r] < E;
-      if (ok) atomicAdd(&cs[sel[r]], 1);
+      const bool ok = in.sel[r] >= 0 && in.sel[r] < E;
+      if (ok) atomicAdd(&cs[in.sel[r]], 1);
       if (__any_sync(0xffffffffu, ok)) {
         ++n;
 #pragma unroll
-        for (int i = 0; i < PL; ++i) h[i] = fmaf(g[r][i], inv[r], h[i]);
+        for (int i = 0; i < PL; ++i) h[i] = fmaf(in.g[r][i], in.inv[r], h[i]);
       }
     }
   }
 #pragma unroll
-  for (int i = 0; i < PL; ++i) hs[warp][lane + 32 * i] = h[i];
+  for (int i = 0; i < PL; ++i) sums.hs[warp][lane + 32 * i] = h[i];
   if (lane == 0 && n) atomicAdd(&ns, n);
   __syncthreads();
   float H = 0.f;
   int C = 0, N = ns;
   if (tid < E) {
-    for (int w = 0; w < kWarps; ++w) H += hs[w][tid];
+    for (int w = 0; w < kWarps; ++w) H += sums.hs[w][tid];
     C = cs[tid];
   }
-  if (runs > 1) {
-    // where a run's partials lie: two runs of longer samples begin in a window of `len` tokens at most, and only one of
-    // them is its sample's last
-    auto row = [&](int run) { return static_cast<size_t>(2 * ((first + run * p.len) / p.len) + (run == runs - 1 ? 1 : 0)); };
-    if (tid < E) {
-      p.part_h[row(c) * E + tid] = H;
-      p.part_c[row(c) * E + tid] = C;
-    }
-    if (tid == 0) p.part_n[row(c)] = N;
-    __threadfence();
+  // where a run's partials lie: with few samples at its block; otherwise two runs of samples that have several begin in a
+  // window of `len` tokens at most, and only one of them is its sample's last
+  auto row = [&](int run) { return static_cast<size_t>(2 * ((first + run * p.len) / p.len) + (run == runs - 1 ? 1 : 0)); };
+  const bool few = p.few != 0;
+  if (few || runs > 1) {
+    const size_t at = few ? blockIdx.x : row(c);
+    if (tid < E) p.part[at * E + tid] = make_uint2(__float_as_uint(H), static_cast<uint32_t>(C));
+    if (tid == 0) p.part_n[at] = N;
     __syncthreads();
-    if (tid == 0) last = atomicAdd(p.ticket + s, 1u) == static_cast<uint32_t>(runs - 1);
+    if (tid == 0) last = few ? arrive(p.loss_ticket) == gridDim.x - 1 : arrive(p.ticket + s) == static_cast<uint32_t>(runs - 1);
     __syncthreads();
     if (!last) return;
-    __threadfence();
+  }
+  if (few) {
+    // every sample: columns of its runs added by kCols threads, then a warp a sample
+    constexpr int kCol = PL * 32, kSl = kThreads / kCol;
+    const int e = tid % kCol, sl = tid / kCol;
+    const int per = p.B < kSl ? kSl / p.B : 1;   // slices a sample (then B * per <= kSl <= kFewSamples: a place for each)
+    for (int q = sl; q < p.B * per; q += kSl) {
+      const int smp = q / per, part = q - smp * per;
+      int from = 0, of = gridDim.x;
+      if (p.per_sample) {
+        from = __ldg(p.base + smp);
+        of = __ldg(p.base + smp + 1) - from;
+      }
+      const int a = from + static_cast<int>(static_cast<long long>(part) * of / per);
+      const int b = from + static_cast<int>(static_cast<long long>(part + 1) * of / per);
+      float hh = 0.f;
+      int cc = 0, nn = 0;
+      constexpr int kU = 10;
+      for (int u0 = a; u0 < b; u0 += kU) {
+        uint2 v[kU];
+        int nv[kU];
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+          const bool in = u0 + u < b;
+          v[u] = in && e < E ? __ldcg(p.part + static_cast<size_t>(u0 + u) * E + e) : make_uint2(0u, 0u);
+          nv[u] = in && e == 0 ? __ldcg(p.part_n + u0 + u) : 0;
+        }
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+          hh += __uint_as_float(v[u].x);
+          cc += static_cast<int>(v[u].y);
+          nn += nv[u];
+        }
+      }
+      sums.few.h[q][e] = hh;
+      sums.few.c[q][e] = cc;
+      if (e == 0) N_s[q] = nn;
+    }
+    __syncthreads();
+    for (int smp = warp; smp < p.B; smp += kWarps) {
+      float hh[PL];
+      int cc[PL], nn = 0, total = 0;
+#pragma unroll
+      for (int i = 0; i < PL; ++i) {
+        hh[i] = 0.f;
+        cc[i] = 0;
+      }
+      for (int q = smp * per; q < (smp + 1) * per; ++q) {
+        nn += N_s[q];
+#pragma unroll
+        for (int i = 0; i < PL; ++i) {
+          hh[i] += sums.few.h[q][lane + 32 * i];
+          cc[i] += sums.few.c[q][lane + 32 * i];
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < PL; ++i) total += cc[i];
+      total = __reduce_add_sync(0xffffffffu, total);
+      const float inv_total = total > 0 ? static_cast<float>(E) / static_cast<float>(total) : 0.f;
+      const float inv_n = nn > 0 ? 1.f / static_cast<float>(nn) : 0.f;
+      float loss = 0.f;
+#pragma unroll
+      for (int i = 0; i < PL; ++i) {
+        const int x = lane + 32 * i;
+        const float f = static_cast<float>(cc[i]) * inv_total;
+        loss = fmaf(f, hh[i] * inv_n, loss);
+        if (x < E) {
+          const size_t at = static_cast<size_t>(smp) * E + x;
+          if (p.counts) p.counts[at] = cc[i];
+          if (p.d_gate) p.d_gate[at] = p.scale * f * inv_n / static_cast<float>(p.B);
+        }
+      }
+      loss = warp_sum(loss);
+      if (lane == 0) scratch[smp] = loss;
+    }
+    __syncthreads();
+    if (warp == 0) {
+      const float sum = warp_sum(lane < p.B ? scratch[lane] : 0.f);
+      if (lane == 0) {
+        *p.loss = sum / static_cast<float>(p.B);
+        *p.loss_ticket = 0u;
+      }
+    }
+    return;
+  }
+  if (runs > 1) {
     const int e = tid % kCols, sl = tid / kCols;
     const int a = static_cast<int>(static_cast<long long>(sl) * runs / kSlices);
     const int b = static_cast<int>(static_cast<long long>(sl + 1) * runs / kSlices);
@@ -127,26 +239,25 @@ __global__ void __launch_bounds__(kThreads) k_expert_balance(const ExpertBalance
     C = N = 0;
     constexpr int kU = 8;
     for (int q = a; q < b; q += kU) {
-      float hv[kU];
-      int cv[kU], nv[kU];
+      uint2 v[kU];
+      int nv[kU];
 #pragma unroll
       for (int u = 0; u < kU; ++u) {
         const bool in = q + u < b;
         const size_t at = in ? row(q + u) : 0;
-        hv[u] = in && e < E ? __ldcg(p.part_h + at * E + e) : 0.f;
-        cv[u] = in && e < E ? __ldcg(p.part_c + at * E + e) : 0;
-        nv[u] = in ? __ldcg(p.part_n + at) : 0;
+        v[u] = in && e < E ? __ldcg(p.part + at * E + e) : make_uint2(0u, 0u);
+        nv[u] = in && e == 0 ? __ldcg(p.part_n + at) : 0;
       }
 #pragma unroll
       for (int u = 0; u < kU; ++u) {
-        H += hv[u];
-        C += cv[u];
+        H += __uint_as_float(v[u].x);
+        C += static_cast<int>(v[u].y);
         N += nv[u];
       }
     }
-    h_sl[sl][e] = H;
-    c_sl[sl][e] = C;
-    if (e == 0) n_sl[sl] = N;
+    sums.slices.h[sl][e] = H;
+    sums.slices.c[sl][e] = C;
+    if (e == 0) N_s[sl] = N;
     if (tid == 0) p.ticket[s] = 0u;
     __syncthreads();
     H = 0.f;
@@ -154,10 +265,10 @@ __global__ void __launch_bounds__(kThreads) k_expert_balance(const ExpertBalance
 #pragma unroll
     for (int q = 0; q < kSlices; ++q) {
       if (tid < E) {
-        H += h_sl[q][tid];
-        C += c_sl[q][tid];
+        H += sums.slices.h[q][tid];
+        C += sums.slices.c[q][tid];
       }
-      N += n_sl[q];
+      N += N_s[q];
     }
   }
   // the sample's loss and gradient (counts stay below 2^24: exact in fp32)
@@ -170,18 +281,12 @@ __global__ void __launch_bounds__(kThreads) k_expert_balance(const ExpertBalance
     if (p.d_gate) p.d_gate[at] = p.scale * f * inv_n / static_cast<float>(p.B);
   }
   const float loss = block_sum(f * (H * inv_n), scratch);
-  if (p.B == 1) {
-    if (tid == 0) *p.loss = loss;
-    return;
-  }
   if (tid == 0) {
     p.sample_loss[s] = loss;
-    __threadfence();
-    last = atomicAdd(p.loss_ticket, 1u) == static_cast<uint32_t>(p.B - 1);
+    last = arrive(p.loss_ticket) == static_cast<uint32_t>(p.B - 1);
   }
   __syncthreads();
   if (!last) return;
-  __threadfence();
   float sum = 0.f;
   for (int i = tid; i < p.B; i += kThreads) sum += __ldcg(p.sample_loss + i);
   sum = block_sum(sum, scratch);
@@ -193,7 +298,8 @@ __global__ void __launch_bounds__(kThreads) k_expert_balance(const ExpertBalance
 
 }  // namespace
 
-cudaError_t launch_expert_balance(const ExpertBalanceParams& p, int blocks, cudaStream_t s) {
+cudaError_t launch_expert_balance(ExpertBalanceParams p, int blocks, cudaStream_t s) {
+  p.few = p.B <= kFewSamples;
   if (p.E < 1 || p.E > kCols || blocks < 1) return cudaErrorInvalidValue;
   // short runs leave most warps of a large block without a token
   const bool wide = p.T / blocks >= 64;

@@ -243,14 +243,14 @@ struct BalParams {
 // runs of samples that have several, tickets (zero between calls), the samples' losses.
 struct ExpertBalanceParams {
   int T, E, k, B, len, per_sample;
+  int few;                   // so few samples that one block finishes them all
   const float* gsave;
   const float* ginv;
   const int32_t* topk_idx;
   const int32_t* offsets;    // [B+1] tokens of a sample
   const int32_t* base;       // [B+1] runs of the samples before
   float scale;
-  float* part_h;             // [2 (T / len + 1)][E]
-  int32_t* part_c;
+  uint2* part;               // [2 (T / len + 1) + 32][E]: sum of the gate values, selections
   int32_t* part_n;
   float* sample_loss;        // [B]
   uint32_t* ticket;          // [B]
@@ -347,7 +347,7 @@ cudaError_t launch_gauss_coef(const float* mu, const float* var, int d, int dcoe
 cudaError_t launch_stats_update(const StatsParams& p, bool bf16, cudaStream_t s);
 cudaError_t launch_adaptive_bins(const BinsParams& p, cudaStream_t s);
 cudaError_t launch_bin_balance(const BalParams& p, cudaStream_t s);
-cudaError_t launch_expert_balance(const ExpertBalanceParams& p, int blocks, cudaStream_t s);
+cudaError_t launch_expert_balance(ExpertBalanceParams p, int blocks, cudaStream_t s);   // fills few
 // Attention forward with the vision score as one more value column (eqs. 2-4), grouped-query
 // heads: K and V have Hkv heads, query head h reads key/value head h / (H / Hkv). O [B, H, S, hd]
 // bf16, M as for the mass-only kernel.
