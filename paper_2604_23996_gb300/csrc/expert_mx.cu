@@ -368,12 +368,16 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
       for (int k0 = 0; ok && k0 < blocks; k0 += kMxRound) {
         ok = warp_wait(&bars.slot_full[slot], lph, wc);
         const uint32_t from = slots + slot * kMxSlot;
-        for (int b = 0; ok && b < kMxRound && k0 + b < blocks; ++b) {
-          uint32_t v[kMxGroups][2];              // lane's row of each group, a block's words
+        const int n_blocks = min(kMxRound, blocks - k0);
+        uint32_t v[kMxGroups][2];                // lane's row of each group, a block's words
+        auto read = [&](int b) {
 #pragma unroll
           for (int g = 0; g < kMxGroups; ++g)
             asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v[g][0]), "=r"(v[g][1])
                          : "r"(scale_at(from, g * 32 + lane, b >> 1) + 8 * (b & 1)));
+        };
+        if (ok) read(0);
+        for (int b = 0; ok && b < n_blocks; ++b) {
           if (stored < kMxSets) {
             ++stored;
           } else {
@@ -386,6 +390,7 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
           tmem_st16(to, {v[0][0], v[1][0], v[2][0], v[3][0], v[4][0], v[5][0], v[6][0], v[7][0], v[8][0], v[9][0], v[10][0], 0u,
                          v[0][1], v[1][1], v[2][1], v[3][1]});
           tmem_st8(to + 16, v[4][1], v[5][1], v[6][1], v[7][1], v[8][1], v[9][1], v[10][1], 0u);
+          if (b + 1 < n_blocks) read(b + 1);     // (under the stores)
           tmem_st_wait();
           tc_fence_before();
           __syncwarp();
