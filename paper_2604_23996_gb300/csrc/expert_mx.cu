@@ -4,20 +4,35 @@
 // Both operands hold pairs of e2m1 codes along the depth and a power-of-two scale for every 32 of it; the tensor cores
 // multiply by both scales. A pair of CTAs forms a tile of 256 features (along M, 128 in each CTA) by up to kRowsMost rows (along
 // N), in blocks of 256 of the depth: 128 bytes a row, in the copy engine's swizzle, as for 64 bf16 values. Each CTA loads its half
-// of both operands; the first CTA issues the products of both. (One CTA a tile of 128 x 192 read every operand byte of the
+// of both operands; the first CTA issues the products of both. (One CTA a tile of 128 x 192 reads every operand byte of the
 // tile for itself: 98304 x 2048 x 2048 took 190 us without an epilogue, at 15.5 TB/s from L2.)
 //
 // Scales lie in memory as they are given, [rows][n_in / 32] bytes. The tensor cores want them in tensor memory: of a CTA's own
 // features, and of all of the tile's rows in both CTAs. The 32 bytes of four blocks of every row (a round) come to shared memory
 // by the copy engine, or where rows are not whole 16-byte words by two copying warps; four warps of each CTA, one for each
 // quarter of its tensor memory's lanes, read four rows 32 apart a lane and store a block's words to one of four sets of
-// columns, which the MMA issuer waits for and gives back. (Not kept, 98304 x 2048 x 2048 gated: words through shared memory
+// columns. A set is free once the block four before is done, and the stores arrive where the block's operands do, so the MMA
+// issuer waits for one barrier a block and commits to one. (Not kept, 98304 x 2048 x 2048 gated: words through shared memory
 // and the tensor cores' own copy, the second CTA's released at cluster scope, 1 us a block: 237 us; the storing warps copying
-// for themselves, 1000 clocks a round: 231 us.)
+// for themselves, 1000 clocks a round: 231 us; barriers and commits of the scales' own: 162 against 145.)
+//
+// What the second CTA's warps store to its tensor memory is complete when they arrive (tcgen05.wait::st, then the fence for a
+// thread's arrival), as the accumulators' loads are in the epilogue; the first CTA's products read no shared memory that threads
+// wrote. (Their arrivals released at cluster scope besides: 378 us instead of 144.)
 //
 // Ragged edges and gated layers are those of expert_gemm.cu: rows of the next expert inside a tile are other columns of
 // D and are not stored; features past the expert's weights and a depth that ends inside a block are zeros of the maps (their scales
 // are set to 2^-127, so no NaN scale meets a zero).
+//
+// Roles of a CTA's warps: 0 and 8 producers of the features and of the rows (one for both issued for 610 clocks a block, whose
+// products take 416), 1 MMA issuer (first CTA), 2-5 scales to tensor memory, 6-7 scales to shared memory, 9-24 epilogue in
+// four groups that take 32-row chunks in turn.
+//
+// Measured: 98304 x 2048 x 2048 of 64 experts gated with silu 142 us (5.8 PFLOP/s; the products alone, without waiting for
+// operands, 95 us), 98304 x 1024 x 2048 99 us (402 MB of output at 4 TB/s), 16384 x 4096 x 4096 84 us (6.5 PFLOP/s), 16
+// tokens of 6 of 64 experts, 2048 x 2048, 18 us (6.4 TB/s). Bound by the warps' turns: 47% of the issue slots are used, and each
+// of scales, math, matrix stores and copies taken out gains 3 to 14 us of 142; not by L2 (all tiles reading the same
+// operands: 142) nor by the ring (six stages: 147). Few rows are bound by the weights' bytes.
 #include <cmath>
 #include <type_traits>
 
@@ -232,7 +247,7 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
     t.rows = min(p.tile_rows, expert_row(off, t.e + 1, R) - t.row0);
   };
   auto search = [&](Tile& t) {
-    const RowTile row = find_row_tile(rt, off, l.E, R, rows_of, t.r);
+    const RowTile row = find_row_tile<true>(rt, off, l.E, R, rows_of, t.r);
     t.e = row.e;
     t.before = row.before;
     t.tiles = row.tiles;
@@ -335,7 +350,7 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
       tc_fence_after();
       const uint32_t d = tmem + acc * kRowsMost;
       for (int kb = 0; kb < blocks; ++kb) {
-        if (!warp_wait(&bars.full[st], ph, wc)) { ok = false; break; }
+        if (!warp_wait<true>(&bars.full[st], ph, wc)) { ok = false; break; }
         tc_fence_after();
         if (elect_one()) {
           const uint64_t at = (st * stage_bytes) >> 4, da = a0 + at, db = b0 + at;

@@ -139,7 +139,7 @@ __device__ __forceinline__ long long expert_begin(const int32_t* off, int e, lon
 struct RowTile {
   int e;
   int row0, row1;            // the tile's first row, the expert's end
-  int before, tiles;         // tiles of the experts before, and of this one
+  int before, tiles;         // (kCounts) tiles of the experts before, and of this one
 };
 struct RowTiles {
   int before;                // lane l: tiles of the experts before 8 l
@@ -166,7 +166,7 @@ __device__ inline void count_row_tiles(const int32_t* offsets, int E, int R, Row
   if (lane == 31) before[32] = run;
 }
 // Tile 0 <= tile < total, by a whole warp.
-template <class Rows>
+template <bool kCounts = false, class Rows>
 __device__ __forceinline__ RowTile find_row_tile(const RowTiles& t, const int32_t* off, int E, int R, Rows of, int tile) {
   const int lane = threadIdx.x & 31;
   const int q = 31 - __clz(__ballot_sync(0xffffffffu, t.before <= tile));   // the last group that starts at or before it
@@ -182,8 +182,10 @@ __device__ __forceinline__ RowTile find_row_tile(const RowTiles& t, const int32_
   const int src = __ffs(__ballot_sync(0xffffffffu, lane < 8 && in < run)) - 1;
   RowTile r;
   r.e = q * 8 + src;
-  r.before = __shfl_sync(0xffffffffu, t.before, q) + __shfl_sync(0xffffffffu, run - n, src);
-  r.tiles = __shfl_sync(0xffffffffu, n, src);
+  if constexpr (kCounts) {
+    r.before = __shfl_sync(0xffffffffu, t.before, q) + __shfl_sync(0xffffffffu, run - n, src);
+    r.tiles = __shfl_sync(0xffffffffu, n, src);
+  }
   r.row0 = expert_row(off, r.e, R) + of.first(in - __shfl_sync(0xffffffffu, run - n, src));
   r.row1 = expert_row(off, r.e + 1, R);
   return r;
