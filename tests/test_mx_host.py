@@ -83,3 +83,10 @@ def test_the_oracle_rounds_as_the_format_says():
     assert list(O.mx_values(q, s)[0, :12]) == [0, 1, 1, 2, 2, 4, 4, 6, 6, 0, -1, 0.5]
     q, s = O.mx_quantise(np.full((1, 32), 2.0 ** -149))
     assert s[0, 0] == 0 and not O.mx_values(q, s).any()
+
+
+@pytest.mark.parametrize("n", [32, 64, 96, 128, 160, 192, 208])
+def test_division_by_a_tiles_rows_is_exact(n):
+    """The product's tiles are counted with the upper half of a product by ceil(2^32 / n)."""
+    x = np.arange((1 << 24) + n, dtype=np.uint64)
+    assert (((x * np.uint64(-(-(1 << 32) // n))) >> np.uint64(32)) == x // np.uint64(n)).all()
