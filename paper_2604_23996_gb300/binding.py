@@ -6,7 +6,6 @@ module fails loudly when the library has not been built: there is no fallback pa
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
 import os
 from typing import NamedTuple, Optional
@@ -378,41 +377,53 @@ def _mx_checked(name, x, shape, index):
     return codes.data_ptr(), scales.data_ptr()
 
 
+def _empty(shape, dtype, device, stream):
+    """A new tensor from the memory of the stream that a call runs on."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+_MX_TYPES = {torch.bfloat16: SMOES_BF16, torch.float32: SMOES_F32}
+
+
 def mx_quantise(X, out=None, stream=None) -> Mx:
     """X [..., n] (bf16 or float32, contiguous, n a multiple of 32) in 4 bits."""
-    if X.dtype not in (torch.bfloat16, torch.float32) or X.dim() < 1 or X.shape[-1] % 32 or X.shape[-1] == 0 or not X.is_contiguous():
-        raise ValueError(f"X: a contiguous bf16 or float32 tensor with a last dimension of 32s is wanted, got {X.dtype} {tuple(X.shape)}")
-    raw, n, lead = _mx_stream(X, stream), X.shape[-1], X.shape[:-1]
+    shape, code = tuple(X.shape), _MX_TYPES.get(X.dtype)
+    n = shape[-1] if shape else 0
+    if code is None or n == 0 or n % 32 or not X.is_contiguous():
+        raise ValueError(f"X: a contiguous bf16 or float32 tensor with a last dimension of 32s is wanted, got {X.dtype} {shape}")
+    raw = _mx_stream(X, stream)
     if out is None:
-        with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
-            out = Mx(X.new_empty(lead + (n // 2,), dtype=torch.uint8), X.new_empty(lead + (n // 32,), dtype=torch.uint8))
+        lead, device = shape[:-1], X.device
+        out = Mx(_empty(lead + (n // 2,), torch.uint8, device, stream), _empty(lead + (n // 32,), torch.uint8, device, stream))
         q, s = out.codes.data_ptr(), out.scales.data_ptr()
     else:
-        q, s = _mx_checked("out", out, X.shape, X.get_device())
-    _check(_lib.smoes_mx_quantise(X.data_ptr(), SMOES_BF16 if X.dtype is torch.bfloat16 else SMOES_F32, X.numel() // n, n, q, s, raw),
-           "smoes_mx_quantise")
+        q, s = _mx_checked("out", out, shape, X.get_device())
+    _check(_lib.smoes_mx_quantise(X.data_ptr(), code, X.numel() // n, n, q, s, raw), "smoes_mx_quantise")
     return out
 
 
 def mx_dequantise(x, dtype=torch.bfloat16, out=None, stream=None) -> torch.Tensor:
     """The values of an Mx, in bf16 or float32."""
     codes = x[0]
-    if codes.dim() < 1 or codes.shape[-1] % 16 or codes.shape[-1] == 0:
-        raise ValueError(f"codes: a last dimension of 16s is wanted, got {tuple(codes.shape)}")
-    raw, n = _mx_stream(codes, stream), 2 * codes.shape[-1]
-    shape = codes.shape[:-1] + (n,)
+    shape = tuple(codes.shape)
+    if not shape or shape[-1] == 0 or shape[-1] % 16:
+        raise ValueError(f"codes: a last dimension of 16s is wanted, got {shape}")
+    raw, n = _mx_stream(codes, stream), 2 * shape[-1]
+    shape = shape[:-1] + (n,)
     q, s = _mx_checked("x", x, shape, codes.get_device())
     if out is not None:
         dtype = out.dtype
         if out.shape != shape or not out.is_contiguous() or out.device != codes.device:
-            raise ValueError(f"out: a contiguous tensor of shape {tuple(shape)} on {codes.device} is wanted")
-    if dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError(f"out: a contiguous tensor of shape {shape} on {codes.device} is wanted")
+    code = _MX_TYPES.get(dtype)
+    if code is None:
         raise ValueError(f"dtype: bf16 or float32 is wanted, got {dtype}")
     if out is None:
-        with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
-            out = codes.new_empty(shape, dtype=dtype)
-    _check(_lib.smoes_mx_dequantise(q, s, codes.numel() * 2 // n, n, SMOES_BF16 if dtype is torch.bfloat16 else SMOES_F32,
-                                    out.data_ptr(), raw), "smoes_mx_dequantise")
+        out = _empty(shape, dtype, codes.device, stream)
+    _check(_lib.smoes_mx_dequantise(q, s, codes.numel() * 2 // n, n, code, out.data_ptr(), raw), "smoes_mx_dequantise")
     return out
 
 
@@ -509,10 +520,9 @@ class Router:
         index = ws.get_device()
         if index != torch._C._cuda_getDevice() or (stream is not None and stream.device_index != index):
             raise ValueError(f"device: the router is on cuda:{index}; the current device, and a stream given, have to be too")
-        with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
-            loss = torch.empty(1, dtype=f32, device=ws.device) if loss is None else loss
-            counts = torch.empty(shape, dtype=i32, device=ws.device) if counts is None else counts
-            d_gate = torch.empty(shape, dtype=f32, device=ws.device) if d_gate is None else d_gate
+        loss = _empty(1, f32, ws.device, stream) if loss is None else loss
+        counts = _empty(shape, i32, ws.device, stream) if counts is None else counts
+        d_gate = _empty(shape, f32, ws.device, stream) if d_gate is None else d_gate
         _check(_lib.smoes_expert_balance(
             self.plan, idx, per_sample, loss_scale, self._table("loss", loss, f32, (1,)), self._table("counts", counts, i32, shape),
             self._table("d_gate", d_gate, f32, shape), ws.data_ptr(), ws.numel(),
@@ -576,10 +586,7 @@ class _Calls:
     def _new(self, t, shape, dtype, stream):
         """The output given, checked, or a new one from the memory of the stream that the call runs on."""
         if t is None:
-            if stream is None:
-                return torch.empty(shape, dtype=dtype, device=self.device)
-            with torch.cuda.stream(stream):
-                return torch.empty(shape, dtype=dtype, device=self.device)
+            return _empty(shape, dtype, self.device, stream)
         self._in("output", t, shape, dtype)
         return t
 

@@ -285,3 +285,42 @@ def test_arguments_are_refused(bd):
     with pytest.raises(bd.SmoesError) as e:
         f32.linear_mx(X, W)
     assert e.value.code == -2
+
+
+def test_two_streams_at_once(bd):
+    """Two layers' products and quantisations on two streams, many at a time: each its own result."""
+    lays = [Layer(bd, 500, 8, 2, seed=s) for s in (1, 2)]
+    data = [(bd.mx_quantise(lay.normal(lay.ex.R, 512)), bd.mx_quantise(lay.normal(8, 256, 512)), lay.normal(500, 512)) for lay in lays]
+    want = [(lay.ex.linear_mx(x, w, act=1, gated=True), lay.ex.dispatch_mx(t)) for lay, (x, w, t) in zip(lays, data)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    got = [[], []]
+    for _ in range(25):
+        for i, (lay, (x, w, t)) in enumerate(zip(lays, data)):
+            got[i].append((lay.ex.linear_mx(x, w, act=1, gated=True, stream=streams[i]), lay.ex.dispatch_mx(t, stream=streams[i])))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert lays[i].ex.device_status() == bd.SMOES_OK
+        for out, q in got[i]:
+            assert torch.equal(out, want[i][0]) and torch.equal(q.codes, want[i][1].codes) and torch.equal(q.scales, want[i][1].scales)
+
+
+def test_graphs_that_share_a_workspace(bd):
+    """Two captured graphs of one layer, replayed in turn on one stream."""
+    lay = Layer(bd, 300, 8, 2, seed=4)
+    ex = lay.ex
+    X, Wa, Wb = lay.normal(300, 256), bd.mx_quantise(lay.normal(8, 128, 256)), bd.mx_quantise(lay.normal(8, 64, 256))
+    graphs, outs = [], []
+    for W in (Wa, Wb):
+        ex.linear_mx(ex.dispatch_mx(X), W)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(ex.linear_mx(ex.dispatch_mx(X), W))
+        graphs.append(g)
+    for seed in range(3):
+        X.copy_(lay.normal(300, 256))
+        for g in graphs:
+            g.replay()
+        for out, W in zip(outs, (Wa, Wb)):
+            assert torch.equal(out, ex.linear_mx(ex.dispatch_mx(X), W))
