@@ -266,7 +266,9 @@ bool encode_tiled(CUtensorMap* m, CUtensorMapDataType type, CUtensorMapSwizzle s
 
 bool smoes::encode_bf16(CUtensorMap* m, const void* ptr, int rank, const uint64_t* dims, const uint64_t* strides,
                         const uint32_t* box) {
-  return encode_tiled(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, CU_TENSOR_MAP_SWIZZLE_128B, ptr, rank, dims, strides, box);
+  const CUtensorMapSwizzle swizzle = box[0] == 16   ? CU_TENSOR_MAP_SWIZZLE_32B
+                                     : box[0] == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B;
+  return encode_tiled(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, swizzle, ptr, rank, dims, strides, box);
 }
 bool smoes::encode_f32(CUtensorMap* m, const void* ptr, int rank, const uint64_t* dims, const uint64_t* strides,
                        const uint32_t* box) {

@@ -29,7 +29,6 @@
 // (1.84 PFLOP/s), 520 dW (which writes 1.07 GB), 16384 x 8192 x 2048 282 us (1.95 PFLOP/s). A layer of this size runs
 // at the power limit: the same calls back to back take 10 to 15% longer. Otherwise bound by the products; small depths
 // (n_in below 500 or so) by the epilogue, few rows by the weights' bytes.
-#include "expert_epilogue.cuh"
 #include "expert_gemm.cuh"
 #include "experts.cuh"
 #include "ptx.cuh"
@@ -38,7 +37,8 @@ namespace smoes {
 namespace {
 
 constexpr int kGemmThreads = 640;
-constexpr int kGemmEpiWarps = 4 * kGemmGroups;
+constexpr int kGemmEpiWarps = 16;
+constexpr int kGemmGroups = 4;                   // of four epilogue warps
 constexpr int kChunkCols = 16;                   // columns of D that a group finishes at a time
 constexpr int kGemmStagesMost = 8;
 constexpr uint32_t kGemmRing = 5 * 32768;        // operand stages: five of 256 columns, eight of 64
@@ -63,6 +63,11 @@ struct GemmBars {
   int before[33];                                // row tiles (count_row_tiles)
 };
 static_assert(sizeof(GemmBars) <= kBarBytes, "barriers");
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
 
 // A chunk is 16 columns of D (a feature per lane, an output row per column) by a CTA's 128 features. It leaves
 // through shared memory as boxes of 64 features by 16 rows, 128 bytes a row in the copy engine's swizzle:
@@ -156,6 +161,37 @@ __device__ __forceinline__ void put_forward(uint8_t* boxes, int f, float (&v)[kC
   for (int i = 0; i < kChunkCols / 4; ++i) {
     const int a = (i >> 1) * 4 + (i & 1);
     put_pair(at, (i >> 1) * 8 + (i & 1), y[a], y[a + 2], pick);
+  }
+}
+
+// The group's staging between its four warps: they fill a chunk's half and arrive; warp 0 of the group waits for them and
+// hands the half to the copy engine. Before the next chunk but one goes into the same half, warp 0 has seen it read and
+// says so when it begins that chunk itself; so the others run up to a chunk ahead instead of meeting at every chunk.
+constexpr int kBarVote = 1, kBarFull = 1 + kGemmGroups, kBarFree = 1 + 2 * kGemmGroups;   // + group
+__device__ __forceinline__ void staging_acquire(int g, bool first_warp, bool issuer) {
+  if (first_warp) {
+    if (issuer) tma_store_wait_read<1>();        // all but the chunk before this one
+    __syncwarp();
+    named_bar_arrive(kBarFree + g, 128);
+  } else {
+    named_bar(kBarFree + g, 128);
+  }
+}
+// all: every warp waits (to copy the chunk itself), not just the first.
+__device__ __forceinline__ void staging_filled(int g, bool first_warp, bool all) {
+  if (first_warp || all)
+    named_bar(kBarFull + g, 128);
+  else
+    named_bar_arrive(kBarFull + g, 128);
+}
+
+// Rows [0, rows) of one box to memory, for a chunk that the copy engine would write past: its expert's rows end
+// inside, or g's features end inside the box and u's follow. by 128 threads, 16 bytes each. base: row 0, the
+// box's first feature; n: features that exist.
+__device__ __forceinline__ void copy_box(const uint8_t* box, __nv_bfloat16* base, long long stride, int rows, int n) {
+  for (int i = threadIdx.x & 127; i < rows * 8; i += 128) {
+    const int r = i >> 3, w = i & 7;
+    if (w * 8 < n) *reinterpret_cast<uint4*>(base + r * stride + w * 8) = *reinterpret_cast<const uint4*>(box + r * 128 + ((w ^ (r & 7)) << 4));
   }
 }
 
@@ -480,12 +516,12 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
           } else {
             for (int i = 0; i < n_out_boxes; ++i)
               copy_box(boxes + i * 2048, static_cast<__nv_bfloat16*>(l.out) + row * ld + f0 + 64 * i, ld, rows,
-                       p.n_feat - f0 - 64 * i, threadIdx.x & 127);
+                       p.n_feat - f0 - 64 * i);
             if (kMode == kGemmForward && l.pre)
               for (int i = 0; i < 2; ++i) {
                 const int f = gated ? f0 : f0 + 64 * i;
                 copy_box(boxes + 4096 + i * 2048, static_cast<__nv_bfloat16*>(l.pre) + row * l.n_z + f + (gated ? i * l.n_out : 0),
-                         l.n_z, rows, p.n_feat - f, threadIdx.x & 127);
+                         l.n_z, rows, p.n_feat - f);
               }
           }
           if (issuer) tma_store_commit();        // (every chunk is a group, an empty one too: staging_acquire counts them)

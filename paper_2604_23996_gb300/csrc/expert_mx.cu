@@ -25,10 +25,10 @@
 // are set to 2^-127, so no NaN scale meets a zero).
 //
 // Roles of a CTA's warps: 0 and 8 producers of the features and of the rows (one for both issued for 610 clocks a block, whose
-// products take 416), 1 MMA issuer (first CTA), 2-5 scales to tensor memory, 6-7 scales to shared memory, 9-24 epilogue in
-// four groups that take 32-row chunks in turn.
+// products take 416), 1 MMA issuer (first CTA), 2-5 scales to tensor memory, 6-7 scales to shared memory, 9-24 epilogue, four
+// for each quarter of the lanes that take 32-row chunks in turn.
 //
-// Measured: 98304 x 2048 x 2048 of 64 experts gated with silu 142 us (5.8 PFLOP/s; the products alone, without waiting for
+// Measured: 98304 x 2048 x 2048 of 64 experts gated with silu 142-145 us (5.8 PFLOP/s; the products alone, without waiting for
 // operands, 95 us), 98304 x 1024 x 2048 99 us (402 MB of output at 4 TB/s), 16384 x 4096 x 4096 84 us (6.5 PFLOP/s), 16
 // tokens of 6 of 64 experts, 2048 x 2048, 18 us (6.4 TB/s). Bound by the warps' turns: 47% of the issue slots are used, and each
 // of scales, math, matrix stores and copies taken out gains 3 to 14 us of 142; not by L2 (all tiles reading the same
@@ -36,7 +36,6 @@
 #include <cmath>
 #include <type_traits>
 
-#include "expert_epilogue.cuh"
 #include "expert_gemm.cuh"
 #include "experts.cuh"
 #include "ptx.cuh"
@@ -49,7 +48,8 @@ constexpr int kMxCopyWarps = 2;
 constexpr int kMxCopy = 2 + kMxScaleWarps;       // 0 producer of the features, 1 MMA issuer, then the scales' warps
 constexpr int kMxRows = kMxCopy + kMxCopyWarps;  // producer of the rows
 constexpr int kMxEpi = kMxRows + 1;              // first epilogue warp
-constexpr int kMxEpiWarps = 4 * kGemmGroups;
+constexpr int kMxTurns = 4;                      // epilogue warps of each quarter of the lanes, on chunks in turn
+constexpr int kMxEpiWarps = 4 * kMxTurns;
 constexpr int kMxGemmThreads = 32 * (kMxEpi + kMxEpiWarps);
 constexpr int kMxBlock = 256;                    // depth of a block: 128 bytes
 constexpr int kMxA = 128 * 128;                  // a block's bytes of the features
@@ -63,10 +63,10 @@ constexpr int kMxGroups = 4 + (kRowsMost + 31) / 32;     // of 32 features or ro
 constexpr int kMxRound = 4;                      // blocks whose scales are copied at a time: 32 bytes a row
 constexpr int kMxSlots = 3;
 constexpr uint32_t kMxSlot = kMxGroups * 32 * 32;
-constexpr int kMxChunk = 32;                     // rows that an epilogue group finishes at a time
-constexpr uint32_t kMxStaging = 8192;            // one group's output boxes of 64 features by 32 rows: two, gated two chunks of one
+constexpr int kMxChunk = 32;                     // rows that an epilogue warp finishes at a time
+constexpr uint32_t kMxStaging = 2048;            // its box of 32 features by 32 rows, or gated two of 16 features
 constexpr uint32_t kMxBarBytes = 1024;
-constexpr uint32_t kMxSmem = 1024 + kMxRing + kMxSlots * kMxSlot + kGemmGroups * kMxStaging + kMxBarBytes + 4 * (kExpertsMax + 1);
+constexpr uint32_t kMxSmem = 1024 + kMxRing + kMxSlots * kMxSlot + kMxEpiWarps * kMxStaging + kMxBarBytes + 4 * (kExpertsMax + 1);
 static_assert(kMxScaleCols + kMxSets * kMxSetCols <= 512, "tensor memory");
 static_assert(kMxSmem <= 227 * 1024, "shared memory of a CTA");
 // The pair's tiles for the epilogue, written by the rows' producer. It is at most the stages, two accumulators and the tile it
@@ -132,6 +132,10 @@ __device__ __forceinline__ uint32_t scale_at(uint32_t slot, int r, int h) {
   return slot + static_cast<uint32_t>(r) * 32u + static_cast<uint32_t>((h ^ (r >> 2)) & 1) * 16u;
 }
 
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
 // The epilogue's sums and products go two at a time (f32x2): of the instructions that an SM issues under dsmoe_vlm's gated layer
 // half were its epilogue's.
 __device__ __forceinline__ void add_bias(float (&v)[16], const float (&bias)[2]) {
@@ -183,8 +187,8 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   uint8_t* scale_ring = smem + kMxRing;
   uint8_t* staging = scale_ring + kMxSlots * kMxSlot;
-  MxBars& bars = *reinterpret_cast<MxBars*>(staging + kGemmGroups * kMxStaging);
-  int32_t* off = reinterpret_cast<int32_t*>(staging + kGemmGroups * kMxStaging + kMxBarBytes);   // [E + 1] offsets
+  MxBars& bars = *reinterpret_cast<MxBars*>(staging + kMxEpiWarps * kMxStaging);
+  int32_t* off = reinterpret_cast<int32_t*>(staging + kMxEpiWarps * kMxStaging + kMxBarBytes);   // [E + 1] offsets
   const ExpertLinearParams& l = p.l;
   const int warp = warp_index(), lane = threadIdx.x & 31;
   const int R = static_cast<int>(l.R);
@@ -483,9 +487,14 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
       }
   } else if (warp >= kMxEpi) {
     // ------------------------------------------------------------------------------- epilogue
+    // Warps work alone. A warp's features are two times 16 (gated: 16, as g and as u). A 16-lane load gives a thread two
+    // neighbouring rows of features lane / 4 and 8 further on; rounded and packed they are stored transposed, 8 features
+    // (16 bytes) of a row at a time, to the warp's box, which the copy engine takes to memory (boxes of 64 features by four warps,
+    // that met at two barriers a chunk: 6007 x 1024 -> 1416 17.5 us instead of 16.8.)
+    constexpr int kHalves = kGated ? 1 : 2;
+    constexpr uint32_t kRow = 32 * kHalves;      // bytes of a row of a box
     const int q = warp & 3, g = (warp - kMxEpi) >> 2;
     const uint32_t lanes = static_cast<uint32_t>(32 * q) << 16;
-    const bool lead = (warp - kMxEpi) % 4 == 0;  // the group's warp that waits and stores
     const int et = threadIdx.x - 32 * kMxEpi;
     const long long end = expert_begin(off, l.E, l.R);
     if (end < l.R) {                             // rows of no expert
@@ -495,41 +504,39 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
            i += static_cast<long long>(gridDim.x) * (32 * kMxEpiWarps))
         o[i] = make_uint4(0u, 0u, 0u, 0u);
     }
-    // A warp's features are two times 16 (gated: 16, as g and as u). A 16-lane load gives a thread two neighbouring rows of
-    // features lane / 4 and 8 further on; rounded and packed they are stored transposed, 8 features (16 bytes) of a row at a time.
-    constexpr int kHalves = kGated ? 1 : 2;
     const int width = kGated ? 64 : 128;
     const int fw = kGated ? 16 * q : 32 * q;     // the warp's first feature among the CTA's
-    const uint32_t st_row = static_cast<uint32_t>(lane & 7);
-    const uint32_t st_at = static_cast<uint32_t>(fw >> 6) * 4096u + (static_cast<uint32_t>(lane >> 4) * 8u + st_row) * 128u;
-    const uint32_t st_chunk = static_cast<uint32_t>((fw & 63) >> 3) + static_cast<uint32_t>((lane >> 3) & 1);
-    const bool issuer = lead && elect_one();
+    uint8_t* mine = staging + (warp - kMxEpi) * kMxStaging;
+    // byte of 16-byte word w of row r in a box, in the copy engine's swizzle
+    auto box_at = [](int r, int w) {
+      return static_cast<uint32_t>(r) * kRow + static_cast<uint32_t>((w ^ (kGated ? r >> 2 : r >> 1)) & (2 * kHalves - 1)) * 16u;
+    };
+    const int st_row = (lane >> 4) * 8 + (lane & 7), st_word = (lane >> 3) & 1;
+    const bool issuer = elect_one();
     int buf = 0, acc = 0;
     uint32_t aph = 0;
     for (int tile = pair, i = 0; tile < n_total; tile += n_pairs, ++i) {
-      const bool told = warp_wait(&bars.note_full[i % kMxNotes], (i / kMxNotes) & 1, wc);
-      const MxNote t = told ? bars.notes[i % kMxNotes] : MxNote{};
-      const int f0 = (t.m * 2 + static_cast<int>(rank)) * width;
-      const bool whole = f0 + width <= l.n_out;
+      if (!warp_wait(&bars.note_full[i % kMxNotes], (i / kMxNotes) & 1, wc)) break;
+      const MxNote t = bars.notes[i % kMxNotes];
+      const int f0 = (t.m * 2 + static_cast<int>(rank)) * width + fw;
       const long long ld = l.n_out;
       float bias[2][2] = {{0.f, 0.f}, {0.f, 0.f}};   // non-gated: of the halves; gated: of g and of u
       if (l.bias) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const int f = f0 + fw + (kGated ? 0 : 16 * h) + 8 * i + (lane >> 2);
-            if (f < l.n_out) bias[h][i] = __ldg(l.bias + static_cast<long long>(t.e) * l.n_z + f + (kGated ? h * l.n_out : 0));
+          for (int j = 0; j < 2; ++j) {
+            const int f = f0 + (kGated ? 0 : 16 * h) + 8 * j + (lane >> 2);
+            if (f < l.n_out) bias[h][j] = __ldg(l.bias + static_cast<long long>(t.e) * l.n_z + f + (kGated ? h * l.n_out : 0));
           }
       }
-      // one answer for the group: a warp whose wait ran out takes the others along
-      if (!named_bar_all(kBarVote + g, 128, told && (!lead || warp_wait(&bars.acc_full[acc], aph, wc)))) break;
+      if (!warp_wait(&bars.acc_full[acc], aph, wc)) break;
       tc_fence_after();
       const int chunks = (t.rows + kMxChunk - 1) / kMxChunk;
-      for (int c = g; c < chunks; c += kGemmGroups) {
+      for (int c = g; c < chunks; c += kMxTurns) {
         const long long row = t.row0 + c * kMxChunk;
         const int rows = min(kMxChunk, t.rows - c * kMxChunk);
-        uint8_t* boxes = staging + g * kMxStaging + (kGated ? buf * 4096 : 0);
+        uint8_t* box = mine + (kGated ? buf * 1024 : 0);
         const uint32_t from = tmem + acc * kRowsMost + c * kMxChunk + lanes;
 #pragma unroll
         for (int h = 0; h < kHalves; ++h) {
@@ -539,18 +546,18 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
           // the residual's words, transposed as the accumulators are: [rows 8 n][features 8 i]
           uint32_t rv[4][2];
           if (l.residual) {
-            const int f = f0 + fw + 16 * h + 2 * (lane & 3);
+            const int f = f0 + 16 * h + 2 * (lane & 3);
             const __nv_bfloat16* res = static_cast<const __nv_bfloat16*>(l.residual) + (row + (lane >> 2)) * ld + f;
 #pragma unroll
             for (int n = 0; n < 4; ++n)
 #pragma unroll
-              for (int i = 0; i < 2; ++i)
-                rv[n][i] = 8 * n + (lane >> 2) < rows && f + 8 * i < l.n_out
-                               ? __ldg(reinterpret_cast<const uint32_t*>(res + 8 * n * ld + 8 * i)) : 0u;
+              for (int j = 0; j < 2; ++j)
+                rv[n][j] = 8 * n + (lane >> 2) < rows && f + 8 * j < l.n_out
+                               ? __ldg(reinterpret_cast<const uint32_t*>(res + 8 * n * ld + 8 * j)) : 0u;
           }
           tmem_ld_ready(raw[0]);
           if constexpr (kGated) tmem_ld_ready(raw[1]);
-          if (h == kHalves - 1 && c + kGemmGroups >= chunks) {   // the accumulator's last use
+          if (h == kHalves - 1 && c + kMxTurns >= chunks) {   // the accumulator's last use
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_peer(peer_smem(&bars.acc_empty[acc], 0));
@@ -568,39 +575,41 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
           } else if (kAct != SMOES_ACT_NONE) {
             activate<kAct>(v);
           }
+          if (h == 0 && issuer) tma_store_wait_read<kGated ? 1 : 0>();   // the box is free again
           __syncwarp();
           if (l.residual) {
 #pragma unroll
             for (int n = 0; n < 4; ++n)
 #pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                const uint32_t w = transpose_8x8(rv[n][i]);
-                v[4 * n + 2 * i] += __uint_as_float(w << 16);
-                v[4 * n + 2 * i + 1] += __uint_as_float(w & 0xffff0000u);
+              for (int j = 0; j < 2; ++j) {
+                const uint32_t w = transpose_8x8(rv[n][j]);
+                v[4 * n + 2 * j] += __uint_as_float(w << 16);
+                v[4 * n + 2 * j + 1] += __uint_as_float(w & 0xffff0000u);
               }
           }
-          if (h == 0) staging_acquire<kGated ? 2 : 1>(g, lead, issuer);
-          __syncwarp();
-          const uint32_t at = smem_u32(boxes) + st_at + (((st_chunk + 2u * h) ^ st_row) << 4);
+          const uint32_t at = smem_u32(box);
 #pragma unroll
           for (int n = 0; n < 2; ++n)            // 16 rows
-            stmatrix_x4_trans(at + 2048u * n, pack_bf16(v[8 * n], v[8 * n + 1]), pack_bf16(v[8 * n + 2], v[8 * n + 3]),
-                              pack_bf16(v[8 * n + 4], v[8 * n + 5]), pack_bf16(v[8 * n + 6], v[8 * n + 7]));
+            stmatrix_x4_trans(at + box_at(16 * n + st_row, 2 * h + st_word), pack_bf16(v[8 * n], v[8 * n + 1]),
+                              pack_bf16(v[8 * n + 2], v[8 * n + 3]), pack_bf16(v[8 * n + 4], v[8 * n + 5]),
+                              pack_bf16(v[8 * n + 6], v[8 * n + 7]));
         }
-        fence_proxy_async_smem();
-        const bool engine = (rows == kMxChunk || rows == 16) && (whole || !kGated);
-        staging_filled(g, lead, !engine);
-        if (engine) {
-          if (issuer)
-            for (int i = 0; i < width / 64; ++i)
-              if (f0 + 64 * i < l.n_out)
-                tma_store_2d(rows == 16 ? &tmOut16 : &tmOut, boxes + i * 4096, f0 + 64 * i, static_cast<int>(row));
-        } else {
-          for (int i = 0; i < width / 64; ++i)
-            copy_box(boxes + i * 4096, static_cast<__nv_bfloat16*>(l.out) + row * ld + f0 + 64 * i, ld, rows, l.n_out - f0 - 64 * i,
-                     et & 127);
+        if (rows == kMxChunk || rows == 16) {      // the engine leaves out what lies past n_out
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (issuer && f0 < l.n_out) tma_store_2d(rows == 16 ? &tmOut16 : &tmOut, box, f0, static_cast<int>(row));
+        } else {                                   // its expert's rows end inside: 16 bytes a lane
+          __syncwarp();
+          constexpr int kWords = 2 * kHalves;
+          for (int j = lane; j < rows * kWords; j += 32) {
+            const int r = j / kWords, w = j % kWords;
+            if (f0 + 8 * w < l.n_out)
+              *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(l.out) + (row + r) * ld + f0 + 8 * w) =
+                  *reinterpret_cast<const uint4*>(box + box_at(r, w));
+          }
+          __syncwarp();
         }
-        if (issuer) tma_store_commit();            // (every chunk is a group, an empty one too: staging_acquire counts them)
+        if (issuer) tma_store_commit();            // (every chunk is a group, an empty one too)
         if (kGated) buf ^= 1;
       }
       if (chunks <= g && lane == 0) mbar_arrive_peer(peer_smem(&bars.acc_empty[acc], 0));
@@ -675,7 +684,8 @@ cudaError_t launch_expert_mx(ExpertMxParams p, int n_sms, cudaStream_t s) {
   const uint64_t R = static_cast<uint64_t>(l.R), bytes = l.n_in / 2, nz = l.n_z, E = l.E, no = l.n_out;
   // the weights as [E][g, u][n_out] (one of the two where there is no gate)
   const uint64_t parts = l.gated ? 2 : 1, da[4] = {bytes, no, parts, E}, sta[3] = {bytes, bytes * no, bytes * nz}, db[2] = {bytes, R}, stb[1] = {bytes};
-  const uint32_t rows_a = l.gated ? 16 : 128, boxa[4] = {128, rows_a, static_cast<uint32_t>(parts), 1}, box16[2] = {128, 16}, box_out[2] = {64, kMxChunk}, box_out16[2] = {64, 16};
+  const uint32_t rows_a = l.gated ? 16 : 128, boxa[4] = {128, rows_a, static_cast<uint32_t>(parts), 1}, box16[2] = {128, 16}, width = l.gated ? 16u : 32u, box_out[2] = {width, kMxChunk},
+                 box_out16[2] = {width, 16};
   const uint64_t dout[2] = {no, R}, stout[1] = {no * 2};
   CUtensorMap a, b16, out, out16;
   if (!encode_u8(&a, l.W, 4, da, sta, boxa) || !encode_u8(&b16, l.X, 2, db, stb, box16) ||

@@ -289,8 +289,8 @@ cudaError_t launch_static_perm_prep(StaticPermScratch* sp, const int32_t* expert
                                     const int32_t* expert_slot, int E, cudaStream_t s);
 
 // Tiled TMA maps of a row-major tensor of `rank` dimensions, innermost first (api.cu); strides in bytes of
-// dimensions 1 and up. Reads outside give zeros. bf16 and byte boxes have the 128-byte swizzle (byte boxes of
-// 32 a row the 32-byte one), fp32 boxes none.
+// dimensions 1 and up. Reads outside give zeros. bf16 and byte boxes have the 128-byte swizzle (those of 64 or 32
+// bytes a row that of their width), fp32 boxes none.
 bool encode_f32(CUtensorMap* m, const void* ptr, int rank, const uint64_t* dims, const uint64_t* strides,
                 const uint32_t* box);
 bool encode_bf16(CUtensorMap* m, const void* ptr, int rank, const uint64_t* dims, const uint64_t* strides,
