@@ -10,8 +10,9 @@
 // ...), kR tokens at work and kR on their way. Runs of a sample that has several leave partials. Up to kFewSamples samples are
 // finished by the block that arrives last of all, a warp a sample; with more of them each by the last of its own blocks, and
 // the losses are added by the one that finishes the last sample. The sums are fp32 in a fixed order, whichever block makes
-// them. Bound by the gate values' bytes (131072 x 128: 20.5 us, of which the tokens take 13 and the hand-over and the last block's sums 6; 10.6 us of HBM); small batches by the latency of a launch, two
-// reads and one hand-over between the blocks (16384 x 64: 10.8 us).
+// them. Bound by the gate values' bytes (131072 x 128: 20.5 us, of which the tokens take 13 and the hand-over and the last
+// block's sums 6; 10.6 us of HBM); small batches by the latency of a launch, two reads and one hand-over between the blocks
+// (16384 x 64: 10.8 us).
 #include "device_common.cuh"
 #include "ptx.cuh"
 #include "smoes_internal.cuh"
@@ -21,7 +22,7 @@ namespace {
 
 constexpr int kR = 4;
 constexpr int kCols = 128;                          // experts at most
-constexpr int kFewSamples = 32;                   // (the workspace has a row for each beside those of whole runs)
+constexpr int kFewSamples = 32;                     // (the workspace has a row for each beside those of whole runs)
 
 // An arrival that hands over what the block wrote, and takes what the blocks before it handed over (thread 0, between two
 // block barriers).
