@@ -335,7 +335,7 @@ k_expert_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
       const uint32_t idesc = idesc_bf16(256, gemm_n<kMode>(t.cols), kMajorA, kMajorB);
       const int chunk = kMode == kGemmGradW ? kGemmChunk : t.blocks;
       for (int k0 = 0; ok && k0 < t.blocks; k0 += chunk) {
-        if (!warp_wait(&bars.acc_empty[acc], aph ^ 1, wc)) { ok = false; break; }
+        if (!warp_wait<true>(&bars.acc_empty[acc], aph ^ 1, wc)) { ok = false; break; }
         tc_fence_after();
         const uint32_t d = tmem + acc * 256;
         const int k1 = min(k0 + chunk, t.blocks);

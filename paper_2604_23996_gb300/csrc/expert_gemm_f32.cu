@@ -259,7 +259,7 @@ k_expert_gemm_f32(const __grid_constant__ CUtensorMap tmA, const __grid_constant
       if (t.blocks == 0) next = tile_at(tile + n_pairs);
       const uint32_t idesc = idesc_bf16(256, gemm_n<kMode>(t.cols), kAcrossA, kAcrossB);
       for (int k0 = 0; ok && k0 < t.blocks; k0 += kF32Chunk) {
-        if (!warp_wait(&bars.acc_empty[acc], aph ^ 1, wc)) { ok = false; break; }
+        if (!warp_wait<true>(&bars.acc_empty[acc], aph ^ 1, wc)) { ok = false; break; }
         tc_fence_after();
         const uint32_t d = tmem + acc * 256;
         const int k1 = min(k0 + kF32Chunk, t.blocks);

@@ -17,8 +17,9 @@
 // for themselves, 1000 clocks a round: 231 us; barriers and commits of the scales' own: 162 against 145.)
 //
 // What the second CTA's warps store to its tensor memory is complete when they arrive (tcgen05.wait::st, then the fence for a
-// thread's arrival), as the accumulators' loads are in the epilogue; the first CTA's products read no shared memory that threads
-// wrote. (Their arrivals released at cluster scope besides: 378 us instead of 144.)
+// thread's arrival), as the accumulators' loads are in the epilogue; the arrivals and the waits for them have cluster scope. The
+// first CTA's products read no shared memory that threads wrote, so the arrivals need not release it. (If they do: 378 us instead
+// of 144.)
 //
 // Ragged edges and gated layers are those of expert_gemm.cu: rows of the next expert inside a tile are other columns of
 // D and are not stored; features past the expert's weights and a depth that ends inside a block are zeros of the maps (their scales
@@ -350,7 +351,7 @@ k_expert_mx(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
       const Tile t = next;
       const int n = min((t.rows + 31) & ~31, p.tile_rows);
       const uint32_t id0 = idesc_mx4(256, n, 0), id1 = idesc_mx4(256, n, 1);
-      if (!warp_wait(&bars.acc_empty[acc], aph ^ 1, wc)) break;
+      if (!warp_wait<true>(&bars.acc_empty[acc], aph ^ 1, wc)) break;
       tc_fence_after();
       const uint32_t d = tmem + acc * kRowsMost;
       for (int kb = 0; kb < blocks; ++kb) {

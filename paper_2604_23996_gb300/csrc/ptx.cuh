@@ -90,7 +90,8 @@ __device__ __forceinline__ void raise_abort(const WaitCtx& w, uint32_t bit) {
   atomicOr(w.status, bit);
 }
 
-// mbar_try_wait at cluster scope: what threads of the other CTA wrote before mbar_arrive_peer_release is visible behind it.
+// mbar_try_wait at cluster scope: the wait for arrivals from the other CTA. What threads wrote before mbar_arrive_peer_release
+// is visible behind it.
 __device__ __forceinline__ bool mbar_try_wait_cluster(uint64_t* bar, uint32_t parity) {
   uint32_t ok;
   asm volatile(
@@ -276,12 +277,13 @@ __device__ __forceinline__ uint32_t peer_smem(const void* p, uint32_t rank) {
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
   return a;
 }
-// Arrivals on a barrier of either CTA (a cluster address). They order this CTA's own accesses only, for what the copy
-// engine and the tensor cores wrote or read: their completion is counted on the barriers, or fenced before the arrival
-// (tc_fence_before). With cluster scope every block of a product waited for a fence in its producer and ran at 1200
-// clocks instead of 520.
+// Arrivals on a barrier of either CTA (a cluster address), to be waited for with warp_wait<true>. They are for what the copy engine
+// and the tensor cores wrote or read, whose completion the barriers count, and for a warp's own loads and stores of tensor memory:
+// complete (tcgen05.wait), then tc_fence_before, this arrival, the wait, tc_fence_after, the pattern that PTX gives for tensor
+// memory between threads. A relaxed arrival at cluster scope orders nothing else. (Released at cluster scope every block of a
+// product waited for a fence in its producer and ran at 1200 clocks instead of 520.)
 __device__ __forceinline__ void mbar_arrive_peer(uint32_t bar) {
-  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 // The arrival for what threads wrote to shared memory themselves (and fenced for the tensor cores, fence_proxy_async_smem):
 // release at cluster scope, to be waited for with warp_wait<true>.
