@@ -747,7 +747,8 @@ class Experts(_Calls):
         return dX, dW
 
     def dispatch_mx(self, X, out=None, stream=None):
-        """Tokens [T, d] into expert order, quantised to 4 bits: an Mx of [R, d]."""
+        """Tokens [T, d] into expert order, quantised to 4 bits: an Mx of [R, d], for ``linear_mx`` of a bf16 layer (the tokens
+        may be a float32 layer's)."""
         d = X.shape[-1]
         if d % 32:
             raise ValueError(f"X: a width of 32s is wanted, got {d}")

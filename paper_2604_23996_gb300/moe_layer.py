@@ -63,6 +63,8 @@ class MoELayer:
         mx = isinstance(W_up, bd.Mx)
         if mx != isinstance(W_down, bd.Mx) or (mx and training):
             raise ValueError("W_up, W_down: both in 4 bits, and not in training")
+        if mx and ex.dtype is not torch.bfloat16:
+            raise ValueError("W_up, W_down: 4 bits are for layers in bf16")
         if (norm is None) != (self.norm is None):
             raise ValueError("norm: a weight and a bias are wanted where the layer was made with norm_eps, and nowhere else")
         if training:
