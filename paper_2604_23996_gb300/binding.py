@@ -492,13 +492,14 @@ class Router:
                  accumulate=False, stream=None, d_gate=None, topk_idx=None):
         """d_gate: what ``expert_balance`` returned, [B, E] or [1, E]; topk_idx: the forward's with dropped selections."""
         idx = self.topk_idx if topk_idx is None else topk_idx
+        if topk_idx is not None:
+            self._table("topk_idx", idx, torch.int32, (self.T, self.k))
         if d_gate is None:
             code = smoes_router_bwd(self.plan, X, W, M, idx, d_topk_w, loss_scale, dW,
                                     accumulate, dX, dlogits, self.ws, stream)
             _check(code, "smoes_router_bwd")
             return
         self._table("d_gate", d_gate, torch.float32, (1, self.E), (self.B, self.E))
-        self._table("topk_idx", idx, torch.int32, (self.T, self.k))
         code = smoes_router_bwd_gates(self.plan, X, W, M, idx, d_topk_w, d_gate, self.B != 1 and len(d_gate) == self.B,
                                       loss_scale, dW, accumulate, dX, dlogits, self.ws, stream)
         _check(code, "smoes_router_bwd_gates")
