@@ -189,8 +189,10 @@ __device__ __noinline__ void sample_reduce(const FwdParams& p, int s, float* red
   const bool has_v = Av > 1e-12f, has_t = At > 1e-12f;   // absent modality: Sbar row = 0
   const float yv = 2.f * Dv / n, yt = 2.f * Dt / n;
   float ev = 0.f, et = 0.f;
-  if (act && has_v) ev = cv ? (2.f * Rv / Q - yv) / (1.f + yv) : Nv * n / (Q * Av) - 1.f;
-  if (act && has_t) et = ct ? (2.f * Rt / Q - yt) / (1.f + yt) : Nt * n / (Q * At) - 1.f;
+  // (a bin that no token of the sample chose, where the gate is masked, has Q = 0; one that a modality's did not, eps = -1)
+  const bool some = act && Q > 0.f;
+  if (some && has_v) ev = cv ? (2.f * Rv / Q - yv) / (1.f + yv) : Nv * n / (Q * Av) - 1.f;
+  if (some && has_t) et = ct ? (2.f * Rt / Q - yt) / (1.f + yt) : Nt * n / (Q * At) - 1.f;
   const float sv = warp_sum(q * ev), st = warp_sum(q * et);
   const float NB = static_cast<float>(dm.N_B);
   float Pv = 0.f, Pt = 0.f, a = 0.f, b = 0.f, h = 0.f, I = 0.f;
@@ -202,13 +204,14 @@ __device__ __noinline__ void sample_reduce(const FwdParams& p, int s, float* red
     Pv = q * (1.f + ev) / nbz;                                     // eq. (13)
     Pt = q * (1.f + et) / nbz;
     const float lk = log1pf(0.5f * (ev + et)), lz = log1pf(0.5f * (sv + st));
-    const float Lv = act ? log1pf(ev) - lk + lz - log1pf(sv) : 0.f;
-    const float Lt = act ? log1pf(et) - lk + lz - log1pf(st) : 0.f;
+    const bool on_v = some && ev > -1.f, on_t = some && et > -1.f;   // elsewhere P = 0: no term, and no logarithm
+    const float Lv = on_v ? log1pf(ev) - lk + lz - log1pf(sv) : 0.f;
+    const float Lt = on_t ? log1pf(et) - lk + lz - log1pf(st) : 0.f;
     I = warp_sum(Pv * Lv + Pt * Lt);                               // eq. (14)
     const float Z = nbz / NB;
     a = act ? (Lv - I) / (Z * NB * Av) : 0.f;
     b = act ? (Lt - I) / (Z * NB * At) : 0.f;
-    if (cv && ct && act) {
+    if (cv && ct && on_v && on_t) {
       // h = (a + b) / 2 is second order (a ~ -b): form L_v + L_t and 1/A_v - 1/A_t directly,
       //   L_v + L_t = log1p(-(d/(1+m))^2) - log1p(-(d_s/(1+m_s))^2),
       // with m, d the half-sum and half-difference of (eps_v, eps_t) and m_s, d_s those of (s_v, s_t).
