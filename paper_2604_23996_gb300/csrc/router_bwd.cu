@@ -19,7 +19,7 @@
 // tile rate with the lo half in dX as well: its 64-token MMAs read 6 KB of operands for 128 x 64 x
 // 16 products. With a gradient of the gate values dX takes the lo half all the same (W^T . lo^T after
 // each hi): where experts' weights have a part in common the sum over them cancels, and eight bits of
-// dz left dX 2.6e-3 off (32768 x 1280, E = 64, with the balance loss: 59.7 -> 62.2 us, dX 1e-4 from a
+// dz left dX 2.6e-3 off (32768 x 1280, E = 64, with the balance loss: 59.7 -> 61.6 us, dX 1e-4 from a
 // plain fp32 form's, which is a tie of the last rounding here and there).
 // X tiles arrive by TMA; the W slice stays resident in shared memory; dX leaves by TMA store.
 // The per-group dW^T slice is written once at the end and summed over groups in fixed order.
@@ -437,7 +437,9 @@ __host__ __device__ inline BwdLayout bwd_layout(int E_pad, int slice_width, int 
 // the other buffers. An X stage is released as soon as the d-block's dW^T MMAs complete (the dX^T
 // MMAs read W and dz only). After the last tile every CTA writes its dW^T partial (both groups,
 // alternate d-blocks); k_dw_reduce sums them.
-template <int E_pad>
+// kDxLo: dX from both halves of dz. (Asked for at run time inside the issue loop it took 22 us of large_fine's 229 where the
+// answer is no.)
+template <int E_pad, bool kDxLo>
 __global__ void __launch_bounds__(kBwdThreads, 1)
 k_router_bwd_tc(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW,
                 const __grid_constant__ CUtensorMap tmDX, const BwdParams p, const int n_xst) {
@@ -470,7 +472,6 @@ k_router_bwd_tc(const __grid_constant__ CUtensorMap tmX, const __grid_constant__
   const int d0 = sl * p.slice_width;
   const int nb = min(p.slice_width, round_up(dm.d - d0, kBwdBD)) / kBwdBD;   // d-blocks here
   const bool want_dx = p.dX != nullptr;
-  const bool dx_lo = p.d_gate != nullptr;      // dX from both halves of dz
   constexpr uint32_t dz_half = static_cast<uint32_t>(E_pad) * 128u;         // one of hi / lo
   constexpr uint32_t dz_buf_bytes = 2u * dz_half;                           // hi + lo
   constexpr int kAccs = bwd_accs(E_pad);
@@ -608,7 +609,7 @@ k_router_bwd_tc(const __grid_constant__ CUtensorMap tmX, const __grid_constant__
               const uint32_t boff = (ke >> 2) * 8192 + (ke & 3) * 32;
               const uint64_t dh = sdesc_sw128(hi + boff, 16, 1024);
               umma_bf16(dxc, da, dh, id_dx, ke > 0 ? 1u : 0u);
-              if (dx_lo) umma_bf16(dxc, da, sdesc_sw128(lo + boff, 16, 1024), id_dx, 1u);
+              if (kDxLo) umma_bf16(dxc, da, sdesc_sw128(lo + boff, 16, 1024), id_dx, 1u);
             }
             umma_commit(dx_full + xb);
           }
@@ -954,7 +955,9 @@ cudaError_t launch_router_bwd_bf16(const BwdParams& p, const CUtensorMap& tmX, c
   while (n_xst > 2 && bwd_layout(E_pad, p.slice_width, n_xst).total > 227u * 1024u) --n_xst;
   const uint32_t smem = bwd_layout(E_pad, p.slice_width, n_xst).total;
   if (smem > 227u * 1024u) return cudaErrorInvalidConfiguration;
-  auto k = (E_pad == 64) ? k_router_bwd_tc<64> : k_router_bwd_tc<128>;
+  const bool lo = p.d_gate != nullptr;
+  auto k = E_pad == 64 ? (lo ? k_router_bwd_tc<64, true> : k_router_bwd_tc<64, false>)
+                       : (lo ? k_router_bwd_tc<128, true> : k_router_bwd_tc<128, false>);
   cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   return launch_pdl(k, dim3(p.groups * p.slices), dim3(kBwdThreads), smem, s, tmX, tmW, tmDX, p, n_xst);
