@@ -292,11 +292,19 @@ smoes_status smoes_expert_balance(smoes_plan plan, const int32_t* topk_idx, int 
 /* smoes_router_bwd with a gradient of the gate values besides: d_gate [n_samples, E] float32, the same for all tokens of
  *   a sample (per_sample = 1), or [E], for all tokens (0); NULL for none. It reaches the tokens that have a selection in
  *   [0, E) in topk_idx, as smoes_expert_balance counts them. With d_gate, dX of a SMOES_BF16 plan is formed from dz as two
- *   bf16 parts, as dW is: within half a step of bf16 of the exact value, plus 2^-16 sum_e |dz_je W_ed|. */
+ *   bf16 parts, as dW is: within half a step of bf16 of the exact value, plus 2^-16 sum_e |dz_je W_ed|.
+ *   The other gradients (of d_topk_w's normalisation, of a masked MI loss, of smoes_bin_balance) read topk_idx too, which
+ *   has to be the forward's for them. Where selections were dropped for smoes_expert_balance, what it was given goes into
+ *   kept_idx [T, k] of the second call, and d_gate reaches the tokens that have a selection left there (NULL: topk_idx). */
 smoes_status smoes_router_bwd_gates(smoes_plan plan, const void* X, const void* W, const float* M,
                                     const int32_t* topk_idx, const float* d_topk_w, const float* d_gate,
                                     int per_sample, float loss_scale, float* dW, int accumulate_dW, void* dX,
                                     float* dlogits, void* ws, size_t ws_bytes, cudaStream_t stream);
+smoes_status smoes_router_bwd_gates_kept(smoes_plan plan, const void* X, const void* W, const float* M,
+                                         const int32_t* topk_idx, const float* d_topk_w, const float* d_gate,
+                                         const int32_t* kept_idx, int per_sample, float loss_scale, float* dW,
+                                         int accumulate_dW, void* dX, float* dlogits, void* ws, size_t ws_bytes,
+                                         cudaStream_t stream);
 
 /* (4) Bin-grouped permutation with de-duplicated dispatch (Sec. 4.5, "DeDup").
  *   One entry per unique (token, bin) pair, ordered by bin ascending then token ascending.

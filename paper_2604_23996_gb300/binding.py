@@ -103,6 +103,7 @@ _sig = {
                                       _vp]),
     "smoes_router_bwd": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _f, _vp, _i, _vp, _vp, _vp, _sz, _vp]),
     "smoes_router_bwd_gates": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _f, _vp, _i, _vp, _vp, _vp, _sz, _vp]),
+    "smoes_router_bwd_gates_kept": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _f, _vp, _i, _vp, _vp, _vp, _sz, _vp]),
     "smoes_expert_balance": (_i, [_vp, _vp, _i, _f, _vp, _vp, _vp, _vp, _sz, _vp]),
     "smoes_bin_permute": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
     "smoes_bin_permute_noalloc": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
@@ -262,11 +263,12 @@ def smoes_router_bwd(plan, X, W, M, topk_idx, d_topk_w, loss_scale, dW, accumula
 
 
 def smoes_router_bwd_gates(plan, X, W, M, topk_idx, d_topk_w, d_gate, per_sample, loss_scale, dW, accumulate_dW, dX,
-                           dlogits, ws, stream=None) -> int:
-    """smoes_router_bwd with a gradient of the gate values, [n_samples, E] (per_sample) or [1, E]."""
-    return _lib.smoes_router_bwd_gates(plan, _p(X), _p(W), _p(M), _p(topk_idx), _p(d_topk_w), _p(d_gate),
-                                       int(per_sample), float(loss_scale), _p(dW), int(accumulate_dW), _p(dX),
-                                       _p(dlogits), _p(ws), ws.numel() * ws.element_size(), _stream(stream))
+                           dlogits, ws, stream=None, kept_idx=None) -> int:
+    """smoes_router_bwd with a gradient of the gate values, [n_samples, E] (per_sample) or [1, E]; kept_idx: the selections
+    that its loss counted, where some of the forward's topk_idx were dropped."""
+    return _lib.smoes_router_bwd_gates_kept(plan, _p(X), _p(W), _p(M), _p(topk_idx), _p(d_topk_w), _p(d_gate), _p(kept_idx),
+                                            int(per_sample), float(loss_scale), _p(dW), int(accumulate_dW), _p(dX),
+                                            _p(dlogits), _p(ws), ws.numel() * ws.element_size(), _stream(stream))
 
 
 def smoes_bin_permute(plan, topk_idx, home, is_vision, bin_offsets, perm_token, perm_mask,
@@ -490,18 +492,19 @@ class Router:
 
     def backward(self, X, W, M, dW, dX=None, dlogits=None, loss_scale=1.0, d_topk_w=None,
                  accumulate=False, stream=None, d_gate=None, topk_idx=None):
-        """d_gate: what ``expert_balance`` returned, [B, E] or [1, E]; topk_idx: the forward's with dropped selections."""
-        idx = self.topk_idx if topk_idx is None else topk_idx
+        """d_gate: what ``expert_balance`` returned, [B, E] or [1, E]; topk_idx: what it was given, the forward's with dropped
+        selections: a token that has none left gets nothing of d_gate. The other gradients are of the forward's selections
+        (``self.topk_idx``, as the forward left it) whatever was dropped."""
         if topk_idx is not None:
-            self._table("topk_idx", idx, torch.int32, (self.T, self.k))
+            self._table("topk_idx", topk_idx, torch.int32, (self.T, self.k))
         if d_gate is None:
-            code = smoes_router_bwd(self.plan, X, W, M, idx, d_topk_w, loss_scale, dW,
+            code = smoes_router_bwd(self.plan, X, W, M, self.topk_idx, d_topk_w, loss_scale, dW,
                                     accumulate, dX, dlogits, self.ws, stream)
             _check(code, "smoes_router_bwd")
             return
         self._table("d_gate", d_gate, torch.float32, (1, self.E), (self.B, self.E))
-        code = smoes_router_bwd_gates(self.plan, X, W, M, idx, d_topk_w, d_gate, self.B != 1 and len(d_gate) == self.B,
-                                      loss_scale, dW, accumulate, dX, dlogits, self.ws, stream)
+        code = smoes_router_bwd_gates(self.plan, X, W, M, self.topk_idx, d_topk_w, d_gate, self.B != 1 and len(d_gate) == self.B,
+                                      loss_scale, dW, accumulate, dX, dlogits, self.ws, stream, topk_idx)
         _check(code, "smoes_router_bwd_gates")
 
     def _table(self, name, t, dtype, *shapes):

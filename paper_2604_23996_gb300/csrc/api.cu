@@ -713,6 +713,15 @@ smoes_status smoes_router_bwd_gates(smoes_plan P, const void* X, const void* W, 
                                     const int32_t* topk_idx, const float* d_topk_w, const float* d_gate,
                                     int per_sample, float loss_scale, float* dW, int accumulate_dW, void* dX,
                                     float* dlogits, void* ws, size_t ws_bytes, cudaStream_t stream) {
+  return smoes_router_bwd_gates_kept(P, X, W, M, topk_idx, d_topk_w, d_gate, nullptr, per_sample, loss_scale, dW,
+                                     accumulate_dW, dX, dlogits, ws, ws_bytes, stream);
+}
+
+smoes_status smoes_router_bwd_gates_kept(smoes_plan P, const void* X, const void* W, const float* M,
+                                         const int32_t* topk_idx, const float* d_topk_w, const float* d_gate,
+                                         const int32_t* kept_idx, int per_sample, float loss_scale, float* dW,
+                                         int accumulate_dW, void* dX, float* dlogits, void* ws, size_t ws_bytes,
+                                         cudaStream_t stream) {
   if (!P) return SMOES_ERR_INVALID_ARG;
   smoes_status st = check_ws(P, ws, ws_bytes);
   if (st != SMOES_OK) return st;
@@ -723,8 +732,8 @@ smoes_status smoes_router_bwd_gates(smoes_plan P, const void* X, const void* W, 
     return cuda_status(cudaMemsetAsync(dW, 0, sizeof(float) * static_cast<size_t>(d.E) * d.d, stream));
   }
   if (!X || !W || !M) return SMOES_ERR_INVALID_ARG;
-  if ((d_topk_w || d_gate || d.mi_topk_mask) && !topk_idx) return SMOES_ERR_INVALID_ARG;
-  if (d_gate && !aligned16(d_gate)) return SMOES_ERR_ALIGNMENT;
+  if ((d_topk_w || d.mi_topk_mask || (d_gate && !kept_idx)) && !topk_idx) return SMOES_ERR_INVALID_ARG;
+  if (d_gate && (!aligned16(d_gate) || (kept_idx && !aligned16(kept_idx)))) return SMOES_ERR_ALIGNMENT;
   if (!aligned16(X) || !aligned16(W) || !aligned16(M) || !aligned16(dW) || (dX && !aligned16(dX)))
     return SMOES_ERR_ALIGNMENT;
   if (d.dtype == SMOES_BF16 && d.E > 128) return SMOES_ERR_UNSUPPORTED;
@@ -751,6 +760,7 @@ smoes_status smoes_router_bwd_gates(smoes_plan P, const void* X, const void* W, 
   p.balance_armed = P->balance_armed ? 1 : 0;
   p.d_gate = d_gate;
   p.d_gate_stride = per_sample ? d.E : 0;
+  p.kept_idx = kept_idx ? kept_idx : topk_idx;
   p.n_sms = P->n_sms;
   cudaError_t e;
   if (d.dtype == SMOES_BF16) {

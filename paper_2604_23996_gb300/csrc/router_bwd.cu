@@ -160,12 +160,21 @@ __device__ __forceinline__ void add_balance_grad(const BwdParams& p, const TopkS
   }
 }
 
-// Whether the token of a GS-lane group has a selection in [0, E), from its slots.
+// Whether the token of a GS-lane group has a selection in [0, E) among those that the loss of the gate values counted (lane c
+// looks at slots c, c + GS, ...; then the group's lanes together).
 template <int GS>
-__device__ __forceinline__ bool takes_part(const BwdParams& p, const TopkSlots<GS>& u) {
+__device__ __forceinline__ int own_selection(const BwdParams& p, int j, bool valid, int c) {
   int any = 0;
 #pragma unroll
-  for (int i = 0; i < TopkSlots<GS>::kPer; ++i) any |= u.idx[i] >= 0 && u.idx[i] < p.dm.E;
+  for (int i = 0; i < TopkSlots<GS>::kPer; ++i) {
+    const int s = i * GS + c;
+    const int e = valid && s < p.dm.k ? __ldg(p.kept_idx + static_cast<size_t>(j) * p.dm.k + s) : -1;
+    any |= e >= 0 && e < p.dm.E;
+  }
+  return any;
+}
+template <int GS>
+__device__ __forceinline__ bool takes_part(int any) {
 #pragma unroll
   for (int o = 1; o < GS; o <<= 1) any |= __shfl_xor_sync(0xffffffffu, any, o);
   return any != 0;
@@ -278,7 +287,7 @@ __global__ void __launch_bounds__(256) k_dz_prep(const BwdParams p) {
     float4 ga, gb;
     float ginv;
     float2 m;
-    int smp;
+    int smp, kept;
     TopkSlots<TPT> slots;
   };
   auto load = [&](int j, In& in) {
@@ -302,7 +311,8 @@ __global__ void __launch_bounds__(256) k_dz_prep(const BwdParams p) {
       in.m = __ldg(reinterpret_cast<const float2*>(p.M) + j);
       in.smp = __ldg(p.ws.token_sample + j);
     }
-    if (kUp || kGates || bal) load_slots<TPT, kUp>(p, j, j < dm.T, c, in.slots);
+    if (kUp || bal) load_slots<TPT, kUp>(p, j, j < dm.T, c, in.slots);
+    if (kGates) in.kept = own_selection<TPT>(p, j, j < dm.T, c);
   };
   // coefficients (a, b, h) of the thread's two bins for sample held (-1: none yet)
   int held = -1;
@@ -367,7 +377,7 @@ __global__ void __launch_bounds__(256) k_dz_prep(const BwdParams p) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) te[i] = e0 + i < E ? __ldg(p.d_gate + row + e0 + i) : 0.f;
       }
-      add_gate_grad<TPT, 8>(g, te, fac, takes_part<TPT>(p, in.slots), dz);
+      add_gate_grad<TPT, 8>(g, te, fac, takes_part<TPT>(in.kept), dz);
     }
     if (valid && p.dlogits) {
       float* dl = p.dlogits + static_cast<size_t>(j) * E;
@@ -766,7 +776,7 @@ k_router_bwd_f32(const BwdParams p) {
     const bool has_up = p.d_topk_w != nullptr;
     const bool bal = p.topk_idx && __ldcg(p.ws.bal_flag) != 0u;   // the balance term (eq. 16); block-uniform
     if (has_up) load_slots<4, true>(p, j, valid, qd, slots);
-    else if (bal || p.d_gate) load_slots<4, false>(p, j, valid, qd, slots);
+    else if (bal) load_slots<4, false>(p, j, valid, qd, slots);
     const float* g = p.ws.gsave + static_cast<size_t>(valid ? j : 0) * E;
     const float ginv = valid ? p.ws.ginv[j] : 0.f;
     // the token's 4-thread group holds experts qd, qd + 4, ...
@@ -794,7 +804,7 @@ k_router_bwd_f32(const BwdParams p) {
       const float* t = p.d_gate + static_cast<size_t>(valid ? p.ws.token_sample[j] : 0) * p.d_gate_stride;
 #pragma unroll
       for (int i = 0; i < NQ; ++i) fq[i] = eidx[i] >= 0 ? __ldg(t + eidx[i]) : 0.f;
-      add_gate_grad<4, NQ>(gq, fq, fac, takes_part<4>(p, slots), dzv);
+      add_gate_grad<4, NQ>(gq, fq, fac, takes_part<4>(own_selection<4>(p, j, valid, qd)), dzv);
     }
 #pragma unroll
     for (int i = 0; i < EB / 4; ++i) {

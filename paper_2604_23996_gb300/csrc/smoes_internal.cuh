@@ -131,6 +131,7 @@ struct BwdParams {
   int balance_armed;         // host's view: smoes_bin_balance was called since the last forward
   const float* d_gate;       // gradient of the gate values by sample or batch, or null
   int d_gate_stride;         // E (a row per sample) or 0
+  const int32_t* kept_idx;   // [T, k] selections that its loss counted: those of the forward but dropped ones
   int n_sms;
 };
 
