@@ -10,9 +10,10 @@
 // ...), kR tokens at work and kR on their way. Runs of a sample that has several leave partials. Up to kFewSamples samples are
 // finished by the block that arrives last of all, a warp a sample; with more of them each by the last of its own blocks, and
 // the losses are added by the one that finishes the last sample. The sums are fp32 in a fixed order, whichever block makes
-// them. Bound by the gate values' bytes (131072 x 128: 20.5 us, of which the tokens take 13 and the hand-over and the last
-// block's sums 6; 10.6 us of HBM); small batches by the latency of a launch, two reads and one hand-over between the blocks
-// (16384 x 64: 10.8 us).
+// them. Bound by the gate values' bytes (131072 x 128: 20.0 us, of which the tokens take 13 and the hand-over and the last
+// block's sums 6; 10.6 us of HBM; for more than 64 experts in blocks of 1024 threads the tokens under way do not fit in 64
+// registers, 80 bytes of a thread lie in local memory); small batches by latency: a launch, the search for the block's run (log2 B
+// + 1 reads of its table that wait for one another), the tokens, one hand-over between the blocks (16384 x 64: 10.8 us).
 #include "device_common.cuh"
 #include "ptx.cuh"
 #include "smoes_internal.cuh"
@@ -272,7 +273,7 @@ __global__ void __launch_bounds__(kThreads) k_expert_balance(const ExpertBalance
       N += N_s[q];
     }
   }
-  // the sample's loss and gradient (counts stay below 2^24: exact in fp32)
+  // the sample's loss and gradient (counts are at most 2^24, T k: exact in fp32)
   const float total = block_sum(static_cast<float>(C), scratch);
   const float f = total > 0.f ? static_cast<float>(E) * static_cast<float>(C) / total : 0.f;
   const float inv_n = N > 0 ? 1.f / static_cast<float>(N) : 0.f;

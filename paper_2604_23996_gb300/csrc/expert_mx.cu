@@ -30,7 +30,7 @@
 // for each quarter of the lanes that take 32-row chunks in turn.
 //
 // Measured: 98304 x 2048 x 2048 of 64 experts gated with silu 142-145 us (5.8 PFLOP/s; the products alone, without waiting for
-// operands, 95 us), 98304 x 1024 x 2048 99 us (402 MB of output at 4 TB/s), 16384 x 4096 x 4096 84 us (6.5 PFLOP/s), 16
+// operands, 95 us: products of 64 of the depth an instruction, four times the bf16 rate at most), 98304 x 1024 x 2048 99 us (402 MB of output at 4 TB/s), 16384 x 4096 x 4096 84 us (6.5 PFLOP/s), 16
 // tokens of 6 of 64 experts, 2048 x 2048, 18 us (6.4 TB/s). Bound by the warps' turns: 47% of the issue slots are used, and each
 // of scales, math, matrix stores and copies taken out gains 3 to 14 us of 142; not by L2 (all tiles reading the same
 // operands: 142) nor by the ring (six stages: 147). Few rows are bound by the weights' bytes.
@@ -662,7 +662,8 @@ cudaError_t launch(ExpertMxParams& p, const CUtensorMap& a, const CUtensorMap& b
   }
   // A few rounds of the widest tiles: the width whose rounds take least, a tile counted as its rows and 64 more (measured, 6007
   // x 1024 -> 1416 with GELU and residual: 208 rows 21.3 us in 2.3 rounds, 192 21.0, 160 19.3 in 3.0, 128 19.0 in 3.7). Several
-  // experts have half an unfilled tile each.
+  // experts have half an unfilled tile each. (At this shape it takes 160, not 128: the cost knows rounds, not how many of a
+  // tile's 32-row chunks the four epilogue warps of a quarter share out evenly.)
   if (p.tile_rows == kRowsMost && tiles < 8ll * pairs) {
     long long least = 0;
     for (int rows : {kRowsMost, 192, 160, 128, 96}) {

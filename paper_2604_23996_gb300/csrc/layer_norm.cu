@@ -169,7 +169,10 @@ __global__ void __launch_bounds__(kThreads) k_norm_fwd(const NormParams p) {
 }
 
 // A round of a block is kRows rows of each of its groups of kTpr threads; the next round's rows are on their way while the
-// block works on this one's. Blocks of 1024 threads have 64 registers each and neither fetch ahead nor keep the weight (kLean).
+// block works on this one's. Blocks of 1024 threads have 64 registers each and neither fetch ahead nor keep the weight (kLean);
+// for bf16 the registers do not suffice all the same (192 bytes of a thread in local memory): 8192 x 16384 with the stream's
+// gradient 336 us, of 159 at the copy's rate; 16384 x 8192 in fp32, which fits, 410 of 318; 16384 x 8192 in bf16, by 512 threads
+// a row, 184 of 159.
 template <class T, int kTpr, int kWords, int kRows, int kThreads, int kBlocks>
 __global__ void __launch_bounds__(kThreads, kBlocks) k_norm_bwd(const NormParams p) {
   constexpr int N = Pack<T>::N;
@@ -366,9 +369,11 @@ __global__ void __launch_bounds__(kSumSlices * kSumCols) k_norm_sum(const NormPa
   *out = a;
 }
 
-// Blocks of the backward: what the device holds at once (with three or four per SM the second round is a short one: 16384 x 2048
-// 53.4 and 47.6 us instead of 44.7), fewer where the partials would weigh against the rows (4091 x 512 in fp32 with the sums over
-// the blocks: 8.6 us with one block per SM, 9.7 with two).
+// Blocks of the backward: two per SM, what the device holds at once of rows of at most 512 words (with three or four the second
+// round is a short one: 16384 x 2048 53.4 and 47.6 us instead of 44.7), fewer where the partials would weigh against the rows
+// (4091 x 512 in fp32 with the sums over the blocks: 8.6 us with one block per SM, 9.7 with two). Of longer rows an SM holds one
+// block, so two per SM are two rounds of half the rows each, with twice the partials; the rule was measured at 512 and 2048
+// features only.
 int norm_blocks(int n_sms, int T) { return T >= 32 * n_sms ? 2 * n_sms : std::max(1, std::min(n_sms, (T + 7) / 8)); }
 
 template <class T, int kTpr, int kWords, int kThreads>
@@ -378,7 +383,7 @@ cudaError_t forward(const NormParams& p, cudaStream_t s) {
 }
 
 template <class T>
-cudaError_t launch_forward(const NormParams& p, int n_sms, cudaStream_t s) {
+cudaError_t launch_forward(const NormParams& p, cudaStream_t s) {
   if (p.words <= 32) return forward<T, 32, 1, 256>(p, s);
   if (p.words <= 64) return forward<T, 32, 2, 256>(p, s);
   if (p.words <= 128) return forward<T, 32, 4, 256>(p, s);
@@ -462,8 +467,8 @@ smoes_status smoes_norm_fwd(smoes_norm P, const void* X, const void* residual, c
   p.Y = Y;
   p.mean = mean;
   p.rstd = rstd;
-  const cudaError_t e = P->desc.dtype == SMOES_BF16 ? launch_forward<__nv_bfloat16>(p, P->n_sms, stream)
-                                                    : launch_forward<float>(p, P->n_sms, stream);
+  const cudaError_t e = P->desc.dtype == SMOES_BF16 ? launch_forward<__nv_bfloat16>(p, stream)
+                                                    : launch_forward<float>(p, stream);
   return e == cudaSuccess ? SMOES_OK : SMOES_ERR_CUDA;
 }
 

@@ -1,9 +1,9 @@
 // mx.cu -- microscaled 4-bit values: quantisation, its inverse, and the quantising copy of tokens into expert order.
 //
 // A block of 32 consecutive values shares the scale 2^(byte - 127), byte - 127 = max(floor(log2 max|x|) - 2, -127) (the
-// largest 4-bit value, 6, is 1.5 x 2^2); a value over the scale, exact in fp32, is rounded to the nearest of 0, 0.5, 1,
-// 1.5, 2, 3, 4, 6 (ties to the even code), above 6 to 6. This is the microscaling formats' MXFP4, with the scale as their
-// specification gives it. A block that holds a NaN or an infinity becomes NaN: scale byte 255, codes 0.
+// largest 4-bit value, 6, is 1.5 x 2^2); a value over the scale is rounded to the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (ties to
+// the even code), above 6 to 6. The quotient is exact in fp32 but where it is subnormal, far below 0.25: 0 either way. This is
+// the microscaling formats' MXFP4, with the scale as their specification gives it. A block that holds a NaN or an infinity becomes NaN: scale byte 255, codes 0.
 //
 // A thread takes 8 consecutive values, four neighbouring threads a block, whose largest magnitude meets in two shuffles;
 // the 4-byte words of a warp's codes are neighbours in memory. Every value is read once. Bound by HBM: 98304 x 1024 bf16
@@ -64,7 +64,7 @@ __device__ __forceinline__ uint32_t quantise(const Eight<T>& in, uint32_t& byte)
     return 0u;
   }
   byte = e > 2u ? e - 2u : 0u;
-  const float inv = __uint_as_float((254u - byte) << 23);   // 1 / scale: 2^2 .. 2^127
+  const float inv = __uint_as_float((254u - byte) << 23);   // 1 / scale: 2^-125 .. 2^127
 #pragma unroll
   for (int i = 0; i < 8; ++i) f[i] *= inv;
   uint32_t r;
