@@ -30,10 +30,11 @@
 // for each quarter of the lanes that take 32-row chunks in turn.
 //
 // Measured: 98304 x 2048 x 2048 of 64 experts gated with silu 142-145 us (5.8 PFLOP/s; the products alone, without waiting for
-// operands, 95 us: products of 64 of the depth an instruction, four times the bf16 rate at most), 98304 x 1024 x 2048 99 us (402 MB of output at 4 TB/s), 16384 x 4096 x 4096 84 us (6.5 PFLOP/s), 16
-// tokens of 6 of 64 experts, 2048 x 2048, 18 us (6.4 TB/s). Bound by the warps' turns: 47% of the issue slots are used, and each
-// of scales, math, matrix stores and copies taken out gains 3 to 14 us of 142; not by L2 (all tiles reading the same
-// operands: 142) nor by the ring (six stages: 147). Few rows are bound by the weights' bytes.
+// operands, 95 us: products of 64 of the depth an instruction, four times the bf16 rate at most), 98304 x 1024 x 2048 99 us (402 MB
+// of output at 4 TB/s), 16384 x 4096 x 4096 84 us (6.5 PFLOP/s), 16 tokens of 6 of 64 experts, 2048 x 2048, 18 us (6.4 TB/s). Bound
+// by the warps' turns: 47% of the issue slots are used, and each of scales, math, matrix stores and copies taken out gains 3 to 14
+// us of 142; not by L2 (all tiles reading the same operands: 142) nor by the ring (six stages: 147). Few rows are bound by the
+// weights' bytes.
 #include <cmath>
 #include <type_traits>
 
